@@ -333,11 +333,145 @@ spindlekv_status spindlekv_decode_attend(const spindlekv_batch* batch, int32_t n
                                          float* out, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * A paged cache held in 8 bits (the storage-type factor r3 of Eq. (15); the paper leaves its form open).
+ *
+ * Pool.  A page holds page_size consecutive tokens of one (layer, sequence), all KV heads, K and V apart; any layer and
+ * sequence may own any page.  Codes are one byte per element; SPINDLEKV_PAGED_BLOCK consecutive tokens of a page and head
+ * share one fp32 scale, and an element stands for code * scale:
+ *   SPINDLEKV_PAGED_INT8  codes -127..127; scale = amax / 127 rounded to fp32 (at least 2^-126), code = the integer nearest
+ *                         to x / scale, ties to even, decided on the exact quotient
+ *   SPINDLEKV_PAGED_E4M3  codes are FP8 E4M3; scale = the least power of two 2^k, k >= -126, with amax <= 448 * 2^k, so
+ *                         that x / scale is exact and is rounded once, ties to even
+ * with amax the block's largest magnitude, scale 0 when that is 0.  A block into which a NaN or an infinity was written
+ * has the scale NaN and stands for NaN as a whole.  page_ref counts the table entries that name a page and is the whole
+ * state of the allocator: 0 means free, and the lowest free page is always taken first.
+ * Table.  pages[layer][seq][i] holds tokens i*page_size .. of that sequence for i < ceil(lens / page_size); entries behind
+ * the last page are neither read nor written.  A page that is not full belongs to one sequence alone: the calls
+ * below keep it so, and paged_append writes into no other kind.
+ * Lengths are clamped to max_pages * page_size, and an entry outside [0, n_pages) is never followed: its tokens are left
+ * out.  A call of one layer passes that layer's rows of `pages` and `lens` with n_layers = 1.
+ * Calls on one pool must be ordered by the caller (one stream, or events between streams).
+ */
+#define SPINDLEKV_PAGED_BLOCK 16
+enum { SPINDLEKV_PAGED_INT8 = 0, SPINDLEKV_PAGED_E4M3 = 1 };
+
+typedef struct {
+  void* k_codes;      /* device [n_pages][n_kv_heads][page_size][head_dim], one byte each, 16-byte aligned */
+  void* v_codes;
+  float* k_scale;     /* device [n_pages][n_kv_heads][page_size / SPINDLEKV_PAGED_BLOCK] */
+  float* v_scale;
+  int32_t* page_ref;  /* device [n_pages] */
+  int32_t n_pages;
+  int32_t page_size;  /* 16, 32, 64 or 128 */
+  int32_t n_kv_heads;
+  int32_t head_dim;   /* 64 or 128 */
+  int32_t format;     /* SPINDLEKV_PAGED_* */
+} spindlekv_page_pool;
+
+typedef struct {
+  int32_t* pages;     /* device [n_layers][n_seqs][max_pages] */
+  int32_t* lens;      /* device [n_layers][n_seqs] */
+  int32_t n_layers;
+  int32_t n_seqs;
+  int32_t max_pages;
+} spindlekv_page_table;
+
+/* Scratch of the three calls below (256-byte aligned; starts with a status word for spindlekv_poll_status).  0 on bad arguments. */
+size_t spindlekv_pages_workspace_bytes(const spindlekv_page_pool* pool, const spindlekv_page_table* table);
+
+/*
+ * Gives every sequence the pages for a new length: pages are taken for what grows and given back for what shrinks.  A page
+ * that would be left partly filled while other sequences share it is replaced by a copy first.
+ *   new_lens  device [n_layers][n_seqs], or NULL: every length changes by `add`
+ *   start     device out [n_layers][n_seqs]: min(old, new length), i.e. where paged_append goes on; -1 when the call failed
+ * All or nothing: with too few free pages (SPINDLEKV_CAPACITY) or a length outside [0, max_pages * page_size]
+ * (SPINDLEKV_INVALID_ARG) the device status word says so, table and pool stay as they were, and every start is -1, which
+ * paged_append skips.  Pages given back by a call are free for the next one, not for itself.
+ */
+spindlekv_status spindlekv_pages_resize(const spindlekv_page_pool* pool, const spindlekv_page_table* table, const int32_t* new_lens,
+                                        int32_t add, int32_t* start, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Replaces the sequences of a table by copies of a list of parents (in every layer): sequence i becomes what sequence
+ * parent[i] was, or empty for parent[i] = -1.  One call keeps, duplicates, drops and reorders sequences, e.g. after a
+ * step of beam search.  Full pages are shared; a page that is not full goes to the first child, and every further child gets a
+ * copy of its filled blocks.  What no child continues is freed.  At most 1024 sequences.
+ *   parent    device [n_seqs], each in [-1, n_seqs)
+ * All or nothing, with the same status words as spindlekv_pages_resize.
+ */
+spindlekv_status spindlekv_pages_fork(const spindlekv_page_pool* pool, const spindlekv_page_table* table, const int32_t* parent,
+                                      void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Moves the live pages to the page numbers 0 .. n_live-1: the live pages at n_live and above move, in ascending order, into the
+ * free ones below, also in ascending order; the rest stays.  `table` must name every live page of the pool.
+ *   n_live    device out [1]
+ */
+spindlekv_status spindlekv_pages_compact(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t* n_live,
+                                         void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Rounds rows to the pool's format and writes them as tokens start .. lens-1 of their sequences (whose pages
+ * spindlekv_pages_resize has provided).  Tokens that share a block with earlier ones share its scale: when it has to grow,
+ * the earlier codes are rounded again at the new scale (half a step of it at most, each time; for E4M3 only values that
+ * become subnormal change).
+ *   start     device [n_layers][n_seqs]; a sequence with start < 0 or start >= lens is skipped
+ *   max_new   upper bound of lens - start; tokens behind it are not written
+ *   K, V      device, new rows [layer][seq][kv head][row][d], fp32 or bf16, both the same: token start + i takes row i
+ *   idx       device, optional [n_layers][n_kv_heads][idx_len]: token start + i of sequence s takes row
+ *             idx[layer][head][s * idx_seq + i] instead (keep_idx of spindlekv_evict_deep: idx_len = T, idx_seq = max_len;
+ *             what eviction kept goes into the cache without a compacted copy in between)
+ *   n_rows    rows that K and V have per (layer, seq, head): row numbers outside [0, n_rows) are taken as rows of zeros
+ */
+spindlekv_status spindlekv_paged_append(const spindlekv_page_pool* pool, const spindlekv_page_table* table, const int32_t* start,
+                                        int32_t max_new, spindlekv_tensor K, spindlekv_tensor V, int32_t n_rows, const int32_t* idx,
+                                        int32_t idx_len, int32_t idx_seq, void* stream);
+
+/*
+ * Attention of the newest tokens over the paged cache.  The n_rows query rows of a sequence are its last n_rows tokens, already
+ * appended: row r sees the tokens 0 .. lens - n_rows + r.  For KV head j and query head g of its group
+ *     out_r = softmax_t( q_r . K_t * scale ) V_t ,
+ * a row that sees no token gives zeros.  Keys are used as stored (rotated already, if the model rotates them).
+ *   q, out    device, [layer][seq][q head][row][d], fp32 or bf16, both the same; may not overlap
+ *   n_rows    1 .. 16;  n_q_heads / n_kv_heads <= 8
+ *   max_len   the longest sequence, as far as the host knows: it only sizes the split over the device, any length is served
+ *   scale     0: 1 / sqrt(head_dim)
+ *   ws        device scratch of spindlekv_paged_workspace_bytes bytes, 256-byte aligned, not to be shared by calls that may
+ *             run at the same time
+ * Sums and softmax statistics are fp32, in an order that depends on the lengths only: the same call gives the same bits.
+ */
+size_t spindlekv_paged_workspace_bytes(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t n_q_heads, int32_t n_rows);
+spindlekv_status spindlekv_paged_attend(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t n_q_heads,
+                                        int32_t n_rows, int32_t max_len, float scale, spindlekv_tensor q, spindlekv_tensor out,
+                                        void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Beam search's selection: among the continuations (beam w, token t) of a sequence the n_out with the largest
+ *     total = score[w] + logits[w][t] - log sum_u exp(logits[w][u]) ,
+ * best first, ties to the lower w * vocab + t.  The totals are formed and compared in double precision from a log-sum-exp
+ * taken in fp32 pieces.  A beam whose log-sum-exp or score is not finite offers its tokens at -infinity; a finished beam offers `eos` at
+ * total = score and all else at -infinity.
+ *   logits      device [n_seqs * n_beams] rows of `vocab` elements, `row_stride` elements apart, fp32 or bf16, any alignment of
+ *               the rows that the element type allows
+ *   score       device [n_seqs * n_beams] fp32
+ *   finished    device [n_seqs * n_beams] bytes (0: not finished), or NULL
+ *   out_score   device out [n_seqs][n_out] fp32: total
+ *   out_parent  device out [n_seqs][n_out]: row seq * n_beams + w, i.e. with n_out = n_beams the parents of spindlekv_pages_fork
+ *   out_token   device out [n_seqs][n_out]
+ * n_beams <= 64, n_out <= 32, n_out <= n_beams * vocab < 2^31.
+ */
+size_t spindlekv_beam_workspace_bytes(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_t n_out);
+spindlekv_status spindlekv_beam_select(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_t n_out, const void* logits, int32_t dtype,
+                                       int64_t row_stride, const float* score, const uint8_t* finished, int32_t eos, float* out_score,
+                                       int32_t* out_parent, int32_t* out_token, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Reads the device status word of a workspace (blocking copy; synchronise the stream first).
  *   ws            the workspace of the call in question; NULL: the built-in scratch that
  *                 spindlekv_evict_deep_noalloc uses on the current device (INVALID_ARG before the first
  *                 such call on this device)
- *   device_status host out: SPINDLEKV_OK or SPINDLEKV_TIMEOUT
+ *   device_status host out: SPINDLEKV_OK or SPINDLEKV_TIMEOUT; after the page calls SPINDLEKV_OK, SPINDLEKV_CAPACITY or
+ *                 SPINDLEKV_INVALID_ARG
  *   detail        host out, optional [4]: {greedy rounds used, live tokens left, units of the call whose
  *                 adjacency was computed as a bit matrix (all of them for fp32 input; for bf16 input only
  *                 those whose candidate pairs did not fit the record pool), neighbour-list entries built
@@ -353,7 +487,8 @@ int64_t spindlekv_launch_count(int32_t reset);
  * spindlekv_timing_enable(1) starts collecting (costs two event records per launch);
  * spindlekv_timing_read synchronises the recorded events and returns, for kernel class `which`
  * (0 window-score, 1 top-k, 2 norms, 3 similarity, 4 neighbour lists, 5 greedy cover, 6 entry numbering, 7 gather,
- * 8 the bit-matrix pass of the similarity kernel over units that overflowed their record pool, 9 decode attention),
+ * 8 the bit-matrix pass of the similarity kernel over units that overflowed their record pool, 9 decode attention,
+ * 10 paged attention, 11 paged append, 12 page tables and page copies, 13 beam selection),
  * the summed milliseconds and the number of launches since the last spindlekv_timing_enable call.
  */
 void spindlekv_timing_enable(int32_t on);

@@ -19,8 +19,10 @@ OK, INVALID_ARG, BUDGET, WORKSPACE_TOO_SMALL, CAPACITY, UNSUPPORTED, CUDA_ERROR,
 F32, BF16 = 0, 1
 MODE_EVICT, MODE_CODEBOOK = 1, 2
 WS_EVICT, WS_CODEBOOK = 0, 1
+PAGED_INT8, PAGED_E4M3 = 0, 1
+PAGED_BLOCK = 16
 KERNEL_CLASSES = ("window_score", "topk", "norms", "similarity", "degree", "greedy", "finalise", "gather",
-                  "similarity_fallback", "decode")
+                  "similarity_fallback", "decode", "paged_attend", "paged_append", "pages", "beam")
 
 
 class SpindleKVError(RuntimeError):
@@ -45,6 +47,16 @@ class _Config(C.Structure):
 class _Batch(C.Structure):
     _fields_ = [("n_layers", C.c_int32), ("n_seqs", C.c_int32), ("max_len", C.c_int32),
                 ("total_len", C.c_int32), ("cu_seqlens", C.c_void_p), ("layer_lens", C.c_void_p), ("layer_lens_heads", C.c_int32)]
+
+
+class _PagePool(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("page_ref", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("format", C.c_int32)]
+
+
+class _PageTable(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("lens", C.c_void_p), ("n_layers", C.c_int32), ("n_seqs", C.c_int32), ("max_pages", C.c_int32)]
 
 
 def _load() -> C.CDLL:
@@ -98,6 +110,28 @@ def _load() -> C.CDLL:
     lib.spindlekv_decode_attend.argtypes = [C.POINTER(_Batch), C.c_int32, C.c_int32, C.c_int32, _Tensor, C.c_void_p,
                                             _Tensor, C.c_void_p, C.c_void_p, _Tensor, C.c_void_p, C.c_void_p,
                                             C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    pool, table = C.POINTER(_PagePool), C.POINTER(_PageTable)
+    lib.spindlekv_pages_workspace_bytes.restype = C.c_size_t
+    lib.spindlekv_pages_workspace_bytes.argtypes = [pool, table]
+    lib.spindlekv_pages_resize.restype = C.c_int32
+    lib.spindlekv_pages_resize.argtypes = [pool, table, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.spindlekv_pages_fork.restype = C.c_int32
+    lib.spindlekv_pages_fork.argtypes = [pool, table, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.spindlekv_pages_compact.restype = C.c_int32
+    lib.spindlekv_pages_compact.argtypes = [pool, table, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.spindlekv_paged_append.restype = C.c_int32
+    lib.spindlekv_paged_append.argtypes = [pool, table, C.c_void_p, C.c_int32, _Tensor, _Tensor, C.c_int32, C.c_void_p, C.c_int32,
+                                           C.c_int32, C.c_void_p]
+    lib.spindlekv_paged_workspace_bytes.restype = C.c_size_t
+    lib.spindlekv_paged_workspace_bytes.argtypes = [pool, table, C.c_int32, C.c_int32]
+    lib.spindlekv_paged_attend.restype = C.c_int32
+    lib.spindlekv_paged_attend.argtypes = [pool, table, C.c_int32, C.c_int32, C.c_int32, C.c_float, _Tensor, _Tensor, C.c_void_p,
+                                           C.c_size_t, C.c_void_p]
+    lib.spindlekv_beam_workspace_bytes.restype = C.c_size_t
+    lib.spindlekv_beam_workspace_bytes.argtypes = [C.c_int32] * 4
+    lib.spindlekv_beam_select.restype = C.c_int32
+    lib.spindlekv_beam_select.argtypes = [C.c_int32] * 4 + [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32,
+                                                            C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.spindlekv_poll_status.restype = C.c_int32
     lib.spindlekv_poll_status.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
     lib.spindlekv_set_tuning.restype = C.c_int32
@@ -336,6 +370,91 @@ def spindlekv_decode_attend(batch: Batch, n_q_heads: int, n_kv_heads: int, head_
                                       _ptr(mag_K), C_V, _ptr(ref_V), _ptr(mag_V), _ptr(positions), _ptr(rope_table),
                                       rope_table.shape[0], _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream))
     _check(st, "spindlekv_decode_attend")
+
+
+class PagePool:
+    """The pages of an 8-bit cache.  ``k_codes``, ``v_codes``: ``[n_pages, H_kv, page_size, d]`` int8 or float8_e4m3fn;
+    ``k_scale``, ``v_scale``: ``[n_pages, H_kv, page_size / 16]`` fp32; ``page_ref``: ``[n_pages]`` int32 (0: free).  All contiguous."""
+
+    def __init__(self, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, page_ref: torch.Tensor):
+        formats = {torch.int8: PAGED_INT8, torch.float8_e4m3fn: PAGED_E4M3}
+        if k_codes.dtype not in formats or v_codes.dtype != k_codes.dtype:
+            raise TypeError(f"unsupported code dtypes {k_codes.dtype}, {v_codes.dtype}")
+        n, h, ps, d = k_codes.shape
+        scales = (n, h, ps // PAGED_BLOCK)
+        if v_codes.shape != k_codes.shape or tuple(k_scale.shape) != scales or tuple(v_scale.shape) != scales or tuple(page_ref.shape) != (n,):
+            raise ValueError("the parts of a page pool do not fit together")
+        if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or page_ref.dtype != torch.int32:
+            raise TypeError("scales are fp32, reference counts int32")
+        self.tensors = (k_codes, v_codes, k_scale, v_scale, page_ref)      # kept alive with the pointers
+        if not all(t.is_contiguous() and t.device == k_codes.device for t in self.tensors):
+            raise ValueError("the parts of a page pool are contiguous and on one device")
+        self.device = k_codes.device
+        self.c = _PagePool(*(t.data_ptr() for t in self.tensors), n, ps, h, d, formats[k_codes.dtype])
+
+
+class PageTable:
+    """``pages``: ``[n_layers, n_seqs, max_pages]`` int32, ``lens``: ``[n_layers, n_seqs]`` int32, both contiguous."""
+
+    def __init__(self, pages: torch.Tensor, lens: torch.Tensor):
+        if pages.dim() != 3 or tuple(lens.shape) != tuple(pages.shape[:2]) or pages.dtype != torch.int32 or lens.dtype != torch.int32:
+            raise ValueError("pages [n_layers, n_seqs, max_pages] and lens [n_layers, n_seqs] are int32 and fit together")
+        if not (pages.is_contiguous() and lens.is_contiguous() and pages.device == lens.device):
+            raise ValueError("pages and lens are contiguous and on one device")
+        self.pages, self.lens = pages, lens
+        self.c = _PageTable(pages.data_ptr(), lens.data_ptr(), *pages.shape)
+
+
+def _bytes(ws: torch.Tensor) -> int:
+    return ws.numel() * ws.element_size()
+
+
+def spindlekv_pages_workspace_bytes(pool: PagePool, table: PageTable) -> int:
+    return int(_lib.spindlekv_pages_workspace_bytes(pool.c, table.c))
+
+
+def spindlekv_pages_resize(pool: PagePool, table: PageTable, new_lens: Optional[torch.Tensor], add: int, start: torch.Tensor,
+                           ws: torch.Tensor, stream=None) -> None:
+    _check(_lib.spindlekv_pages_resize(pool.c, table.c, _ptr(new_lens), add, _ptr(start), _ptr(ws), _bytes(ws), _stream(stream)),
+           "spindlekv_pages_resize")
+
+
+def spindlekv_pages_fork(pool: PagePool, table: PageTable, parent: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    _check(_lib.spindlekv_pages_fork(pool.c, table.c, _ptr(parent), _ptr(ws), _bytes(ws), _stream(stream)), "spindlekv_pages_fork")
+
+
+def spindlekv_pages_compact(pool: PagePool, table: PageTable, n_live: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    _check(_lib.spindlekv_pages_compact(pool.c, table.c, _ptr(n_live), _ptr(ws), _bytes(ws), _stream(stream)), "spindlekv_pages_compact")
+
+
+def spindlekv_paged_append(pool: PagePool, table: PageTable, start: torch.Tensor, max_new: int, K: _Tensor, V: _Tensor, n_rows: int,
+                           idx: Optional[torch.Tensor] = None, idx_seq: int = 0, stream=None) -> None:
+    """``idx``: ``[n_layers, H_kv, T]`` row numbers, sequence ``s`` from column ``s * idx_seq`` on (``keep_idx`` of an eviction)."""
+    _check(_lib.spindlekv_paged_append(pool.c, table.c, _ptr(start), max_new, K, V, n_rows, _ptr(idx), 0 if idx is None else idx.shape[-1],
+                                       idx_seq, _stream(stream)), "spindlekv_paged_append")
+
+
+def spindlekv_paged_workspace_bytes(pool: PagePool, table: PageTable, n_q_heads: int, n_rows: int) -> int:
+    return int(_lib.spindlekv_paged_workspace_bytes(pool.c, table.c, n_q_heads, n_rows))
+
+
+def spindlekv_paged_attend(pool: PagePool, table: PageTable, n_q_heads: int, n_rows: int, max_len: int, scale: float, q: _Tensor,
+                           out: _Tensor, ws: torch.Tensor, stream=None) -> None:
+    _check(_lib.spindlekv_paged_attend(pool.c, table.c, n_q_heads, n_rows, max_len, scale, q, out, _ptr(ws), _bytes(ws), _stream(stream)),
+           "spindlekv_paged_attend")
+
+
+def spindlekv_beam_workspace_bytes(n_seqs: int, n_beams: int, vocab: int, n_out: int) -> int:
+    return int(_lib.spindlekv_beam_workspace_bytes(n_seqs, n_beams, vocab, n_out))
+
+
+def spindlekv_beam_select(n_seqs: int, n_beams: int, vocab: int, n_out: int, logits: torch.Tensor, score: torch.Tensor,
+                          finished: Optional[torch.Tensor], eos: int, out_score: torch.Tensor, out_parent: torch.Tensor,
+                          out_token: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """``logits``: ``[n_seqs * n_beams, vocab]`` with any row stride, the row itself contiguous."""
+    _check(_lib.spindlekv_beam_select(n_seqs, n_beams, vocab, n_out, _ptr(logits), _dtype_code(logits), logits.stride(0), _ptr(score),
+                                      _ptr(finished), eos, _ptr(out_score), _ptr(out_parent), _ptr(out_token), _ptr(ws), _bytes(ws),
+                                      _stream(stream)), "spindlekv_beam_select")
 
 
 def spindlekv_poll_status(ws: Optional[torch.Tensor]):

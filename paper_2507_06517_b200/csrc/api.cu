@@ -9,6 +9,7 @@
 
 #include "args.cuh"
 #include "common.cuh"
+#include "paged.cuh"
 #include "spindlekv_test_hooks.h"
 
 namespace skv {
@@ -51,6 +52,26 @@ spindlekv_status append_impl(const spindlekv_batch& b, int n_heads, int head_dim
                              const float* mag_left, const int32_t* ref_left, const int32_t* centre_left,
                              const int32_t* n_left_entries, const int32_t* left_idx, const int32_t* left_cnt,
                              const spindlekv_tensor& C, int c_rows, int32_t* n_entries, int32_t* ref_new, cudaStream_t st);
+
+size_t pages_workspace_bytes(const spindlekv_page_pool& p, const spindlekv_page_table& t);
+spindlekv_status pages_resize_impl(const spindlekv_page_pool& pool, const spindlekv_page_table& table, const int32_t* new_lens, int add,
+                                   int32_t* start, void* ws, size_t ws_bytes, cudaStream_t st);
+spindlekv_status pages_fork_impl(const spindlekv_page_pool& pool, const spindlekv_page_table& table, const int32_t* parent, void* ws,
+                                 size_t ws_bytes, cudaStream_t st);
+spindlekv_status pages_compact_impl(const spindlekv_page_pool& pool, const spindlekv_page_table& table, int32_t* n_live, void* ws,
+                                    size_t ws_bytes, cudaStream_t st);
+spindlekv_status paged_append_impl(const spindlekv_page_pool& pool, const spindlekv_page_table& table, const int32_t* start, int max_new,
+                                   const spindlekv_tensor& K, const spindlekv_tensor& V, int n_rows, const int32_t* idx, int idx_len,
+                                   int idx_seq, cudaStream_t st);
+size_t paged_workspace_bytes(const spindlekv_page_pool& pool, const spindlekv_page_table& t, int n_q_heads, int n_rows);
+spindlekv_status paged_attend_impl(const spindlekv_page_pool& pool, const spindlekv_page_table& table, int n_q_heads, int n_rows, int max_len,
+                                   float scale, const spindlekv_tensor& q, const spindlekv_tensor& out, void* ws, size_t ws_bytes,
+                                   cudaStream_t st);
+
+size_t beam_workspace_bytes(int n_seqs, int n_beams, int vocab, int k);
+spindlekv_status beam_select_impl(int n_seqs, int n_beams, int vocab, int k, const void* logits, int dtype, int64_t row_stride,
+                                  const float* score, const uint8_t* finished, int eos, float* out_score, int32_t* out_parent,
+                                  int32_t* out_token, void* ws, size_t ws_bytes, cudaStream_t st);
 
 spindlekv_status selftest_mbarrier_impl(uint32_t* hdr, long long wait_cycles, cudaStream_t st);
 
@@ -311,6 +332,95 @@ spindlekv_status spindlekv_decode_attend(const spindlekv_batch* batch, int32_t n
   if (n_q_heads / n_kv_heads > 8) return SPINDLEKV_UNSUPPORTED;
   return decode_attend_impl(*batch, n_q_heads, n_kv_heads, head_dim, q, pos_q, C_K, ref_K, mag_K, C_V, ref_V, mag_V, positions,
                             rope_table, table_positions, out, ws, ws_bytes, (cudaStream_t)stream);
+}
+
+static bool ws_ok(const void* ws) { return ws && reinterpret_cast<uintptr_t>(ws) % 256 == 0; }
+
+size_t spindlekv_pages_workspace_bytes(const spindlekv_page_pool* pool, const spindlekv_page_table* table) {
+  if (pool_table_status(pool, table) != SPINDLEKV_OK) return 0;
+  return pages_workspace_bytes(*pool, *table);
+}
+
+spindlekv_status spindlekv_pages_resize(const spindlekv_page_pool* pool, const spindlekv_page_table* table, const int32_t* new_lens,
+                                        int32_t add, int32_t* start, void* ws, size_t ws_bytes, void* stream) {
+  const spindlekv_status ps = pool_table_status(pool, table);
+  if (ps != SPINDLEKV_OK) return ps;
+  if (!start || !ws_ok(ws) || new_lens == table->lens) return SPINDLEKV_INVALID_ARG;
+  return pages_resize_impl(*pool, *table, new_lens, add, start, ws, ws_bytes, (cudaStream_t)stream);
+}
+
+spindlekv_status spindlekv_pages_fork(const spindlekv_page_pool* pool, const spindlekv_page_table* table, const int32_t* parent, void* ws,
+                                      size_t ws_bytes, void* stream) {
+  const spindlekv_status ps = pool_table_status(pool, table);
+  if (ps != SPINDLEKV_OK) return ps;
+  if (!parent || !ws_ok(ws)) return SPINDLEKV_INVALID_ARG;
+  return pages_fork_impl(*pool, *table, parent, ws, ws_bytes, (cudaStream_t)stream);
+}
+
+spindlekv_status spindlekv_pages_compact(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t* n_live, void* ws,
+                                         size_t ws_bytes, void* stream) {
+  const spindlekv_status ps = pool_table_status(pool, table);
+  if (ps != SPINDLEKV_OK) return ps;
+  if (!n_live || !ws_ok(ws)) return SPINDLEKV_INVALID_ARG;
+  return pages_compact_impl(*pool, *table, n_live, ws, ws_bytes, (cudaStream_t)stream);
+}
+
+spindlekv_status spindlekv_paged_append(const spindlekv_page_pool* pool, const spindlekv_page_table* table, const int32_t* start,
+                                        int32_t max_new, spindlekv_tensor K, spindlekv_tensor V, int32_t n_rows, const int32_t* idx,
+                                        int32_t idx_len, int32_t idx_seq, void* stream) {
+  const spindlekv_status ps = pool_table_status(pool, table);
+  if (ps != SPINDLEKV_OK) return ps;
+  if (!start || max_new <= 0 || n_rows <= 0 || !tensor_ok(K) || !tensor_ok(V)) return SPINDLEKV_INVALID_ARG;
+  // every token of a sequence must find its entry of the list inside the list
+  if (idx && (idx_seq < max_new || (int64_t)table->n_seqs * idx_seq > idx_len)) return SPINDLEKV_INVALID_ARG;
+  if (K.dtype != V.dtype) return SPINDLEKV_UNSUPPORTED;
+  return paged_append_impl(*pool, *table, start, max_new, K, V, n_rows, idx, idx_len, idx_seq, (cudaStream_t)stream);
+}
+
+static spindlekv_status paged_shape_status(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t n_q_heads, int32_t n_rows) {
+  const spindlekv_status ps = pool_table_status(pool, table);
+  if (ps != SPINDLEKV_OK) return ps;
+  if (n_q_heads <= 0 || n_q_heads % pool->n_kv_heads || n_rows <= 0) return SPINDLEKV_INVALID_ARG;
+  if (n_q_heads / pool->n_kv_heads > 8 || n_rows > 16) return SPINDLEKV_UNSUPPORTED;
+  return SPINDLEKV_OK;
+}
+
+size_t spindlekv_paged_workspace_bytes(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t n_q_heads, int32_t n_rows) {
+  if (paged_shape_status(pool, table, n_q_heads, n_rows) != SPINDLEKV_OK) return 0;
+  return paged_workspace_bytes(*pool, *table, n_q_heads, n_rows);
+}
+
+spindlekv_status spindlekv_paged_attend(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t n_q_heads,
+                                        int32_t n_rows, int32_t max_len, float scale, spindlekv_tensor q, spindlekv_tensor out,
+                                        void* ws, size_t ws_bytes, void* stream) {
+  const spindlekv_status ps = paged_shape_status(pool, table, n_q_heads, n_rows);
+  if (ps != SPINDLEKV_OK) return ps;
+  if (max_len <= 0 || !(fabsf(scale) < INFINITY) || !tensor_ok(q) || !tensor_ok(out) || !ws_ok(ws)) return SPINDLEKV_INVALID_ARG;
+  if (q.dtype != out.dtype) return SPINDLEKV_UNSUPPORTED;
+  return paged_attend_impl(*pool, *table, n_q_heads, n_rows, max_len, scale, q, out, ws, ws_bytes, (cudaStream_t)stream);
+}
+
+static bool beam_shape_ok(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_t n_out) {
+  if (n_seqs <= 0 || n_beams <= 0 || vocab <= 0 || n_out <= 0) return false;
+  return (int64_t)n_beams * vocab < 0x7FFFFFFF && n_out <= (int64_t)n_beams * vocab;
+}
+
+size_t spindlekv_beam_workspace_bytes(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_t n_out) {
+  if (!beam_shape_ok(n_seqs, n_beams, vocab, n_out) || n_beams > 64 || n_out > 32 || (int64_t)n_seqs * n_beams > 65535) return 0;
+  return beam_workspace_bytes(n_seqs, n_beams, vocab, n_out);
+}
+
+spindlekv_status spindlekv_beam_select(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_t n_out, const void* logits, int32_t dtype,
+                                       int64_t row_stride, const float* score, const uint8_t* finished, int32_t eos, float* out_score,
+                                       int32_t* out_parent, int32_t* out_token, void* ws, size_t ws_bytes, void* stream) {
+  if (!beam_shape_ok(n_seqs, n_beams, vocab, n_out)) return SPINDLEKV_INVALID_ARG;
+  if (!logits || !score || !out_score || !out_parent || !out_token || !ws_ok(ws) || row_stride < 0) return SPINDLEKV_INVALID_ARG;
+  if (dtype != SPINDLEKV_F32 && dtype != SPINDLEKV_BF16) return SPINDLEKV_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(logits) % (dtype == SPINDLEKV_F32 ? 4 : 2)) return SPINDLEKV_INVALID_ARG;
+  if (finished && (eos < 0 || eos >= vocab)) return SPINDLEKV_INVALID_ARG;
+  if (n_beams > 64 || n_out > 32 || (int64_t)n_seqs * n_beams > 65535) return SPINDLEKV_UNSUPPORTED;
+  return beam_select_impl(n_seqs, n_beams, vocab, n_out, logits, dtype, row_stride, score, finished, eos, out_score, out_parent,
+                          out_token, ws, ws_bytes, (cudaStream_t)stream);
 }
 
 spindlekv_status spindlekv_poll_status(const void* ws, int32_t* device_status, int32_t* detail) {

@@ -70,6 +70,7 @@ class SpindleKVPass:
         if self.n_deep:
             self.deep_batch = B.Batch(self.n_deep, self.n_seqs, self.max_len, T, self.cu)
             self.k_ctx = torch.from_numpy(np.ascontiguousarray(self.k_ctx_host[self.n_shallow:])).to(dev)
+            self.kept_lens = torch.from_numpy(np.ascontiguousarray(self.k_ctx_host[self.n_shallow:] + cfg.window, dtype=np.int32)).to(dev)
             self.keep_idx = torch.zeros((self.n_deep, H, T), **i32)
             self.keep_cnt = torch.zeros((self.n_deep, self.n_seqs, H), **i32)
             self.scores = torch.zeros((self.n_deep, H, T), dtype=torch.float32, device=dev)
@@ -175,6 +176,21 @@ class SpindleKVPass:
             self.evict(K[ns:], V[ns:], Q, sE)
             cur.wait_stream(sE)
         cur.wait_stream(sV)
+
+    def store_paged(self, K: torch.Tensor, V: torch.Tensor, cache: "SpindleKVPagedCache", stream=None) -> None:
+        """What the last eviction kept of ``K`` and ``V`` (every layer's, or the evicting layers' alone) becomes the content of
+        ``cache``, whose layers are the evicting ones; what it held is given back.  The kept rows go from the prompt's tensors into
+        the pages in one step.  Equal-length batches."""
+        if self.packed:
+            raise ValueError("store_paged needs sequences of equal length")
+        if (cache.n_layers, cache.n_seqs, cache.Hkv, cache.d) != (self.n_deep, self.n_seqs, self.cfg.n_kv_heads, self.cfg.head_dim):
+            raise ValueError("the cache does not have the evicting layers' shape")
+        if K.shape[0] != self.n_deep:
+            K, V = K[self.n_shallow:], V[self.n_shallow:]
+        cache.resize(cache.no_tokens, stream=stream)
+        cache.resize(self.kept_lens, stream=stream)
+        cache.append(K, V, idx=self.keep_idx, idx_seq=self.max_len, max_new=int(self.k_ctx_host[self.n_shallow:].max()) + self.cfg.window,
+                     stream=stream)
 
     # -- the same pass fed from host memory ----------------------------------------------------
     def host_outputs(self) -> Dict[str, torch.Tensor]:
@@ -524,3 +540,186 @@ class SpindleKVDecodeAttention:
                                   cb_k["ref"], cb_k["mag"], B.desc_bhnd(cb_v["C"]), cb_v["ref"], cb_v["mag"], positions,
                                   self.table, self.out, self.ws, stream)
         return self.out
+
+
+class _OnDevice:
+    """Calls go to the current device and stream; this makes the owner's device current for them where it is not."""
+
+    def _on(self, stream, call) -> None:
+        if torch.cuda.current_device() == self.device.index:
+            call(stream)
+        else:
+            with torch.cuda.device(self.device):
+                call(stream)
+
+    def _mine(self, name: str, t: torch.Tensor, dtype=None, shape=None) -> torch.Tensor:
+        """``t``, if the library may be given its address as it is."""
+        if t.device != self.device or (dtype is not None and t.dtype != dtype) or (shape is not None and tuple(t.shape) != tuple(shape)) \
+                or not t.is_contiguous():
+            want = " ".join(str(x) for x in (dtype, None if shape is None else list(shape)) if x is not None)
+            raise ValueError(f"{name}: contiguous {want} on {self.device} expected, got {t.dtype} {list(t.shape)} on {t.device}")
+        return t
+
+
+def _device_of(device) -> torch.device:
+    dev = torch.device(device)
+    return torch.device(dev.type, torch.cuda.current_device()) if dev.type == "cuda" and dev.index is None else dev
+
+
+class SpindleKVPagedCache(_OnDevice):
+    """A cache in 8 bits on pages: the pool, the page table of ``n_layers`` x ``n_seqs`` sequences, the scratch, and the calls on them.
+    A step of decoding is ``resize(add=1)``, then for every layer ``append`` and ``attend``; a step of beam search ends with ``fork``.
+    ``max_pages`` bounds a sequence's pages, ``n_pages`` the pool's.  All calls of one object must be ordered (one stream, or
+    events): they share its scratch.  Buffers and call order only."""
+
+    def __init__(self, n_layers: int, n_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int, n_pages: int, max_pages: int,
+                 page_size: int = 64, fmt: str = "int8", device="cuda"):
+        dev = _device_of(device)
+        codes = dict(dtype={"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[fmt], device=dev)
+        shape = (n_pages, n_kv_heads, page_size, head_dim)
+        pool = {g + "_codes": torch.zeros(shape, **codes) for g in ("k", "v")}
+        pool.update({g + "_scale": torch.zeros((n_pages, n_kv_heads, page_size // B.PAGED_BLOCK), dtype=torch.float32, device=dev) for g in ("k", "v")})
+        pool["page_ref"] = torch.zeros(n_pages, dtype=torch.int32, device=dev)
+        pages = torch.full((n_layers, n_seqs, max_pages), -1, dtype=torch.int32, device=dev)
+        self._init(pool, pages, torch.zeros((n_layers, n_seqs), dtype=torch.int32, device=dev), n_q_heads)
+
+    @classmethod
+    def over(cls, pool: Dict[str, torch.Tensor], pages: torch.Tensor, lens: torch.Tensor, n_q_heads: Optional[int] = None):
+        """The same over buffers that exist: ``pool`` has ``k_codes``, ``v_codes``, ``k_scale``, ``v_scale`` and ``page_ref``."""
+        self = cls.__new__(cls)
+        self._init(pool, pages, lens, n_q_heads)
+        return self
+
+    def _init(self, pool, pages, lens, n_q_heads) -> None:
+        self.pool = B.PagePool(*(pool[k] for k in ("k_codes", "v_codes", "k_scale", "v_scale", "page_ref")))
+        self.table = B.PageTable(pages, lens)
+        self.device, self.pages, self.lens, self.page_ref = self.pool.device, pages, lens, pool["page_ref"]
+        if pages.device != self.device:
+            raise ValueError(f"pages on {pages.device}, the pool on {self.device}")
+        self.n_layers, self.n_seqs, max_pages = pages.shape
+        self.Hkv, self.page_size, self.d = pool["k_codes"].shape[1:]
+        self.Hq = n_q_heads
+        self.capacity = max_pages * self.page_size
+        n = B.spindlekv_pages_workspace_bytes(self.pool, self.table)
+        if n == 0:
+            raise ValueError(f"unsupported page pool: {tuple(pool['k_codes'].shape)}, table {tuple(pages.shape)}")
+        self.ws_pages = torch.zeros(n, dtype=torch.uint8, device=self.device)
+        self.start = torch.full((self.n_layers, self.n_seqs), -1, dtype=torch.int32, device=self.device)
+        self.no_tokens = torch.zeros((self.n_layers, self.n_seqs), dtype=torch.int32, device=self.device)
+        self.n_live = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._tables = {}
+        self._out: Dict[tuple, torch.Tensor] = {}
+        self.ws_attend = None
+
+    def _rows_of(self, layer: Optional[int]) -> B.PageTable:
+        """The table of all layers, or of one."""
+        if layer is None:
+            return self.table
+        if layer not in self._tables:
+            if not 0 <= layer < self.n_layers:
+                raise IndexError(f"layer {layer} of {self.n_layers}")
+            self._tables[layer] = B.PageTable(self.pages[layer:layer + 1], self.lens[layer:layer + 1])
+        return self._tables[layer]
+
+    def _cache_rows(self, name: str, t: torch.Tensor, n_l: int, heads: int) -> B._Tensor:
+        if t.dim() != 5 or t.shape[0] != n_l or t.shape[1] != self.n_seqs or t.shape[2] != heads or t.shape[4] != self.d or t.device != self.device:
+            raise ValueError(f"{name}: [{n_l}, {self.n_seqs}, {heads}, rows, {self.d}] on {self.device} expected, got {list(t.shape)} on {t.device}")
+        return B.desc_bhnd(t)
+
+    def resize(self, new_lens: Optional[torch.Tensor] = None, add: int = 0, stream=None) -> torch.Tensor:
+        """Pages for new lengths (``[n_layers, n_seqs]`` int32 on the device, or every length plus ``add``).  Returns ``start``, where
+        ``append`` goes on; ``status()`` tells when there were too few pages."""
+        if new_lens is not None:
+            self._mine("new_lens", new_lens, torch.int32, (self.n_layers, self.n_seqs))
+        self._on(stream, lambda st: B.spindlekv_pages_resize(self.pool, self.table, new_lens, add, self.start, self.ws_pages, st))
+        return self.start
+
+    def append(self, K: torch.Tensor, V: torch.Tensor, start: Optional[torch.Tensor] = None, idx: Optional[torch.Tensor] = None,
+               idx_seq: Optional[int] = None, max_new: Optional[int] = None, layer: Optional[int] = None, stream=None) -> None:
+        """Writes tokens ``start .. lens-1`` (``start`` of the last ``resize`` by default) from rows ``[n_layers or 1, n_seqs, H_kv, rows, d]``;
+        with ``idx`` ``[n_layers or 1, H_kv, n_seqs * idx_seq]`` from the rows it names."""
+        table = self._rows_of(layer)
+        n_l = table.c.n_layers
+        if start is None:
+            start = self.start
+        if layer is not None and start.shape[0] == self.n_layers:
+            start = start[layer:layer + 1]
+        self._mine("start", start, torch.int32, (n_l, self.n_seqs))
+        if V.shape[3] != K.shape[3]:
+            raise ValueError("K and V have different numbers of rows")
+        if idx is not None:
+            self._mine("idx", idx, torch.int32)
+            if idx.dim() != 3 or idx.shape[0] != n_l or idx.shape[1] != self.Hkv:
+                raise ValueError(f"idx: [{n_l}, {self.Hkv}, n_seqs * idx_seq] expected, got {list(idx.shape)}")
+            idx_seq = idx.shape[2] // self.n_seqs if idx_seq is None else idx_seq
+        if max_new is None:
+            max_new = K.shape[3] if idx is None else idx_seq
+        k, v = self._cache_rows("K", K, n_l, self.Hkv), self._cache_rows("V", V, n_l, self.Hkv)
+        self._on(stream, lambda st: B.spindlekv_paged_append(self.pool, table, start, max_new, k, v, K.shape[3], idx, idx_seq or 0, st))
+
+    def attend(self, q: torch.Tensor, out: Optional[torch.Tensor] = None, max_len: Optional[int] = None, scale: float = 0.0,
+               layer: Optional[int] = None, stream=None) -> torch.Tensor:
+        """Attention of the last ``rows`` tokens, ``q`` ``[n_layers or 1, n_seqs, H_q, rows, d]``.  Without ``out`` the result lies in a
+        buffer of this object that the next call of the same shape overwrites.  ``max_len`` (the longest sequence, a capacity by
+        default) sizes the split."""
+        table = self._rows_of(layer)
+        n_l = table.c.n_layers
+        hq = q.shape[2] if self.Hq is None else self.Hq
+        qd = self._cache_rows("q", q, n_l, hq)
+        rows = q.shape[3]
+        if out is None:
+            key = (q.shape, q.dtype)
+            out = self._out.get(key)
+            if out is None:
+                out = self._out[key] = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+        elif out.shape != q.shape:
+            raise ValueError(f"out: {list(q.shape)} expected, got {list(out.shape)}")
+        od = self._cache_rows("out", out, n_l, hq)
+        if self.ws_attend is None:
+            need = B.spindlekv_paged_workspace_bytes(self.pool, self.table, hq, 16)
+            self.ws_attend = torch.empty(need, dtype=torch.uint8, device=self.device)
+        self._on(stream, lambda st: B.spindlekv_paged_attend(self.pool, table, hq, rows, max_len or self.capacity, scale, qd, od, self.ws_attend, st))
+        return out
+
+    def fork(self, parent: torch.Tensor, stream=None) -> None:
+        """Sequence ``i`` becomes what sequence ``parent[i]`` was (int32 ``[n_seqs]`` on the device; -1: empty), in every layer."""
+        self._mine("parent", parent, torch.int32, (self.n_seqs,))
+        self._on(stream, lambda st: B.spindlekv_pages_fork(self.pool, self.table, parent, self.ws_pages, st))
+
+    def compact(self, stream=None) -> torch.Tensor:
+        """Live pages to the lowest page numbers; returns their number (a device tensor)."""
+        self._on(stream, lambda st: B.spindlekv_pages_compact(self.pool, self.table, self.n_live, self.ws_pages, st))
+        return self.n_live
+
+    def status(self) -> int:
+        """Status word of the last ``resize``, ``fork`` or ``compact`` (synchronises the device)."""
+        torch.cuda.synchronize(self.device)
+        return B.spindlekv_poll_status(self.ws_pages)[0]
+
+
+class SpindleKVBeamSelect(_OnDevice):
+    """Beam search's selection for batches of one shape: scratch and result buffers of ``spindlekv_beam_select``."""
+
+    def __init__(self, n_seqs: int, n_beams: int, vocab: int, n_out: Optional[int] = None, device="cuda"):
+        self.n_seqs, self.n_beams, self.vocab, self.n_out = n_seqs, n_beams, vocab, n_beams if n_out is None else n_out
+        self.device = dev = _device_of(device)
+        n = B.spindlekv_beam_workspace_bytes(n_seqs, n_beams, vocab, self.n_out)
+        if n == 0:
+            raise ValueError(f"unsupported beam search: {n_seqs} x {n_beams} beams, vocabulary {vocab}, {self.n_out} wanted")
+        self.ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        self.score = torch.empty((n_seqs, self.n_out), dtype=torch.float32, device=dev)
+        self.parent = torch.empty((n_seqs, self.n_out), dtype=torch.int32, device=dev)
+        self.token = torch.empty((n_seqs, self.n_out), dtype=torch.int32, device=dev)
+
+    def run(self, logits: torch.Tensor, score: torch.Tensor, finished: Optional[torch.Tensor] = None, eos: int = 0, stream=None):
+        """``logits`` ``[n_seqs * n_beams, vocab]`` (any row stride), ``score`` and ``finished`` (bool) ``[n_seqs * n_beams]``.  Returns
+        ``(score, parent, token)``, each ``[n_seqs, n_out]``, best first, in buffers that the next call overwrites."""
+        rows = self.n_seqs * self.n_beams
+        if tuple(logits.shape) != (rows, self.vocab) or (self.vocab > 1 and logits.stride(1) != 1) or logits.device != self.device:
+            raise ValueError(f"logits: [{rows}, {self.vocab}] on {self.device} expected, got {list(logits.shape)} on {logits.device}")
+        self._mine("score", score, torch.float32, (rows,))
+        if finished is not None:
+            self._mine("finished", finished, torch.bool, (rows,))
+        self._on(stream, lambda st: B.spindlekv_beam_select(self.n_seqs, self.n_beams, self.vocab, self.n_out, logits, score, finished, eos,
+                                                           self.score, self.parent, self.token, self.ws, st))
+        return self.score, self.parent, self.token

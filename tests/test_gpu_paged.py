@@ -1,0 +1,544 @@
+"""The 8-bit paged cache on the GPU against float64 forms: codes, scales, tables and reference counts exactly, attention within
+bounds derived from its roundings."""
+import numpy as np
+import pytest
+import torch
+
+import paged_ref as R
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def make(n_layers, n_seqs, hq, h, d, n_pages, max_pages, ps, fmt, seed=0):
+    """A cache whose memory holds leftovers: every byte pattern in the codes, NaN in the scales."""
+    from paper_2507_06517_b200.pipeline import SpindleKVPagedCache
+    c = SpindleKVPagedCache(n_layers, n_seqs, hq, h, d, n_pages, max_pages, ps, fmt)
+    gen = torch.Generator().manual_seed(seed)
+    k, v, ks, vs, _ = c.pool.tensors
+    for t in (k, v):
+        t.view(torch.uint8).copy_(torch.randint(0, 256, t.shape, generator=gen, dtype=torch.int32).to(torch.uint8))
+    for t in (ks, vs):
+        t.fill_(float("nan"))
+    c.pages.fill_(2 ** 31 - 1)
+    return c
+
+
+def ref_of(c):
+    k, v, ks, vs, ref = (t.view(torch.uint8) if i < 2 else t for i, t in enumerate(c.pool.tensors))
+    return R.RefCache(*(x.cpu().numpy() for x in (k, v, ks, vs, ref, c.pages, c.lens)), "int8" if c.pool.c.format == 0 else "e4m3")
+
+
+def same_state(c, r):
+    now = ref_of(c)
+    for what in ("ref", "lens", "pages"):
+        assert np.array_equal(getattr(now, what), getattr(r, what)), what
+    for g in "kv":
+        assert np.array_equal(now.scale[g].view(np.uint32) & 0x7FFFFFFF, r.scale[g].view(np.uint32) & 0x7FFFFFFF) \
+            or np.array_equal(now.scale[g], r.scale[g], equal_nan=True), g
+        assert np.array_equal(now.codes[g], r.codes[g]), g
+
+
+def lens_t(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def rows(shape, dtype, seed, spread=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    x = torch.randn(shape, generator=gen) * torch.exp(spread * torch.randn(shape[:-1] + (1,), generator=gen))
+    return x.to(DT[dtype]).cuda()
+
+
+def fill(c, lens, dtype="bf16", seed=1, spread=1.0):
+    """Gives the sequences these lengths and writes random rows into what is new; the reference does the same."""
+    r = ref_of(c)
+    start = r.resize(np.array(lens))
+    assert start is not None
+    c.resize(lens_t(lens))
+    n = max(1, int((np.array(lens) - start).max()))
+    K, V = (rows((c.n_layers, c.n_seqs, c.Hkv, n, c.d), dtype, seed + i, spread) for i in (0, 100))
+    c.append(K, V)
+    r.append(start, f64(K), f64(V))
+    return r
+
+
+# ---- append ------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,ps", [(64, 16), (128, 64)])
+def test_append_writes_the_same_codes_and_scales(fmt, dtype, d, ps):
+    c = make(2, 4, None, 3, d, 60, 240 // ps, ps, fmt)
+    r = ref_of(c)
+    was = r.lens.copy()
+    # nothing, one token, a block's end and beyond it; then on from there, with larger values so that open blocks are rescaled
+    for step, (lens, spread) in enumerate([([[0, 1, 15, 16], [17, 33, 47, 64]], 0.5), ([[1, 2, 16, 17], [17, 34, 90, 65]], 2.0),
+                                           ([[1, 30, 50, 17], [80, 35, 100, 66]], 3.0), ([[2, 31, 51, 18], [81, 36, 101, 67]], 3.0)]):
+        r = fill(c, lens, dtype, seed=10 * step, spread=spread)
+        assert c.status() == 0
+        same_state(c, r)
+    assert not np.array_equal(was, r.lens)
+
+
+def test_append_takes_rows_in_any_order_and_from_strided_tensors():
+    fmt, d, h, n = "int8", 128, 2, 50
+    c = make(2, 3, None, h, d, 40, 4, 32, fmt)
+    lens = [[50, 7, 0], [33, 16, 50]]
+    r = ref_of(c)
+    start = r.resize(np.array(lens))
+    c.resize(lens_t(lens))
+    # token-major tensors [L, B, row, head, d] with a gap behind every row; rows picked from 70 by lists with numbers outside
+    K, V = (rows((2, 3, 70, h, 2 * d), "bf16", s)[..., :d].transpose(2, 3) for s in (1, 2))
+    idx = torch.randint(-3, 75, (2, h, 3 * n), generator=torch.Generator().manual_seed(3), dtype=torch.int32).cuda()
+    c.append(K, V, idx=idx)
+    r.append(start, f64(K), f64(V), idx.cpu().numpy(), n)
+    same_state(c, r)
+    c.append(K, V, start=lens_t([[-1, 7, 3], [40, -1, 50]]), max_new=50)      # nothing but tokens 40 .. 49 of none: start >= lens or < 0
+    same_state(c, r)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_append_shows_a_nan_or_infinity_in_the_blocks_scale(fmt, bad):
+    c = make(1, 2, None, 1, 64, 8, 2, 32, fmt)
+    fill(c, [[20, 20]], "f32")
+    r = ref_of(c)
+    start = r.resize(np.array([[21, 38]]))
+    c.resize(lens_t([[21, 38]]))
+    K, V = rows((1, 2, 1, 18, 64), "f32", 5), rows((1, 2, 1, 18, 64), "f32", 6)
+    K[0, 0, 0, 0, 63] = bad
+    V[0, 1, 0, 17, 0] = bad
+    c.append(K, V)
+    r.append(start, np.where(np.isfinite(f64(K)), f64(K), np.nan), np.where(np.isfinite(f64(V)), f64(V), np.nan))
+    same_state(c, r)
+    assert np.isnan(r.scale["k"]).sum() > 0
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_append_of_zeros_and_of_the_smallest_and_largest_numbers(fmt):
+    c = make(1, 5, None, 1, 64, 8, 1, 32, fmt)
+    r = ref_of(c)
+    start = r.resize(np.full((1, 5), 16))
+    c.resize(lens_t([[16] * 5]))
+    K = torch.randn((1, 5, 1, 16, 64), generator=torch.Generator().manual_seed(1)).cuda()
+    for s, f in enumerate((0.0, 1e-44, 1e-38, 1e-30, 1e37)):
+        K[0, s] *= f
+    K[0, 4, 0, 0, 0] = 3.4e38
+    c.append(K, -K)
+    r.append(start, f64(K), f64(-K))
+    same_state(c, r)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_int8_codes_on_exact_halves_go_to_even(dtype):
+    # amax 127 gives scale 1: k + 1/2 must go to the even neighbour, whatever the reciprocal rounds to
+    c = make(1, 1, None, 1, 128, 4, 1, 16, "int8")
+    r = ref_of(c)
+    start = r.resize(np.array([[16]]))
+    c.resize(lens_t([[16]]))
+    K = (torch.arange(16 * 128) % 254 / 2 - 63.5).view(1, 1, 1, 16, 128).to(DT[dtype]).cuda()
+    K[..., 0, 0] = 127
+    V = K * 3                                       # scale 3: quotients that only nearly are halves
+    c.append(K, V)
+    r.append(start, f64(K), f64(V))
+    same_state(c, r)
+
+
+def test_append_leaves_out_tokens_on_pages_outside_the_pool():
+    c = make(1, 2, None, 1, 64, 8, 4, 16, "int8")
+    r = fill(c, [[40, 40]])
+    c.pages[0, 0, 1] = -7
+    c.pages[0, 1, 2] = 8
+    before = ref_of(c)
+    K = rows((1, 2, 1, 40, 64), "bf16", 9)
+    c.append(K, K, start=lens_t([[0, 0]]))
+    after = ref_of(c)
+    for s, gone in ((0, 1), (1, 2)):
+        assert np.array_equal(after.codes["k"][r.pages[0, s, gone]], before.codes["k"][r.pages[0, s, gone]])
+        assert not np.array_equal(after.codes["k"][r.pages[0, s, 0]], before.codes["k"][r.pages[0, s, 0]])
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------
+
+def check_attention(c, r, q, out, dtype, scale=None):
+    """|error| <= half a step of the output type, plus A = sum of weight * |value| times: the weight's rounding to fp16 pieces (2^-12
+    for one, 2^-22 for two), and twice the relative error of a weight.  That is the absolute error of its score: d + 16 fp32
+    additions and products, each 2^-23 of S = sum |q_i k_i| * scale at most (the tensor cores cut off where a sum would round), the query's own pieces
+    (2^-22 of S, fp32 only) and 2^-20 for the power function and the score's own fp32 step (scores below 16 here).  What fades out of
+    fp16 is below 2^-30 of the largest value per token."""
+    want, mag, top = r.attend(f64(q), scale)
+    got = f64(out)
+    half = torch.finfo(DT[dtype]).eps / 2
+    weight = 2.0 ** -12 if dtype == "bf16" else 2.0 ** -22
+    err = ((c.d + 16) * 2.0 ** -23 + (0 if dtype == "bf16" else 2.0 ** -22)) * top[..., None] + 2.0 ** -20
+    big = max(np.nanmax(np.abs(r.rows("v", l, s)[0]), initial=0.0) for l, s in r.units())
+    bound = half * np.abs(want) + mag * (weight + 2 * err) * 1.01 + r.lens.max() * big * 2.0 ** -30
+    assert np.isfinite(got).all()
+    worst = (np.abs(got - want) / np.maximum(bound, 1e-300)).max()
+    assert worst <= 1, worst
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,ps,h,hn,n_rows", [(128, 64, 2, 4, 1), (64, 16, 3, 1, 1), (128, 32, 1, 8, 1), (64, 128, 2, 7, 2), (128, 16, 2, 8, 3),
+                                             (128, 64, 1, 5, 5), (64, 32, 2, 8, 16), (128, 128, 1, 8, 16), (128, 16, 4, 2, 4)])
+def test_attention_matches_float64(fmt, dtype, d, ps, h, hn, n_rows):
+    c = make(2, 6, hn * h, h, d, 2 * 6 * (640 // ps), 640 // ps, ps, fmt)
+    r = fill(c, [[0, 1, 15, 16, 17, 333], [2, 5, 31, 64, 130, 640]], dtype, spread=0.3)
+    q = rows((2, 6, hn * h, n_rows, d), dtype, 77, 0.2)
+    out = c.attend(q, max_len=640)
+    check_attention(c, r, q, out, dtype)
+    seen = r.lens[:, :, None] - n_rows + 1 + np.arange(n_rows)
+    assert (f64(out).transpose(0, 1, 3, 2, 4)[seen <= 0] == 0).all()        # rows that see nothing
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("max_len", [1, 700, 100000])
+def test_attention_over_many_runs_whatever_the_length_hint(dtype, max_len):
+    # one unit over many runs, runs over several units, and a hint far from the truth
+    c = make(1, 3, 8, 2, 128, 400, 320, 16, "int8")
+    r = fill(c, [[5000, 3, 700]], dtype, spread=0.3)
+    q = rows((1, 3, 8, 1, 128), dtype, 5, 0.2)
+    check_attention(c, r, q, c.attend(q, max_len=max_len), dtype)
+
+
+def test_attention_with_very_uneven_scales():
+    # a value of 1e30 that has no weight must not drown the others, nor one of 1e-30 with all of it
+    c = make(1, 2, 2, 1, 64, 20, 4, 32, "int8")
+    K, V = torch.zeros((1, 2, 1, 100, 64), device="cuda"), rows((1, 2, 1, 100, 64), "f32", 3, 0.1)
+    K[0, 0, 0, 40, 0] = -1e4
+    V[0, 0, 0, 40] = 1e30
+    K[0, 1, 0, 40, 0] = 1e4
+    V[0, 1, 0, 40] = 1e-30
+    r = ref_of(c)
+    start = r.resize(np.full((1, 2), 100))
+    c.resize(lens_t([[100, 100]]))
+    c.append(K, V)
+    r.append(start, f64(K), f64(V))
+    q = torch.zeros((1, 2, 2, 1, 64), device="cuda")
+    q[..., 0] = 1.0
+    got, (want, mag, _) = f64(c.attend(q)), r.attend(f64(q))
+    assert (np.abs(got - want) <= 1e-5 * mag + 1e-45).all()
+    # the value of 1e-30 shares a block, and so a scale, with values near 1: its code is 0
+    assert np.abs(want[0, 0]).max() < 10 and (want[0, 1] == 0).all()
+
+
+def test_attention_with_a_block_of_tiny_values():
+    # all the weight on a block of its own scale, 1e-30 of its neighbours'
+    c = make(1, 1, 2, 1, 64, 20, 4, 32, "e4m3")
+    K, V = torch.zeros((1, 1, 1, 100, 64), device="cuda"), rows((1, 1, 1, 100, 64), "f32", 3, 0.1)
+    K[0, 0, 0, 32:48, 0] = 1e4
+    V[0, 0, 0, 32:48] *= 1e-30
+    r = ref_of(c)
+    start = r.resize(np.full((1, 1), 100))
+    c.resize(lens_t([[100]]))
+    c.append(K, V)
+    r.append(start, f64(K), f64(V))
+    q = torch.zeros((1, 1, 2, 1, 64), device="cuda")
+    q[..., 0] = 1.0
+    got, (want, mag, _) = f64(c.attend(q)), r.attend(f64(q))
+    assert (np.abs(got - want) <= 1e-5 * mag).all() and 0 < np.abs(want).max() < 1e-29
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [1e-30, 1e30])
+def test_attention_with_tiny_and_huge_queries(dtype, size):
+    c = make(1, 1, 4, 1, 128, 8, 2, 64, "e4m3")
+    r = fill(c, [[90]], dtype, spread=0.3)
+    q = (rows((1, 1, 4, 1, 128), "f32", 5, 0.2) * size).to(DT[dtype])
+    check_attention(c, r, q, c.attend(q, scale=0.1 / size), dtype, scale=0.1 / size)
+
+
+def test_attention_of_poisoned_blocks_reaches_only_rows_that_see_them():
+    c = make(1, 2, 4, 2, 64, 16, 3, 16, "int8")
+    fill(c, [[32, 32]], "f32", spread=0.3)
+    r = ref_of(c)
+    start = r.resize(np.full((1, 2), 33))
+    c.resize(lens_t([[33, 33]]))
+    K, V = rows((1, 2, 2, 1, 64), "f32", 1), rows((1, 2, 2, 1, 64), "f32", 2)
+    K[0, 0, 1] = float("nan")
+    V[0, 1, 0] = float("inf")
+    c.append(K, V)
+    q = rows((1, 2, 4, 2, 64), "f32", 3)
+    nan = np.isnan(f64(c.attend(q))).all(-1)
+    want = np.zeros((1, 2, 4, 2), bool)
+    want[0, 0, 2:, 1] = want[0, 1, :2, 1] = True           # the last row alone, of the KV head that holds it
+    assert np.array_equal(nan, want)
+    r.append(start, np.nan_to_num(f64(K)), np.where(np.isinf(f64(V)), 0, f64(V)))
+    clean, _, _ = r.attend(f64(q))
+    got = f64(c._out[(q.shape, q.dtype)])
+    assert np.abs(got - clean)[~want].max() < 1e-4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_with_nan_or_infinite_queries_keeps_to_their_rows(dtype):
+    c = make(1, 1, 4, 1, 64, 8, 4, 16, "int8")
+    r = fill(c, [[50]], dtype, spread=0.3)
+    q = rows((1, 1, 4, 2, 64), dtype, 3)
+    clean = f64(c.attend(q).clone())
+    q[0, 0, 1, 0, 5] = float("nan")
+    q[0, 0, 2, 1, 7] = float("inf")
+    got = f64(c.attend(q))
+    bad = np.zeros((1, 1, 4, 2), bool)
+    bad[0, 0, 1, 0] = bad[0, 0, 2, 1] = True
+    assert np.isnan(got[bad]).all() and np.array_equal(got[~bad], clean[~bad])
+    assert r.lens[0, 0] == 50
+
+
+def test_attention_leaves_out_tokens_on_pages_outside_the_pool():
+    c = make(1, 2, 4, 2, 128, 16, 8, 16, "e4m3")
+    fill(c, [[100, 20]], spread=0.3)
+    c.pages[0, 0, 2] = -1
+    c.pages[0, 0, 4] = 16
+    c.pages[0, 1, :] = 1 << 30                     # none left: zeros
+    q = rows((1, 2, 4, 1, 128), "bf16", 4, 0.2)
+    out = c.attend(q)
+    check_attention(c, ref_of(c), q, out, "bf16")
+    assert (out[0, 1] == 0).all()
+
+
+def test_attention_clamps_lengths_to_the_table():
+    c = make(1, 2, 2, 1, 64, 8, 2, 16, "int8")
+    r = fill(c, [[32, 32]], spread=0.3)
+    c.lens.copy_(lens_t([[2 ** 31 - 1, -5]]))
+    q = rows((1, 2, 2, 1, 64), "bf16", 4, 0.2)
+    out = c.attend(q)
+    r.lens = np.array([[32, 0]])
+    check_attention(c, r, q, out, "bf16")
+
+
+def test_attention_strides_streams_graphs_and_bits():
+    from paper_2507_06517_b200.pipeline import record_graph
+    c = make(2, 3, 8, 2, 128, 200, 64, 32, "int8")
+    r = fill(c, [[1000, 40, 2000], [16, 999, 1]], spread=0.3)
+    wide = rows((2, 3, 3, 8, 2 * 128), "bf16", 4, 0.2)
+    q = wide[..., :128].transpose(2, 3)                           # [L, B, Hq, rows, d], token-major with a gap
+    held = torch.full((2, 3, 3, 8, 2 * 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = held[..., 128:].transpose(2, 3)
+    c.attend(q, out=out)
+    check_attention(c, r, q, out, "bf16")
+    assert (held[..., :128] == 7).all()
+    first = out.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    c.attend(q, out=out, stream=side)
+    side.synchronize()
+    assert torch.equal(out, first)
+    graph = record_graph(lambda: c.attend(q, out=out))
+    out.zero_()
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, first)
+    for layer in range(2):                                        # one layer at a time, from the same table
+        got = c.attend(q[layer:layer + 1].contiguous(), layer=layer, max_len=2000)
+        r1 = ref_of(c)
+        r1.pages, r1.lens, r1.n_layers = r1.pages[layer:layer + 1], r1.lens[layer:layer + 1], 1
+        check_attention(c, r1, q[layer:layer + 1], got, "bf16")
+
+
+def test_attention_over_a_pool_beyond_four_gigabytes():
+    # the pages of one sequence at both ends of a pool whose byte offsets pass 32 bits
+    from paper_2507_06517_b200.pipeline import SpindleKVPagedCache
+    n = (5 << 30) // (8 * 128 * 128)
+    c = SpindleKVPagedCache(1, 1, 8, 8, 128, n, 8, 128, "int8")
+    c.pages.copy_(torch.tensor([[[n - 1, 0, n - 2, 1, n // 2, n - 3, 2, n - 4]]], dtype=torch.int32))
+    c.page_ref[c.pages.view(-1).long()] = 1
+    c.lens.fill_(1000)
+    K, V = rows((1, 1, 8, 1000, 128), "bf16", 1, 0.3), rows((1, 1, 8, 1000, 128), "bf16", 2, 0.3)
+    c.append(K, V, start=lens_t([[0]]))
+    q = rows((1, 1, 8, 1, 128), "bf16", 4, 0.2)
+    got = c.attend(q).clone()
+    small = SpindleKVPagedCache(1, 1, 8, 8, 128, 8, 8, 128, "int8")
+    small.resize(lens_t([[1000]]))
+    small.append(K, V)
+    assert torch.equal(got, small.attend(q))
+    assert int(c.compact()) == 8
+    assert torch.equal(c.attend(q), got)
+
+
+# ---- pages -------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt,ps,d,h", [("int8", 16, 64, 3), ("e4m3", 64, 128, 2)])
+def test_random_histories_of_page_operators(fmt, ps, d, h):
+    rng = np.random.default_rng(ps)
+    c = make(3, 7, 2 * h, h, d, 150, 5, ps, fmt)
+    for step in range(25):
+        r = ref_of(c)
+        what = rng.integers(0, 4)
+        if what == 0:
+            lens = rng.integers(0, 5 * ps + 1, (3, 7))
+            fits = r.resize(lens)
+            c.resize(lens_t(lens))
+            if fits is None:
+                assert c.status() == 4 and (c.start == -1).all()           # capacity
+            else:
+                assert c.status() == 0 and np.array_equal(c.start.cpu().numpy(), fits)
+                n = max(1, int((lens - fits).max()))
+                K, V = rows((3, 7, h, n, d), "bf16", step), rows((3, 7, h, n, d), "bf16", step + 50)
+                c.append(K, V)
+                r.append(fits, f64(K), f64(V))
+        elif what == 1:
+            add = int(rng.integers(-3, 4))
+            ok = r.resize(r.lens + add)
+            c.resize(add=add)
+            assert c.status() == (0 if ok is not None else 1 if (r.lens + add < 0).any() or (r.lens + add > 5 * ps).any() else 4)
+            if ok is not None:          # what a new token holds before it is written is nobody's business
+                K, V = rows((3, 7, h, 3, d), "bf16", step), rows((3, 7, h, 3, d), "bf16", step + 50)
+                c.append(K, V)
+                r.append(ok, f64(K), f64(V))
+        elif what == 2:
+            parent = rng.integers(-1 if rng.random() < 0.3 else 0, 7, 7)
+            ok = r.fork(parent)
+            c.fork(lens_t(parent))
+            assert c.status() == (0 if ok else 4)
+        else:
+            assert int(c.compact()) == r.compact()
+            assert c.status() == 0
+        same_state(c, r)
+        n = int((r.ref > 0).sum())
+        counted = np.zeros_like(r.ref)
+        for l, s in r.units():
+            np.add.at(counted, r.pages[l, s, :r.count(r.lens[l, s])], 1)
+        assert np.array_equal(counted, r.ref) and n <= 150                 # every reference is a table entry
+
+
+def test_page_operators_refuse_on_the_device_and_change_nothing():
+    c = make(1, 3, 2, 1, 64, 4, 4, 16, "int8")
+    r = fill(c, [[20, 16, 16]])
+    for lens in ([[20, 16, 17]], [[20, 16, 65]], [[20, -1, 16]], [[2 ** 31 - 1, 0, 0]]):
+        c.resize(lens_t(lens))
+        assert c.status() == (4 if lens[0][2] == 17 else 1)
+        assert (c.start == -1).all()
+        c.append(rows((1, 3, 1, 8, 64), "bf16", 1), rows((1, 3, 1, 8, 64), "bf16", 1))      # start -1: nothing is written
+        same_state(c, r)
+    for parent, why in (([0, 0, 1], 4), ([0, 1, 3], 1), ([-2, 1, 2], 1)):
+        c.fork(lens_t(parent))
+        assert c.status() == why
+        same_state(c, r)
+    c.resize(c.no_tokens)
+    assert c.status() == 0 and (c.page_ref == 0).all()
+
+
+def test_fork_of_many_sequences_and_of_wide_tables():
+    # more sequences than threads of a copying block, tables wider than a tile, full and open pages
+    c = make(2, 300, 2, 1, 64, 9000, 75, 16, "int8")
+    rng = np.random.default_rng(1)
+    lens = np.where(rng.random((2, 300)) < 0.03, rng.integers(1, 75 * 16 + 1, (2, 300)), rng.integers(0, 40, (2, 300)))
+    r = fill(c, lens.tolist())
+    parent = rng.integers(-1, 300, 300)
+    assert r.fork(parent)
+    c.fork(lens_t(parent))
+    assert c.status() == 0
+    same_state(c, r)
+
+
+def test_page_operators_in_a_graph():
+    from paper_2507_06517_b200.pipeline import record_graph
+    c = make(2, 4, 2, 1, 64, 64, 8, 16, "e4m3")
+    fill(c, [[20, 3, 0, 17], [1, 1, 40, 2]])
+    r = ref_of(c)
+    parent = lens_t([1, 0, 2, 2])
+    K, V = rows((2, 4, 1, 1, 64), "bf16", 1), rows((2, 4, 1, 1, 64), "bf16", 2)
+
+    def step():
+        c.fork(parent)
+        c.resize(add=1)
+        c.append(K, V)
+
+    graph = record_graph(step)          # runs once beforehand
+    graph.replay()
+    torch.cuda.synchronize()
+    for _ in range(2):
+        assert r.fork([1, 0, 2, 2])
+        start = r.resize(r.lens + 1)
+        r.append(start, f64(K), f64(V))
+    assert c.status() == 0
+    same_state(c, r)
+
+
+# ---- as they are used --------------------------------------------------------------------------------------------
+
+def test_python_layer_refuses_before_launching():
+    c = make(2, 3, 4, 2, 64, 16, 4, 16, "int8")
+    q = rows((2, 3, 4, 1, 64), "bf16", 1)
+    with pytest.raises(ValueError):
+        c.attend(q.cpu())
+    with pytest.raises(ValueError):
+        c.attend(q[:1])
+    with pytest.raises(ValueError):
+        c.attend(q, out=q[:, :, :2])
+    with pytest.raises(IndexError):
+        c.attend(q[:1], layer=2)
+    with pytest.raises(ValueError):
+        c.fork(torch.zeros(3, dtype=torch.int64, device="cuda"))
+    with pytest.raises(ValueError):
+        c.resize(torch.zeros((2, 3), dtype=torch.int32))
+    with pytest.raises(ValueError):
+        c.append(q, q)
+    with pytest.raises(ValueError):
+        c.append(q[:, :, :2], q[:, :, :2], idx=torch.zeros((2, 3, 3), dtype=torch.int32, device="cuda"))
+    from paper_2507_06517_b200.binding import SpindleKVError
+    with pytest.raises(SpindleKVError):
+        c.attend(rows((2, 3, 4, 17, 64), "bf16", 1))
+
+
+def test_evicted_prompt_decodes_from_the_paged_cache():
+    # eviction of a prompt, what it kept stored in 8 bits, then decoding with beams: fork, resize, append, attend per layer.
+    # The float64 reference takes the same steps from the rows that eviction kept
+    from gpu_util import generate, make_config, stack_layers, torch_dtype
+    from paper_2507_06517_b200 import synth
+    from paper_2507_06517_b200.pipeline import SpindleKVBeamSelect, SpindleKVPagedCache, SpindleKVPass
+    wl = synth.Workload("paged", 3, 1, 8, 2, 128, "bf16", 32, (700, 700), 40, (0.05, 0.3), 4, "recency", budget_tokens=200.0, seed=21)
+    host = generate(wl)
+    p = SpindleKVPass(make_config(wl), wl.seq_lens, torch_dtype(wl))
+    layers = [0, 1, 2]
+    K, V = stack_layers(wl, host, layers, "K"), stack_layers(wl, host, layers, "V")
+    p.run(K, V, stack_layers(wl, host, [1, 2], "Q"))
+    c = SpindleKVPagedCache(2, 2, 8, 2, 128, 64, 12, 32, "int8")
+    p.store_paged(K, V, c)
+    assert c.status() == 0
+    r = ref_of(c)
+    keep = p.keep_idx.cpu().numpy()
+    fresh = R.RefCache(*(np.zeros_like(x) for x in (r.codes["k"], r.codes["v"], r.scale["k"], r.scale["v"], r.ref, r.pages, r.lens)), "int8")
+    fresh.pages[:] = -1
+    start = fresh.resize(p.kept_lens.cpu().numpy())
+    fresh.append(start, f64(K[1:]), f64(V[1:]), keep, 700)
+    same_state(c, fresh)
+    # against the kept rows themselves: rounding moves a value by half a step of its block's scale at most
+    for l in range(2):
+        for s in range(2):
+            n = int(fresh.lens[l, s])
+            for g, kept in (("k", p.K_kept), ("v", p.V_kept)):
+                step = np.repeat(fresh.scale[g][fresh.pages[l, s, :fresh.count(n)]].transpose(1, 0, 2).reshape(2, -1), 16, 1)[:, :n, None]
+                assert (np.abs(fresh.rows(g, l, s)[0] - f64(kept[l, s, :, :n])) <= 0.5 * step).all()
+    select = SpindleKVBeamSelect(1, 2, 1000)
+    rng = np.random.default_rng(2)
+    score = torch.zeros(2, device="cuda")
+    for step in range(20):
+        r = fresh
+        logits = torch.from_numpy(rng.standard_normal((2, 1000)).astype(np.float32)).cuda()
+        new_score, parent, _ = select.run(logits, score)
+        want = R.beam(f64(logits), f64(score), 2, 2)
+        assert np.array_equal(parent.cpu().numpy(), want[1])
+        score = new_score.view(-1).clone()
+        c.fork(parent.view(-1))
+        assert r.fork(want[1][0].tolist())
+        c.resize(add=1)
+        at = r.resize(r.lens + 1)
+        k1, v1, q = (rows((2, 2, n, 1, 128), "bf16", 3 * step + i, 0.2) for i, n in enumerate((2, 2, 8)))
+        outs = []
+        for l in range(2):
+            c.append(k1[l:l + 1], v1[l:l + 1], layer=l)
+            outs.append(c.attend(q[l:l + 1], layer=l, max_len=230).clone())
+        r.append(at, f64(k1), f64(v1))
+        check_attention(c, r, q, torch.cat(outs), "bf16")
+    assert c.status() == 0
+    same_state(c, r)
