@@ -216,9 +216,18 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _stream(stream) -> int:
+    if type(stream) is int:
+        return stream
     if stream is None:
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+try:
+    raw_stream = torch._C._cuda_getCurrentRawStream      # the handle alone, without a stream object around it
+except AttributeError:
+    def raw_stream(device_index: int) -> int:
+        return torch.cuda.current_stream(device_index).cuda_stream
 
 
 def _check(status: int, where: str) -> None:
@@ -401,7 +410,7 @@ class PageTable:
             raise ValueError("pages [n_layers, n_seqs, max_pages] and lens [n_layers, n_seqs] are int32 and fit together")
         if not (pages.is_contiguous() and lens.is_contiguous() and pages.device == lens.device):
             raise ValueError("pages and lens are contiguous and on one device")
-        self.pages, self.lens = pages, lens
+        self.pages, self.lens, self.n_layers = pages, lens, pages.shape[0]
         self.c = _PageTable(pages.data_ptr(), lens.data_ptr(), *pages.shape)
 
 

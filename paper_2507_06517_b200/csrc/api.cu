@@ -63,7 +63,7 @@ spindlekv_status pages_compact_impl(const spindlekv_page_pool& pool, const spind
 spindlekv_status paged_append_impl(const spindlekv_page_pool& pool, const spindlekv_page_table& table, const int32_t* start, int max_new,
                                    const spindlekv_tensor& K, const spindlekv_tensor& V, int n_rows, const int32_t* idx, int idx_len,
                                    int idx_seq, cudaStream_t st);
-size_t paged_workspace_bytes(const spindlekv_page_pool& pool, const spindlekv_page_table& t, int n_q_heads, int n_rows);
+size_t paged_workspace_bytes(const spindlekv_page_pool& pool);
 spindlekv_status paged_attend_impl(const spindlekv_page_pool& pool, const spindlekv_page_table& table, int n_q_heads, int n_rows, int max_len,
                                    float scale, const spindlekv_tensor& q, const spindlekv_tensor& out, void* ws, size_t ws_bytes,
                                    cudaStream_t st);
@@ -387,7 +387,7 @@ static spindlekv_status paged_shape_status(const spindlekv_page_pool* pool, cons
 
 size_t spindlekv_paged_workspace_bytes(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t n_q_heads, int32_t n_rows) {
   if (paged_shape_status(pool, table, n_q_heads, n_rows) != SPINDLEKV_OK) return 0;
-  return paged_workspace_bytes(*pool, *table, n_q_heads, n_rows);
+  return paged_workspace_bytes(*pool);
 }
 
 spindlekv_status spindlekv_paged_attend(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t n_q_heads,

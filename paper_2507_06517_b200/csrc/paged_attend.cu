@@ -3,8 +3,8 @@
 // Bound: every cached byte has to come from memory once (2 d bytes per token and KV head, plus 8/16 bytes of scales), so all
 // query heads of a KV head, and all new rows, are served by one pass over its codes.
 //
-// Mathematics.  The tensor cores multiply fp16 by fp16 into fp32.  Codes are exact in fp16: int8 directly, E4M3 as value * 2^-8 (its
-// bits moved into place).  Queries enter scaled by a power of two per row: bf16 queries are exact in one fp16 piece (elements below
+// Mathematics.  The tensor cores multiply fp16 by fp16 into fp32.  Codes are exact in fp16, and so are the numbers
+// of E4M3.  Queries enter scaled by a power of two per row: bf16 queries are exact in one fp16 piece (elements below
 // 2^-29 of the row's largest fade out), fp32 queries in two pieces (22 bits).  S^T = K Q^T, then p = 2^(S s_k c - m) with a running
 // reference m per query that moves only when a score exceeds it by 8 (p stays below 2^8), O^T += s_v (V^T P^T) with P in one fp16
 // piece for bf16 (2^-12 relative, below the output's rounding) or two for fp32; the scale s_v of a block is applied to the product of
@@ -43,9 +43,11 @@ struct AttendParams {
   int hn, n_rows, cols;      // query heads per KV head, new rows, columns in all
   int groups;                // column groups of a (layer, seq, KV head): its units
   int units_per;             // heads * groups
+  int per_shift;             // log2 of the blocks of a page
   float scale;               // softmax scale * log2(e)
-  float* part;               // [2 * runs][kAttMaxCols][d + 2]: O, m, sum
-  int2* span;                // [units] first and last run of a unit
+  float* part;               // [2 * kAttMaxRuns][kAttMaxCols][d]: O of the parts of units that several runs share
+  float2* stat;              // [2 * kAttMaxRuns][kAttMaxCols]: their m and sum
+  int32_t* lead;             // [runs] the unit that a run begins in the middle of, or -1
 };
 
 __device__ __forceinline__ uint4 load_code16(const uint8_t* p) {
@@ -63,6 +65,18 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y));
+}
+// the same from zero
+__device__ __forceinline__ void mma16816_first(float (&d)[4], const uint32_t (&a)[4], uint2 b) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y), "f"(0.f));
+}
+// 2^x, to two units in the last place of fp32; results below the smallest normal number are 0
+__device__ __forceinline__ float pow2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
@@ -85,14 +99,17 @@ __device__ __forceinline__ uint32_t codes_to_half2(uint32_t w) {
     const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&x), off);
     return *reinterpret_cast<const uint32_t*>(&v);
   } else {
-    // sign, then exponent and fraction one bit further down; the exponents' biases differ by 8.  The two NaN patterns, which only a
-    // slot behind the last token can hold, come out as finite numbers
-    const uint32_t x = __byte_perm(w, 0u, HI ? 0x3424 : 0x1404);
-    return (x & 0x80008000u) | ((x & 0x7F007F00u) >> 1);
+    uint32_t v;
+    if constexpr (HI) asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, hi; }" : "=r"(v) : "r"(w));
+    else asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, lo; }" : "=r"(v) : "r"(w));
+    return v;
   }
 }
 template <int FMT>
 __device__ __forceinline__ uint32_t prepare_codes(uint32_t w) { return FMT == SPINDLEKV_PAGED_INT8 ? w ^ 0x80808080u : w; }
+// E4M3 codes of slots behind the last token may be its NaN patterns, whose product with a weight of 0 is not 0: a bit less, and
+// they are numbers
+__device__ __forceinline__ uint32_t without_nan(uint32_t w) { return w ^ ((((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u); }
 
 // the line of blocks: unit (ls, head, group) has blocks_of(ls) of them, all units of a (layer, seq) side by side
 __device__ __forceinline__ int blocks_of(const AttendParams& p, int ls) { return (unit_len(p.table, p.pool, ls) + kPagedBlock - 1) / kPagedBlock; }
@@ -105,7 +122,7 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
   constexpr int VW = D / 32;                      // words of a V row per lane
   constexpr int COLS = 8 * NT;
   constexpr int OP = D + 4;                       // row pitch of the partial outputs in shared memory
-  constexpr float kVFactor = (FMT == SPINDLEKV_PAGED_E4M3 ? 256.f : 1.f) / kAttPScale;
+  constexpr float kVFactor = 1.f / kAttPScale;
   extern __shared__ uint4 smem_raw[];
   // prefix sums over the (layer, seq) pairs; then the queries' fragments, per-column factors, the warps' results
   const int n_ls = p.table.n_layers * p.table.n_seqs;
@@ -131,9 +148,23 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
   if (tid == 0) prefix[n_ls] = total;
   __syncthreads();
   const long long all = (long long)total * p.units_per;
-  long long at = all * blockIdx.x / gridDim.x;
-  const long long stop = all * (blockIdx.x + 1) / gridDim.x;
-  if (at >= stop) return;
+  const long long per_run = (all + gridDim.x - 1) / gridDim.x;      // runs without blocks are the last ones
+  long long at = per_run * blockIdx.x;
+  const long long stop = min(at + per_run, all);
+  // sequences without tokens give zeros
+  for (int e = blockIdx.x; e < n_ls; e += gridDim.x)
+    if (prefix[e + 1] == prefix[e]) {
+      const int layer = e / p.table.n_seqs, seq = e - layer * p.table.n_seqs, per_head = p.n_rows * D;
+      T* dst = reinterpret_cast<T*>(const_cast<void*>(p.out.ptr)) + (int64_t)layer * p.out.sl + (int64_t)seq * p.out.ss;
+      for (int i = tid; i < p.pool.heads * p.hn * per_head; i += kAttThreads) {
+        const int h = i / per_head, r = (i - h * per_head) / D, d = i % D;
+        dst[(int64_t)h * p.out.sh + (int64_t)r * p.out.st + d] = T(0.f);
+      }
+    }
+  if (at >= stop) {
+    if (tid == 0) p.lead[blockIdx.x] = -1;
+    return;
+  }
   int ls;
   {   // the (layer, seq) that holds block `at`
     int lo = 0, hi = n_ls - 1;
@@ -150,7 +181,7 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
     const int uh = (int)(inside / nb), b0 = (int)(inside - (long long)uh * nb);       // (head, group), first block
     const int b1 = (int)min((long long)nb, b0 + (stop - at));
     const int head = uh / p.groups, group = uh - head * p.groups;
-    const int unit = ls * p.units_per + uh;
+    if (tid == 0 && at == per_run * blockIdx.x) p.lead[blockIdx.x] = b0 > 0 ? ls * p.units_per + uh : -1;
     const int layer = ls / p.table.n_seqs, seq = ls - layer * p.table.n_seqs;
     const int len = unit_len(p.table, p.pool, ls);
     const int col0 = group * COLS, ncols = min(COLS, p.cols - col0);
@@ -177,7 +208,7 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
       if (amax > 0.f && amax < CUDART_INF_F) e = min(max(14 - ilogbf(amax), -126), 126);
       const float up = __int_as_float((127 + e) << 23);
       const float down = __int_as_float((127 - e) << 23);
-      if (lane == 0) sfac[col] = p.scale * down * (FMT == SPINDLEKV_PAGED_E4M3 ? 256.f : 1.f);
+      if (lane == 0) sfac[col] = p.scale * down;
       // element d sits in k-step (d / 64) * 4 + (d % 16) / 4 of the lanes with (d % 64) / 16 as their place in the quad
       constexpr int E = D / 32;          // this lane's elements: 4 or 2 neighbours
       const int d0 = lane * E;
@@ -220,10 +251,10 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
         for (int i = 0; i < 4; ++i) o[k][t][i] = 0.f;
     }
     const int32_t* row = p.table.pages + (int64_t)ls * p.table.max_pages;
-    const int per = p.pool.per_page();
+    const int sh = p.per_shift;
     // block b of the sequence -> its place in the pool, or -1
     auto place = [&](int page, int b) -> int64_t {
-      return page >= 0 && page < p.pool.n_pages ? ((int64_t)page * p.pool.heads + head) * per + b % per : -1;
+      return page >= 0 && page < p.pool.n_pages ? (((int64_t)page * p.pool.heads + head) << sh) + (b & ((1 << sh) - 1)) : -1;
     };
     uint4 kr[2][KH];
     uint32_t vr[4][VW];
@@ -257,21 +288,17 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
     int b = b0 + warp;
     int64_t cur = -1, nxt = -1;
     if (b < b1) {
-      cur = place(__ldg(row + b / per), b);
+      cur = place(__ldg(row + (b >> sh)), b);
       load_k(cur);
       load_v(cur);
     }
-    int page_n = b + kAttWarps < b1 ? __ldg(row + (b + kAttWarps) / per) : -1;
+    int page_n = b + kAttWarps < b1 ? __ldg(row + ((b + kAttWarps) >> sh)) : -1;
     for (; b < b1; b += kAttWarps) {
       const int bn = b + kAttWarps;
       nxt = bn < b1 ? place(page_n, bn) : -1;
-      page_n = bn + kAttWarps < b1 ? __ldg(row + (bn + kAttWarps) / per) : -1;
+      page_n = bn + kAttWarps < b1 ? __ldg(row + ((bn + kAttWarps) >> sh)) : -1;
       // ---- scores ----
       float sc[NT][4];
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sc[t][i] = 0.f;
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         const uint4& r0 = kr[0][k / 4];
@@ -282,7 +309,11 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int pc = 0; pc < NP; ++pc) mma16816(sc[t], a, sq[((pc * NT + t) * KS + k) * 32 + lane]);
+          for (int pc = 0; pc < NP; ++pc) {
+            const uint2 b = sq[((pc * NT + t) * KS + k) * 32 + lane];
+            if (k == 0 && pc == 0) mma16816_first(sc[t], a, b);
+            else mma16816(sc[t], a, b);
+          }
       }
       const float ks_b = ks_c;
       load_k(nxt);
@@ -310,7 +341,7 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
 #pragma unroll
             for (int d = 4; d <= 16; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
             x = fmaxf(x, m[t][i]);
-            const float f = x == m[t][i] ? 1.f : exp2f(m[t][i] - x);
+            const float f = x == m[t][i] ? 1.f : pow2(m[t][i] - x);
             m[t][i] = x;
             l[t][i] *= f;
 #pragma unroll
@@ -327,7 +358,7 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float ref = m[t][i & 1] == -CUDART_INF_F ? 0.f : m[t][i & 1];
-          w[i] = exp2f(sc[t][i] - ref);
+          w[i] = pow2(sc[t][i] - ref);
         }
         l[t][0] += w[0] + w[2];
         l[t][1] += w[1] + w[3];
@@ -354,7 +385,10 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
       for (int q = 0; q < VW; ++q) {
         uint32_t w[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) w[r] = prepare_codes<FMT>(vr[r][q]);
+        for (int r = 0; r < 4; ++r) {
+          w[r] = prepare_codes<FMT>(vr[r][q]);
+          if (FMT == SPINDLEKV_PAGED_E4M3 && masked) w[r] = without_nan(w[r]);
+        }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           // elements 4 q + 2 x and + 1 of the lane's piece: tokens 2c, 2c+1 in one word, 2c+8, 2c+9 in the other
@@ -362,9 +396,9 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
           const uint32_t a[4] = {codes_to_half2<FMT, 0>(lo), codes_to_half2<FMT, 1>(lo), codes_to_half2<FMT, 0>(hi), codes_to_half2<FMT, 1>(hi)};
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int pc = 0; pc < NP; ++pc) mma16816(acc, a, pf[t][pc]);
+            float acc[4];
+            mma16816_first(acc, a, pf[t][0]);
+            if constexpr (NP == 2) mma16816(acc, a, pf[t][1]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[2 * q + x][t][i] = fmaf(svc[t][i & 1], acc[i], o[2 * q + x][t][i]);
           }
@@ -394,12 +428,8 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
           *reinterpret_cast<float2*>(so + (warp * COLS + 8 * t + 2 * c + i) * OP + g * (D / 8) + 2 * k) = make_float2(o[k][t][i], o[k][t][i + 2]);
     __syncthreads();
     const bool whole = b0 == 0 && b1 == nb;
-    if (tid == 0) {
-      if (b0 == 0) p.span[unit].x = blockIdx.x;
-      if (b1 == nb) p.span[unit].y = blockIdx.x;
-    }
     // what is left for the join: a unit that began in an earlier run is this run's first, one that begins here and goes on its last
-    float* part = p.part + (int64_t)(2 * blockIdx.x + (b0 == 0 ? 1 : 0)) * kAttMaxCols * (D + 2);
+    const int64_t slot = (int64_t)(2 * blockIdx.x + (b0 == 0 ? 1 : 0)) * kAttMaxCols;
     for (int i = tid; i < ncols * (D / 4); i += kAttThreads) {
       const int col = i / (D / 4), d = (i - col * (D / 4)) * 4;
       float top = -CUDART_INF_F;
@@ -410,7 +440,7 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
 #pragma unroll
       for (int w = 0; w < kAttWarps; ++w) {
         const float mw = sm_m[w * COLS + col];
-        const float f = mw == top ? 1.f : exp2f(mw - top);
+        const float f = mw == top ? 1.f : pow2(mw - top);
         const float4 v = *reinterpret_cast<const float4*>(so + (w * COLS + col) * OP + d);
         sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y); sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
         den = fmaf(f, sm_l[w * COLS + col], den);
@@ -428,10 +458,8 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
           *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&e));
         }
       } else {
-        float* to = part + col * (D + 2);
-        *reinterpret_cast<float2*>(to + d) = make_float2(sum.x, sum.y);
-        *reinterpret_cast<float2*>(to + d + 2) = make_float2(sum.z, sum.w);
-        if (d == 0) { to[D] = top; to[D + 1] = den; }
+        *reinterpret_cast<float4*>(p.part + (slot + col) * D + d) = sum;
+        if (d == 0) p.stat[slot + col] = make_float2(top, den);
       }
     }
     __syncthreads();          // the shared memory is free for the next segment
@@ -440,41 +468,73 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// joins the runs of a unit, and gives zeros to sequences without tokens
+// Joins the parts of a unit: block (j, x) takes four columns of the unit that run j is the first to continue.  Four warps to a
+// column, each with every fourth run; the order of the sums is the order of the runs.
+constexpr int kJoinThreads = 512;
+
 template <typename T, int D>
-__global__ void __launch_bounds__(kAttThreads) paged_join_kernel(AttendParams p, int cols_per_unit) {
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(AttendParams p, int cols_per_unit) {
+  constexpr int E = D / 32;
+  __shared__ float so[4][4][D];
+  __shared__ float sden[4];
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int unit = blockIdx.x;
+  const int run = blockIdx.x, unit = p.lead[run];
+  if (unit < 0 || (run > 0 && p.lead[run - 1] == unit)) return;
+  int n = 1;                                 // parts: the run before, which the unit begins in, and those that continue it
+  for (int r = run; r < (int)gridDim.x; r += kJoinThreads) n += __syncthreads_count(r + (int)threadIdx.x < (int)gridDim.x && p.lead[r + threadIdx.x] == unit);
   const int ls = unit / p.units_per, uh = unit - ls * p.units_per, head = uh / p.groups, group = uh - head * p.groups;
   const int layer = ls / p.table.n_seqs, seq = ls - layer * p.table.n_seqs;
   const int col0 = group * cols_per_unit, ncols = min(cols_per_unit, p.cols - col0);
-  const bool no_tokens = unit_len(p.table, p.pool, ls) == 0;
-  int2 span = make_int2(0, 0);
-  if (!no_tokens) {
-    span = p.span[unit];
-    if (span.x == span.y) return;          // finished where it was computed
-  }
-  for (int i = threadIdx.x; i < ncols * D; i += kAttThreads) {
-    const int col = i / D, d = i - col * D;
-    float num = 0.f, den = 0.f;
-    if (!no_tokens) {
-      const float* part = p.part + (int64_t)col * (D + 2);
-      auto of = [&](int run) { return part + (int64_t)(2 * run + (run == span.x ? 1 : 0)) * kAttMaxCols * (D + 2); };
-      float top = -CUDART_INF_F;
-      for (int run = span.x; run <= span.y; ++run) top = fmaxf(top, of(run)[D]);
-      for (int run = span.x; run <= span.y; ++run) {
-        const float* q = of(run);
-        const float f = q[D] == top ? 1.f : exp2f(q[D] - top);
-        num = fmaf(f, q[d], num);
-        den = fmaf(f, q[D + 1], den);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, which = warp & 3, turn = warp >> 2;
+  const int col = blockIdx.y * 4 + which;
+  const bool mine = col < ncols;
+  auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * (run - 1) + 1 : 2 * (run - 1 + i)) * kAttMaxCols + col; };
+  float num[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) num[e] = 0.f;
+  if (mine) {
+    float top = -CUDART_INF_F;
+    for (int i = lane; i < n; i += 32) top = fmaxf(top, p.stat[slot(i)].x);
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float den = 0.f;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+      float f = 0.f;
+      if (i0 + lane < n) {
+        const float2 st = p.stat[slot(i0 + lane)];
+        f = st.x == top ? 1.f : pow2(st.x - top);
+        den = fmaf(f, st.y, den);
+      }
+      const int last = min(32, n - i0);
+#pragma unroll 4
+      for (int k = turn; k < last; k += 4) {
+        const float w = __shfl_sync(0xffffffffu, f, k);
+        const float* src = p.part + slot(i0 + k) * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          const float2 v = *reinterpret_cast<const float2*>(src + e);
+          num[e] = fmaf(w, v.x, num[e]);
+          num[e + 1] = fmaf(w, v.y, num[e + 1]);
+        }
       }
     }
-    const int gi = (col0 + col) / p.n_rows, r = (col0 + col) - gi * p.n_rows;
-    T* dst = reinterpret_cast<T*>(const_cast<void*>(p.out.ptr)) + (int64_t)layer * p.out.sl + (int64_t)seq * p.out.ss +
-             (int64_t)(head * p.hn + gi) * p.out.sh + (int64_t)r * p.out.st + d;
-    const float v = den == 0.f ? 0.f : num / den;
-    if constexpr (sizeof(T) == 4) *dst = v;
-    else *dst = __float2bfloat16_rn(v);
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+    if (turn == 0 && lane == 0) sden[which] = den;
+#pragma unroll
+    for (int e = 0; e < E; ++e) so[turn][which][lane * E + e] = num[e];
+  }
+  __syncthreads();
+  if (!mine || turn) return;
+  const int gi = (col0 + col) / p.n_rows, r = (col0 + col) - gi * p.n_rows;
+  T* dst = reinterpret_cast<T*>(const_cast<void*>(p.out.ptr)) + (int64_t)layer * p.out.sl + (int64_t)seq * p.out.ss +
+           (int64_t)(head * p.hn + gi) * p.out.sh + (int64_t)r * p.out.st;
+  const float den = sden[which];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int d = e * 32 + lane;
+    const float sum = so[0][which][d] + so[1][which][d] + so[2][which][d] + so[3][which][d];
+    dst[d] = T(den == 0.f ? 0.f : sum / den);
   }
 }
 
@@ -493,12 +553,10 @@ static int resident_blocks(K kernel, size_t smem, int (&cache)[kMaxDevices], int
 
 static int column_tiles(int cols) { return cols <= 8 ? 1 : cols <= 16 ? 2 : 4; }
 
-static size_t part_bytes(int d) { return align_up((size_t)2 * kAttMaxRuns * kAttMaxCols * (d + 2) * sizeof(float), 256); }
+constexpr size_t kPartRows = (size_t)2 * kAttMaxRuns * kAttMaxCols;
 
-size_t paged_workspace_bytes(const spindlekv_page_pool& pool, const spindlekv_page_table& t, int n_q_heads, int n_rows) {
-  const int cols = n_q_heads / pool.n_kv_heads * n_rows, groups = ceil_div(cols, 8 * column_tiles(cols));
-  const size_t units = (size_t)t.n_layers * t.n_seqs * pool.n_kv_heads * groups;
-  return kHeaderBytes + part_bytes(pool.head_dim) + align_up(units * sizeof(int2), 256);
+size_t paged_workspace_bytes(const spindlekv_page_pool& pool) {
+  return kHeaderBytes + kPartRows * (pool.head_dim * sizeof(float) + sizeof(float2)) + kAttMaxRuns * sizeof(int32_t);
 }
 
 template <typename T, int FMT, int D, int NT>
@@ -524,8 +582,8 @@ static spindlekv_status launch_attend(AttendParams& p, int max_len, cudaStream_t
   }
   if (cudaGetLastError() != cudaSuccess) return SPINDLEKV_CUDA;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n_ls * p.units_per);
-  cfg.blockDim = dim3(kAttThreads);
+  cfg.gridDim = dim3(runs, ceil_div(std::min(COLS, p.cols), 4));
+  cfg.blockDim = dim3(kJoinThreads);
   cfg.stream = st;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -556,18 +614,20 @@ static spindlekv_status launch_format(AttendParams& p, int format, int max_len, 
 spindlekv_status paged_attend_impl(const spindlekv_page_pool& pool, const spindlekv_page_table& table, int n_q_heads, int n_rows, int max_len,
                                    float scale, const spindlekv_tensor& q, const spindlekv_tensor& out, void* ws, size_t ws_bytes,
                                    cudaStream_t st) {
-  if (ws_bytes < paged_workspace_bytes(pool, table, n_q_heads, n_rows)) return SPINDLEKV_WORKSPACE_TOO_SMALL;
+  if (ws_bytes < paged_workspace_bytes(pool)) return SPINDLEKV_WORKSPACE_TOO_SMALL;
   AttendParams p;
   p.pool = make_pool(pool);
   p.table = make_table(table);
   p.q = make_view(q);
   p.out = make_view(out);
+  p.per_shift = pool.page_size == 16 ? 0 : pool.page_size == 32 ? 1 : pool.page_size == 64 ? 2 : 3;
   p.hn = n_q_heads / pool.n_kv_heads;
   p.n_rows = n_rows;
   p.cols = p.hn * n_rows;
   p.scale = (scale == 0.f ? 1.f / sqrtf((float)pool.head_dim) : scale) * 1.44269504088896340736f;
   p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kHeaderBytes);
-  p.span = reinterpret_cast<int2*>(static_cast<uint8_t*>(ws) + kHeaderBytes + part_bytes(pool.head_dim));
+  p.stat = reinterpret_cast<float2*>(p.part + kPartRows * pool.head_dim);
+  p.lead = reinterpret_cast<int32_t*>(p.stat + kPartRows);
   return q.dtype == SPINDLEKV_BF16 ? launch_format<__nv_bfloat16>(p, pool.format, max_len, st) : launch_format<float>(p, pool.format, max_len, st);
 }
 

@@ -543,19 +543,17 @@ class SpindleKVDecodeAttention:
 
 
 class _OnDevice:
-    """Calls go to the current device and stream; this makes the owner's device current for them where it is not."""
+    """Calls go to the current device and stream; ``_elsewhere`` says that the owner's device has to be made current first."""
 
-    def _on(self, stream, call) -> None:
-        if torch.cuda.current_device() == self.device.index:
-            call(stream)
-        else:
-            with torch.cuda.device(self.device):
-                call(stream)
+    def _elsewhere(self) -> bool:
+        return torch.cuda.current_device() != self.device.index
+
+    def _raw(self, stream) -> int:
+        return B.raw_stream(self.device.index) if stream is None else B._stream(stream)
 
     def _mine(self, name: str, t: torch.Tensor, dtype=None, shape=None) -> torch.Tensor:
         """``t``, if the library may be given its address as it is."""
-        if t.device != self.device or (dtype is not None and t.dtype != dtype) or (shape is not None and tuple(t.shape) != tuple(shape)) \
-                or not t.is_contiguous():
+        if t.device != self.device or (dtype is not None and t.dtype != dtype) or (shape is not None and t.shape != shape) or not t.is_contiguous():
             want = " ".join(str(x) for x in (dtype, None if shape is None else list(shape)) if x is not None)
             raise ValueError(f"{name}: contiguous {want} on {self.device} expected, got {t.dtype} {list(t.shape)} on {t.device}")
         return t
@@ -622,24 +620,31 @@ class SpindleKVPagedCache(_OnDevice):
         return self._tables[layer]
 
     def _cache_rows(self, name: str, t: torch.Tensor, n_l: int, heads: int) -> B._Tensor:
-        if t.dim() != 5 or t.shape[0] != n_l or t.shape[1] != self.n_seqs or t.shape[2] != heads or t.shape[4] != self.d or t.device != self.device:
-            raise ValueError(f"{name}: [{n_l}, {self.n_seqs}, {heads}, rows, {self.d}] on {self.device} expected, got {list(t.shape)} on {t.device}")
-        return B.desc_bhnd(t)
+        shape = t.shape
+        if len(shape) != 5 or shape[:3] != (n_l, self.n_seqs, heads) or shape[4] != self.d or t.device != self.device or t.stride(4) != 1:
+            raise ValueError(f"{name}: [{n_l}, {self.n_seqs}, {heads}, rows, {self.d}] on {self.device} expected, rows contiguous, got {list(shape)} on {t.device}")
+        return B._Tensor(t.data_ptr(), B._dtype_code(t), *t.stride()[:4])
 
     def resize(self, new_lens: Optional[torch.Tensor] = None, add: int = 0, stream=None) -> torch.Tensor:
         """Pages for new lengths (``[n_layers, n_seqs]`` int32 on the device, or every length plus ``add``).  Returns ``start``, where
         ``append`` goes on; ``status()`` tells when there were too few pages."""
+        if self._elsewhere():
+            with torch.cuda.device(self.device):
+                return self.resize(new_lens, add, stream)
         if new_lens is not None:
             self._mine("new_lens", new_lens, torch.int32, (self.n_layers, self.n_seqs))
-        self._on(stream, lambda st: B.spindlekv_pages_resize(self.pool, self.table, new_lens, add, self.start, self.ws_pages, st))
+        B.spindlekv_pages_resize(self.pool, self.table, new_lens, add, self.start, self.ws_pages, self._raw(stream))
         return self.start
 
     def append(self, K: torch.Tensor, V: torch.Tensor, start: Optional[torch.Tensor] = None, idx: Optional[torch.Tensor] = None,
                idx_seq: Optional[int] = None, max_new: Optional[int] = None, layer: Optional[int] = None, stream=None) -> None:
         """Writes tokens ``start .. lens-1`` (``start`` of the last ``resize`` by default) from rows ``[n_layers or 1, n_seqs, H_kv, rows, d]``;
         with ``idx`` ``[n_layers or 1, H_kv, n_seqs * idx_seq]`` from the rows it names."""
+        if self._elsewhere():
+            with torch.cuda.device(self.device):
+                return self.append(K, V, start, idx, idx_seq, max_new, layer, stream)
         table = self._rows_of(layer)
-        n_l = table.c.n_layers
+        n_l = table.n_layers
         if start is None:
             start = self.start
         if layer is not None and start.shape[0] == self.n_layers:
@@ -655,40 +660,49 @@ class SpindleKVPagedCache(_OnDevice):
         if max_new is None:
             max_new = K.shape[3] if idx is None else idx_seq
         k, v = self._cache_rows("K", K, n_l, self.Hkv), self._cache_rows("V", V, n_l, self.Hkv)
-        self._on(stream, lambda st: B.spindlekv_paged_append(self.pool, table, start, max_new, k, v, K.shape[3], idx, idx_seq or 0, st))
+        B.spindlekv_paged_append(self.pool, table, start, max_new, k, v, K.shape[3], idx, idx_seq or 0, self._raw(stream))
 
     def attend(self, q: torch.Tensor, out: Optional[torch.Tensor] = None, max_len: Optional[int] = None, scale: float = 0.0,
                layer: Optional[int] = None, stream=None) -> torch.Tensor:
         """Attention of the last ``rows`` tokens, ``q`` ``[n_layers or 1, n_seqs, H_q, rows, d]``.  Without ``out`` the result lies in a
         buffer of this object that the next call of the same shape overwrites.  ``max_len`` (the longest sequence, a capacity by
         default) sizes the split."""
+        if self._elsewhere():
+            with torch.cuda.device(self.device):
+                return self.attend(q, out, max_len, scale, layer, stream)
         table = self._rows_of(layer)
-        n_l = table.c.n_layers
         hq = q.shape[2] if self.Hq is None else self.Hq
-        qd = self._cache_rows("q", q, n_l, hq)
-        rows = q.shape[3]
+        qd = self._cache_rows("q", q, table.n_layers, hq)
+        shape = q.shape
         if out is None:
-            key = (q.shape, q.dtype)
-            out = self._out.get(key)
-            if out is None:
-                out = self._out[key] = torch.empty(q.shape, dtype=q.dtype, device=self.device)
-        elif out.shape != q.shape:
-            raise ValueError(f"out: {list(q.shape)} expected, got {list(out.shape)}")
-        od = self._cache_rows("out", out, n_l, hq)
+            held = self._out.get((shape, q.dtype))
+            if held is None:
+                out = torch.empty(shape, dtype=q.dtype, device=self.device)
+                held = self._out[(shape, q.dtype)] = (out, self._cache_rows("out", out, table.n_layers, hq))
+            out, od = held
+        else:
+            if out.shape != shape:
+                raise ValueError(f"out: {list(shape)} expected, got {list(out.shape)}")
+            od = self._cache_rows("out", out, table.n_layers, hq)
         if self.ws_attend is None:
-            need = B.spindlekv_paged_workspace_bytes(self.pool, self.table, hq, 16)
-            self.ws_attend = torch.empty(need, dtype=torch.uint8, device=self.device)
-        self._on(stream, lambda st: B.spindlekv_paged_attend(self.pool, table, hq, rows, max_len or self.capacity, scale, qd, od, self.ws_attend, st))
+            self.ws_attend = torch.empty(B.spindlekv_paged_workspace_bytes(self.pool, self.table, hq, shape[3]), dtype=torch.uint8, device=self.device)
+        B.spindlekv_paged_attend(self.pool, table, hq, shape[3], max_len or self.capacity, scale, qd, od, self.ws_attend, self._raw(stream))
         return out
 
     def fork(self, parent: torch.Tensor, stream=None) -> None:
         """Sequence ``i`` becomes what sequence ``parent[i]`` was (int32 ``[n_seqs]`` on the device; -1: empty), in every layer."""
+        if self._elsewhere():
+            with torch.cuda.device(self.device):
+                return self.fork(parent, stream)
         self._mine("parent", parent, torch.int32, (self.n_seqs,))
-        self._on(stream, lambda st: B.spindlekv_pages_fork(self.pool, self.table, parent, self.ws_pages, st))
+        B.spindlekv_pages_fork(self.pool, self.table, parent, self.ws_pages, self._raw(stream))
 
     def compact(self, stream=None) -> torch.Tensor:
         """Live pages to the lowest page numbers; returns their number (a device tensor)."""
-        self._on(stream, lambda st: B.spindlekv_pages_compact(self.pool, self.table, self.n_live, self.ws_pages, st))
+        if self._elsewhere():
+            with torch.cuda.device(self.device):
+                return self.compact(stream)
+        B.spindlekv_pages_compact(self.pool, self.table, self.n_live, self.ws_pages, self._raw(stream))
         return self.n_live
 
     def status(self) -> int:
@@ -714,12 +728,15 @@ class SpindleKVBeamSelect(_OnDevice):
     def run(self, logits: torch.Tensor, score: torch.Tensor, finished: Optional[torch.Tensor] = None, eos: int = 0, stream=None):
         """``logits`` ``[n_seqs * n_beams, vocab]`` (any row stride), ``score`` and ``finished`` (bool) ``[n_seqs * n_beams]``.  Returns
         ``(score, parent, token)``, each ``[n_seqs, n_out]``, best first, in buffers that the next call overwrites."""
+        if self._elsewhere():
+            with torch.cuda.device(self.device):
+                return self.run(logits, score, finished, eos, stream)
         rows = self.n_seqs * self.n_beams
-        if tuple(logits.shape) != (rows, self.vocab) or (self.vocab > 1 and logits.stride(1) != 1) or logits.device != self.device:
+        if logits.shape != (rows, self.vocab) or (self.vocab > 1 and logits.stride(1) != 1) or logits.device != self.device:
             raise ValueError(f"logits: [{rows}, {self.vocab}] on {self.device} expected, got {list(logits.shape)} on {logits.device}")
         self._mine("score", score, torch.float32, (rows,))
         if finished is not None:
             self._mine("finished", finished, torch.bool, (rows,))
-        self._on(stream, lambda st: B.spindlekv_beam_select(self.n_seqs, self.n_beams, self.vocab, self.n_out, logits, score, finished, eos,
-                                                           self.score, self.parent, self.token, self.ws, st))
+        B.spindlekv_beam_select(self.n_seqs, self.n_beams, self.vocab, self.n_out, logits, score, finished, eos, self.score, self.parent,
+                                self.token, self.ws, self._raw(stream))
         return self.score, self.parent, self.token
