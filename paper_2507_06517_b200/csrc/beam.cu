@@ -2,11 +2,11 @@
 //
 // Bound by reading the logits once.  First kernel, one block per slice of a row: the slice is in registers after one pass of wide
 // loads; its maximum and exp-sum go to the workspace, and so do its n_out largest logits.  Those are found without sorting: the
-// n_out-th largest of the threads' own maxima is a bound that only n_out threads reach, so at most n_out times a thread's elements
-// remain (a dozen, mostly), whatever the values are; they are ranked by counting.  Keys are (value, index) with the lower index above,
-// so no two are equal and ties need no care.  Within a row the order of logits is the order of totals.
-// Second kernel, one block per sequence: log-sum-exp of the beams in double from the slices' pieces, totals in double, and the same
-// selection over the slices' lists, 2048 entries at a time beside the best so far.
+// block's threads form 64 groups of four, and the n_out-th largest of the groups' maxima is a bound that only n_out groups reach, so at
+// most n_out times a group's elements remain (a dozen or two, mostly), whatever the values are; they are ranked by counting.  Keys are
+// (value, index) with the lower index above, so no two are equal and ties need no care.  Within a row the order of logits is the order of totals.
+// Second kernel, one block per sequence: log-sum-exp of the beams from the slices' pieces (added in double), totals in double, and the
+// same selection over the slices' lists, 2048 entries at a time beside the best so far.
 #include <algorithm>
 
 #include <math_constants.h>
@@ -18,6 +18,9 @@ namespace skv {
 constexpr int kBeamThreads = 256;
 constexpr int kBeamMaxOut = 32;
 constexpr int kBeamPer = 8;            // entries per thread and step of the second kernel
+constexpr int kBeamGroups = 64;        // groups of threads whose maxima give the bound; at least kBeamMaxOut
+constexpr int kBeamGroup = kBeamThreads / kBeamGroups;
+static_assert(kBeamGroups >= kBeamMaxOut && kBeamGroup == 4, "the bound is the n_out-th of the groups' maxima; a group is a quad of lanes");
 
 struct BeamParams {
   int n_seqs, n_beams, vocab, k, slices;
@@ -31,6 +34,13 @@ struct BeamParams {
   float2* stat;        // [rows][slices] maximum and exp-sum
   int2* cand;          // [rows][slices][k] (logit bits, token), best first; token -1: none
 };
+
+// 2^x, to two units in the last place of fp32; results below the smallest normal number are 0
+__device__ __forceinline__ float pow2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 // a key whose unsigned order is the order of the value, then of falling index; never 0
 __device__ __forceinline__ unsigned long long key_of(float x, int i) {
@@ -53,8 +63,8 @@ __device__ __forceinline__ bool row_runs(const BeamParams& p, int row) {
 template <typename T, int EPT, bool VEC>
 __global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(BeamParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  __shared__ __align__(16) unsigned long long tops[kBeamThreads];
-  __shared__ unsigned long long found[kBeamMaxOut * EPT];
+  __shared__ __align__(16) unsigned long long tops[kBeamGroups];
+  __shared__ unsigned long long found[kBeamMaxOut * kBeamGroup * EPT];
   __shared__ unsigned long long bound;
   __shared__ float red[2 * (kBeamThreads / 32)];
   __shared__ int n_found;
@@ -92,40 +102,51 @@ __global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(BeamParams p) 
       v[j] = at < p.vocab ? to_f32(x[at]) : -CUDART_INF_F;
     }
   }
-  // ---- maximum, exp-sum (a NaN anywhere must show in the sum) ----
+  // ---- maximum and its lowest place (a thread's indices rise with i) ----
   float mx = -CUDART_INF_F;
 #pragma unroll
   for (int i = 0; i < EPT; ++i) mx = fmaxf(mx, v[i]);
   unsigned long long top = 0;
+  if (mx > -CUDART_INF_F) {
+    int first = 0;
 #pragma unroll
-  for (int i = 0; i < EPT; ++i) {
-    const int at = index(i);
-    if (v[i] == mx && at < p.vocab) { const unsigned long long q = key_of(v[i], at); top = q > top ? q : top; }
+    for (int i = EPT - 1; i >= 0; --i) first = v[i] == mx ? i : first;
+    top = key_of(mx, s0 + ((first / W) * kBeamThreads + tid) * W + first % W);
+  } else {          // nothing but -infinity (or NaN), some of it perhaps behind the row's end
+#pragma unroll
+    for (int i = EPT - 1; i >= 0; --i)
+      if (v[i] == mx && index(i) < p.vocab) top = key_of(mx, index(i));
   }
-  tops[tid] = top;
   float all = mx;
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
+  unsigned long long quad = top;
+#pragma unroll
+  for (int o = 1; o < kBeamGroup; o <<= 1) quad = max(quad, __shfl_xor_sync(0xffffffffu, quad, o));
+  if (tid % kBeamGroup == 0) tops[tid / kBeamGroup] = quad;
   if (lane == 0) red[warp] = all;
   __syncthreads();
+  // ---- exp-sum (a NaN anywhere must show in it); beside it the n_out-th largest of the groups' maxima ----
   all = red[0];
 #pragma unroll
   for (int w = 1; w < kBeamThreads / 32; ++w) all = fmaxf(all, red[w]);
   float sum = 0.f;
   const float ref = all == -CUDART_INF_F ? 0.f : all;
 #pragma unroll
-  for (int i = 0; i < EPT; ++i) sum += exp2f((v[i] - ref) * 1.44269504f);
+  for (int i = 0; i < EPT; ++i) sum += pow2((v[i] - ref) * 1.44269504f);
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) red[kBeamThreads / 32 + warp] = sum;
-  // ---- the k-th largest of the threads' maxima ----
-  int rank = 0;
+  if (tid < kBeamGroups) {
+    const unsigned long long own = tops[tid];
+    int rank = 0;
 #pragma unroll 8
-  for (int i = 0; i < kBeamThreads; i += 2) {
-    const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(tops + i);
-    rank += (q.x > top) + (q.y > top);
+    for (int i = 0; i < kBeamGroups; i += 2) {
+      const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(tops + i);
+      rank += (q.x > own) + (q.y > own);
+    }
+    if (rank == p.k - 1 && own) bound = own;
   }
-  if (rank == p.k - 1 && top) bound = top;
   __syncthreads();
   if (tid == 0) {
     float s = 0.f;
@@ -165,8 +186,8 @@ __device__ __forceinline__ Entry make_entry(double total, int flat) {
 }
 
 __global__ void __launch_bounds__(kBeamThreads) beam_join_kernel(BeamParams p) {
-  __shared__ Entry tops[kBeamThreads];
-  __shared__ Entry found[kBeamMaxOut * (kBeamPer + 1)];
+  __shared__ Entry tops[kBeamGroups];
+  __shared__ Entry found[kBeamMaxOut * kBeamGroup * (kBeamPer + 1)];
   __shared__ Entry best[kBeamMaxOut];
   __shared__ Entry bound;
   __shared__ double base[64];
@@ -174,12 +195,21 @@ __global__ void __launch_bounds__(kBeamThreads) beam_join_kernel(BeamParams p) {
   __shared__ int n_found;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int seq = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per_beam = p.slices * p.k, entries = p.n_beams * per_beam;
+  const int2* cand = p.cand + (int64_t)seq * entries;
+  int2 raw[kBeamPer];            // the first step's entries are on their way while the log-sum-exps are formed
+#pragma unroll
+  for (int i = 0; i < kBeamPer; ++i) {
+    const int e = i * kBeamThreads + tid;
+    raw[i] = e < entries ? cand[e] : make_int2(0, -1);
+  }
   for (int w = warp; w < p.n_beams; w += kBeamThreads / 32) {
     const int row = seq * p.n_beams + w;
     const float sc = p.score[row];
+    const bool done = p.finished && p.finished[row];
     if (!(fabsf(sc) < CUDART_INF_F)) {
       if (lane == 0) kind[w] = 2;
-    } else if (p.finished && p.finished[row]) {
+    } else if (done) {
       if (lane == 0) { kind[w] = 1; base[w] = sc; }
     } else {
       const float2* st = p.stat + (int64_t)row * p.slices;
@@ -188,12 +218,14 @@ __global__ void __launch_bounds__(kBeamThreads) beam_join_kernel(BeamParams p) {
 #pragma unroll
       for (int o = 16; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
       double sum = 0.0;
-      for (int i = lane; i < p.slices; i += 32)
-        sum += st[i].x == -CUDART_INF_F ? (double)(st[i].y != st[i].y ? st[i].y : 0.f) : (double)st[i].y * exp((double)st[i].x - (double)mx);
+      for (int i = lane; i < p.slices; i += 32) {
+        const float2 s = st[i];   // a slice of -infinity alone has the sum 0, or NaN
+        sum += s.x == -CUDART_INF_F ? s.y : s.y * expf(s.x - mx);
+      }
 #pragma unroll
       for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      const double lse = (double)mx + log(sum);
       if (lane == 0) {
+        const double lse = (double)mx + log(sum);
         const bool fine = lse > -CUDART_INF && lse < CUDART_INF;
         kind[w] = fine ? 0 : 2;
         base[w] = (double)sc - lse;
@@ -202,21 +234,19 @@ __global__ void __launch_bounds__(kBeamThreads) beam_join_kernel(BeamParams p) {
   }
   for (int i = tid; i < p.k; i += kBeamThreads) best[i] = Entry{0, 0};
   __syncthreads();
-  const int per_beam = p.slices * p.k;
-  const long long entries = (long long)p.n_beams * per_beam;
   const int offered = min(p.k, p.vocab);      // entries of a beam that does not take part
-  for (long long e0 = 0; e0 < entries; e0 += kBeamThreads * kBeamPer) {
+  for (int e0 = 0; e0 < entries; e0 += kBeamThreads * kBeamPer) {
     if (tid == 0) { n_found = 0; bound = Entry{0, 1}; }
     Entry mine[kBeamPer + 1];
     Entry top{0, 0};
 #pragma unroll
     for (int i = 0; i < kBeamPer; ++i) {
       mine[i] = Entry{0, 0};
-      const long long e = e0 + i * kBeamThreads + tid;
+      const int e = e0 + i * kBeamThreads + tid;
       if (e < entries) {
-        const int w = (int)(e / per_beam), at = (int)(e - (long long)w * per_beam);
+        const int w = e / per_beam, at = e - w * per_beam;
         if (kind[w] == 0) {
-          const int2 c = p.cand[((int64_t)(seq * p.n_beams + w)) * per_beam + at];
+          const int2 c = e0 ? cand[e] : raw[i];
           if (c.y >= 0) mine[i] = make_entry(base[w] + (double)__int_as_float(c.x), w * p.vocab + c.y);
         } else if (at < offered) {
           int token = at;
@@ -232,12 +262,21 @@ __global__ void __launch_bounds__(kBeamThreads) beam_join_kernel(BeamParams p) {
     }
     mine[kBeamPer] = tid < p.k ? best[tid] : Entry{0, 0};
     if (better(mine[kBeamPer], top)) top = mine[kBeamPer];
-    tops[tid] = top;
+    Entry quad = top;
+#pragma unroll
+    for (int o = 1; o < kBeamGroup; o <<= 1) {
+      const Entry other{__shfl_xor_sync(0xffffffffu, quad.value, o), __shfl_xor_sync(0xffffffffu, quad.index, o)};
+      if (better(other, quad)) quad = other;
+    }
+    if (tid % kBeamGroup == 0) tops[tid / kBeamGroup] = quad;
     __syncthreads();
-    int rank = 0;
+    if (tid < kBeamGroups) {
+      const Entry own = tops[tid];
+      int rank = 0;
 #pragma unroll 8
-    for (int i = 0; i < kBeamThreads; ++i) rank += better(tops[i], top);
-    if (rank == p.k - 1 && top.value) bound = top;
+      for (int i = 0; i < kBeamGroups; ++i) rank += better(tops[i], own);
+      if (rank == p.k - 1 && own.value) bound = own;
+    }
     __syncthreads();
     const Entry least = bound;
 #pragma unroll
