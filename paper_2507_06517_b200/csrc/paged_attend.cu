@@ -11,10 +11,11 @@
 // that block in fp32, so blocks of very different scale do not disturb one another.  m, the sum of p and O are fp32.
 //
 // Layout.  A warp takes one block of 16 tokens at a time: K is the 16 x d operand of m16n8k16, the queries are its 8 columns.  Which
-// token or element a lane's fragment registers stand for is free as long as both operands agree, so codes go from memory straight into
-// the registers that need them, 16 bytes per lane, without shared memory: a lane's 16 bytes of a K row are four k-steps; for V it reads
-// the same 16 bytes of four tokens and transposes bytes between registers.  The next block's loads are in flight while this one is
-// computed.  P changes layout by an 8x8 transposition inside the warp.
+// token or element a lane's fragment registers stand for is free as long as both operands agree: a lane's 16 bytes of a K row are four
+// k-steps, and for V it takes the same 16 bytes of four tokens and transposes bytes between registers.  Two blocks are computed
+// side by side.  They arrive by TMA, in their warp's own slots (the next keys as soon as these are read, the next values likewise), in swizzled rows and
+// with the tokens assigned so that no two lanes meet in a bank; nothing but the warp waits for them.  P changes layout by an 8x8
+// transposition inside the warp.
 //
 // Split.  All blocks of all (layer, sequence, head) units form one line, cut into equal runs, one per resident thread block;
 // the eight warps of a thread block deal a run's blocks among themselves.  Every run thus has the same work however
@@ -26,8 +27,11 @@
 #include <math_constants.h>
 
 #include "paged.cuh"
+#include "sm100_ptx.cuh"
 
 namespace skv {
+
+bool make_code_map(CUtensorMap* map, const void* codes, int head_dim, int rows, int n_pages);
 
 constexpr int kAttThreads = 256;
 constexpr int kAttWarps = kAttThreads / 32;
@@ -47,19 +51,10 @@ struct AttendParams {
   float scale;               // softmax scale * log2(e)
   float* part;               // [2 * kAttMaxRuns][kAttMaxCols][d]: O of the parts of units that several runs share
   float2* stat;              // [2 * kAttMaxRuns][kAttMaxCols]: their m and sum
-  int32_t* lead;             // [runs] the unit that a run begins in the middle of, or -1
+  int2* lead;                // [runs] the unit that a run is the first to continue and its number of parts; unit -1: none, -2: a wait gave up
+  uint32_t* hdr;             // status block of the workspace
+  long long wait_cycles;     // bound of a wait
 };
-
-__device__ __forceinline__ uint4 load_code16(const uint8_t* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
-__device__ __forceinline__ uint2 load_code8(const uint8_t* p) {
-  uint2 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-  return v;
-}
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint2 b) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -89,6 +84,33 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 }
 __device__ __forceinline__ float2 unpack_half2(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
 
+// N = 2 or 4 neighbouring elements
+template <int N>
+__device__ __forceinline__ void load_elements(const float* p, float (&x)[N]) {
+  if constexpr (N == 4) {
+    const float4 v = *reinterpret_cast<const float4*>(p);
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+  } else {
+    const float2 v = *reinterpret_cast<const float2*>(p);
+    x[0] = v.x; x[1] = v.y;
+  }
+}
+template <int N>
+__device__ __forceinline__ void load_elements(const __nv_bfloat16* p, float (&x)[N]) {
+  uint32_t w[N / 2];
+  if constexpr (N == 4) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    w[0] = v.x; w[1] = v.y;
+  } else {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  }
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+
 // two of the four codes in w (bytes 0, 1 with HI = 0; 2, 3 with HI = 1) as two fp16 numbers
 template <int FMT, int HI>
 __device__ __forceinline__ uint32_t codes_to_half2(uint32_t w) {
@@ -105,52 +127,122 @@ __device__ __forceinline__ uint32_t codes_to_half2(uint32_t w) {
     return v;
   }
 }
+// the same, offset int8 codes as subnormal numbers
+template <int HI>
+__device__ __forceinline__ uint32_t offset_to_half2(uint32_t w) { return __byte_perm(w, 0u, HI ? 0x4342 : 0x4140); }
 template <int FMT>
 __device__ __forceinline__ uint32_t prepare_codes(uint32_t w) { return FMT == SPINDLEKV_PAGED_INT8 ? w ^ 0x80808080u : w; }
 // E4M3 codes of slots behind the last token may be its NaN patterns, whose product with a weight of 0 is not 0: a bit less, and
 // they are numbers
 __device__ __forceinline__ uint32_t without_nan(uint32_t w) { return w ^ ((((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u); }
 
-// the line of blocks: unit (ls, head, group) has blocks_of(ls) of them, all units of a (layer, seq) side by side
-__device__ __forceinline__ int blocks_of(const AttendParams& p, int ls) { return (unit_len(p.table, p.pool, ls) + kPagedBlock - 1) / kPagedBlock; }
+// The line: unit (ls, head, group) takes kSetUp places, which stand for looking up its pages, reading its queries and joining its
+// warps, and then one for each pair of blocks; all units of a (layer, seq) lie side by side.  Without those places a run with the ends
+// of two or three units in it finishes last.
+constexpr int kSetUp = 6;
+__device__ __forceinline__ int places_of(const AttendParams& p, int ls) {
+  const int len = unit_len(p.table, p.pool, ls);
+  return len ? (len + 2 * kPagedBlock - 1) / (2 * kPagedBlock) + kSetUp : 0;
+}
+
+template <int D, int NT>
+__host__ __device__ constexpr size_t ring_bytes() {   // the warps' results take the ring's place when a segment ends
+  const size_t ring = (size_t)kAttWarps * 4 * kPagedBlock * D, results = (size_t)kAttWarps * 8 * NT * (D + 4) * 4;
+  return ring > results ? ring : results;
+}
+
+// The token of a block that fragment row i (and i + 8, eight tokens on) stands for.  With it the lanes that read shared memory
+// together find their 16 bytes of the swizzled rows (128 bytes for d = 128, 64 for d = 64) in different banks, for K and for V.
+template <int D>
+__device__ __forceinline__ int token_of(int i) { return ((D == 128 ? 0x37156240 : 0x65742130) >> (4 * i)) & 7; }
 
 template <typename T, int FMT, int D, int NT>
-__global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_kernel(AttendParams p) {
+__global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_kernel(const __grid_constant__ CUtensorMap kmap,
+                                                                                  const __grid_constant__ CUtensorMap vmap, AttendParams p) {
   constexpr int NP = sizeof(T) == 4 ? 2 : 1;      // fp16 pieces of a query and of a weight
   constexpr int KS = D / 16;                      // k-steps of a score, and m-tiles of an output
   constexpr int KH = D / 64;                      // 16-byte pieces of a K row per lane
   constexpr int VW = D / 32;                      // words of a V row per lane
   constexpr int COLS = 8 * NT;
+  // int8 keys under one query piece enter as (code + 128) 2^-24, a subnormal fp16 number, which saves a subtraction per two of them;
+  // the scores lose 128 times the query's sum.  The accumulator is three times larger then, too much for fp32 queries only
+  constexpr bool kOffset = FMT == SPINDLEKV_PAGED_INT8 && NP == 1 && NT == 1;
   constexpr int OP = D + 4;                       // row pitch of the partial outputs in shared memory
-  constexpr float kVFactor = 1.f / kAttPScale;
-  extern __shared__ uint4 smem_raw[];
+  constexpr int kHalf = kPagedBlock * D;          // bytes of a block's K, or V
+  constexpr int kSlot = 2 * kHalf;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
   // prefix sums over the (layer, seq) pairs; then the queries' fragments, per-column factors, the warps' results
   const int n_ls = p.table.n_layers * p.table.n_seqs;
-  float* so = reinterpret_cast<float*>(smem_raw);                       // [kAttWarps][COLS][OP]
-  uint2* sq = reinterpret_cast<uint2*>(so + kAttWarps * COLS * OP);     // [NP][NT][KS][32]
+  float* so = reinterpret_cast<float*>(smem);                            // [kAttWarps][COLS][OP], over the ring
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + ring_bytes<D, NT>());    // [kAttWarps][2]
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + kAttWarps * 2);   // a wait gave up; and one for the waits after that
+  uint2* sq = reinterpret_cast<uint2*>(bars + kAttWarps * 2 + 2);             // [NP][NT][KS][32]
   float* sfac = reinterpret_cast<float*>(sq + NP * NT * KS * 32);       // [COLS] score factor
-  float* sm_m = sfac + COLS;                                            // [kAttWarps][COLS]
+  float* scorr = sfac + COLS;                                           // [COLS] and what the codes' offset adds to it
+  float* sm_m = scorr + COLS;                                            // [kAttWarps][COLS]
   float* sm_l = sm_m + kAttWarps * COLS;                                // [kAttWarps][COLS]
   int* warp_sums = reinterpret_cast<int*>(sm_l + kAttWarps * COLS);     // [33]
   int* prefix = warp_sums + 36;                                         // [n_ls + 1]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;   // g, c: the fragments' rows and columns
 
-  // blocks of a (layer, seq) per unit, summed
-  int total = 0;
-  for (int base = 0; base < n_ls; base += kAttThreads) {
-    const int ls = base + tid;
-    const int n = ls < n_ls ? blocks_of(p, ls) : 0;
-    int sum;
-    const int at = block_exclusive_scan(n, warp_sums, sum);
-    if (ls < n_ls) prefix[ls] = total + at;
-    total += sum;
+  if (lane == 0) {       // each warp its own
+    ptx::mbar_init(bars + warp * 2, 1);
+    ptx::mbar_init(bars + warp * 2 + 1, 1);
+    ptx::fence_barrier_init();
+    if (warp == 0) {
+      abort_flag[0] = abort_flag[1] = 0;
+      ptx::prefetch_tensormap(&kmap);
+      ptx::prefetch_tensormap(&vmap);
+    }
   }
-  if (tid == 0) prefix[n_ls] = total;
-  __syncthreads();
-  const long long all = (long long)total * p.units_per;
-  const long long per_run = (all + gridDim.x - 1) / gridDim.x;      // runs without blocks are the last ones
-  long long at = per_run * blockIdx.x;
-  const long long stop = min(at + per_run, all);
+  // up to here nothing was read or written that an earlier kernel of the stream knows of
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  uint8_t* ring = smem + warp * 2 * kSlot;   // K of a pair, V of a pair
+  uint64_t* full = bars + warp * 2;          // the keys, the values have arrived
+  uint32_t phase = 0;
+  // places of a (layer, seq) per unit, summed
+  int total = 0;
+  if (n_ls <= 32) {      // every warp for itself, the same values
+    const int n = lane < n_ls ? places_of(p, lane) : 0;
+    int upto = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int below = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += below;
+    }
+    if (lane < n_ls) prefix[lane] = upto - n;
+    total = __shfl_sync(0xffffffffu, upto, 31);
+    if (lane == 0) prefix[n_ls] = total;
+    __syncwarp();
+  } else {
+    for (int base = 0; base < n_ls; base += kAttThreads) {
+      const int ls = base + tid;
+      const int n = ls < n_ls ? places_of(p, ls) : 0;
+      int sum;
+      const int at = block_exclusive_scan(n, warp_sums, sum);
+      if (ls < n_ls) prefix[ls] = total + at;
+      total += sum;
+    }
+    if (tid == 0) prefix[n_ls] = total;
+    __syncthreads();
+  }
+  // run i has the places from all * i / runs (rounded down) on; runs without any are the last ones
+  const int all = total * p.units_per, runs = min((int)gridDim.x, max(all, 1));
+  const int share = all / runs, left = all - share * runs;
+  const float per_runs = 1.f / (float)runs, runs_per_place = (float)runs / (float)max(all, 1);
+  // left * i < 2^20 and runs < 2^10: the product is off by less than half of 1 / runs, so the quotient is exact
+  auto run_start = [&](int i) { return share * i + (int)(((float)(left * i) + 0.5f) * per_runs); };
+  auto run_of = [&](int place) {
+    int i = (int)((float)place * runs_per_place);
+    while (run_start(i) > place) --i;
+    while (run_start(i + 1) <= place) ++i;
+    return i;
+  };
+  int at = run_start(blockIdx.x);
+  const int stop = (int)blockIdx.x < runs ? run_start(blockIdx.x + 1) : at;
+  if (tid == 0) p.lead[blockIdx.x] = make_int2(-1, 0);
   // sequences without tokens give zeros
   for (int e = blockIdx.x; e < n_ls; e += gridDim.x)
     if (prefix[e + 1] == prefix[e]) {
@@ -161,46 +253,114 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
         dst[(int64_t)h * p.out.sh + (int64_t)r * p.out.st + d] = T(0.f);
       }
     }
-  if (at >= stop) {
-    if (tid == 0) p.lead[blockIdx.x] = -1;
-    return;
-  }
+  if (at >= stop) return;
   int ls;
-  {   // the (layer, seq) that holds block `at`
+  {   // the (layer, seq) that holds place `at`
     int lo = 0, hi = n_ls - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if ((long long)prefix[mid] * p.units_per <= at) lo = mid; else hi = mid - 1;
+      if (prefix[mid] * p.units_per <= at) lo = mid; else hi = mid - 1;
     }
     ls = lo;
   }
   while (at < stop) {
-    while (prefix[ls + 1] == prefix[ls] || (long long)prefix[ls + 1] * p.units_per <= at) ++ls;
-    const int nb = prefix[ls + 1] - prefix[ls];
-    const long long inside = at - (long long)prefix[ls] * p.units_per;
-    const int uh = (int)(inside / nb), b0 = (int)(inside - (long long)uh * nb);       // (head, group), first block
-    const int b1 = (int)min((long long)nb, b0 + (stop - at));
-    const int head = uh / p.groups, group = uh - head * p.groups;
-    if (tid == 0 && at == per_run * blockIdx.x) p.lead[blockIdx.x] = b0 > 0 ? ls * p.units_per + uh : -1;
+    while (prefix[ls + 1] == prefix[ls] || prefix[ls + 1] * p.units_per <= at) ++ls;
+    const int places = prefix[ls + 1] - prefix[ls], nb = places - kSetUp;
+    const int inside = at - prefix[ls] * p.units_per;
+    const int uh = inside / places, v0 = inside - uh * places;            // (head, group), and how far into it
+    const int v1 = min(places, v0 + (stop - at));
+    const int b0 = max(v0 - kSetUp, 0), b1 = max(v1 - kSetUp, 0);         // first pair, and the one behind the last
+    const int begin = at - v0;
+    at += v1 - v0;
+    if (b0 == b1) continue;
+    const int head = p.groups == 1 ? uh : uh / p.groups, group = uh - head * p.groups;
+    if (tid == 0 && b0 > 0) {
+      // a unit's parts: of the run with its first pair, of the next one (which leads the join), and on to the one with its last
+      const int first = run_of(begin + kSetUp);
+      if (first == (int)blockIdx.x - 1) p.lead[blockIdx.x] = make_int2(ls * p.units_per + uh, run_of(begin + places - 1) - first + 1);
+    }
     const int layer = ls / p.table.n_seqs, seq = ls - layer * p.table.n_seqs;
     const int len = unit_len(p.table, p.pool, ls);
     const int col0 = group * COLS, ncols = min(COLS, p.cols - col0);
-    // ---- queries -> fragments: warp w takes columns w, w + 8, ... ----
-    for (int col = warp; col < COLS; col += kAttWarps) {
-      float x[D / 32];
-      float amax = 0.f;
+    // this warp's queries: columns w, w + 8, ...  Asked for before the keys, behind which they would have to wait
+    constexpr int E = D / 32;          // a lane's elements
+    float xq[NT][E];
+#pragma unroll
+    for (int y = 0; y < NT; ++y) {
+      const int col = warp + y * kAttWarps;
+#pragma unroll
+      for (int i = 0; i < E; ++i) xq[y][i] = 0.f;
       if (col < ncols) {
-        const int gi = (col0 + col) / p.n_rows, r = (col0 + col) - gi * p.n_rows;
-        const T* row = reinterpret_cast<const T*>(p.q.ptr) + (int64_t)layer * p.q.sl + (int64_t)seq * p.q.ss +
-                       (int64_t)(head * p.hn + gi) * p.q.sh + (int64_t)r * p.q.st;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) x[i] = to_f32(row[lane * (D / 32) + i]);
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) amax = fmaxf(amax, fabsf(x[i]));
-      } else {
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) x[i] = 0.f;
+        const int gi = p.n_rows == 1 ? col0 + col : (col0 + col) / p.n_rows, r = (col0 + col) - gi * p.n_rows;
+        load_elements<E>(reinterpret_cast<const T*>(p.q.ptr) + (int64_t)layer * p.q.sl + (int64_t)seq * p.q.ss +
+                             (int64_t)(head * p.hn + gi) * p.q.sh + (int64_t)r * p.q.st + lane * E,
+                         xq[y]);
       }
+    }
+    const int32_t* row = p.table.pages + (int64_t)ls * p.table.max_pages;
+    const int sh = p.per_shift;
+    int koff[KH], voff[2];              // where this lane's bytes of a K row and of the V rows of two tokens lie in a stage
+    {
+      const int r = token_of<D>(g);
+#pragma unroll
+      for (int h = 0; h < KH; ++h) koff[h] = r * D + (D == 128 ? (c + 4 * h) ^ r : c ^ (r >> 1)) * 16;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int t = token_of<D>(2 * c + i);
+        voff[i] = kSlot + t * D + (D == 128 ? (g ^ t) * 16 : ((g >> 1) ^ (t >> 1)) * 16 + (g & 1) * 8);
+      }
+    }
+    // this warp's pairs are b0 + warp + 8 n.  Lane i knows the pages and the scales of the i-th of 32 at a time; the next 32 are
+    // looked up while these are computed
+    const int n_it = b0 + warp < b1 ? (b1 - b0 - warp + kAttWarps - 1) / kAttWarps : 0;
+    auto block_of = [&](int n, int x) { return 2 * (b0 + warp + n * kAttWarps) + x; };
+    auto look_up = [&](int n, int x) {          // a page outside the pool, and a block behind the last token: -1
+      const int blk = block_of(n, x);
+      const int page = n < n_it && blk * kPagedBlock < len ? __ldg(row + (blk >> sh)) : -1;
+      return page < p.pool.n_pages ? page : -1;
+    };
+    auto scales_of = [&](int n, int x, int page) {
+      if (page < 0) return make_float2(-1.f, 0.f);
+      const int64_t at_block = (((int64_t)page * p.pool.heads + head) << sh) + (block_of(n, x) & ((1 << sh) - 1));
+      return make_float2(__ldg(p.pool.ks + at_block), __ldg(p.pool.vs + at_block));
+    };
+    int page[2], page_next[2];
+    float2 scales[2], scales_next[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      page[x] = look_up(lane, x);
+      page_next[x] = -1;
+      scales_next[x] = make_float2(-1.f, 0.f);
+    }
+    // K or V of pair n on its way: the lane that knows its pages sends for it
+    auto fetch = [&](int n, bool next, int v) {
+      if (lane == (n & 31)) {
+        const int pg[2] = {next ? page_next[0] : page[0], next ? page_next[1] : page[1]};
+        uint64_t* bar = full + v;
+        const int blocks = (pg[0] >= 0) + (pg[1] >= 0);
+        if (blocks) ptx::mbar_expect_tx(bar, blocks * kHalf);
+        else ptx::mbar_arrive(bar);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (pg[x] >= 0)
+            ptx::tma_load_3d(ring + v * kSlot + x * kHalf, v ? &vmap : &kmap, bar, 0, head * p.pool.ps + (block_of(n, x) & ((1 << sh) - 1)) * kPagedBlock, pg[x]);
+      }
+    };
+    if (n_it > 0) {
+      fetch(0, false, 0);
+      fetch(0, false, 1);
+    }
+    int owed = 0;                       // copies that a wait which gave up has left: 1 the keys', 2 the values', 4 the next keys'
+#pragma unroll
+    for (int x = 0; x < 2; ++x) scales[x] = scales_of(lane, x, page[x]);
+    // ---- queries -> fragments ----
+#pragma unroll
+    for (int y = 0; y < NT; ++y) {
+      const int col = warp + y * kAttWarps;
+      float (&x)[E] = xq[y];
+      float amax = 0.f;
+#pragma unroll
+      for (int i = 0; i < E; ++i) amax = fmaxf(amax, fabsf(x[i]));
 #pragma unroll
       for (int o = 16; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
       // power of two that brings the largest element into [2^14, 2^15); an infinite or NaN row goes through as it is
@@ -208,11 +368,10 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
       if (amax > 0.f && amax < CUDART_INF_F) e = min(max(14 - ilogbf(amax), -126), 126);
       const float up = __int_as_float((127 + e) << 23);
       const float down = __int_as_float((127 - e) << 23);
-      if (lane == 0) sfac[col] = p.scale * down;
       // element d sits in k-step (d / 64) * 4 + (d % 16) / 4 of the lanes with (d % 64) / 16 as their place in the quad
-      constexpr int E = D / 32;          // this lane's elements: 4 or 2 neighbours
       const int d0 = lane * E;
       const int ks = (d0 / 64) * 4 + (d0 % 16) / 4, owner = (col & 7) * 4 + (d0 % 64) / 16;
+      float sum = 0.f;
 #pragma unroll
       for (int pc = 0; pc < NP; ++pc) {
         uint32_t h[E / 2];
@@ -223,14 +382,23 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
           const float2 got = unpack_half2(h[i]);
           x[2 * i] = a - got.x;
           x[2 * i + 1] = b - got.y;
+          sum += got.x + got.y;
         }
-        uint2* slot = sq + ((pc * NT + (col >> 3)) * KS + ks) * 32 + owner;
-        if constexpr (E == 4) *slot = make_uint2(h[0], h[1]);
-        else reinterpret_cast<uint32_t*>(slot)[(d0 % 4) / 2] = h[0];
+        uint2* to = sq + ((pc * NT + (col >> 3)) * KS + ks) * 32 + owner;
+        if constexpr (E == 4) *to = make_uint2(h[0], h[1]);
+        else reinterpret_cast<uint32_t*>(to)[(d0 % 4) / 2] = h[0];
+      }
+      if constexpr (kOffset) {
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      }
+      if (lane == 0) {
+        sfac[col] = kOffset ? p.scale * down * 16777216.f : p.scale * down;
+        scorr[col] = kOffset ? p.scale * down * sum * 128.f : 0.f;
       }
     }
     __syncthreads();
-    float fac[NT][2];
+    float fac[NT][2], corr[NT][2];
     int lim[NT][2];                     // tokens that a column sees
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -238,9 +406,11 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
       for (int i = 0; i < 2; ++i) {
         const int col = 8 * t + 2 * c + i;
         fac[t][i] = sfac[col];
-        lim[t][i] = col < ncols ? len - p.n_rows + 1 + (col0 + col) % p.n_rows : 0;
+        corr[t][i] = scorr[col];
+        lim[t][i] = col < ncols ? len - p.n_rows + 1 + (p.n_rows == 1 ? 0 : (col0 + col) % p.n_rows) : 0;
       }
     float o[KS][NT][4], m[NT][2], l[NT][2];
+    float vref = 0.f;                   // one piece: O is in units of this, a power of two above every scale so far
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       m[t][0] = m[t][1] = -CUDART_INF_F;
@@ -250,94 +420,102 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[k][t][i] = 0.f;
     }
-    const int32_t* row = p.table.pages + (int64_t)ls * p.table.max_pages;
-    const int sh = p.per_shift;
-    // block b of the sequence -> its place in the pool, or -1
-    auto place = [&](int page, int b) -> int64_t {
-      return page >= 0 && page < p.pool.n_pages ? (((int64_t)page * p.pool.heads + head) << sh) + (b & ((1 << sh) - 1)) : -1;
-    };
-    uint4 kr[2][KH];
-    uint32_t vr[4][VW];
-    float ks_c = 0.f, vs_c = 0.f;
-    const int koff = g * D + c * 16, voff = 2 * c * D + g * (D / 8);
-    auto load_k = [&](int64_t at_block) {
-      if (at_block < 0) return;
-      const uint8_t* src = p.pool.kc + at_block * (kPagedBlock * D) + koff;
+    for (int n = 0; n < n_it; ++n) {
+      if ((n & 31) == 0 && n) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
+        for (int x = 0; x < 2; ++x) { page[x] = page_next[x]; scales[x] = scales_next[x]; }
+      }
+      if ((n & 31) == 8) {
 #pragma unroll
-        for (int h = 0; h < KH; ++h) kr[r][h] = load_code16(src + r * 8 * D + h * 64);
-      ks_c = __ldg(p.pool.ks + at_block);
-    };
-    auto load_v = [&](int64_t at_block) {
-      if (at_block < 0) return;
-      const uint8_t* src = p.pool.vc + at_block * (kPagedBlock * D) + voff;
+        for (int x = 0; x < 2; ++x) page_next[x] = look_up((n & ~31) + 32 + lane, x);
+      }
+      if ((n & 31) == 20) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const uint8_t* s = src + ((r & 1) + (r >> 1) * 8) * D;
-        if constexpr (VW == 4) {
-          const uint4 v = load_code16(s);
-          vr[r][0] = v.x; vr[r][1] = v.y; vr[r][2] = v.z; vr[r][3] = v.w;
-        } else {
-          const uint2 v = load_code8(s);
-          vr[r][0] = v.x; vr[r][1] = v.y;
+        for (int x = 0; x < 2; ++x) scales_next[x] = scales_of((n & ~31) + 32 + lane, x, page_next[x]);
+      }
+      float ks_b[2], vs_b[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        ks_b[x] = __shfl_sync(0xffffffffu, scales[x].x, n & 31);
+        vs_b[x] = __shfl_sync(0xffffffffu, scales[x].y, n & 31);
+      }
+      if (!ptx::mbar_wait(full, phase, abort_flag, p.wait_cycles)) {
+        owed = 3;
+        break;
+      }
+      // ---- scores of both blocks ----
+      float sc[2][NT][4];
+#pragma unroll
+      for (int h = 0; h < KH; ++h) {
+        uint4 kr[2][2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) kr[x][r] = *reinterpret_cast<const uint4*>(ring + koff[h] + x * kHalf + r * 8 * D);
+#pragma unroll
+        for (int k4 = 0; k4 < 4; ++k4) {
+          const int k = 4 * h + k4;
+          uint32_t a[2][4];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const uint4 &r0 = kr[x][0], &r1 = kr[x][1];
+            const uint32_t w0 = prepare_codes<FMT>(k4 == 0 ? r0.x : k4 == 1 ? r0.y : k4 == 2 ? r0.z : r0.w);
+            const uint32_t w1 = prepare_codes<FMT>(k4 == 0 ? r1.x : k4 == 1 ? r1.y : k4 == 2 ? r1.z : r1.w);
+            a[x][0] = kOffset ? offset_to_half2<0>(w0) : codes_to_half2<FMT, 0>(w0);
+            a[x][1] = kOffset ? offset_to_half2<0>(w1) : codes_to_half2<FMT, 0>(w1);
+            a[x][2] = kOffset ? offset_to_half2<1>(w0) : codes_to_half2<FMT, 1>(w0);
+            a[x][3] = kOffset ? offset_to_half2<1>(w1) : codes_to_half2<FMT, 1>(w1);
+          }
+#pragma unroll
+          for (int pc = 0; pc < NP; ++pc)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              const uint2 qf = sq[((pc * NT + t) * KS + k) * 32 + lane];
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                if (k == 0 && pc == 0) mma16816_first(sc[x][t], a[x], qf);
+                else mma16816(sc[x][t], a[x], qf);
+              }
+            }
         }
       }
-      vs_c = __ldg(p.pool.vs + at_block);
-    };
-    int b = b0 + warp;
-    int64_t cur = -1, nxt = -1;
-    if (b < b1) {
-      cur = place(__ldg(row + (b >> sh)), b);
-      load_k(cur);
-      load_v(cur);
-    }
-    int page_n = b + kAttWarps < b1 ? __ldg(row + ((b + kAttWarps) >> sh)) : -1;
-    for (; b < b1; b += kAttWarps) {
-      const int bn = b + kAttWarps;
-      nxt = bn < b1 ? place(page_n, bn) : -1;
-      page_n = bn + kAttWarps < b1 ? __ldg(row + ((bn + kAttWarps) >> sh)) : -1;
-      // ---- scores ----
-      float sc[NT][4];
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const uint4& r0 = kr[0][k / 4];
-        const uint4& r1 = kr[1][k / 4];
-        const uint32_t w0 = prepare_codes<FMT>((k & 3) == 0 ? r0.x : (k & 3) == 1 ? r0.y : (k & 3) == 2 ? r0.z : r0.w);
-        const uint32_t w1 = prepare_codes<FMT>((k & 3) == 0 ? r1.x : (k & 3) == 1 ? r1.y : (k & 3) == 2 ? r1.z : r1.w);
-        const uint32_t a[4] = {codes_to_half2<FMT, 0>(w0), codes_to_half2<FMT, 0>(w1), codes_to_half2<FMT, 1>(w0), codes_to_half2<FMT, 1>(w1)};
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int pc = 0; pc < NP; ++pc) {
-            const uint2 b = sq[((pc * NT + t) * KS + k) * 32 + lane];
-            if (k == 0 && pc == 0) mma16816_first(sc[t], a, b);
-            else mma16816(sc[t], a, b);
-          }
-      }
-      const float ks_b = ks_c;
-      load_k(nxt);
+      __syncwarp();                     // every lane has read the keys
+      const bool more = n + 1 < n_it, crosses = (n & 31) == 31;
+      if (more) fetch(n + 1, crosses, 0);
       // ---- softmax weights ----
-      const int t0 = b * kPagedBlock;
-      const bool masked = cur < 0 || t0 + kPagedBlock > len - p.n_rows + 1;
-      bool rise = false;
+      const int t0 = block_of(n, 0) * kPagedBlock;
+      const bool masked = ks_b[0] == -1.f || ks_b[1] == -1.f || t0 + 2 * kPagedBlock > len - p.n_rows + 1;
+      float high[NT][2];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sc[t][i] *= ks_b * fac[t][i & 1];
-        if (masked) {
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (cur < 0 || t0 + g + (i >> 1) * 8 >= lim[t][i & 1]) sc[t][i] = -CUDART_INF_F;
-        }
-        rise |= fmaxf(sc[t][0], sc[t][2]) > m[t][0] + kAttLazy || fmaxf(sc[t][1], sc[t][3]) > m[t][1] + kAttLazy;
+          for (int x = 0; x < 2; ++x) sc[x][t][i] = kOffset ? fmaf(sc[x][t][i], fac[t][i & 1], -corr[t][i & 1]) * ks_b[x] : sc[x][t][i] * (ks_b[x] * fac[t][i & 1]);
       }
+      if (masked) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (ks_b[x] == -1.f || t0 + x * kPagedBlock + token_of<D>(g) + (i >> 1) * 8 >= lim[t][i & 1]) sc[x][t][i] = -CUDART_INF_F;
+      }
+      bool rise = false;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          high[t][i] = fmaxf(fmaxf(sc[0][t][i], sc[0][t][i + 2]), fmaxf(sc[1][t][i], sc[1][t][i + 2]));
+          rise |= high[t][i] > m[t][i] + kAttLazy;
+        }
       if (__any_sync(0xffffffffu, rise)) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float x = fmaxf(sc[t][i], sc[t][i + 2]);
+            float x = high[t][i];
 #pragma unroll
             for (int d = 4; d <= 16; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
             x = fmaxf(x, m[t][i]);
@@ -351,63 +529,134 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
             }
           }
       }
-      uint2 pf[NT][NP];
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        float w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float ref = m[t][i & 1] == -CUDART_INF_F ? 0.f : m[t][i & 1];
-          w[i] = pow2(sc[t][i] - ref);
-        }
-        l[t][0] += w[0] + w[2];
-        l[t][1] += w[1] + w[3];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] *= kAttPScale;
-#pragma unroll
-        for (int pc = 0; pc < NP; ++pc) {
-          const uint32_t h0 = pack_half2(w[0], w[1]), h1 = pack_half2(w[2], w[3]);
-          pf[t][pc] = make_uint2(transpose8x8(h0), transpose8x8(h1));
-          if (pc + 1 < NP) {
-            const float2 g0 = unpack_half2(h0), g1 = unpack_half2(h1);
-            w[0] -= g0.x; w[1] -= g0.y; w[2] -= g1.x; w[3] -= g1.y;
-          }
-        }
-      }
-      // ---- values ----
-      const float sv = (cur < 0 ? 0.f : vs_c) * kVFactor;
-      float svc[NT][2];      // a column that sees nothing of the block takes nothing from it, not even a NaN
+      float ref[NT][2];
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) svc[t][i] = masked && t0 >= lim[t][i] ? 0.f : sv;
+        for (int i = 0; i < 2; ++i) ref[t][i] = m[t][i] == -CUDART_INF_F ? 0.f : m[t][i];
+      if (!ptx::mbar_wait(full + 1, phase, abort_flag, p.wait_cycles)) {
+        owed = more ? 6 : 2;
+        break;
+      }
+      phase ^= 1;
 #pragma unroll
-      for (int q = 0; q < VW; ++q) {
-        uint32_t w[4];
+      for (int x = 0; x < 2; ++x) {
+        // one piece: a block's scale joins its weights, relative to the largest scale so far, unless it is much smaller (the weights
+        // would run out of fp16's range) or the block is masked; then, and for two pieces always, it is applied to the block's product
+        float ratio = vs_b[x];
+        bool joined = false;
+        if constexpr (NP == 1) {
+          if (vs_b[x] > vref) {                      // (not for a NaN)
+            const float to = __uint_as_float((__float_as_uint(vs_b[x]) & 0x7F800000u) + 0x00800000u);   // the next power of two
+            const float f = vref / to;
+            vref = to;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          w[r] = prepare_codes<FMT>(vr[r][q]);
-          if (FMT == SPINDLEKV_PAGED_E4M3 && masked) w[r] = without_nan(w[r]);
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+              for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[k][t][i] *= f;
+          }
+          ratio = vs_b[x] == 0.f ? 0.f : vs_b[x] / vref;
+          joined = !masked && ratio >= 0.00390625f;
         }
+        const float wfac = joined ? ratio * kAttPScale : kAttPScale;
+        uint2 pf[NT][NP];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          // elements 4 q + 2 x and + 1 of the lane's piece: tokens 2c, 2c+1 in one word, 2c+8, 2c+9 in the other
-          const uint32_t lo = __byte_perm(w[0], w[1], x ? 0x7362 : 0x5140), hi = __byte_perm(w[2], w[3], x ? 0x7362 : 0x5140);
-          const uint32_t a[4] = {codes_to_half2<FMT, 0>(lo), codes_to_half2<FMT, 1>(lo), codes_to_half2<FMT, 0>(hi), codes_to_half2<FMT, 1>(hi)};
+        for (int t = 0; t < NT; ++t) {
+          float w[4];
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            float acc[4];
-            mma16816_first(acc, a, pf[t][0]);
-            if constexpr (NP == 2) mma16816(acc, a, pf[t][1]);
+          for (int i = 0; i < 4; ++i) w[i] = pow2(sc[x][t][i] - ref[t][i & 1]);
+          l[t][0] += w[0] + w[2];
+          l[t][1] += w[1] + w[3];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[2 * q + x][t][i] = fmaf(svc[t][i & 1], acc[i], o[2 * q + x][t][i]);
+          for (int i = 0; i < 4; ++i) w[i] *= wfac;
+#pragma unroll
+          for (int pc = 0; pc < NP; ++pc) {
+            const uint32_t h0 = pack_half2(w[0], w[1]), h1 = pack_half2(w[2], w[3]);
+            pf[t][pc] = make_uint2(transpose8x8(h0), transpose8x8(h1));
+            if (pc + 1 < NP) {
+              const float2 g0 = unpack_half2(h0), g1 = unpack_half2(h1);
+              w[0] -= g0.x; w[1] -= g0.y; w[2] -= g1.x; w[3] -= g1.y;
+            }
           }
         }
+        // ---- values ----
+        uint32_t vr[4][VW];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint8_t* src = ring + voff[r & 1] + x * kHalf + (r >> 1) * 8 * D;
+          if constexpr (VW == 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(src);
+            vr[r][0] = v.x; vr[r][1] = v.y; vr[r][2] = v.z; vr[r][3] = v.w;
+          } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(src);
+            vr[r][0] = v.x; vr[r][1] = v.y;
+          }
+        }
+        if (FMT == SPINDLEKV_PAGED_E4M3 && masked) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int q = 0; q < VW; ++q) vr[r][q] = without_nan(vr[r][q]);
+        }
+        // elements 4 q + 2 y and + 1 of the lane's piece: tokens of columns 2c, 2c+1 in one word, 2c+8, 2c+9 in the other
+        auto operand = [&](int q, int y, uint32_t (&a)[4]) {
+          uint32_t w[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) w[r] = prepare_codes<FMT>(vr[r][q]);
+          const uint32_t lo = __byte_perm(w[0], w[1], y ? 0x7362 : 0x5140), hi = __byte_perm(w[2], w[3], y ? 0x7362 : 0x5140);
+          a[0] = codes_to_half2<FMT, 0>(lo);
+          a[1] = codes_to_half2<FMT, 1>(lo);
+          a[2] = codes_to_half2<FMT, 0>(hi);
+          a[3] = codes_to_half2<FMT, 1>(hi);
+        };
+        if (joined) {
+#pragma unroll
+          for (int q = 0; q < VW; ++q)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              uint32_t a[4];
+              operand(q, y, a);
+#pragma unroll
+              for (int t = 0; t < NT; ++t) mma16816(o[2 * q + y][t], a, pf[t][0]);
+            }
+        } else {
+          float svc[NT][2];      // a column that sees nothing of the block takes nothing from it, not even a NaN
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) svc[t][i] = masked && t0 + x * kPagedBlock >= lim[t][i] ? 0.f : ratio;
+#pragma unroll
+          for (int q = 0; q < VW; ++q)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              uint32_t a[4];
+              operand(q, y, a);
+#pragma unroll
+              for (int t = 0; t < NT; ++t) {
+                float acc[4];
+                mma16816_first(acc, a, pf[t][0]);
+                if constexpr (NP == 2) mma16816(acc, a, pf[t][1]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[2 * q + y][t][i] = fmaf(svc[t][i & 1], acc[i], o[2 * q + y][t][i]);
+              }
+            }
+        }
       }
-      load_v(nxt);
-      cur = nxt;
+      __syncwarp();                     // and the values
+      if (more) fetch(n + 1, crosses, 1);
     }
-    // ---- the warps' results meet ----
+    // ---- the warps' results meet, where the ring was ----
+    __syncthreads();
+    if (*abort_flag) {
+      // give up, but not before what is still on its way has arrived (within the same bound)
+      if (owed & 1) ptx::mbar_wait(full, phase, abort_flag + 1, p.wait_cycles);
+      if (owed & 2) ptx::mbar_wait(full + 1, phase, abort_flag + 1, p.wait_cycles);
+      if (owed & 4) ptx::mbar_wait(full, phase ^ 1, abort_flag + 1, p.wait_cycles);
+      if (tid == 0) p.lead[blockIdx.x] = make_int2(-2, 0);
+      return;
+    }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -419,17 +668,18 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
           sm_l[warp * COLS + 8 * t + 2 * c + i] = l[t][i];
         }
       }
+    const float unit = (NP == 1 ? vref : 1.f) / kAttPScale;
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int i = 0; i < 2; ++i)   // elements d, d + 1 of column 2c + i
-          *reinterpret_cast<float2*>(so + (warp * COLS + 8 * t + 2 * c + i) * OP + g * (D / 8) + 2 * k) = make_float2(o[k][t][i], o[k][t][i + 2]);
+          *reinterpret_cast<float2*>(so + (warp * COLS + 8 * t + 2 * c + i) * OP + g * (D / 8) + 2 * k) = make_float2(o[k][t][i] * unit, o[k][t][i + 2] * unit);
     __syncthreads();
     const bool whole = b0 == 0 && b1 == nb;
     // what is left for the join: a unit that began in an earlier run is this run's first, one that begins here and goes on its last
-    const int64_t slot = (int64_t)(2 * blockIdx.x + (b0 == 0 ? 1 : 0)) * kAttMaxCols;
+    const int64_t place = (int64_t)(2 * blockIdx.x + (b0 == 0 ? 1 : 0)) * kAttMaxCols;
     for (int i = tid; i < ncols * (D / 4); i += kAttThreads) {
       const int col = i / (D / 4), d = (i - col * (D / 4)) * 4;
       float top = -CUDART_INF_F;
@@ -458,14 +708,13 @@ __global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_ker
           *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&e));
         }
       } else {
-        *reinterpret_cast<float4*>(p.part + (slot + col) * D + d) = sum;
-        if (d == 0) p.stat[slot + col] = make_float2(top, den);
+        *reinterpret_cast<float4*>(p.part + (place + col) * D + d) = sum;
+        if (d == 0) p.stat[place + col] = make_float2(top, den);
       }
     }
-    __syncthreads();          // the shared memory is free for the next segment
-    at += b1 - b0;
+    ptx::fence_proxy_async();
+    __syncthreads();          // the shared memory is free for the next segment's copies
   }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 // Joins the parts of a unit: block (j, x) takes four columns of the unit that run j is the first to continue.  Four warps to a
@@ -478,10 +727,17 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(AttendParams p
   __shared__ float so[4][4][D];
   __shared__ float sden[4];
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int run = blockIdx.x, unit = p.lead[run];
-  if (unit < 0 || (run > 0 && p.lead[run - 1] == unit)) return;
-  int n = 1;                                 // parts: the run before, which the unit begins in, and those that continue it
-  for (int r = run; r < (int)gridDim.x; r += kJoinThreads) n += __syncthreads_count(r + (int)threadIdx.x < (int)gridDim.x && p.lead[r + threadIdx.x] == unit);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (blockIdx.x == 0 && blockIdx.y == 0) {
+    bool gave_up = false;
+    for (int r = threadIdx.x; r < (int)gridDim.x; r += kJoinThreads) gave_up |= p.lead[r].x == -2;
+    gave_up = __syncthreads_or(gave_up);
+    if (threadIdx.x == 0) p.hdr[kHdrStatus] = gave_up ? SPINDLEKV_TIMEOUT : SPINDLEKV_OK;
+  }
+  const int run = blockIdx.x;
+  const int2 lead = p.lead[run];
+  const int unit = lead.x, n = lead.y;       // parts: of the run before, in which the unit begins, of this one, and so on
+  if (unit < 0) return;
   const int ls = unit / p.units_per, uh = unit - ls * p.units_per, head = uh / p.groups, group = uh - head * p.groups;
   const int layer = ls / p.table.n_seqs, seq = ls - layer * p.table.n_seqs;
   const int col0 = group * cols_per_unit, ncols = min(cols_per_unit, p.cols - col0);
@@ -489,32 +745,39 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(AttendParams p
   const int col = blockIdx.y * 4 + which;
   const bool mine = col < ncols;
   auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * (run - 1) + 1 : 2 * (run - 1 + i)) * kAttMaxCols + col; };
-  float num[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) num[e] = 0.f;
   if (mine) {
-    float top = -CUDART_INF_F;
-    for (int i = lane; i < n; i += 32) top = fmaxf(top, p.stat[slot(i)].x);
+    float num[E], den = 0.f, top = -CUDART_INF_F;
 #pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    float den = 0.f;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-      float f = 0.f;
-      if (i0 + lane < n) {
-        const float2 st = p.stat[slot(i0 + lane)];
-        f = st.x == top ? 1.f : pow2(st.x - top);
-        den = fmaf(f, st.y, den);
+    for (int e = 0; e < E; ++e) num[e] = 0.f;
+    // 64 parts at a time, 16 to a warp, all of them asked for at once; the weights are formed meanwhile
+    for (int i0 = 0; i0 < n; i0 += 64) {
+      float v[16][E];
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (i0 + 4 * k + turn < n) load_elements<E>(p.part + slot(i0 + 4 * k + turn) * D + lane * E, v[k]);
+      float2 st[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) st[h] = i0 + 32 * h + lane < n ? p.stat[slot(i0 + 32 * h + lane)] : make_float2(-CUDART_INF_F, 0.f);
+      float high = fmaxf(top, fmaxf(st[0].x, st[1].x));
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
+      const float old = top == high ? 1.f : pow2(top - high);
+      top = high;
+      den *= old;
+#pragma unroll
+      for (int e = 0; e < E; ++e) num[e] *= old;
+      float f[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        f[h] = st[h].x == top ? 1.f : pow2(st[h].x - top);
+        den = fmaf(f[h], st[h].y, den);
       }
-      const int last = min(32, n - i0);
-#pragma unroll 4
-      for (int k = turn; k < last; k += 4) {
-        const float w = __shfl_sync(0xffffffffu, f, k);
-        const float* src = p.part + slot(i0 + k) * D + lane * E;
 #pragma unroll
-        for (int e = 0; e < E; e += 2) {
-          const float2 v = *reinterpret_cast<const float2*>(src + e);
-          num[e] = fmaf(w, v.x, num[e]);
-          num[e + 1] = fmaf(w, v.y, num[e + 1]);
+      for (int k = 0; k < 16; ++k) {
+        const float w = __shfl_sync(0xffffffffu, f[k >> 3], (4 * k + turn) & 31);
+        if (i0 + 4 * k + turn < n) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) num[e] = fmaf(w, v[k][e], num[e]);
         }
       }
     }
@@ -556,52 +819,61 @@ static int column_tiles(int cols) { return cols <= 8 ? 1 : cols <= 16 ? 2 : 4; }
 constexpr size_t kPartRows = (size_t)2 * kAttMaxRuns * kAttMaxCols;
 
 size_t paged_workspace_bytes(const spindlekv_page_pool& pool) {
-  return kHeaderBytes + kPartRows * (pool.head_dim * sizeof(float) + sizeof(float2)) + kAttMaxRuns * sizeof(int32_t);
+  return kHeaderBytes + kPartRows * (pool.head_dim * sizeof(float) + sizeof(float2)) + kAttMaxRuns * sizeof(int2);
 }
 
 template <typename T, int FMT, int D, int NT>
-static spindlekv_status launch_attend(AttendParams& p, int max_len, cudaStream_t st) {
+static spindlekv_status launch_attend(AttendParams& p, const CUtensorMap& kmap, const CUtensorMap& vmap, int max_len, cudaStream_t st) {
   static int resident[kMaxDevices] = {};
   const int dev = PerDeviceOnce::current();
   if (dev < 0) return SPINDLEKV_CUDA;
   constexpr int NP = sizeof(T) == 4 ? 2 : 1, COLS = 8 * NT;
   const int n_ls = p.table.n_layers * p.table.n_seqs;
   auto kernel = paged_attend_kernel<T, FMT, D, NT>;
-  const size_t fixed = (size_t)kAttWarps * COLS * (D + 4) * 4 + (size_t)NP * NT * (D / 16) * 32 * 8 + (size_t)COLS * 4 * (1 + 2 * kAttWarps) + 36 * 4;
+  const size_t fixed = 1024 + ring_bytes<D, NT>() + (size_t)kAttWarps * 16 + 16 + (size_t)NP * NT * (D / 16) * 32 * 8 + (size_t)COLS * 4 * (2 + 2 * kAttWarps) + 36 * 4;
   const size_t smem = align_up(fixed + (size_t)(n_ls + 1) * 4, 16);
   // the prefix sums of a usual batch do not change how many blocks fit; with those of thousands of sequences fewer may, and
   // the rest simply follow
   const int slots = resident_blocks(kernel, align_up(fixed + 1024, 16), resident, dev);
   if (slots <= 0) return SPINDLEKV_CUDA;
-  // a run of fewer blocks than there are warps leaves warps idle
-  const int64_t line = (int64_t)n_ls * p.units_per * ceil_div((int)std::min<int64_t>(max_len, (int64_t)p.table.max_pages * p.pool.ps), kPagedBlock);
+  // a run of fewer pairs than there are warps leaves warps idle
+  const int64_t capacity = (int64_t)p.table.max_pages * p.pool.ps;
+  const int64_t line = (int64_t)n_ls * p.units_per * ceil_div((int)std::min<int64_t>(max_len, capacity), 2 * kPagedBlock);   // pairs
+  if ((int64_t)n_ls * p.units_per * ((capacity + 2 * kPagedBlock - 1) / (2 * kPagedBlock) + kSetUp) > 0x7FFFFFFF) return SPINDLEKV_UNSUPPORTED;
   const int runs = (int)std::min<int64_t>(std::min(slots, kAttMaxRuns), std::max<int64_t>((line + kAttWarps - 1) / kAttWarps, 1));
-  {
-    LaunchScope ls(KC_PAGED_ATTEND, st);
-    kernel<<<runs, kAttThreads, smem, st>>>(p);
-  }
-  if (cudaGetLastError() != cudaSuccess) return SPINDLEKV_CUDA;
+  // both kernels may be made ready while the one before them on the stream still runs; they wait for it before they touch memory
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(runs, ceil_div(std::min(COLS, p.cols), 4));
-  cfg.blockDim = dim3(kJoinThreads);
+  cfg.gridDim = dim3(runs);
+  cfg.blockDim = dim3(kAttThreads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
+  {
+    LaunchScope ls(KC_PAGED_ATTEND, st);
+    if (cudaLaunchKernelEx(&cfg, kernel, kmap, vmap, p) != cudaSuccess) return SPINDLEKV_CUDA;
+  }
+  cfg.gridDim = dim3(runs, ceil_div(std::min(COLS, p.cols), 4));
+  cfg.blockDim = dim3(kJoinThreads);
+  cfg.dynamicSmemBytes = 0;
   LaunchScope ls(KC_PAGED_ATTEND, st);
   return cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D>, p, COLS) == cudaSuccess ? SPINDLEKV_OK : SPINDLEKV_CUDA;
 }
 
 template <typename T, int FMT, int D>
 static spindlekv_status launch_columns(AttendParams& p, int max_len, cudaStream_t st) {
+  CUtensorMap kmap, vmap;
+  const int rows = p.pool.heads * p.pool.ps;
+  if (!make_code_map(&kmap, p.pool.kc, D, rows, p.pool.n_pages) || !make_code_map(&vmap, p.pool.vc, D, rows, p.pool.n_pages)) return SPINDLEKV_CUDA;
   const int nt = column_tiles(p.cols);
   p.groups = ceil_div(p.cols, 8 * nt);
   p.units_per = p.pool.heads * p.groups;
-  if (nt == 1) return launch_attend<T, FMT, D, 1>(p, max_len, st);
-  if (nt == 2) return launch_attend<T, FMT, D, 2>(p, max_len, st);
-  return launch_attend<T, FMT, D, 4>(p, max_len, st);
+  if (nt == 1) return launch_attend<T, FMT, D, 1>(p, kmap, vmap, max_len, st);
+  if (nt == 2) return launch_attend<T, FMT, D, 2>(p, kmap, vmap, max_len, st);
+  return launch_attend<T, FMT, D, 4>(p, kmap, vmap, max_len, st);
 }
 
 template <typename T>
@@ -626,8 +898,10 @@ spindlekv_status paged_attend_impl(const spindlekv_page_pool& pool, const spindl
   p.cols = p.hn * n_rows;
   p.scale = (scale == 0.f ? 1.f / sqrtf((float)pool.head_dim) : scale) * 1.44269504088896340736f;
   p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kHeaderBytes);
+  p.hdr = static_cast<uint32_t*>(ws);
+  p.wait_cycles = current_tuning().mbar_wait_cycles;
   p.stat = reinterpret_cast<float2*>(p.part + kPartRows * pool.head_dim);
-  p.lead = reinterpret_cast<int32_t*>(p.stat + kPartRows);
+  p.lead = reinterpret_cast<int2*>(p.stat + kPartRows);
   return q.dtype == SPINDLEKV_BF16 ? launch_format<__nv_bfloat16>(p, pool.format, max_len, st) : launch_format<float>(p, pool.format, max_len, st);
 }
 
