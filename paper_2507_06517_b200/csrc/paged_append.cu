@@ -1,14 +1,14 @@
 // Rows -> codes of the 8-bit paged cache, one scale per block of 16 tokens and head.
 //
 // One warp per (layer, sequence, KV head, block, K or V).  A lane holds 8 neighbouring elements of every (D/8)th ... row of
-// the block, so that a block's rows are in registers once: the largest magnitude is an integer maximum of the magnitudes'
-// bits (a NaN is larger than an infinity, an infinity larger than any number, so either shows), one warp reduction gives the
-// scale, and the codes leave from the same registers.  A block that begins with earlier tokens takes the larger of both scales; only if
+// the block, so that a block's rows are in registers once: the largest magnitude (in which a NaN or an infinity shows), one warp
+// reduction of its bits, the scale, and the codes leave from the same registers.  A block that begins with earlier tokens takes the larger of both scales; only if
 // that grows are the earlier codes read and rounded again.
 //
 // int8: code = nearest integer to x / s, ties to even, on the exact quotient.  q0 = rint(x * (1/s)) is off by one at most;
 // r = x - q0 s is exact in fp32 (one fused multiply-add: |r| <= s, and both x and q0 s are multiples of a unit within 24 bits of
-// s), so comparing |r| with s/2 settles the rest without a division per element.
+// s), so comparing |r| with s/2 settles the rest without a division per element.  Rounding is the addition of 1.5 2^23, whose sum's low
+// byte is the code; only a warp in which some |r| reaches s/2 (one in fifty) takes the second look.
 // E4M3: s is a power of two, x / s exact, the conversion instruction rounds once.
 #include <algorithm>
 
@@ -53,20 +53,39 @@ __device__ __forceinline__ int round_int8(float x, float s, float inv) {
   return (int)fminf(fmaxf(q, -127.f), 127.f);
 }
 
+// low bytes of eight words
+__device__ __forceinline__ uint2 low_bytes(const uint32_t (&t)[8]) {
+  return make_uint2(__byte_perm(__byte_perm(t[0], t[1], 0x0040), __byte_perm(t[2], t[3], 0x0040), 0x5410),
+                    __byte_perm(__byte_perm(t[4], t[5], 0x0040), __byte_perm(t[6], t[7], 0x0040), 0x5410));
+}
+
+// worst: the largest |x - code * s| so far (int8)
 template <int FMT>
-__device__ __forceinline__ uint2 encode8(const float (&x)[8], float s, float inv) {
-  uint32_t w[2] = {0u, 0u};
+__device__ __forceinline__ uint2 encode8(const float (&x)[8], float s, float inv, float& worst) {
   if constexpr (FMT == SPINDLEKV_PAGED_INT8) {
+    uint32_t t[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t)(round_int8(x[i], s, inv) & 0xFF) << (8 * (i & 3));
+    for (int i = 0; i < 8; ++i) {
+      const float sum = fmaf(x[i], inv, 12582912.f);
+      t[i] = __float_as_uint(sum);
+      worst = fmaxf(worst, fabsf(fmaf(12582912.f - sum, s, x[i])));
+    }
+    return low_bytes(t);
   } else {
+    uint32_t w[2] = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t two = __nv_cvt_float2_to_fp8x2(make_float2(x[2 * i] * inv, x[2 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
       w[i >> 1] |= two << (16 * (i & 1));
     }
+    return make_uint2(w[0], w[1]);
   }
-  return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ uint2 encode8_exactly(const float (&x)[8], float s, float inv) {
+  uint32_t t[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t[i] = (uint32_t)round_int8(x[i], s, inv);
+  return low_bytes(t);
 }
 
 // codes at scale `was` -> codes at the larger scale `s`
@@ -99,12 +118,19 @@ __device__ __forceinline__ uint2 recode8(uint2 c, float was, float s) {
 // 8 elements as they lie in memory
 template <typename T> struct Raw8;
 template <> struct Raw8<__nv_bfloat16> {
+  using Max = __nv_bfloat162;
+  __device__ __forceinline__ static Max none() { return __floats2bfloat162_rn(0.f, 0.f); }
+  __device__ __forceinline__ static uint32_t bits(Max m) {     // of the fp32 magnitude; a NaN is above all numbers
+    const float2 f = __bfloat1622float2(m);
+    return max(__float_as_uint(f.x) & 0x7FFFFFFFu, __float_as_uint(f.y) & 0x7FFFFFFFu);
+  }
   uint4 v;
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldg(reinterpret_cast<const uint4*>(p)); }
   __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ uint32_t amax() const {   // bits of the largest magnitude, as fp32
-    const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
-    return max(m & 0xFFFF0000u, m << 16);
+  // the largest magnitude, two at a time; NaN if there is one
+  __device__ __forceinline__ static __nv_bfloat162 pair(uint32_t w) { return __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w)); }
+  __device__ __forceinline__ void amax(__nv_bfloat162& m) const {
+    m = __hmax2_nan(m, __hmax2_nan(__hmax2_nan(pair(v.x), pair(v.y)), __hmax2_nan(pair(v.z), pair(v.w))));
   }
   __device__ __forceinline__ void floats(float (&x)[8]) const {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -116,15 +142,23 @@ template <> struct Raw8<__nv_bfloat16> {
   }
 };
 template <> struct Raw8<float> {
+  using Max = float2;
+  __device__ __forceinline__ static Max none() { return make_float2(0.f, 0.f); }
+  __device__ __forceinline__ static uint32_t bits(Max m) { return m.y == 0.f ? __float_as_uint(m.x) : 0x7FC00000u; }
   uint4 a, b;
   __device__ __forceinline__ void load(const float* p) {
     a = __ldg(reinterpret_cast<const uint4*>(p));
     b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
   }
   __device__ __forceinline__ void zero() { a = b = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ uint32_t amax() const {
-    const uint32_t k = 0x7FFFFFFFu;
-    return max(max(max(a.x & k, a.y & k), max(a.z & k, a.w & k)), max(max(b.x & k, b.y & k), max(b.z & k, b.w & k)));
+  // .x: the largest magnitude; .y: 0, or NaN if there is a NaN or an infinity
+  __device__ __forceinline__ void amax(float2& m) const {
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      m.x = fmaxf(m.x, fabsf(__uint_as_float(w[i])));
+      m.y = fmaf(__uint_as_float(w[i]), 0.f, m.y);
+    }
   }
   __device__ __forceinline__ void floats(float (&x)[8]) const {
     const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
@@ -175,7 +209,7 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(AppendPara
   }
   const int sub = lane / LPR, col = (lane % LPR) * 8;
   Raw8<T> x[NI];
-  uint32_t amax = 0;
+  typename Raw8<T>::Max most = Raw8<T>::none();
   const float was = first > 0 ? *scale : 0.f;
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
@@ -184,8 +218,8 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(AppendPara
     else x[i].zero();
   }
 #pragma unroll
-  for (int i = 0; i < NI; ++i) amax = max(amax, x[i].amax());
-  amax = __reduce_max_sync(0xffffffffu, amax);
+  for (int i = 0; i < NI; ++i) x[i].amax(most);
+  const uint32_t amax = __reduce_max_sync(0xffffffffu, Raw8<T>::bits(most));
   const bool poisoned = amax >= 0x7F800000u || !(was < __uint_as_float(0x7F800000u));
   const float sc = poisoned ? __uint_as_float(0x7FC00000u) : fmaxf(was, scale_of<FMT>(amax));
   __syncwarp();                          // every lane has read the old scale
@@ -202,13 +236,25 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(AppendPara
       }
     }
   }
+  float worst = 0.f;
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const int slot = i * RPI + sub;
     if (slot >= first && slot < last) {
       float f[8];
       x[i].floats(f);
-      *reinterpret_cast<uint2*>(codes + slot * D + col) = empty ? make_uint2(0, 0) : encode8<FMT>(f, sc, inv);
+      *reinterpret_cast<uint2*>(codes + slot * D + col) = empty ? make_uint2(0, 0) : encode8<FMT>(f, sc, inv, worst);
+    }
+  }
+  if (FMT == SPINDLEKV_PAGED_INT8 && !empty && worst >= 0.5f * sc) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int slot = i * RPI + sub;
+      if (slot >= first && slot < last) {
+        float f[8];
+        x[i].floats(f);
+        *reinterpret_cast<uint2*>(codes + slot * D + col) = encode8_exactly(f, sc, inv);
+      }
     }
   }
 }

@@ -4,7 +4,7 @@
 // has an order -- who gets which page -- by prefix sums over the sequences and over page_ref, so that the outcome does not depend
 // on the order of atomics; reference counts change by atomic integer additions, whose order does not show.  The plan
 // (a list of page copies, new entries, a map) lies in the workspace, and a second kernel carries it out over the whole device: the
-// copies move 16 bytes per thread and step and are bound by memory.  The second kernel is launched with
+// copies move eight 16-byte pieces per lane at a time and are bound by memory.  The second kernel is launched with
 // programmatic stream serialization, so that its blocks are on the device already when the plan is done.
 #include <algorithm>
 
@@ -21,14 +21,14 @@ constexpr int kForkMaxSeqs = 1024;     // kForkCols entries of every sequence li
 struct PageCopy { int32_t src, dst, blocks; };
 
 struct PagesWs {             // the workspace's parts
-  int32_t* hdr;              // status block; word 8: number of copies, 9: go (0: the call failed)
+  int32_t* hdr;              // status block; word 8: number of copies, 9: go (0: the call failed), 10: live pages
   int32_t* old_len;          // [units]
   int32_t* fresh;            // [units] first page taken for a unit
   int32_t* children;         // [n_seqs]
   PageCopy* copies;          // [max(units, n_pages)]
-  int32_t* map;              // [n_pages]; also the list of pages taken
+  int32_t* map;              // [n_pages] new number of a page that moves; or the list of pages taken
 };
-constexpr int kHdrCopies = 8, kHdrGo = 9;
+constexpr int kHdrCopies = 8, kHdrGo = 9, kHdrPagesLive = 10;
 
 __device__ __forceinline__ void let_dependents_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_plan() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -58,26 +58,31 @@ size_t pages_workspace_bytes(const spindlekv_page_pool& p, const spindlekv_page_
 
 __device__ __forceinline__ int pages_of(int len, int ps) { return (int)(((long long)len + ps - 1) / ps); }
 
+// Which of the 32 pages from `first` on (a lane's own 32: first = base + 32 * lane) satisfy a test on their reference count: the warp
+// reads its 1024 counts in order, and the votes on 32 of them at a time are handed to the lane that they belong to.
+template <typename Test>
+__device__ __forceinline__ uint32_t vote_pages(const Pool& pool, int base, Test test) {
+  const int lane = threadIdx.x & 31;
+  uint32_t mine = 0;
+#pragma unroll 8
+  for (int j = 0; j < 32; ++j) {
+    const int at = base + 32 * j + lane;
+    const uint32_t votes = __ballot_sync(0xffffffffu, at < pool.n_pages && test(pool.ref[at]));
+    if (lane == j) mine = votes;
+  }
+  return mine;
+}
+
 // Lists the lowest `wanted` free pages, ascending, in taken[]; false (for every thread) when there are fewer.  One block.
 __device__ bool take_free(const Pool& pool, int wanted, int32_t* taken, int* warp_sums) {
   int have = 0;
-  for (int base = 0; base < pool.n_pages && have < wanted; base += 4 * kPlanThreads) {
-    const int at = base + 4 * (int)threadIdx.x;
-    bool f[4];
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[i] = at + i < pool.n_pages && pool.ref[at + i] == 0;
-      n += f[i];
-    }
+  for (int base = 0; base < pool.n_pages && have < wanted; base += 32 * kPlanThreads) {
+    const int first = base + 32 * (int)threadIdx.x;      // this thread's pages
+    uint32_t free = 0;
+    if (base + 1024 * ((int)threadIdx.x >> 5) < pool.n_pages) free = vote_pages(pool, base + 1024 * (threadIdx.x >> 5), [](int32_t r) { return r == 0; });
     int total;
-    int k = have + block_exclusive_scan(n, warp_sums, total);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (f[i]) {
-        if (k < wanted) taken[k] = at + i;
-        ++k;
-      }
+    int k = have + block_exclusive_scan(__popc(free), warp_sums, total);
+    for (; free && k < wanted; free &= free - 1) taken[k++] = first + __ffs(free) - 1;
     have += total;
   }
   __syncthreads();
@@ -207,37 +212,38 @@ __global__ void __launch_bounds__(kPlanThreads) resize_plan_kernel(ResizeParams 
 
 // ---- copies ----------------------------------------------------------------------------------------------------------
 
-// 16-byte pieces of the codes of a copy, then its scales.  The plan's copies read pages that stay (or that nobody writes) and write
-// pages that were free: no piece is read and written.
+// The copies, a warp at a time: all copied blocks of one (copy, head, K or V), which are contiguous, eight 16-byte pieces per lane in
+// flight; then their scales.  The plan's copies read pages that nobody writes and write pages that were free: no piece is both read
+// and written.
 template <int D>
 __device__ __forceinline__ void copy_pages(const Pool& pool, const PageCopy* list, int n, int part, int parts) {
   constexpr int kPiece = kPagedBlock * D / 16;        // 16-byte pieces of a block
-  constexpr int kUnroll = 4;
-  const int per = pool.per_page();
-  // one work item: all copied blocks of one (copy, head, K or V), which are contiguous
+  constexpr int kUnroll = 8;
+  constexpr int kWarps = kCopyThreads / 32;
+  const int per = pool.per_page(), lane = threadIdx.x & 31;
   const long long items = (long long)n * pool.heads * 2;
-  for (long long it = part; it < items; it += parts) {
-    const long long ch = it >> 1;
-    const PageCopy c = list[ch / pool.heads];
-    const int head = (int)(ch % pool.heads);
+  for (long long it = (long long)part * kWarps + (threadIdx.x >> 5); it < items; it += (long long)parts * kWarps) {
+    const unsigned ch = (unsigned)(it >> 1);            // at most 2^20 copies of 2^10 heads
+    const unsigned which = ch / (unsigned)pool.heads;
+    const PageCopy c = list[which];
+    const int head = (int)(ch - which * (unsigned)pool.heads);
     const bool v = (it & 1) != 0;
     const int64_t src = ((int64_t)c.src * pool.heads + head) * per, dst = ((int64_t)c.dst * pool.heads + head) * per;
-    const uint4* from = reinterpret_cast<const uint4*>((v ? pool.vc : pool.kc) + src * kPagedBlock * D);
-    uint4* to = reinterpret_cast<uint4*>((v ? pool.vc : pool.kc) + dst * kPagedBlock * D);
-    const int pieces = c.blocks * kPiece;
-    for (int i = threadIdx.x; i < pieces; i += kCopyThreads * kUnroll) {
+    const uint4* from = reinterpret_cast<const uint4*>((v ? pool.vc : pool.kc) + src * kPagedBlock * D) + lane;
+    uint4* to = reinterpret_cast<uint4*>((v ? pool.vc : pool.kc) + dst * kPagedBlock * D) + lane;
+    const float* scales = (v ? pool.vs : pool.ks) + src;
+    const float scale = lane < c.blocks ? scales[lane] : 0.f;
+    const int pieces = c.blocks * kPiece;               // a multiple of 32
+    for (int i = 0; i < pieces; i += 32 * kUnroll) {
       uint4 x[kUnroll];
 #pragma unroll
       for (int k = 0; k < kUnroll; ++k)
-        if (i + k * kCopyThreads < pieces) x[k] = __ldcs(from + i + k * kCopyThreads);
+        if (i + 32 * k < pieces) x[k] = __ldcs(from + i + 32 * k);
 #pragma unroll
       for (int k = 0; k < kUnroll; ++k)
-        if (i + k * kCopyThreads < pieces) __stcs(to + i + k * kCopyThreads, x[k]);
+        if (i + 32 * k < pieces) __stcs(to + i + 32 * k, x[k]);
     }
-    if (threadIdx.x < c.blocks) {
-      float* sc = v ? pool.vs : pool.ks;
-      sc[dst + threadIdx.x] = sc[src + threadIdx.x];
-    }
+    if (lane < c.blocks) (v ? pool.vs : pool.ks)[dst + lane] = scale;
   }
 }
 
@@ -359,37 +365,33 @@ struct CompactParams {
 __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CompactParams p) {
   let_dependents_start();
   __shared__ int warp_sums[33];
-  const int n = p.pool.n_pages, tid = threadIdx.x;
+  const int n = p.pool.n_pages, tid = threadIdx.x, group = 1024 * (tid >> 5);
+  const auto used = [](int32_t r) { return r > 0; };
+  // a thread's 32 pages of the first 32768 stay in a register; pools beyond that are read twice
+  uint32_t kept = 0;
   int mine = 0;
-  for (int i = tid; i < n; i += kPlanThreads) mine += p.pool.ref[i] > 0;
+  for (int base = 0; base < n; base += 32 * kPlanThreads) {
+    const uint32_t live = base + group < n ? vote_pages(p.pool, base + group, used) : 0;
+    if (base == 0) kept = live;
+    mine += __popc(live);
+  }
   int live;
   (void)block_exclusive_scan(mine, warp_sums, live);
   // the r-th free page below `live` takes the r-th live page at or above it: there are equally many
   int holes = 0, moves = 0;
-  for (int base = 0; base < n; base += 4 * kPlanThreads) {
-    const int at = base + 4 * tid;
-    int h = 0, m = 0;
-    bool used[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      used[i] = at + i < n && p.pool.ref[at + i] > 0;
-      h += at + i < live && !used[i];
-      m += at + i >= live && used[i];
-    }
+  for (int base = 0; base < n; base += 32 * kPlanThreads) {
+    const int first = base + 32 * tid;
+    const uint32_t mask = base == 0 ? kept : base + group < n ? vote_pages(p.pool, base + group, used) : 0;
+    const int below = min(max(live - first, 0), 32);          // of this thread's pages, those below `live`
+    const uint32_t low = below == 32 ? 0xFFFFFFFFu : (1u << below) - 1u;
+    uint32_t h = ~mask & low, m = mask & ~low;
     int total_h, total_m;
-    int kh = holes + block_exclusive_scan(h, warp_sums, total_h);
-    int km = moves + block_exclusive_scan(m, warp_sums, total_m);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (at + i >= n) continue;
-      if (at + i < live && !used[i]) p.ws.copies[kh++].dst = at + i;
-      if (at + i >= live && used[i]) {
-        p.ws.copies[km].src = at + i;
-        p.ws.copies[km].blocks = p.pool.per_page();
-        ++km;
-      } else {
-        p.ws.map[at + i] = at + i;
-      }
+    int kh = holes + block_exclusive_scan(__popc(h), warp_sums, total_h);
+    int km = moves + block_exclusive_scan(__popc(m), warp_sums, total_m);
+    for (; h; h &= h - 1) p.ws.copies[kh++].dst = first + __ffs(h) - 1;
+    for (; m; m &= m - 1) {
+      p.ws.copies[km].src = first + __ffs(m) - 1;
+      p.ws.copies[km++].blocks = p.pool.per_page();
     }
     holes += total_h;
     moves += total_m;
@@ -397,7 +399,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CompactParam
   __syncthreads();
   for (int i = tid; i < moves; i += kPlanThreads) {
     const PageCopy c = p.ws.copies[i];
-    p.ws.map[c.src] = c.dst;
+    p.ws.map[c.src] = c.dst;             // of a page below `live` the map says nothing: it stays
     p.pool.ref[c.dst] = p.pool.ref[c.src];
     p.pool.ref[c.src] = 0;
   }
@@ -405,6 +407,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CompactParam
     *p.n_live = live;
     p.ws.hdr[kHdrStatus] = SPINDLEKV_OK;
     p.ws.hdr[kHdrCopies] = moves;
+    p.ws.hdr[kHdrPagesLive] = live;
   }
 }
 
@@ -412,12 +415,14 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CompactParam
 template <int D>
 __global__ void __launch_bounds__(kCopyThreads) compact_kernel(CompactParams p) {
   wait_for_plan();
-  const int units = p.table.n_layers * p.table.n_seqs;
+  const int units = p.table.n_layers * p.table.n_seqs, live = p.ws.hdr[kHdrPagesLive];
   for (int u = blockIdx.x; u < units; u += gridDim.x) {
     const int used = pages_of(unit_len(p.table, p.pool, u), p.pool.ps);
     int32_t* row = p.table.pages + (int64_t)u * p.table.max_pages;
-    for (int i = threadIdx.x; i < used; i += kCopyThreads)
-      if (page_ok(p.pool, row[i])) row[i] = p.ws.map[row[i]];
+    for (int i = threadIdx.x; i < used; i += kCopyThreads) {
+      const int page = row[i];
+      if (page >= live && page < p.pool.n_pages && p.ws.hdr[kHdrCopies]) row[i] = p.ws.map[page];
+    }
   }
   copy_pages<D>(p.pool, p.ws.copies, p.ws.hdr[kHdrCopies], blockIdx.x, gridDim.x);
 }
@@ -468,7 +473,7 @@ spindlekv_status pages_resize_impl(const spindlekv_page_pool& pool, const spindl
   }
   if (cudaGetLastError() != cudaSuccess) return SPINDLEKV_CUDA;
   const int units = table.n_layers * table.n_seqs;
-  const unsigned grid = (unsigned)std::min<int64_t>((int64_t)units * pool.n_kv_heads * 2, 4 * sms);
+  const unsigned grid = (unsigned)std::min<int64_t>(((int64_t)units * pool.n_kv_heads * 2 + kCopyThreads / 32 - 1) / (kCopyThreads / 32), 4 * sms);
   return pool.head_dim == 64 ? launch_behind(copy_kernel<64>, grid, 0, st, p.pool, p.ws) : launch_behind(copy_kernel<128>, grid, 0, st, p.pool, p.ws);
 }
 
@@ -496,7 +501,7 @@ spindlekv_status pages_fork_impl(const spindlekv_page_pool& pool, const spindlek
   }
   if (cudaGetLastError() != cudaSuccess) return SPINDLEKV_CUDA;
   const int64_t units = (int64_t)table.n_layers * table.n_seqs;
-  const unsigned grid = (unsigned)(p.tiles * table.n_layers + std::min<int64_t>(units * pool.n_kv_heads * 2, 4 * sms));
+  const unsigned grid = (unsigned)(p.tiles * table.n_layers + std::min<int64_t>((units * pool.n_kv_heads * 2 + kCopyThreads / 32 - 1) / (kCopyThreads / 32), 4 * sms));
   const size_t smem = (size_t)table.n_seqs * kForkCols * 4;
   return pool.head_dim == 64 ? launch_behind(fork_kernel<64>, grid, smem, st, p) : launch_behind(fork_kernel<128>, grid, smem, st, p);
 }
