@@ -1,12 +1,14 @@
 // Beam search's selection: the n_out best of n_beams x vocab continuations of every sequence.
 //
-// Bound by reading the logits once.  First kernel, one block per slice of a row: the slice is in registers after one pass of wide
-// loads; its maximum and exp-sum go to the workspace, and so do its n_out largest logits.  Those are found without sorting: the
-// block's threads form 64 groups of four, and the n_out-th largest of the groups' maxima is a bound that only n_out groups reach, so at
-// most n_out times a group's elements remain (a dozen or two, mostly), whatever the values are; they are ranked by counting.  Keys are
-// (value, index) with the lower index above, so no two are equal and ties need no care.  Within a row the order of logits is the order of totals.
-// Second kernel, one block per sequence: log-sum-exp of the beams from the slices' pieces (added in double), totals in double, and the
-// same selection over the slices' lists, 2048 entries at a time beside the best so far.
+// Bound by reading the logits once.  One block per slice of a row: the slice is in registers after one pass of wide loads; its maximum
+// and exp-sum go to the workspace, and so do its n_out largest logits.  Those are found without sorting: the block's threads form 64
+// groups of four, and the n_out-th largest of the groups' maxima is a bound that n_out logits reach and, mostly, a dozen or two in all;
+// these are ranked by counting.  Where many logits equal the bound (rows that are masked for the most part) there are more of them than
+// fit, and the same is done once more on keys (value, index) with the lower index above, of which no two are equal: then only n_out groups
+// reach the bound.  Within a row the order of logits is the order of totals.
+// The last block of a sequence to arrive joins its slices: log-sum-exp of the beams from the slices' pieces (added in double), totals in
+// double, and the same selection over the slices' lists, 2048 entries at a time beside the best so far.  (A second kernel for that cost
+// 2 us more, and 3 us on the host.)
 #include <algorithm>
 
 #include <math_constants.h>
@@ -17,10 +19,10 @@ namespace skv {
 
 constexpr int kBeamThreads = 256;
 constexpr int kBeamMaxOut = 32;
-constexpr int kBeamPer = 8;            // entries per thread and step of the second kernel
+constexpr int kBeamPer = 8;            // entries per thread and step of the join
 constexpr int kBeamGroups = 64;        // groups of threads whose maxima give the bound; at least kBeamMaxOut
 constexpr int kBeamGroup = kBeamThreads / kBeamGroups;
-static_assert(kBeamGroups >= kBeamMaxOut && kBeamGroup == 4, "the bound is the n_out-th of the groups' maxima; a group is a quad of lanes");
+static_assert(kBeamGroups >= kBeamMaxOut && kBeamGroup == 4, "the bound is the n_out-th of the groups' maxima; a group is a quad of lanes, and four threads rank one");
 
 struct BeamParams {
   int n_seqs, n_beams, vocab, k, slices;
@@ -33,7 +35,12 @@ struct BeamParams {
   int32_t *out_parent, *out_token;
   float2* stat;        // [rows][slices] maximum and exp-sum
   int2* cand;          // [rows][slices][k] (logit bits, token), best first; token -1: none
+  unsigned long long* arrived;   // [n_seqs]
 };
+constexpr int kBeamFound = 512;        // candidates of a slice that are held without keys
+constexpr float kLog2e = 1.44269504f;
+
+
 
 // 2^x, to two units in the last place of fp32; results below the smallest normal number are 0
 __device__ __forceinline__ float pow2(float x) {
@@ -60,17 +67,59 @@ __device__ __forceinline__ bool row_runs(const BeamParams& p, int row) {
   return fabsf(p.score[row]) < CUDART_INF_F;
 }
 
+struct Entry {                 // larger: the better one
+  unsigned long long value;    // ordered bits of the total
+  uint32_t index;              // ~(beam * vocab + token); 0 with value 0: none
+};
+__device__ __forceinline__ bool better(const Entry& a, const Entry& b) {   // without branches: the loops over it are unrolled
+  return (a.value > b.value) | ((a.value == b.value) & (a.index > b.index));
+}
+__device__ __forceinline__ Entry make_entry(double total, int flat) {
+  const unsigned long long b = (unsigned long long)__double_as_longlong(total + 0.0);
+  return Entry{(b >> 63) ? ~b : b | 0x8000000000000000ull, (uint32_t)~flat};
+}
+
+struct JoinScratch {           // shared memory of the join, where the slice's candidates were
+  Entry tops[kBeamGroups];
+  Entry found[kBeamMaxOut * kBeamGroup * (kBeamPer + 1)];
+  Entry best[kBeamMaxOut];
+  Entry bound;
+  double base[64];
+  int kind[64];                // 0: takes part, 1: finished, 2: offers its tokens at -infinity
+  int n_found;
+};
+__device__ __noinline__ void beam_join(const BeamParams& p, int seq, JoinScratch& sm);
+
 template <typename T, int EPT, bool VEC>
-__global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(BeamParams p) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  __shared__ __align__(16) unsigned long long tops[kBeamGroups];
-  __shared__ unsigned long long found[kBeamMaxOut * kBeamGroup * EPT];
-  __shared__ unsigned long long bound;
+__global__ void __launch_bounds__(kBeamThreads, 4) beam_kernel(const __grid_constant__ BeamParams p) {
+  __shared__ __align__(16) float tops[kBeamGroups];
+  __shared__ unsigned long long keys[kBeamGroups];
+  constexpr int kFound = kBeamMaxOut * kBeamGroup * EPT;
+  static_assert(kFound >= kBeamFound, "room for either kind of candidates");
+  __shared__ __align__(16) unsigned char scratch[kFound * 8 > sizeof(JoinScratch) ? kFound * 8 : sizeof(JoinScratch)];
+  unsigned long long* found = reinterpret_cast<unsigned long long*>(scratch);
+  __shared__ unsigned long long key_bound;
+  __shared__ float bound;
   __shared__ float red[2 * (kBeamThreads / 32)];
-  __shared__ int n_found;
+  __shared__ int n_found, last;
   const int row = blockIdx.y, slice = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (!row_runs(p, row)) return;
-  if (tid == 0) { n_found = 0; bound = 1; }
+  // the block's results are written: the last block of the sequence joins them
+  auto arrive = [&]() {
+    __threadfence();
+    __syncthreads();
+    const int seq = row / p.n_beams;
+    if (tid == 0) last = last_to_arrive(p.arrived + seq, p.n_beams * p.slices);
+    __syncthreads();
+    if (last) {
+      __threadfence();
+      beam_join(p, seq, *reinterpret_cast<JoinScratch*>(scratch));
+    }
+  };
+  if (!row_runs(p, row)) {
+    arrive();
+    return;
+  }
+  if (tid == 0) n_found = 0;
   constexpr int W = VEC ? 16 / (int)sizeof(T) : 1;          // elements per load
   const T* x = reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.row_stride;
   const int s0 = slice * (kBeamThreads * EPT);
@@ -102,51 +151,45 @@ __global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(BeamParams p) 
       v[j] = at < p.vocab ? to_f32(x[at]) : -CUDART_INF_F;
     }
   }
-  // ---- maximum and its lowest place (a thread's indices rise with i) ----
+  // ---- maxima ----
   float mx = -CUDART_INF_F;
 #pragma unroll
   for (int i = 0; i < EPT; ++i) mx = fmaxf(mx, v[i]);
-  unsigned long long top = 0;
-  if (mx > -CUDART_INF_F) {
-    int first = 0;
+  float quad = mx;
 #pragma unroll
-    for (int i = EPT - 1; i >= 0; --i) first = v[i] == mx ? i : first;
-    top = key_of(mx, s0 + ((first / W) * kBeamThreads + tid) * W + first % W);
-  } else {          // nothing but -infinity (or NaN), some of it perhaps behind the row's end
-#pragma unroll
-    for (int i = EPT - 1; i >= 0; --i)
-      if (v[i] == mx && index(i) < p.vocab) top = key_of(mx, index(i));
-  }
-  float all = mx;
-#pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
-  unsigned long long quad = top;
-#pragma unroll
-  for (int o = 1; o < kBeamGroup; o <<= 1) quad = max(quad, __shfl_xor_sync(0xffffffffu, quad, o));
+  for (int o = 1; o < kBeamGroup; o <<= 1) quad = fmaxf(quad, __shfl_xor_sync(0xffffffffu, quad, o));
   if (tid % kBeamGroup == 0) tops[tid / kBeamGroup] = quad;
-  if (lane == 0) red[warp] = all;
+#pragma unroll
+  for (int o = kBeamGroup; o < 32; o <<= 1) quad = fmaxf(quad, __shfl_xor_sync(0xffffffffu, quad, o));
+  if (lane == 0) red[warp] = quad;
   __syncthreads();
-  // ---- exp-sum (a NaN anywhere must show in it); beside it the n_out-th largest of the groups' maxima ----
-  all = red[0];
+  float all = red[0];
 #pragma unroll
   for (int w = 1; w < kBeamThreads / 32; ++w) all = fmaxf(all, red[w]);
-  float sum = 0.f;
-  const float ref = all == -CUDART_INF_F ? 0.f : all;
+  // ---- the n_out-th largest of the groups' maxima (equal ones by their number) ----
+  {   // four threads to a group, each against a quarter of the groups
+    const int mine = tid / 4, from = tid % 4 * (kBeamGroups / 4);
+    const float own = tops[mine];
+    int rank = 0;
 #pragma unroll
-  for (int i = 0; i < EPT; ++i) sum += pow2((v[i] - ref) * 1.44269504f);
+    for (int i = from; i < from + kBeamGroups / 4; i += 4) {
+      const float4 q = *reinterpret_cast<const float4*>(tops + i);
+      rank += ((q.x > own) | ((q.x == own) & (i < mine))) + ((q.y > own) | ((q.y == own) & (i + 1 < mine))) +
+              ((q.z > own) | ((q.z == own) & (i + 2 < mine))) + ((q.w > own) | ((q.w == own) & (i + 3 < mine)));
+    }
+    rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+    rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+    if (rank == p.k - 1) bound = own;
+  }
+  // ---- exp-sum relative to the maximum (a NaN anywhere must show in it).  The difference first: a product of the type's lowest value
+  // overflows, and a row of nothing else is a uniform one ----
+  const float ref = all == -CUDART_INF_F ? 0.f : all;
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < EPT; ++i) sum += pow2((v[i] - ref) * kLog2e);
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) red[kBeamThreads / 32 + warp] = sum;
-  if (tid < kBeamGroups) {
-    const unsigned long long own = tops[tid];
-    int rank = 0;
-#pragma unroll 8
-    for (int i = 0; i < kBeamGroups; i += 2) {
-      const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(tops + i);
-      rank += (q.x > own) + (q.y > own);
-    }
-    if (rank == p.k - 1 && own) bound = own;
-  }
   __syncthreads();
   if (tid == 0) {
     float s = 0.f;
@@ -154,89 +197,111 @@ __global__ void __launch_bounds__(kBeamThreads) beam_slice_kernel(BeamParams p) 
     for (int w = 0; w < kBeamThreads / 32; ++w) s += red[kBeamThreads / 32 + w];
     p.stat[(int64_t)row * p.slices + slice] = make_float2(all, s);
   }
-  const unsigned long long least = bound;
-  if (top >= least) {
+  // ---- what reaches the bound; then the places of a thread's hits are read once more ----
+  const float least_value = bound;
+  if (mx >= least_value) {
+    uint32_t hits = 0;
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) {
-      const int at = index(i);
-      const unsigned long long q = key_of(v[i], at);
-      if (at < p.vocab && q >= least) found[atomicAdd(&n_found, 1)] = q;
+    for (int i = 0; i < EPT; ++i) hits |= v[i] >= least_value ? 1u << i : 0u;
+    for (; hits; hits &= hits - 1) {
+      const int at = index(__ffs(hits) - 1);
+      if (at >= p.vocab) continue;
+      const int slot = atomicAdd(&n_found, 1);
+      if (slot < kBeamFound) found[slot] = key_of(to_f32(x[at]), at);
     }
   }
   __syncthreads();
+  if (n_found > kBeamFound) {      // the same on keys
+    __syncthreads();
+    unsigned long long top = 0;
+#pragma unroll
+    for (int i = EPT - 1; i >= 0; --i) {
+      const int at = index(i);
+      if (v[i] == mx && at < p.vocab) top = key_of(mx, at);
+    }
+    unsigned long long best = top;
+#pragma unroll
+    for (int o = 1; o < kBeamGroup; o <<= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+    if (tid % kBeamGroup == 0) keys[tid / kBeamGroup] = best;
+    if (tid == 0) { n_found = 0; key_bound = 1; }
+    __syncthreads();
+    if (tid < kBeamGroups) {
+      const unsigned long long own = keys[tid];
+      int rank = 0;
+      for (int i = 0; i < kBeamGroups; ++i) rank += keys[i] > own;
+      if (rank == p.k - 1 && own) key_bound = own;
+    }
+    __syncthreads();
+    const unsigned long long least = key_bound;
+    if (top >= least) {
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) {
+        const int at = index(i);
+        const unsigned long long q = key_of(v[i], at);
+        if (at < p.vocab && q >= least) found[atomicAdd(&n_found, 1)] = q;
+      }
+    }
+    __syncthreads();
+  }
   const int n = n_found;
   int2* out = p.cand + ((int64_t)row * p.slices + slice) * p.k;
   for (int i = tid; i < n; i += kBeamThreads) {
     const unsigned long long q = found[i];
     int r = 0;
+#pragma unroll 4
     for (int j = 0; j < n; ++j) r += found[j] > q;
     if (r < p.k) out[r] = make_int2((int)key_value_bits(q), key_index(q));
   }
   for (int i = n + tid; i < p.k; i += kBeamThreads) out[i] = make_int2(0, -1);
+  arrive();
 }
 
-struct Entry {                 // larger: the better one
-  unsigned long long value;    // ordered bits of the total
-  uint32_t index;              // ~(beam * vocab + token); 0 with value 0: none
-};
-__device__ __forceinline__ bool better(const Entry& a, const Entry& b) { return a.value > b.value || (a.value == b.value && a.index > b.index); }
-__device__ __forceinline__ Entry make_entry(double total, int flat) {
-  const unsigned long long b = (unsigned long long)__double_as_longlong(total + 0.0);
-  return Entry{(b >> 63) ? ~b : b | 0x8000000000000000ull, (uint32_t)~flat};
-}
-
-__global__ void __launch_bounds__(kBeamThreads) beam_join_kernel(BeamParams p) {
-  __shared__ Entry tops[kBeamGroups];
-  __shared__ Entry found[kBeamMaxOut * kBeamGroup * (kBeamPer + 1)];
-  __shared__ Entry best[kBeamMaxOut];
-  __shared__ Entry bound;
-  __shared__ double base[64];
-  __shared__ int kind[64];       // 0: takes part, 1: finished, 2: offers its tokens at -infinity
-  __shared__ int n_found;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int seq = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+// All threads of the block.  (A function of its own, so that its registers do not count against the slices' loop.)
+__device__ __noinline__ void beam_join(const BeamParams& p, int seq, JoinScratch& sm) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per_beam = p.slices * p.k, entries = p.n_beams * per_beam;
   const int2* cand = p.cand + (int64_t)seq * entries;
   int2 raw[kBeamPer];            // the first step's entries are on their way while the log-sum-exps are formed
 #pragma unroll
   for (int i = 0; i < kBeamPer; ++i) {
     const int e = i * kBeamThreads + tid;
-    raw[i] = e < entries ? cand[e] : make_int2(0, -1);
+    raw[i] = e < entries ? __ldcg(cand + e) : make_int2(0, -1);
   }
   for (int w = warp; w < p.n_beams; w += kBeamThreads / 32) {
     const int row = seq * p.n_beams + w;
     const float sc = p.score[row];
     const bool done = p.finished && p.finished[row];
+    const float2* st = p.stat + (int64_t)row * p.slices;
+    const float2 mine = lane < p.slices ? __ldcg(st + lane) : make_float2(-CUDART_INF_F, 0.f);   // (of a row that runs)
     if (!(fabsf(sc) < CUDART_INF_F)) {
-      if (lane == 0) kind[w] = 2;
+      if (lane == 0) sm.kind[w] = 2;
     } else if (done) {
-      if (lane == 0) { kind[w] = 1; base[w] = sc; }
+      if (lane == 0) { sm.kind[w] = 1; sm.base[w] = sc; }
     } else {
-      const float2* st = p.stat + (int64_t)row * p.slices;
-      float mx = -CUDART_INF_F;
-      for (int i = lane; i < p.slices; i += 32) mx = fmaxf(mx, st[i].x);
+      float mx = mine.x;
+      for (int i = lane + 32; i < p.slices; i += 32) mx = fmaxf(mx, __ldcg(st + i).x);
 #pragma unroll
       for (int o = 16; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-      double sum = 0.0;
-      for (int i = lane; i < p.slices; i += 32) {
-        const float2 s = st[i];   // a slice of -infinity alone has the sum 0, or NaN
-        sum += s.x == -CUDART_INF_F ? s.y : s.y * expf(s.x - mx);
-      }
+      // a slice of -infinity alone has the sum 0, or NaN
+      auto part = [&](float2 s) { return (double)(s.x == -CUDART_INF_F ? s.y : s.y * expf(s.x - mx)); };
+      double sum = part(mine);
+      for (int i = lane + 32; i < p.slices; i += 32) sum += part(__ldcg(st + i));
 #pragma unroll
       for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
       if (lane == 0) {
         const double lse = (double)mx + log(sum);
         const bool fine = lse > -CUDART_INF && lse < CUDART_INF;
-        kind[w] = fine ? 0 : 2;
-        base[w] = (double)sc - lse;
+        sm.kind[w] = fine ? 0 : 2;
+        sm.base[w] = (double)sc - lse;
       }
     }
   }
-  for (int i = tid; i < p.k; i += kBeamThreads) best[i] = Entry{0, 0};
+  for (int i = tid; i < p.k; i += kBeamThreads) sm.best[i] = Entry{0, 0};
   __syncthreads();
   const int offered = min(p.k, p.vocab);      // entries of a beam that does not take part
+  const float per_entry = 1.f / (float)per_beam;
   for (int e0 = 0; e0 < entries; e0 += kBeamThreads * kBeamPer) {
-    if (tid == 0) { n_found = 0; bound = Entry{0, 1}; }
+    if (tid == 0) { sm.n_found = 0; sm.bound = Entry{0, 1}; }
     Entry mine[kBeamPer + 1];
     Entry top{0, 0};
 #pragma unroll
@@ -244,23 +309,25 @@ __global__ void __launch_bounds__(kBeamThreads) beam_join_kernel(BeamParams p) {
       mine[i] = Entry{0, 0};
       const int e = e0 + i * kBeamThreads + tid;
       if (e < entries) {
-        const int w = e / per_beam, at = e - w * per_beam;
-        if (kind[w] == 0) {
-          const int2 c = e0 ? cand[e] : raw[i];
-          if (c.y >= 0) mine[i] = make_entry(base[w] + (double)__int_as_float(c.x), w * p.vocab + c.y);
+        int w = (int)((float)e * per_entry), at = e - w * per_beam;   // a quotient that may be one off
+        if (at < 0) { --w; at += per_beam; }
+        if (at >= per_beam) { ++w; at -= per_beam; }
+        if (sm.kind[w] == 0) {
+          const int2 c = e0 ? __ldcg(cand + e) : raw[i];
+          if (c.y >= 0) mine[i] = make_entry(sm.base[w] + (double)__int_as_float(c.x), w * p.vocab + c.y);
         } else if (at < offered) {
           int token = at;
           double total = -CUDART_INF;
-          if (kind[w] == 1) {                 // the end token first, then the others in order
+          if (sm.kind[w] == 1) {                 // the end token first, then the others in order
             token = at == 0 ? p.eos : at <= p.eos ? at - 1 : at;
-            if (at == 0) total = base[w];
+            if (at == 0) total = sm.base[w];
           }
           mine[i] = make_entry(total, w * p.vocab + token);
         }
       }
       if (better(mine[i], top)) top = mine[i];
     }
-    mine[kBeamPer] = tid < p.k ? best[tid] : Entry{0, 0};
+    mine[kBeamPer] = tid < p.k ? sm.best[tid] : Entry{0, 0};
     if (better(mine[kBeamPer], top)) top = mine[kBeamPer];
     Entry quad = top;
 #pragma unroll
@@ -268,32 +335,35 @@ __global__ void __launch_bounds__(kBeamThreads) beam_join_kernel(BeamParams p) {
       const Entry other{__shfl_xor_sync(0xffffffffu, quad.value, o), __shfl_xor_sync(0xffffffffu, quad.index, o)};
       if (better(other, quad)) quad = other;
     }
-    if (tid % kBeamGroup == 0) tops[tid / kBeamGroup] = quad;
+    if (tid % kBeamGroup == 0) sm.tops[tid / kBeamGroup] = quad;
     __syncthreads();
-    if (tid < kBeamGroups) {
-      const Entry own = tops[tid];
+    {   // four threads to a group, each against a quarter of the groups
+      const Entry own = sm.tops[tid / 4];
       int rank = 0;
-#pragma unroll 8
-      for (int i = 0; i < kBeamGroups; ++i) rank += better(tops[i], own);
-      if (rank == p.k - 1 && own.value) bound = own;
+#pragma unroll
+      for (int i = 0; i < kBeamGroups / 4; ++i) rank += better(sm.tops[i * 4 + tid % 4], own);
+      rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+      rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+      if (rank == p.k - 1 && own.value) sm.bound = own;
     }
     __syncthreads();
-    const Entry least = bound;
+    const Entry least = sm.bound;
 #pragma unroll
     for (int i = 0; i <= kBeamPer; ++i)
-      if (mine[i].value && !better(least, mine[i])) found[atomicAdd(&n_found, 1)] = mine[i];
+      if (mine[i].value && !better(least, mine[i])) sm.found[atomicAdd(&sm.n_found, 1)] = mine[i];
     __syncthreads();
-    const int n = n_found;
+    const int n = sm.n_found;
     for (int i = tid; i < n; i += kBeamThreads) {
-      const Entry q = found[i];
+      const Entry q = sm.found[i];
       int r = 0;
-      for (int j = 0; j < n; ++j) r += better(found[j], q);
-      if (r < p.k) best[r] = q;
+#pragma unroll 4
+      for (int j = 0; j < n; ++j) r += better(sm.found[j], q);
+      if (r < p.k) sm.best[r] = q;
     }
     __syncthreads();
   }
   for (int i = tid; i < p.k; i += kBeamThreads) {
-    const Entry q = best[i];
+    const Entry q = sm.best[i];
     const int flat = (int)~q.index, w = flat / p.vocab;
     const unsigned long long b = (q.value >> 63) ? q.value & 0x7FFFFFFFFFFFFFFFull : ~q.value;
     const int64_t at = (int64_t)seq * p.k + i;
@@ -303,21 +373,21 @@ __global__ void __launch_bounds__(kBeamThreads) beam_join_kernel(BeamParams p) {
   }
 }
 
-// Elements per thread of a slice: 32 keep the lists that the second kernel reads short; 8 give a call of few rows four times the
+// Elements per thread of a slice: 32 keep the lists that the joining block reads short; 8 give a call of few rows four times the
 // blocks.  The border is one block per SM.
 static int beam_per_thread(int64_t rows, int vocab) { return rows * ceil_div(vocab, kBeamThreads * 32) >= 148 ? 32 : 8; }
 
 size_t beam_workspace_bytes(int n_seqs, int n_beams, int vocab, int k) {
   const size_t rows = (size_t)n_seqs * n_beams, slices = (size_t)ceil_div(vocab, kBeamThreads * beam_per_thread((int64_t)rows, vocab));
-  return kHeaderBytes + align_up(rows * slices * sizeof(float2), 256) + align_up(rows * slices * k * sizeof(int2), 256);
+  return kHeaderBytes + align_up(rows * slices * sizeof(float2), 256) + align_up(rows * slices * k * sizeof(int2), 256) + align_up((size_t)n_seqs * 8, 256);
 }
 
 template <typename T, int EPT>
 static void launch_slices(const BeamParams& p, bool vec, cudaStream_t st) {
   const dim3 grid(p.slices, p.n_seqs * p.n_beams);
   LaunchScope ls(KC_BEAM, st);
-  if (vec) beam_slice_kernel<T, EPT, true><<<grid, kBeamThreads, 0, st>>>(p);
-  else beam_slice_kernel<T, EPT, false><<<grid, kBeamThreads, 0, st>>>(p);
+  if (vec) beam_kernel<T, EPT, true><<<grid, kBeamThreads, 0, st>>>(p);
+  else beam_kernel<T, EPT, false><<<grid, kBeamThreads, 0, st>>>(p);
 }
 
 spindlekv_status beam_select_impl(int n_seqs, int n_beams, int vocab, int k, const void* logits, int dtype, int64_t row_stride,
@@ -328,10 +398,13 @@ spindlekv_status beam_select_impl(int n_seqs, int n_beams, int vocab, int k, con
   if (rows > 65535) return SPINDLEKV_UNSUPPORTED;
   const int per = beam_per_thread(rows, vocab);
   BeamParams p{n_seqs, n_beams, vocab, k, ceil_div(vocab, kBeamThreads * per), logits, row_stride, score, finished, eos,
-               out_score, out_parent, out_token, nullptr, nullptr};
+               out_score, out_parent, out_token, nullptr, nullptr, nullptr};
   uint8_t* at = static_cast<uint8_t*>(ws) + kHeaderBytes;
   p.stat = reinterpret_cast<float2*>(at);
   p.cand = reinterpret_cast<int2*>(at + align_up((size_t)rows * p.slices * sizeof(float2), 256));
+  p.arrived = reinterpret_cast<unsigned long long*>(at + align_up((size_t)rows * p.slices * sizeof(float2), 256) +
+                                                    align_up((size_t)rows * p.slices * k * sizeof(int2), 256));
+  if ((int64_t)n_beams * p.slices > 0xFFFF) return SPINDLEKV_UNSUPPORTED;   // the count has 16 bits
   const int size = dtype == SPINDLEKV_BF16 ? 2 : 4;
   const bool vec = reinterpret_cast<uintptr_t>(logits) % 16 == 0 && row_stride * size % 16 == 0;
   if (dtype == SPINDLEKV_BF16) {
@@ -341,18 +414,7 @@ spindlekv_status beam_select_impl(int n_seqs, int n_beams, int vocab, int k, con
     if (per == 32) launch_slices<float, 32>(p, vec, st);
     else launch_slices<float, 8>(p, vec, st);
   }
-  if (cudaGetLastError() != cudaSuccess) return SPINDLEKV_CUDA;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n_seqs);
-  cfg.blockDim = dim3(kBeamThreads);
-  cfg.stream = st;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  LaunchScope ls(KC_BEAM, st);
-  return cudaLaunchKernelEx(&cfg, beam_join_kernel, p) == cudaSuccess ? SPINDLEKV_OK : SPINDLEKV_CUDA;
+  return cudaGetLastError() == cudaSuccess ? SPINDLEKV_OK : SPINDLEKV_CUDA;
 }
 
 }  // namespace skv

@@ -163,6 +163,23 @@ __device__ __forceinline__ int block_exclusive_scan(int v, int* warp_sums, int& 
   return res;
 }
 
+// ---- counting blocks that bring something to a common end -----------------------------------------------
+// A word in the workspace counts arrivals.  A call finds it at zero, because the last arrival of the call before put it back, or finds
+// something that is no count (upper 48 bits) and makes it one: the workspace needs no preparation.  The arriving thread calls this
+// after its block's writes and a __threadfence(); the last one gets true.
+constexpr unsigned long long kCountTag = 0x51BDC0F7A93Eull;
+__device__ __forceinline__ bool last_to_arrive(unsigned long long* word, int n) {
+  unsigned long long old = atomicAdd(word, 1ull);
+  while (old >> 16 != kCountTag) {
+    const unsigned long long now = *reinterpret_cast<volatile unsigned long long*>(word);
+    if (now >> 16 == kCountTag) old = atomicAdd(word, 1ull);
+    else if (atomicCAS(word, now, kCountTag << 16 | 1ull) == now) old = kCountTag << 16;
+  }
+  const bool last = (int)(old & 0xFFFFu) + 1 == n;
+  if (last) atomicExch(word, kCountTag << 16);
+  return last;
+}
+
 // Per-device "done once" flags for host-side set-up (function attributes, occupancy queries): the
 // library may be used from several devices of one process.
 constexpr int kMaxDevices = 64;

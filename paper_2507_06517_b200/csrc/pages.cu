@@ -4,7 +4,7 @@
 // has an order -- who gets which page -- by prefix sums over the sequences and over page_ref, so that the outcome does not depend
 // on the order of atomics; reference counts change by atomic integer additions, whose order does not show.  The plan
 // (a list of page copies, new entries, a map) lies in the workspace, and a second kernel carries it out over the whole device: the
-// copies move eight 16-byte pieces per lane at a time and are bound by memory.  The second kernel is launched with
+// copies move four 16-byte pieces per lane at a time and are bound by memory.  The second kernel is launched with
 // programmatic stream serialization, so that its blocks are on the device already when the plan is done.
 #include <algorithm>
 
@@ -58,15 +58,19 @@ size_t pages_workspace_bytes(const spindlekv_page_pool& p, const spindlekv_page_
 
 __device__ __forceinline__ int pages_of(int len, int ps) { return (int)(((long long)len + ps - 1) / ps); }
 
-// Which of the 32 pages from `first` on (a lane's own 32: first = base + 32 * lane) satisfy a test on their reference count: the warp
-// reads its 1024 counts in order, and the votes on 32 of them at a time are handed to the lane that they belong to.
+// The planning block looks at 32 * per * 32 pages at a time: every warp at 32 * per in order, every lane of it keeps the votes on 32 of
+// them, lanes from `per` on none.  `per` is what the pool needs, at most 32.
+__device__ __forceinline__ int votes_per_lane(const Pool& pool) { return min((pool.n_pages + kPlanThreads - 1) / kPlanThreads, 32); }
+// first page of this thread's 32
+__device__ __forceinline__ int first_voted(int base, int per) { return base + ((int)(threadIdx.x >> 5) * per + (int)(threadIdx.x & 31)) * 32; }
+// which of them satisfy a test on their reference count (0 in lanes without pages)
 template <typename Test>
-__device__ __forceinline__ uint32_t vote_pages(const Pool& pool, int base, Test test) {
-  const int lane = threadIdx.x & 31;
+__device__ __forceinline__ uint32_t vote_pages(const Pool& pool, int base, int per, Test test) {
+  const int lane = threadIdx.x & 31, from = base + (int)(threadIdx.x >> 5) * per * 32 + lane;
   uint32_t mine = 0;
 #pragma unroll 8
-  for (int j = 0; j < 32; ++j) {
-    const int at = base + 32 * j + lane;
+  for (int j = 0; j < per; ++j) {
+    const int at = from + 32 * j;
     const uint32_t votes = __ballot_sync(0xffffffffu, at < pool.n_pages && test(pool.ref[at]));
     if (lane == j) mine = votes;
   }
@@ -76,10 +80,10 @@ __device__ __forceinline__ uint32_t vote_pages(const Pool& pool, int base, Test 
 // Lists the lowest `wanted` free pages, ascending, in taken[]; false (for every thread) when there are fewer.  One block.
 __device__ bool take_free(const Pool& pool, int wanted, int32_t* taken, int* warp_sums) {
   int have = 0;
-  for (int base = 0; base < pool.n_pages && have < wanted; base += 32 * kPlanThreads) {
-    const int first = base + 32 * (int)threadIdx.x;      // this thread's pages
-    uint32_t free = 0;
-    if (base + 1024 * ((int)threadIdx.x >> 5) < pool.n_pages) free = vote_pages(pool, base + 1024 * (threadIdx.x >> 5), [](int32_t r) { return r == 0; });
+  const int per = votes_per_lane(pool);
+  for (int base = 0; base < pool.n_pages && have < wanted; base += per * kPlanThreads) {
+    const int first = first_voted(base, per);
+    uint32_t free = vote_pages(pool, base, per, [](int32_t r) { return r == 0; });
     int total;
     int k = have + block_exclusive_scan(__popc(free), warp_sums, total);
     for (; free && k < wanted; free &= free - 1) taken[k++] = first + __ffs(free) - 1;
@@ -212,13 +216,13 @@ __global__ void __launch_bounds__(kPlanThreads) resize_plan_kernel(ResizeParams 
 
 // ---- copies ----------------------------------------------------------------------------------------------------------
 
-// The copies, a warp at a time: all copied blocks of one (copy, head, K or V), which are contiguous, eight 16-byte pieces per lane in
+// The copies, a warp at a time: all copied blocks of one (copy, head, K or V), which are contiguous, four 16-byte pieces per lane in
 // flight; then their scales.  The plan's copies read pages that nobody writes and write pages that were free: no piece is both read
 // and written.
 template <int D>
 __device__ __forceinline__ void copy_pages(const Pool& pool, const PageCopy* list, int n, int part, int parts) {
   constexpr int kPiece = kPagedBlock * D / 16;        // 16-byte pieces of a block
-  constexpr int kUnroll = 8;
+  constexpr int kUnroll = 4;
   constexpr int kWarps = kCopyThreads / 32;
   const int per = pool.per_page(), lane = threadIdx.x & 31;
   const long long items = (long long)n * pool.heads * 2;
@@ -248,7 +252,7 @@ __device__ __forceinline__ void copy_pages(const Pool& pool, const PageCopy* lis
 }
 
 template <int D>
-__global__ void __launch_bounds__(kCopyThreads) copy_kernel(Pool pool, PagesWs ws) {
+__global__ void __launch_bounds__(kCopyThreads, 6) copy_kernel(Pool pool, PagesWs ws) {
   wait_for_plan();
   copy_pages<D>(pool, ws.copies, ws.hdr[kHdrCopies], blockIdx.x, gridDim.x);
 }
@@ -319,7 +323,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(ForkParams p) {
 // Blocks 0 .. layers*tiles-1 rewrite kForkCols columns of a layer's table in place (all old entries of the columns are in shared
 // memory before the first is replaced) and count references; the blocks behind them copy pages.
 template <int D>
-__global__ void __launch_bounds__(kCopyThreads) fork_kernel(ForkParams p) {
+__global__ void __launch_bounds__(kCopyThreads, 6) fork_kernel(ForkParams p) {
   extern __shared__ int32_t tile[];     // [n_seqs][kForkCols]
   wait_for_plan();
   if (!p.ws.hdr[kHdrGo]) return;
@@ -365,13 +369,13 @@ struct CompactParams {
 __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CompactParams p) {
   let_dependents_start();
   __shared__ int warp_sums[33];
-  const int n = p.pool.n_pages, tid = threadIdx.x, group = 1024 * (tid >> 5);
+  const int n = p.pool.n_pages, tid = threadIdx.x, per = votes_per_lane(p.pool), lane = tid & 31;
   const auto used = [](int32_t r) { return r > 0; };
-  // a thread's 32 pages of the first 32768 stay in a register; pools beyond that are read twice
+  // a thread's votes on the first 32768 pages stay in a register; pools beyond that are read twice
   uint32_t kept = 0;
   int mine = 0;
-  for (int base = 0; base < n; base += 32 * kPlanThreads) {
-    const uint32_t live = base + group < n ? vote_pages(p.pool, base + group, used) : 0;
+  for (int base = 0; base < n; base += per * kPlanThreads) {
+    const uint32_t live = vote_pages(p.pool, base, per, used);
     if (base == 0) kept = live;
     mine += __popc(live);
   }
@@ -379,10 +383,10 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CompactParam
   (void)block_exclusive_scan(mine, warp_sums, live);
   // the r-th free page below `live` takes the r-th live page at or above it: there are equally many
   int holes = 0, moves = 0;
-  for (int base = 0; base < n; base += 32 * kPlanThreads) {
-    const int first = base + 32 * tid;
-    const uint32_t mask = base == 0 ? kept : base + group < n ? vote_pages(p.pool, base + group, used) : 0;
-    const int below = min(max(live - first, 0), 32);          // of this thread's pages, those below `live`
+  for (int base = 0; base < n; base += per * kPlanThreads) {
+    const int first = first_voted(base, per);
+    const uint32_t mask = base == 0 ? kept : vote_pages(p.pool, base, per, used);
+    const int below = lane < per ? min(max(live - first, 0), 32) : 0;          // of this thread's pages, those below `live`
     const uint32_t low = below == 32 ? 0xFFFFFFFFu : (1u << below) - 1u;
     uint32_t h = ~mask & low, m = mask & ~low;
     int total_h, total_m;
@@ -413,7 +417,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CompactParam
 
 // Block b maps the entries of unit b, b + gridDim, ...; then all blocks copy.
 template <int D>
-__global__ void __launch_bounds__(kCopyThreads) compact_kernel(CompactParams p) {
+__global__ void __launch_bounds__(kCopyThreads, 6) compact_kernel(CompactParams p) {
   wait_for_plan();
   const int units = p.table.n_layers * p.table.n_seqs, live = p.ws.hdr[kHdrPagesLive];
   for (int u = blockIdx.x; u < units; u += gridDim.x) {
@@ -473,7 +477,7 @@ spindlekv_status pages_resize_impl(const spindlekv_page_pool& pool, const spindl
   }
   if (cudaGetLastError() != cudaSuccess) return SPINDLEKV_CUDA;
   const int units = table.n_layers * table.n_seqs;
-  const unsigned grid = (unsigned)std::min<int64_t>(((int64_t)units * pool.n_kv_heads * 2 + kCopyThreads / 32 - 1) / (kCopyThreads / 32), 4 * sms);
+  const unsigned grid = (unsigned)std::min<int64_t>(((int64_t)units * pool.n_kv_heads * 2 + kCopyThreads / 32 - 1) / (kCopyThreads / 32), 6 * sms);
   return pool.head_dim == 64 ? launch_behind(copy_kernel<64>, grid, 0, st, p.pool, p.ws) : launch_behind(copy_kernel<128>, grid, 0, st, p.pool, p.ws);
 }
 
@@ -501,7 +505,7 @@ spindlekv_status pages_fork_impl(const spindlekv_page_pool& pool, const spindlek
   }
   if (cudaGetLastError() != cudaSuccess) return SPINDLEKV_CUDA;
   const int64_t units = (int64_t)table.n_layers * table.n_seqs;
-  const unsigned grid = (unsigned)(p.tiles * table.n_layers + std::min<int64_t>((units * pool.n_kv_heads * 2 + kCopyThreads / 32 - 1) / (kCopyThreads / 32), 4 * sms));
+  const unsigned grid = (unsigned)(p.tiles * table.n_layers + std::min<int64_t>((units * pool.n_kv_heads * 2 + kCopyThreads / 32 - 1) / (kCopyThreads / 32), 6 * sms));
   const size_t smem = (size_t)table.n_seqs * kForkCols * 4;
   return pool.head_dim == 64 ? launch_behind(fork_kernel<64>, grid, smem, st, p) : launch_behind(fork_kernel<128>, grid, smem, st, p);
 }
@@ -518,7 +522,7 @@ spindlekv_status pages_compact_impl(const spindlekv_page_pool& pool, const spind
     compact_plan_kernel<<<1, kPlanThreads, 0, st>>>(p);
   }
   if (cudaGetLastError() != cudaSuccess) return SPINDLEKV_CUDA;
-  const unsigned grid = (unsigned)(8 * sms);
+  const unsigned grid = (unsigned)(6 * sms);
   return pool.head_dim == 64 ? launch_behind(compact_kernel<64>, grid, 0, st, p) : launch_behind(compact_kernel<128>, grid, 0, st, p);
 }
 

@@ -77,6 +77,15 @@ def test_masked_tokens_dead_beams_and_bad_rows():
     check(x[:4].contiguous(), torch.full((4,), -float("inf"), device="cuda"), 4, 9)       # nothing is alive
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_of_the_lowest_value(dtype):
+    # a row of nothing but the type's lowest value is a uniform one; slices of it next to ordinary ones weigh nothing
+    x = logits_of(4, 20000, dtype, 8)
+    x[0] = torch.finfo(dtype).min
+    x[1, :17000] = torch.finfo(dtype).min
+    check(x, torch.zeros(4, device="cuda"), 2, 12)
+
+
 @pytest.mark.parametrize("eos", [0, 2, 2999])
 def test_finished_beams(eos):
     x = logits_of(8, 3000, torch.bfloat16, 9)
