@@ -1,11 +1,13 @@
 // Beam search's selection: the n_out best of n_beams x vocab continuations of every sequence.
 //
-// Bound by reading the logits once.  One block per slice of a row: the slice is in registers after one pass of wide loads; its maximum
-// and exp-sum go to the workspace, and so do its n_out largest logits.  Those are found without sorting: the block's threads form 64
-// groups of four, and the n_out-th largest of the groups' maxima is a bound that n_out logits reach and, mostly, a dozen or two in all;
-// these are ranked by counting.  Where many logits equal the bound (rows that are masked for the most part) there are more of them than
-// fit, and the same is done once more on keys (value, index) with the lower index above, of which no two are equal: then only n_out groups
-// reach the bound.  Within a row the order of logits is the order of totals.
+// Bound by reading the logits once.  One block walks a slice of a row, tile by tile (8192 logits, 32 per thread in registers after one
+// pass of wide loads).  Every thread keeps a running maximum and exp-sum of its own; the slice's go to the workspace, and so do its
+// n_out largest logits.  Those are found without sorting: in the first tile the block's threads form 64 groups of four, and the
+// n_out-th largest of the groups' maxima is a bound that n_out logits reach and, mostly, a dozen or two in all; in later tiles only what
+// exceeds the bound counts (an equal logit has a higher index than n_out others).  The candidates, keys of value and index with the lower
+// index above, are ranked by counting.  Where many logits equal the bound (rows that are masked for the most part) the lowest of them are
+// read off in order; where a later tile exceeds the bound too often it makes a new one as the first did.  Within a row the order of
+// logits is the order of totals.
 // The last block of a sequence to arrive joins its slices: log-sum-exp of the beams from the slices' pieces (added in double), totals in
 // double, and the same selection over the slices' lists, 2048 entries at a time beside the best so far.  (A second kernel for that cost
 // 2 us more, and 3 us on the host.)
@@ -26,6 +28,7 @@ static_assert(kBeamGroups >= kBeamMaxOut && kBeamGroup == 4, "the bound is the n
 
 struct BeamParams {
   int n_seqs, n_beams, vocab, k, slices;
+  int tiles;           // of a slice
   const void* logits;
   int64_t row_stride;
   const float* score;
@@ -37,7 +40,8 @@ struct BeamParams {
   int2* cand;          // [rows][slices][k] (logit bits, token), best first; token -1: none
   unsigned long long* arrived;   // [n_seqs]
 };
-constexpr int kBeamFound = 512;        // candidates of a slice that are held without keys
+constexpr int kBeamKeep = 256;         // candidates of a slice beyond which only the n_out best are kept
+constexpr int kBeamTies = 512;         // candidates of a tile beyond which those equal to the bound are read off in order
 constexpr float kLog2e = 1.44269504f;
 
 
@@ -93,14 +97,11 @@ __device__ __noinline__ void beam_join(const BeamParams& p, int seq, JoinScratch
 template <typename T, int EPT, bool VEC>
 __global__ void __launch_bounds__(kBeamThreads, 4) beam_kernel(const __grid_constant__ BeamParams p) {
   __shared__ __align__(16) float tops[kBeamGroups];
-  __shared__ unsigned long long keys[kBeamGroups];
-  constexpr int kFound = kBeamMaxOut * kBeamGroup * EPT;
-  static_assert(kFound >= kBeamFound, "room for either kind of candidates");
+  // what a compaction leaves or a tile adds at most: fewer than n_out groups exceed a bound
+  constexpr int kFound = kBeamKeep + kBeamMaxOut * kBeamGroup * EPT + 2 * kBeamTies;
   __shared__ __align__(16) unsigned char scratch[kFound * 8 > sizeof(JoinScratch) ? kFound * 8 : sizeof(JoinScratch)];
   unsigned long long* found = reinterpret_cast<unsigned long long*>(scratch);
-  __shared__ unsigned long long key_bound;
-  __shared__ float bound;
-  __shared__ float red[2 * (kBeamThreads / 32)];
+  __shared__ float bound, red[2 * (kBeamThreads / 32)];
   __shared__ int n_found, last;
   const int row = blockIdx.y, slice = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   // the block's results are written: the last block of the sequence joins them
@@ -119,130 +120,165 @@ __global__ void __launch_bounds__(kBeamThreads, 4) beam_kernel(const __grid_cons
     arrive();
     return;
   }
-  if (tid == 0) n_found = 0;
+  if (tid == 0) { n_found = 0; bound = -CUDART_INF_F; }
   constexpr int W = VEC ? 16 / (int)sizeof(T) : 1;          // elements per load
+  constexpr int kTile = kBeamThreads * EPT;
   const T* x = reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.row_stride;
-  const int s0 = slice * (kBeamThreads * EPT);
-  float v[EPT];
-  auto index = [&](int i) { return s0 + ((i / W) * kBeamThreads + tid) * W + i % W; };
+  float m = -CUDART_INF_F, sum = 0.f;                       // of this thread's logits
+  const int begin = slice * p.tiles * kTile, end = min(begin + p.tiles * kTile, p.vocab);
+  for (int s0 = begin; s0 < end; s0 += kTile) {
+    float v[EPT];
+    auto index = [&](int i) { return s0 + ((i / W) * kBeamThreads + tid) * W + i % W; };   // rises with i
 #pragma unroll
-  for (int j = 0; j < EPT / W; ++j) {
-    const int at = index(j * W);
-    if constexpr (VEC) {
-      // whole pieces: the row is 16-byte aligned; the last piece may be short
-      if (at + W <= p.vocab) {
-        const uint4 raw = __ldcs(reinterpret_cast<const uint4*>(x + at));
-        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-        if constexpr (sizeof(T) == 4) {
+    for (int j = 0; j < EPT / W; ++j) {
+      const int at = index(j * W);
+      if constexpr (VEC) {
+        // whole pieces: the row is 16-byte aligned; the last piece may be short
+        if (at + W <= p.vocab) {
+          const uint4 raw = __ldcs(reinterpret_cast<const uint4*>(x + at));
+          const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+          if constexpr (sizeof(T) == 4) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[j * W + i] = __uint_as_float(w[i]);
+            for (int i = 0; i < 4; ++i) v[j * W + i] = __uint_as_float(w[i]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              v[j * W + 2 * i] = __uint_as_float(w[i] << 16);
+              v[j * W + 2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            }
+          }
         } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            v[j * W + 2 * i] = __uint_as_float(w[i] << 16);
-            v[j * W + 2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-          }
+          for (int i = 0; i < W; ++i) v[j * W + i] = at + i < p.vocab ? to_f32(x[at + i]) : -CUDART_INF_F;
         }
       } else {
-#pragma unroll
-        for (int i = 0; i < W; ++i) v[j * W + i] = at + i < p.vocab ? to_f32(x[at + i]) : -CUDART_INF_F;
+        v[j] = at < p.vocab ? to_f32(x[at]) : -CUDART_INF_F;
       }
-    } else {
-      v[j] = at < p.vocab ? to_f32(x[at]) : -CUDART_INF_F;
+    }
+    float mx = -CUDART_INF_F;
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) mx = fmaxf(mx, v[i]);
+    // exp-sum relative to the thread's maximum (a NaN must show in it).  The difference first: a product of the type's lowest value
+    // overflows, and a row of nothing else is a uniform one
+    {
+      const float high = fmaxf(m, mx), ref = high == -CUDART_INF_F ? 0.f : high;
+      sum *= m == high ? 1.f : pow2((m - ref) * kLog2e);
+      m = high;
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) sum += pow2((v[i] - ref) * kLog2e);
+    }
+    // hits of this tile: what exceeds `least`, or what equals it
+    auto push = [&](float least, bool equal) {
+      uint32_t hits = 0;
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) hits |= (equal ? v[i] == least : v[i] > least) ? 1u << i : 0u;
+      for (; hits; hits &= hits - 1) {
+        const int at = index(__ffs(hits) - 1);
+        if (at >= p.vocab) continue;                        // only what stands behind the row's end, at -infinity
+        const int slot = atomicAdd(&n_found, 1);
+        if (slot < kFound) found[slot] = key_of(to_f32(x[at]), at);      // read once more: the place is not known before
+      }
+    };
+    const int before = s0 == begin ? 0 : n_found;           // (nobody adds to it before the next barrier)
+    bool anew = s0 == begin;
+    if (!anew) {
+      __syncthreads();                                      // everybody knows `before`
+      if (mx > bound) push(bound, false);
+      __syncthreads();
+      anew = n_found > before + kBeamTies;
+    }
+    if (anew) {
+      // ---- a bound from this tile: the n_out-th largest of the groups' maxima (equal ones by their number) ----
+      float quad = mx;
+#pragma unroll
+      for (int o = 1; o < kBeamGroup; o <<= 1) quad = fmaxf(quad, __shfl_xor_sync(0xffffffffu, quad, o));
+      if (tid % kBeamGroup == 0) tops[tid / kBeamGroup] = quad;
+      __syncthreads();
+      {   // four threads to a group, each against a quarter of the groups
+        const int mine = tid / 4, from = tid % 4 * (kBeamGroups / 4);
+        const float own = tops[mine];
+        int rank = 0;
+#pragma unroll
+        for (int i = from; i < from + kBeamGroups / 4; i += 4) {
+          const float4 q = *reinterpret_cast<const float4*>(tops + i);
+          rank += ((q.x > own) | ((q.x == own) & (i < mine))) + ((q.y > own) | ((q.y == own) & (i + 1 < mine))) +
+                  ((q.z > own) | ((q.z == own) & (i + 2 < mine))) + ((q.w > own) | ((q.w == own) & (i + 3 < mine)));
+        }
+        rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+        rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+        if (rank == p.k - 1 && tid % 4 == 0) {
+          n_found = before;
+          bound = fmaxf(bound, own);                        // (a lower one would not have been exceeded so often)
+        }
+      }
+      __syncthreads();
+      const float least = bound;
+      if (mx > least) push(least, false);
+      __syncthreads();
+      const int above = n_found;
+      __syncthreads();
+      if (mx >= least) push(least, true);
+      __syncthreads();
+      if (n_found > above + kBeamTies) {
+        // too many equal it: the lowest n_out of them, in order
+        __syncthreads();
+        if (warp == 0) {
+          int got = 0;
+          const int stop = min(s0 + kTile, p.vocab);
+          for (int at = s0 + lane; __any_sync(0xffffffffu, at < stop) && got < p.k; at += 32) {
+            const bool tie = at < stop && to_f32(x[at]) == least;
+            const uint32_t votes = __ballot_sync(0xffffffffu, tie);
+            if (tie) found[above + got + __popc(votes & ((1u << lane) - 1u))] = key_of(least, at);
+            got += __popc(votes);
+          }
+          if (lane == 0) n_found = above + got;
+        }
+        __syncthreads();
+      }
+    }
+    if (n_found > kBeamKeep) {
+      // ---- only the n_out best stay; the last of them is the bound ----
+      const int n = n_found;
+      constexpr int kMine = (kFound + kBeamThreads - 1) / kBeamThreads;
+      uint32_t rank_of[kMine];
+      unsigned long long mine[kMine];
+#pragma unroll 1
+      for (int c = 0; c < kMine; ++c) {
+        const int at = c * kBeamThreads + tid;
+        mine[c] = at < n ? found[at] : 0;
+        uint32_t r = 0;
+        if (at < n) {
+#pragma unroll 4
+          for (int j = 0; j < n; ++j) r += found[j] > mine[c];
+        }
+        rank_of[c] = r;
+      }
+      __syncthreads();
+#pragma unroll 1
+      for (int c = 0; c < kMine; ++c) {
+        if (mine[c] && rank_of[c] < (uint32_t)p.k) {
+          found[rank_of[c]] = mine[c];
+          if (rank_of[c] == (uint32_t)p.k - 1) bound = __uint_as_float(key_value_bits(mine[c]));
+        }
+      }
+      if (tid == 0) n_found = min(n, p.k);
+      __syncthreads();
     }
   }
-  // ---- maxima ----
-  float mx = -CUDART_INF_F;
+  // ---- the slice's maximum and exp-sum ----
+  float all = m;
 #pragma unroll
-  for (int i = 0; i < EPT; ++i) mx = fmaxf(mx, v[i]);
-  float quad = mx;
-#pragma unroll
-  for (int o = 1; o < kBeamGroup; o <<= 1) quad = fmaxf(quad, __shfl_xor_sync(0xffffffffu, quad, o));
-  if (tid % kBeamGroup == 0) tops[tid / kBeamGroup] = quad;
-#pragma unroll
-  for (int o = kBeamGroup; o < 32; o <<= 1) quad = fmaxf(quad, __shfl_xor_sync(0xffffffffu, quad, o));
-  if (lane == 0) red[warp] = quad;
+  for (int o = 16; o >= 1; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
+  if (lane == 0) red[warp] = all;
   __syncthreads();
-  float all = red[0];
+  all = red[0];
 #pragma unroll
   for (int w = 1; w < kBeamThreads / 32; ++w) all = fmaxf(all, red[w]);
-  // ---- the n_out-th largest of the groups' maxima (equal ones by their number) ----
-  {   // four threads to a group, each against a quarter of the groups
-    const int mine = tid / 4, from = tid % 4 * (kBeamGroups / 4);
-    const float own = tops[mine];
-    int rank = 0;
-#pragma unroll
-    for (int i = from; i < from + kBeamGroups / 4; i += 4) {
-      const float4 q = *reinterpret_cast<const float4*>(tops + i);
-      rank += ((q.x > own) | ((q.x == own) & (i < mine))) + ((q.y > own) | ((q.y == own) & (i + 1 < mine))) +
-              ((q.z > own) | ((q.z == own) & (i + 2 < mine))) + ((q.w > own) | ((q.w == own) & (i + 3 < mine)));
-    }
-    rank += __shfl_xor_sync(0xffffffffu, rank, 1);
-    rank += __shfl_xor_sync(0xffffffffu, rank, 2);
-    if (rank == p.k - 1) bound = own;
-  }
-  // ---- exp-sum relative to the maximum (a NaN anywhere must show in it).  The difference first: a product of the type's lowest value
-  // overflows, and a row of nothing else is a uniform one ----
-  const float ref = all == -CUDART_INF_F ? 0.f : all;
-  float sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < EPT; ++i) sum += pow2((v[i] - ref) * kLog2e);
+  sum *= m == all ? 1.f : pow2((m - (all == -CUDART_INF_F ? 0.f : all)) * kLog2e);
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) red[kBeamThreads / 32 + warp] = sum;
-  __syncthreads();
-  if (tid == 0) {
-    float s = 0.f;
-#pragma unroll
-    for (int w = 0; w < kBeamThreads / 32; ++w) s += red[kBeamThreads / 32 + w];
-    p.stat[(int64_t)row * p.slices + slice] = make_float2(all, s);
-  }
-  // ---- what reaches the bound; then the places of a thread's hits are read once more ----
-  const float least_value = bound;
-  if (mx >= least_value) {
-    uint32_t hits = 0;
-#pragma unroll
-    for (int i = 0; i < EPT; ++i) hits |= v[i] >= least_value ? 1u << i : 0u;
-    for (; hits; hits &= hits - 1) {
-      const int at = index(__ffs(hits) - 1);
-      if (at >= p.vocab) continue;
-      const int slot = atomicAdd(&n_found, 1);
-      if (slot < kBeamFound) found[slot] = key_of(to_f32(x[at]), at);
-    }
-  }
-  __syncthreads();
-  if (n_found > kBeamFound) {      // the same on keys
-    __syncthreads();
-    unsigned long long top = 0;
-#pragma unroll
-    for (int i = EPT - 1; i >= 0; --i) {
-      const int at = index(i);
-      if (v[i] == mx && at < p.vocab) top = key_of(mx, at);
-    }
-    unsigned long long best = top;
-#pragma unroll
-    for (int o = 1; o < kBeamGroup; o <<= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-    if (tid % kBeamGroup == 0) keys[tid / kBeamGroup] = best;
-    if (tid == 0) { n_found = 0; key_bound = 1; }
-    __syncthreads();
-    if (tid < kBeamGroups) {
-      const unsigned long long own = keys[tid];
-      int rank = 0;
-      for (int i = 0; i < kBeamGroups; ++i) rank += keys[i] > own;
-      if (rank == p.k - 1 && own) key_bound = own;
-    }
-    __syncthreads();
-    const unsigned long long least = key_bound;
-    if (top >= least) {
-#pragma unroll
-      for (int i = 0; i < EPT; ++i) {
-        const int at = index(i);
-        const unsigned long long q = key_of(v[i], at);
-        if (at < p.vocab && q >= least) found[atomicAdd(&n_found, 1)] = q;
-      }
-    }
-    __syncthreads();
-  }
+  // ---- its best candidates ----
   const int n = n_found;
   int2* out = p.cand + ((int64_t)row * p.slices + slice) * p.k;
   for (int i = tid; i < n; i += kBeamThreads) {
@@ -253,6 +289,13 @@ __global__ void __launch_bounds__(kBeamThreads, 4) beam_kernel(const __grid_cons
     if (r < p.k) out[r] = make_int2((int)key_value_bits(q), key_index(q));
   }
   for (int i = n + tid; i < p.k; i += kBeamThreads) out[i] = make_int2(0, -1);
+  __syncthreads();
+  if (tid == 0) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < kBeamThreads / 32; ++w) s += red[kBeamThreads / 32 + w];
+    p.stat[(int64_t)row * p.slices + slice] = make_float2(all, s);
+  }
   arrive();
 }
 
@@ -373,12 +416,18 @@ __device__ __noinline__ void beam_join(const BeamParams& p, int seq, JoinScratch
   }
 }
 
-// Elements per thread of a slice: 32 keep the lists that the joining block reads short; 8 give a call of few rows four times the
-// blocks.  The border is one block per SM.
-static int beam_per_thread(int64_t rows, int vocab) { return rows * ceil_div(vocab, kBeamThreads * 32) >= 148 ? 32 : 8; }
+// How a row is cut.  Tiles of 32 logits per thread, as many to a block as keep all blocks on the device at once (four to an SM); where
+// that leaves SMs without a block, tiles of 8 per thread and one to a block.
+struct BeamCut { int per_thread, tiles, slices; };
+static BeamCut beam_cut(int64_t rows, int vocab) {
+  const int tiles = ceil_div(vocab, kBeamThreads * 32);
+  if (rows * tiles < 148) return BeamCut{8, 1, ceil_div(vocab, kBeamThreads * 8)};
+  const int blocks = (int)std::max<int64_t>(1, 592 / rows), per = ceil_div(tiles, blocks);
+  return BeamCut{32, per, ceil_div(tiles, per)};
+}
 
 size_t beam_workspace_bytes(int n_seqs, int n_beams, int vocab, int k) {
-  const size_t rows = (size_t)n_seqs * n_beams, slices = (size_t)ceil_div(vocab, kBeamThreads * beam_per_thread((int64_t)rows, vocab));
+  const size_t rows = (size_t)n_seqs * n_beams, slices = (size_t)beam_cut((int64_t)rows, vocab).slices;
   return kHeaderBytes + align_up(rows * slices * sizeof(float2), 256) + align_up(rows * slices * k * sizeof(int2), 256) + align_up((size_t)n_seqs * 8, 256);
 }
 
@@ -396,8 +445,8 @@ spindlekv_status beam_select_impl(int n_seqs, int n_beams, int vocab, int k, con
   if (ws_bytes < beam_workspace_bytes(n_seqs, n_beams, vocab, k)) return SPINDLEKV_WORKSPACE_TOO_SMALL;
   const int64_t rows = (int64_t)n_seqs * n_beams;
   if (rows > 65535) return SPINDLEKV_UNSUPPORTED;
-  const int per = beam_per_thread(rows, vocab);
-  BeamParams p{n_seqs, n_beams, vocab, k, ceil_div(vocab, kBeamThreads * per), logits, row_stride, score, finished, eos,
+  const BeamCut cut = beam_cut(rows, vocab);
+  BeamParams p{n_seqs, n_beams, vocab, k, cut.slices, cut.tiles, logits, row_stride, score, finished, eos,
                out_score, out_parent, out_token, nullptr, nullptr, nullptr};
   uint8_t* at = static_cast<uint8_t*>(ws) + kHeaderBytes;
   p.stat = reinterpret_cast<float2*>(at);
@@ -408,10 +457,10 @@ spindlekv_status beam_select_impl(int n_seqs, int n_beams, int vocab, int k, con
   const int size = dtype == SPINDLEKV_BF16 ? 2 : 4;
   const bool vec = reinterpret_cast<uintptr_t>(logits) % 16 == 0 && row_stride * size % 16 == 0;
   if (dtype == SPINDLEKV_BF16) {
-    if (per == 32) launch_slices<__nv_bfloat16, 32>(p, vec, st);
+    if (cut.per_thread == 32) launch_slices<__nv_bfloat16, 32>(p, vec, st);
     else launch_slices<__nv_bfloat16, 8>(p, vec, st);
   } else {
-    if (per == 32) launch_slices<float, 32>(p, vec, st);
+    if (cut.per_thread == 32) launch_slices<float, 32>(p, vec, st);
     else launch_slices<float, 8>(p, vec, st);
   }
   return cudaGetLastError() == cudaSuccess ? SPINDLEKV_OK : SPINDLEKV_CUDA;
