@@ -158,7 +158,7 @@ template <int D>
 __device__ __forceinline__ int token_of(int i) { return ((D == 128 ? 0x37156240 : 0x65742130) >> (4 * i)) & 7; }
 
 template <typename T, int FMT, int D, int NT>
-__global__ void __launch_bounds__(kAttThreads, NT == 4 ? 1 : 2) paged_attend_kernel(const __grid_constant__ CUtensorMap kmap,
+__global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_kernel(const __grid_constant__ CUtensorMap kmap,
                                                                                   const __grid_constant__ CUtensorMap vmap, AttendParams p) {
   constexpr int NP = sizeof(T) == 4 ? 2 : 1;      // fp16 pieces of a query and of a weight
   constexpr int KS = D / 16;                      // k-steps of a score, and m-tiles of an output
