@@ -4,7 +4,7 @@
 // has an order -- who gets which page -- by prefix sums over the sequences and over page_ref, so that the outcome does not depend
 // on the order of atomics; reference counts change by atomic integer additions, whose order does not show.  The plan
 // (a list of page copies, new entries, a map) lies in the workspace, and a second kernel carries it out over the whole device: the
-// copies move four 16-byte pieces per lane at a time and are bound by memory.  The second kernel is launched with
+// copies move four or eight 16-byte pieces per lane at a time and are bound by memory.  The second kernel is launched with
 // programmatic stream serialization, so that its blocks are on the device already when the plan is done.
 #include <algorithm>
 
@@ -56,7 +56,8 @@ size_t pages_workspace_bytes(const spindlekv_page_pool& p, const spindlekv_page_
   return pages_ws_layout(t.n_layers * t.n_seqs, t.n_seqs, p.n_pages, nullptr, nullptr);
 }
 
-__device__ __forceinline__ int pages_of(int len, int ps) { return (int)(((long long)len + ps - 1) / ps); }
+// pages of a length (page sizes are powers of two; lengths stay clear of the top of 32 bits)
+__device__ __forceinline__ int pages_of(int len, int ps) { return (len + ps - 1) >> (31 - __clz(ps)); }
 
 // The planning block looks at 32 * per * 32 pages at a time: every warp at 32 * per in order, every lane of it keeps the votes on 32 of
 // them, lanes from `per` on none.  `per` is what the pool needs, at most 32.
@@ -77,13 +78,19 @@ __device__ __forceinline__ uint32_t vote_pages(const Pool& pool, int base, int p
   return mine;
 }
 
+struct IsFree {
+  __device__ __forceinline__ bool operator()(int32_t r) const { return r == 0; }
+};
+constexpr IsFree is_free{};
+
 // Lists the lowest `wanted` free pages, ascending, in taken[]; false (for every thread) when there are fewer.  One block.
-__device__ bool take_free(const Pool& pool, int wanted, int32_t* taken, int* warp_sums) {
+// `early`: the votes on the first pages, where the caller has them already.
+__device__ bool take_free(const Pool& pool, int wanted, int32_t* taken, int* warp_sums, uint32_t early) {
   int have = 0;
   const int per = votes_per_lane(pool);
   for (int base = 0; base < pool.n_pages && have < wanted; base += per * kPlanThreads) {
     const int first = first_voted(base, per);
-    uint32_t free = vote_pages(pool, base, per, [](int32_t r) { return r == 0; });
+    uint32_t free = base == 0 ? early : vote_pages(pool, base, per, is_free);
     int total;
     int k = have + block_exclusive_scan(__popc(free), warp_sums, total);
     for (; free && k < wanted; free &= free - 1) taken[k++] = first + __ffs(free) - 1;
@@ -131,6 +138,7 @@ __global__ void __launch_bounds__(kPlanThreads) resize_plan_kernel(ResizeParams 
   let_dependents_start();
   __shared__ int warp_sums[33];
   const int units = p.table.n_layers * p.table.n_seqs, tid = threadIdx.x;
+  const uint32_t early = vote_pages(p.pool, 0, votes_per_lane(p.pool), is_free);
   // 1. how many pages everybody needs, and where each one's run of taken pages begins
   bool bad = false;
   int total_pages = 0, total_copies = 0;
@@ -156,7 +164,7 @@ __global__ void __launch_bounds__(kPlanThreads) resize_plan_kernel(ResizeParams 
   }
   bad = __syncthreads_or(bad);
   // 2. the pages
-  const bool enough = total_pages <= p.pool.n_pages && take_free(p.pool, total_pages, p.ws.map, warp_sums);
+  const bool enough = total_pages <= p.pool.n_pages && take_free(p.pool, total_pages, p.ws.map, warp_sums, early);
   const bool go = !bad && enough;
   if (tid == 0) {
     p.ws.hdr[kHdrStatus] = bad ? SPINDLEKV_INVALID_ARG : enough ? SPINDLEKV_OK : SPINDLEKV_CAPACITY;
@@ -216,13 +224,12 @@ __global__ void __launch_bounds__(kPlanThreads) resize_plan_kernel(ResizeParams 
 
 // ---- copies ----------------------------------------------------------------------------------------------------------
 
-// The copies, a warp at a time: all copied blocks of one (copy, head, K or V), which are contiguous, four 16-byte pieces per lane in
-// flight; then their scales.  The plan's copies read pages that nobody writes and write pages that were free: no piece is both read
+// The copies, a warp at a time: all copied blocks of one (copy, head, K or V), which are contiguous, kUnroll 16-byte pieces per lane
+// in flight (four for a few blocks of many pages, eight for whole pages); then their scales.  The plan's copies read pages that nobody writes and write pages that were free: no piece is both read
 // and written.
-template <int D>
+template <int D, int kUnroll>
 __device__ __forceinline__ void copy_pages(const Pool& pool, const PageCopy* list, int n, int part, int parts) {
   constexpr int kPiece = kPagedBlock * D / 16;        // 16-byte pieces of a block
-  constexpr int kUnroll = 4;
   constexpr int kWarps = kCopyThreads / 32;
   const int per = pool.per_page(), lane = threadIdx.x & 31;
   const long long items = (long long)n * pool.heads * 2;
@@ -254,7 +261,7 @@ __device__ __forceinline__ void copy_pages(const Pool& pool, const PageCopy* lis
 template <int D>
 __global__ void __launch_bounds__(kCopyThreads, 6) copy_kernel(Pool pool, PagesWs ws) {
   wait_for_plan();
-  copy_pages<D>(pool, ws.copies, ws.hdr[kHdrCopies], blockIdx.x, gridDim.x);
+  copy_pages<D, 4>(pool, ws.copies, ws.hdr[kHdrCopies], blockIdx.x, gridDim.x);
 }
 
 // ---- fork ------------------------------------------------------------------------------------------------------------
@@ -273,6 +280,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(ForkParams p) {
   __shared__ int children[kForkMaxSeqs], first[kForkMaxSeqs];
   const int n = p.table.n_seqs, units = p.table.n_layers * n, tid = threadIdx.x;
   for (int s = tid; s < n; s += kPlanThreads) { children[s] = 0; first[s] = n; }
+  const uint32_t early = vote_pages(p.pool, 0, votes_per_lane(p.pool), is_free);
   __syncthreads();
   bool bad = false;
   for (int s = tid; s < n; s += kPlanThreads) {
@@ -296,7 +304,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(ForkParams p) {
     if (u < units) p.ws.fresh[u] = copy ? at : -1;
     copies += total;
   }
-  const bool enough = !bad && copies <= p.pool.n_pages && take_free(p.pool, copies, p.ws.map, warp_sums);
+  const bool enough = !bad && copies <= p.pool.n_pages && take_free(p.pool, copies, p.ws.map, warp_sums, early);
   if (tid == 0) {
     p.ws.hdr[kHdrStatus] = bad ? SPINDLEKV_INVALID_ARG : enough ? SPINDLEKV_OK : SPINDLEKV_CAPACITY;
     p.ws.hdr[kHdrCopies] = enough ? copies : 0;
@@ -324,36 +332,36 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(ForkParams p) {
 // memory before the first is replaced) and count references; the blocks behind them copy pages.
 template <int D>
 __global__ void __launch_bounds__(kCopyThreads, 6) fork_kernel(ForkParams p) {
-  extern __shared__ int32_t tile[];     // [n_seqs][kForkCols]
+  extern __shared__ __align__(16) int32_t tile[];     // [n_seqs][kForkCols], then four numbers per sequence
   wait_for_plan();
   if (!p.ws.hdr[kHdrGo]) return;
   const int table_blocks = p.table.n_layers * p.tiles;
   if ((int)blockIdx.x >= table_blocks) {
-    copy_pages<D>(p.pool, p.ws.copies, p.ws.hdr[kHdrCopies], blockIdx.x - table_blocks, gridDim.x - table_blocks);
+    copy_pages<D, 4>(p.pool, p.ws.copies, p.ws.hdr[kHdrCopies], blockIdx.x - table_blocks, gridDim.x - table_blocks);
     return;
   }
   const int n = p.table.n_seqs, layer = blockIdx.x / p.tiles, c0 = (blockIdx.x - layer * p.tiles) * kForkCols;
   const int ps = p.pool.ps;
-  const int32_t* old_len = p.ws.old_len + layer * n;
+  // per sequence: its length before, its children, its parent, its own copy of the parent's open page (or -1)
+  int4* seqs = reinterpret_cast<int4*>(tile + n * kForkCols);
+  for (int s = threadIdx.x; s < n; s += kCopyThreads)
+    seqs[s] = make_int4(p.ws.old_len[layer * n + s], p.ws.children[s], p.parent[s], p.ws.fresh[layer * n + s]);
+  __syncthreads();
   int32_t* pages = p.table.pages + (int64_t)layer * n * p.table.max_pages;
+#pragma unroll 4
   for (int i = threadIdx.x; i < n * kForkCols; i += kCopyThreads) {
     const int s = i / kForkCols, c = c0 + i % kForkCols;
-    int e = -1;
-    if (c < pages_of(old_len[s], ps)) {
-      e = pages[(int64_t)s * p.table.max_pages + c];
-      const int kids = p.ws.children[s];
-      const bool open = c == old_len[s] / ps;            // not full: the first child's alone
-      const int by = open ? min(kids, 1) - 1 : kids - 1;
-      if (by) add_ref(p.pool, e, by);
-    }
-    tile[i] = e;
+    const int len = seqs[s].x, kids = seqs[s].y;
+    tile[i] = c < pages_of(len, ps) ? pages[(int64_t)s * p.table.max_pages + c] : -1;
+    const int by = c == len / ps ? min(kids, 1) - 1 : kids - 1;       // a page that is not full is the first child's alone
+    if (by && c < pages_of(len, ps)) add_ref(p.pool, tile[i], by);
   }
   __syncthreads();
+#pragma unroll 4
   for (int i = threadIdx.x; i < n * kForkCols; i += kCopyThreads) {
-    const int s = i / kForkCols, c = c0 + i % kForkCols, q = p.parent[s];
-    if (q < 0 || c >= pages_of(old_len[q], ps)) continue;
-    const int page = p.ws.fresh[layer * n + s];
-    pages[(int64_t)s * p.table.max_pages + c] = page >= 0 && c == old_len[q] / ps ? page : tile[q * kForkCols + i % kForkCols];
+    const int s = i / kForkCols, c = c0 + i % kForkCols, q = seqs[s].z, page = seqs[s].w;
+    const int len = q >= 0 ? seqs[q].x : 0;
+    if (c < pages_of(len, ps)) pages[(int64_t)s * p.table.max_pages + c] = page >= 0 && c == len / ps ? page : tile[q * kForkCols + i % kForkCols];
   }
 }
 
@@ -417,7 +425,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CompactParam
 
 // Block b maps the entries of unit b, b + gridDim, ...; then all blocks copy.
 template <int D>
-__global__ void __launch_bounds__(kCopyThreads, 6) compact_kernel(CompactParams p) {
+__global__ void __launch_bounds__(kCopyThreads, 4) compact_kernel(CompactParams p) {
   wait_for_plan();
   const int units = p.table.n_layers * p.table.n_seqs, live = p.ws.hdr[kHdrPagesLive];
   for (int u = blockIdx.x; u < units; u += gridDim.x) {
@@ -428,7 +436,7 @@ __global__ void __launch_bounds__(kCopyThreads, 6) compact_kernel(CompactParams 
       if (page >= live && page < p.pool.n_pages && p.ws.hdr[kHdrCopies]) row[i] = p.ws.map[page];
     }
   }
-  copy_pages<D>(p.pool, p.ws.copies, p.ws.hdr[kHdrCopies], blockIdx.x, gridDim.x);
+  copy_pages<D, 8>(p.pool, p.ws.copies, p.ws.hdr[kHdrCopies], blockIdx.x, gridDim.x);
 }
 
 // ---- launches --------------------------------------------------------------------------------------------------------
@@ -493,7 +501,7 @@ spindlekv_status pages_fork_impl(const spindlekv_page_pool& pool, const spindlek
   static PerDeviceOnce once;
   const int dev = PerDeviceOnce::current();
   if (!once.done[dev]) {
-    const int most = kForkMaxSeqs * kForkCols * 4;
+    const int most = kForkMaxSeqs * (kForkCols * 4 + 16);
     if (cudaFuncSetAttribute(fork_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
         cudaFuncSetAttribute(fork_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess)
       return SPINDLEKV_CUDA;
@@ -506,7 +514,7 @@ spindlekv_status pages_fork_impl(const spindlekv_page_pool& pool, const spindlek
   if (cudaGetLastError() != cudaSuccess) return SPINDLEKV_CUDA;
   const int64_t units = (int64_t)table.n_layers * table.n_seqs;
   const unsigned grid = (unsigned)(p.tiles * table.n_layers + std::min<int64_t>((units * pool.n_kv_heads * 2 + kCopyThreads / 32 - 1) / (kCopyThreads / 32), 6 * sms));
-  const size_t smem = (size_t)table.n_seqs * kForkCols * 4;
+  const size_t smem = (size_t)table.n_seqs * (kForkCols * 4 + 16);
   return pool.head_dim == 64 ? launch_behind(fork_kernel<64>, grid, smem, st, p) : launch_behind(fork_kernel<128>, grid, smem, st, p);
 }
 
@@ -522,7 +530,7 @@ spindlekv_status pages_compact_impl(const spindlekv_page_pool& pool, const spind
     compact_plan_kernel<<<1, kPlanThreads, 0, st>>>(p);
   }
   if (cudaGetLastError() != cudaSuccess) return SPINDLEKV_CUDA;
-  const unsigned grid = (unsigned)(6 * sms);
+  const unsigned grid = (unsigned)(4 * sms);
   return pool.head_dim == 64 ? launch_behind(compact_kernel<64>, grid, 0, st, p) : launch_behind(compact_kernel<128>, grid, 0, st, p);
 }
 
