@@ -438,7 +438,10 @@ spindlekv_status spindlekv_paged_append(const spindlekv_page_pool* pool, const s
  *   scale     0: 1 / sqrt(head_dim)
  *   ws        device scratch of spindlekv_paged_workspace_bytes bytes, 256-byte aligned, not to be shared by calls that may
  *             run at the same time
- * Sums and softmax statistics are fp32, in an order that depends on the lengths only: the same call gives the same bits.
+ * Sums and softmax statistics are fp32, in an order that the lengths, max_len and the device fix: the same call gives the same bits.
+ * bf16 queries are multiplied as they are and the weights enter in 11 bits; fp32 queries and weights in 22.  The device status word of
+ * `ws` (a bounded wait that gave up) is read with spindlekv_poll_status.
+ * UNSUPPORTED beyond 2^31 pairs of blocks in n_layers * n_seqs * n_kv_heads * max_pages * page_size: split the layers.
  */
 size_t spindlekv_paged_workspace_bytes(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t n_q_heads, int32_t n_rows);
 spindlekv_status spindlekv_paged_attend(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t n_q_heads,
@@ -458,7 +461,8 @@ spindlekv_status spindlekv_paged_attend(const spindlekv_page_pool* pool, const s
  *   out_score   device out [n_seqs][n_out] fp32: total
  *   out_parent  device out [n_seqs][n_out]: row seq * n_beams + w, i.e. with n_out = n_beams the parents of spindlekv_pages_fork
  *   out_token   device out [n_seqs][n_out]
- * n_beams <= 64, n_out <= 32, n_out <= n_beams * vocab < 2^31.
+ * n_beams <= 64, n_out <= 32, vocab <= 2^30, n_out <= n_beams * vocab < 2^31, n_seqs * n_beams < 2^16.  The workspace needs no
+ * preparation, and is not to be shared by calls that may run at the same time.
  */
 size_t spindlekv_beam_workspace_bytes(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_t n_out);
 spindlekv_status spindlekv_beam_select(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_t n_out, const void* logits, int32_t dtype,

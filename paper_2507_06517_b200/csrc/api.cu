@@ -405,8 +405,13 @@ static bool beam_shape_ok(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_
   return (int64_t)n_beams * vocab < 0x7FFFFFFF && n_out <= (int64_t)n_beams * vocab;
 }
 
+// 2^30: a position in a row and a tile beyond it are 32-bit
+static bool beam_size_ok(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_t n_out) {
+  return n_beams <= 64 && n_out <= 32 && vocab <= (1 << 30) && (int64_t)n_seqs * n_beams <= 65535;
+}
+
 size_t spindlekv_beam_workspace_bytes(int32_t n_seqs, int32_t n_beams, int32_t vocab, int32_t n_out) {
-  if (!beam_shape_ok(n_seqs, n_beams, vocab, n_out) || n_beams > 64 || n_out > 32 || (int64_t)n_seqs * n_beams > 65535) return 0;
+  if (!beam_shape_ok(n_seqs, n_beams, vocab, n_out) || !beam_size_ok(n_seqs, n_beams, vocab, n_out)) return 0;
   return beam_workspace_bytes(n_seqs, n_beams, vocab, n_out);
 }
 
@@ -418,7 +423,7 @@ spindlekv_status spindlekv_beam_select(int32_t n_seqs, int32_t n_beams, int32_t 
   if (dtype != SPINDLEKV_F32 && dtype != SPINDLEKV_BF16) return SPINDLEKV_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == SPINDLEKV_F32 ? 4 : 2)) return SPINDLEKV_INVALID_ARG;
   if (finished && (eos < 0 || eos >= vocab)) return SPINDLEKV_INVALID_ARG;
-  if (n_beams > 64 || n_out > 32 || (int64_t)n_seqs * n_beams > 65535) return SPINDLEKV_UNSUPPORTED;
+  if (!beam_size_ok(n_seqs, n_beams, vocab, n_out)) return SPINDLEKV_UNSUPPORTED;
   return beam_select_impl(n_seqs, n_beams, vocab, n_out, logits, dtype, row_stride, score, finished, eos, out_score, out_parent,
                           out_token, ws, ws_bytes, (cudaStream_t)stream);
 }

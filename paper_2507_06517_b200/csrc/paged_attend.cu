@@ -662,10 +662,10 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
     // ---- the warps' results meet, where the ring was ----
     __syncthreads();
     if (*abort_flag) {
-      // give up, but not before what is still on its way has arrived (within the same bound)
-      if (owed & 1) ptx::mbar_wait(full, phase, abort_flag + 1, p.wait_cycles);
-      if (owed & 2) ptx::mbar_wait(full + 1, phase, abort_flag + 1, p.wait_cycles);
-      if (owed & 4) ptx::mbar_wait(full, phase ^ 1, abort_flag + 1, p.wait_cycles);
+      // give up, but not before what is still on its way has arrived (within the default bound)
+      if (owed & 1) ptx::mbar_wait(full, phase, abort_flag + 1, kDefaultMbarWaitCycles);
+      if (owed & 2) ptx::mbar_wait(full + 1, phase, abort_flag + 1, kDefaultMbarWaitCycles);
+      if (owed & 4) ptx::mbar_wait(full, phase ^ 1, abort_flag + 1, kDefaultMbarWaitCycles);
       if (tid == 0) {
         if (p.whole_units) atomicExch(&p.hdr[kHdrStatus], (uint32_t)SPINDLEKV_TIMEOUT);
         else p.lead[blockIdx.x] = make_int2(-2, 0);

@@ -685,7 +685,8 @@ class SpindleKVPagedCache(_OnDevice):
                 raise ValueError(f"out: {list(shape)} expected, got {list(out.shape)}")
             od = self._cache_rows("out", out, table.n_layers, hq)
         if self.ws_attend is None:
-            self.ws_attend = torch.empty(B.spindlekv_paged_workspace_bytes(self.pool, self.table, hq, shape[3]), dtype=torch.uint8, device=self.device)
+            need = B.spindlekv_paged_workspace_bytes(self.pool, self.table, self.Hkv, 1)      # the same for every shape that is served
+            self.ws_attend = torch.zeros(need, dtype=torch.uint8, device=self.device)
         B.spindlekv_paged_attend(self.pool, table, hq, shape[3], max_len or self.capacity, scale, qd, od, self.ws_attend, self._raw(stream))
         return out
 
@@ -706,9 +707,13 @@ class SpindleKVPagedCache(_OnDevice):
         return self.n_live
 
     def status(self) -> int:
-        """Status word of the last ``resize``, ``fork`` or ``compact`` (synchronises the device)."""
+        """Status word of the last ``resize``, ``fork`` or ``compact``, or else of the last ``attend`` (synchronises the device)."""
         torch.cuda.synchronize(self.device)
-        return B.spindlekv_poll_status(self.ws_pages)[0]
+        if self._elsewhere():
+            with torch.cuda.device(self.device):
+                return self.status()
+        st = B.spindlekv_poll_status(self.ws_pages)[0]
+        return B.spindlekv_poll_status(self.ws_attend)[0] if st == B.OK and self.ws_attend is not None else st
 
 
 class SpindleKVBeamSelect(_OnDevice):

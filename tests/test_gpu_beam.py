@@ -122,6 +122,34 @@ def test_same_bits_in_a_graph_and_beside_another_call():
     assert all(torch.equal(p, q) for p, q in zip((b.score, b.parent, b.token), other))
 
 
+def test_workspace_needs_no_preparation_and_serves_other_shapes():
+    from paper_2507_06517_b200 import binding as B
+    shapes = ((4, 8, 40000, 16), (1, 2, 300, 3), (2, 16, 9000, 32), (4, 8, 40000, 16))
+    ws = torch.empty(max(B.spindlekv_beam_workspace_bytes(*s) for s in shapes), dtype=torch.uint8, device="cuda")
+    for n, w, v, k in shapes:
+        ws.random_(0, 256)
+        x, s = logits_of(n * w, v, torch.float32, n + v), torch.zeros(n * w, device="cuda")
+        out = torch.empty((n, k), device="cuda"), torch.empty((n, k), dtype=torch.int32, device="cuda"), torch.empty((n, k), dtype=torch.int32, device="cuda")
+        for _ in range(3):
+            B.spindlekv_beam_select(n, w, v, k, x, s, None, 0, *out, ws)
+        want = R.beam(x.double().cpu().numpy(), np.zeros(n * w), w, k)
+        assert np.array_equal(out[1].cpu().numpy(), want[1]) and np.array_equal(out[2].cpu().numpy(), want[2])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_long_rows_whose_later_tiles_hold_the_best(dtype):
+    # many blocks walk several tiles: rising logits (every tile exceeds the bound of the one before), a late plateau, a masked front
+    n = 75
+    x = torch.zeros((n, 100000), device="cuda")
+    x[0::3] = torch.linspace(-4, 4, 100000, device="cuda")
+    x[1::3, 60000:] = 3.0
+    x[2::3, :90001] = -float("inf")
+    x[2::3, 90001:] = logits_of(n // 3, 9999, torch.float32, 3)
+    x += torch.arange(n, device="cuda")[:, None] % 3 * 0.25
+    check(x.to(dtype), torch.zeros(n, device="cuda"), 3, 32)
+    check(x.to(dtype)[:72], torch.zeros(72, device="cuda"), 8, 5)
+
+
 def test_refusals():
     from paper_2507_06517_b200.pipeline import SpindleKVBeamSelect
     with pytest.raises(ValueError):

@@ -207,6 +207,35 @@ def test_attention_over_many_runs_whatever_the_length_hint(dtype, max_len):
     check_attention(c, r, q, c.attend(q, max_len=max_len), dtype)
 
 
+@pytest.mark.parametrize("max_len", [40, 250, 100000])
+@pytest.mark.parametrize("n_layers,n_seqs", [(2, 16), (3, 41)])
+def test_attention_of_many_short_sequences(n_layers, n_seqs, max_len):
+    # more sequences than lanes, many of them empty; a block per unit, or runs with several units in each
+    c = make(n_layers, n_seqs, 4, 2, 64, n_layers * n_seqs * 16, 16, 16, "e4m3")
+    rng = np.random.default_rng(n_seqs)
+    lens = np.where(rng.random((n_layers, n_seqs)) < 0.3, 0, rng.integers(1, 251, (n_layers, n_seqs)))
+    r = fill(c, lens.tolist(), spread=0.3)
+    q = rows((n_layers, n_seqs, 4, 2, 64), "bf16", 5, 0.2)
+    out = torch.full_like(q, 7.0)
+    c.attend(q, out=out, max_len=max_len)
+    check_attention(c, r, q, out, "bf16")
+    assert c.status() == 0
+
+
+def test_one_workspace_serves_attention_of_every_shape():
+    c = make(1, 2, None, 2, 128, 64, 16, 32, "int8")
+    r = fill(c, [[500, 33]], spread=0.3)
+    from paper_2507_06517_b200.binding import SpindleKVError
+    with pytest.raises(SpindleKVError):
+        c.attend(rows((1, 2, 4, 17, 128), "bf16", 1))
+    c.ws_attend = None
+    for hq, n_rows, dtype in ((16, 16, "f32"), (2, 1, "bf16"), (6, 5, "bf16"), (16, 1, "f32")):
+        q = rows((1, 2, hq, n_rows, 128), dtype, 5, 0.2)
+        if c.ws_attend is not None:
+            c.ws_attend.random_(0, 256)                   # it needs no preparation
+        check_attention(c, r, q, c.attend(q), dtype)
+
+
 def test_attention_with_very_uneven_scales():
     # a value of 1e30 that has no weight must not drown the others, nor one of 1e-30 with all of it
     c = make(1, 2, 2, 1, 64, 20, 4, 32, "int8")

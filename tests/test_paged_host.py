@@ -88,6 +88,8 @@ def test_attend_checks_its_arguments():
     assert call(out=F32) == B.UNSUPPORTED
     assert call(ws=C.c_void_p(128)) == B.INVALID_ARG
     assert call(n=need - 1) == B.WORKSPACE_TOO_SMALL
+    assert need == lib.spindlekv_paged_workspace_bytes(pool(), table(), 16, 16)      # one workspace serves every shape of a pool
+    assert lib.spindlekv_paged_workspace_bytes(pool(), table(), 18, 1) == 0
 
 
 def test_beam_checks_its_arguments():
@@ -101,6 +103,7 @@ def test_beam_checks_its_arguments():
     assert call(w=65) == B.UNSUPPORTED
     assert call(k=33) == B.UNSUPPORTED
     assert call(n=40000) == B.UNSUPPORTED
+    assert call(w=1, v=(1 << 30) + 1) == B.UNSUPPORTED
     assert call(logits=None) == B.INVALID_ARG
     assert call(logits=C.c_void_p(258)) == B.INVALID_ARG
     assert call(dtype=5) == B.INVALID_ARG
