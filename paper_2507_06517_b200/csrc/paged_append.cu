@@ -27,7 +27,8 @@ struct AppendParams {
   const int32_t* idx;
   int idx_len, idx_seq;
   int max_new, n_rows, n_blocks;
-  long long n_items;
+  int per_shift, page_shift;   // log2 of the blocks and of the tokens of a page
+  unsigned n_items;
 };
 
 template <int FMT>
@@ -174,15 +175,11 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(AppendPara
   constexpr int LPR = D / 8;            // lanes of a row
   constexpr int RPI = 32 / LPR;         // rows side by side in a warp
   constexpr int NI = kPagedBlock / RPI;
-  const long long item = (long long)blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5);
+  const unsigned item = blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5);   // of this unit: (head, block, K or V)
   if (item >= p.n_items) return;
   const int lane = threadIdx.x & 31;
   const bool is_v = (item & 1) != 0;
-  long long rest = item >> 1;
-  const int rel = (int)(rest % p.n_blocks);
-  rest /= p.n_blocks;
-  const int head = (int)(rest % p.pool.heads);
-  const int u = (int)(rest / p.pool.heads);
+  const int head = (int)((item >> 1) / (unsigned)p.n_blocks), rel = (int)(item >> 1) - head * p.n_blocks, u = blockIdx.y;
   const int layer = u / p.table.n_seqs, s = u - layer * p.table.n_seqs;
   const int start = p.start[u];
   if (start < 0) return;
@@ -190,13 +187,12 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(AppendPara
   const int blk = start / kPagedBlock + rel;
   const int t0 = blk * kPagedBlock;
   if (t0 >= end || start >= end) return;
-  const int page = p.table.pages[(int64_t)u * p.table.max_pages + t0 / p.pool.ps];
+  const int page = p.table.pages[(int64_t)u * p.table.max_pages + (t0 >> p.page_shift)];
   if (page < 0 || page >= p.pool.n_pages) return;
-  const int per = p.pool.per_page();
-  const int64_t slab = ((int64_t)page * p.pool.heads + head) * per + blk % per;   // index of the block
+  const int64_t slab = (((int64_t)page * p.pool.heads + head) << p.per_shift) + (blk & ((1 << p.per_shift) - 1));   // index of the block
   uint8_t* codes = (is_v ? p.pool.vc : p.pool.kc) + slab * (kPagedBlock * D);
   float* scale = (is_v ? p.pool.vs : p.pool.ks) + slab;
-  const View& src = is_v ? p.V : p.K;
+  const View src = is_v ? p.V : p.K;
   const T* rows = reinterpret_cast<const T*>(src.ptr) + (int64_t)layer * src.sl + (int64_t)s * src.ss + (int64_t)head * src.sh;
   const int first = max(start - t0, 0), last = min(end - t0, kPagedBlock);   // new slots of the block: [first, last)
   // row of this lane's slot (lanes 0..15), handed to the lanes that load it
@@ -261,7 +257,7 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(AppendPara
 
 template <typename T, int FMT>
 static void launch_append(const AppendParams& p, cudaStream_t st) {
-  const unsigned grid = (unsigned)((p.n_items + kAppendThreads / 32 - 1) / (kAppendThreads / 32));
+  const dim3 grid((p.n_items + kAppendThreads / 32 - 1) / (kAppendThreads / 32), p.table.n_layers * p.table.n_seqs);   // at most 8192 units
   LaunchScope ls(KC_PAGED_APPEND, st);
   if (p.pool.d == 64) paged_append_kernel<T, FMT, 64><<<grid, kAppendThreads, 0, st>>>(p);
   else paged_append_kernel<T, FMT, 128><<<grid, kAppendThreads, 0, st>>>(p);
@@ -283,8 +279,11 @@ spindlekv_status paged_append_impl(const spindlekv_page_pool& pool, const spindl
   p.max_new = (int)std::min<int64_t>(max_new, (int64_t)table.max_pages * pool.page_size);
   p.n_rows = n_rows;
   p.n_blocks = (int)(((int64_t)p.max_new + kPagedBlock - 2) / kPagedBlock) + 1;   // a run that begins inside a block touches one more
-  p.n_items = 2ll * table.n_layers * table.n_seqs * pool.n_kv_heads * p.n_blocks;
-  if (p.n_items / (kAppendThreads / 32) >= 0x7FFFFFFFll) return SPINDLEKV_UNSUPPORTED;
+  const int64_t items = 2ll * pool.n_kv_heads * p.n_blocks;
+  if (items > 0x7FFFFFFF) return SPINDLEKV_UNSUPPORTED;
+  p.n_items = (unsigned)items;
+  p.page_shift = pool.page_size == 16 ? 4 : pool.page_size == 32 ? 5 : pool.page_size == 64 ? 6 : 7;
+  p.per_shift = p.page_shift - 4;
   const bool bf = K.dtype == SPINDLEKV_BF16, i8 = pool.format == SPINDLEKV_PAGED_INT8;
   if (bf && i8) launch_append<__nv_bfloat16, SPINDLEKV_PAGED_INT8>(p, st);
   else if (bf) launch_append<__nv_bfloat16, SPINDLEKV_PAGED_E4M3>(p, st);
