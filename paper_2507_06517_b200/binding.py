@@ -192,10 +192,11 @@ class Batch:
 
 
 def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype == torch.bfloat16:
+    dtype = t.dtype
+    if dtype == torch.bfloat16:
         return BF16
+    if dtype == torch.float32:
+        return F32
     raise TypeError(f"unsupported dtype {t.dtype}")
 
 
@@ -223,9 +224,11 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-try:
-    raw_stream = torch._C._cuda_getCurrentRawStream      # the handle alone, without a stream object around it
+try:      # the handle alone, without a stream object around it; the number alone, without a check that CUDA is initialised
+    raw_stream, current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 except AttributeError:
+    current_device = torch.cuda.current_device
+
     def raw_stream(device_index: int) -> int:
         return torch.cuda.current_stream(device_index).cuda_stream
 
@@ -415,7 +418,7 @@ class PageTable:
 
 
 def _bytes(ws: torch.Tensor) -> int:
-    return ws.numel() * ws.element_size()
+    return ws.nbytes
 
 
 def spindlekv_pages_workspace_bytes(pool: PagePool, table: PageTable) -> int:

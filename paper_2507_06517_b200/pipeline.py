@@ -546,10 +546,10 @@ class _OnDevice:
     """Calls go to the current device and stream; ``_elsewhere`` says that the owner's device has to be made current first."""
 
     def _elsewhere(self) -> bool:
-        return torch.cuda.current_device() != self.device.index
+        return B.current_device() != self._index
 
     def _raw(self, stream) -> int:
-        return B.raw_stream(self.device.index) if stream is None else B._stream(stream)
+        return B.raw_stream(self._index) if stream is None else B._stream(stream)
 
     def _mine(self, name: str, t: torch.Tensor, dtype=None, shape=None) -> torch.Tensor:
         """``t``, if the library may be given its address as it is."""
@@ -573,7 +573,10 @@ class SpindleKVPagedCache(_OnDevice):
     def __init__(self, n_layers: int, n_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int, n_pages: int, max_pages: int,
                  page_size: int = 64, fmt: str = "int8", device="cuda"):
         dev = _device_of(device)
-        codes = dict(dtype={"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[fmt], device=dev)
+        formats = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}
+        if fmt not in formats:
+            raise ValueError(f"unknown format {fmt!r}: one of {sorted(formats)}")
+        codes = dict(dtype=formats[fmt], device=dev)
         shape = (n_pages, n_kv_heads, page_size, head_dim)
         pool = {g + "_codes": torch.zeros(shape, **codes) for g in ("k", "v")}
         pool.update({g + "_scale": torch.zeros((n_pages, n_kv_heads, page_size // B.PAGED_BLOCK), dtype=torch.float32, device=dev) for g in ("k", "v")})
@@ -592,6 +595,7 @@ class SpindleKVPagedCache(_OnDevice):
         self.pool = B.PagePool(*(pool[k] for k in ("k_codes", "v_codes", "k_scale", "v_scale", "page_ref")))
         self.table = B.PageTable(pages, lens)
         self.device, self.pages, self.lens, self.page_ref = self.pool.device, pages, lens, pool["page_ref"]
+        self._index = self.device.index
         if pages.device != self.device:
             raise ValueError(f"pages on {pages.device}, the pool on {self.device}")
         self.n_layers, self.n_seqs, max_pages = pages.shape
@@ -620,10 +624,11 @@ class SpindleKVPagedCache(_OnDevice):
         return self._tables[layer]
 
     def _cache_rows(self, name: str, t: torch.Tensor, n_l: int, heads: int) -> B._Tensor:
-        shape = t.shape
-        if len(shape) != 5 or shape[:3] != (n_l, self.n_seqs, heads) or shape[4] != self.d or t.device != self.device or t.stride(4) != 1:
+        shape, strides = t.shape, t.stride()
+        if len(shape) != 5 or shape[0] != n_l or shape[1] != self.n_seqs or shape[2] != heads or shape[4] != self.d or strides[4] != 1 \
+                or t.device != self.device:
             raise ValueError(f"{name}: [{n_l}, {self.n_seqs}, {heads}, rows, {self.d}] on {self.device} expected, rows contiguous, got {list(shape)} on {t.device}")
-        return B._Tensor(t.data_ptr(), B._dtype_code(t), *t.stride()[:4])
+        return B._Tensor(t.data_ptr(), B._dtype_code(t), strides[0], strides[1], strides[2], strides[3])
 
     def resize(self, new_lens: Optional[torch.Tensor] = None, add: int = 0, stream=None) -> torch.Tensor:
         """Pages for new lengths (``[n_layers, n_seqs]`` int32 on the device, or every length plus ``add``).  Returns ``start``, where
@@ -670,10 +675,10 @@ class SpindleKVPagedCache(_OnDevice):
         if self._elsewhere():
             with torch.cuda.device(self.device):
                 return self.attend(q, out, max_len, scale, layer, stream)
-        table = self._rows_of(layer)
-        hq = q.shape[2] if self.Hq is None else self.Hq
-        qd = self._cache_rows("q", q, table.n_layers, hq)
+        table = self.table if layer is None else self._rows_of(layer)
         shape = q.shape
+        hq = shape[2] if self.Hq is None else self.Hq
+        qd = self._cache_rows("q", q, table.n_layers, hq)
         if out is None:
             held = self._out.get((shape, q.dtype))
             if held is None:
@@ -722,6 +727,7 @@ class SpindleKVBeamSelect(_OnDevice):
     def __init__(self, n_seqs: int, n_beams: int, vocab: int, n_out: Optional[int] = None, device="cuda"):
         self.n_seqs, self.n_beams, self.vocab, self.n_out = n_seqs, n_beams, vocab, n_beams if n_out is None else n_out
         self.device = dev = _device_of(device)
+        self._index = dev.index
         n = B.spindlekv_beam_workspace_bytes(n_seqs, n_beams, vocab, self.n_out)
         if n == 0:
             raise ValueError(f"unsupported beam search: {n_seqs} x {n_beams} beams, vocabulary {vocab}, {self.n_out} wanted")
