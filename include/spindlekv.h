@@ -431,7 +431,8 @@ spindlekv_status spindlekv_paged_append(const spindlekv_page_pool* pool, const s
  * Attention of the newest tokens over the paged cache.  The n_rows query rows of a sequence are its last n_rows tokens, already
  * appended: row r sees the tokens 0 .. lens - n_rows + r.  For KV head j and query head g of its group
  *     out_r = softmax_t( q_r . K_t * scale ) V_t ,
- * a row that sees no token gives zeros.  Keys are used as stored (rotated already, if the model rotates them).
+ * a row that sees no token gives zeros, and one whose query holds a NaN or an infinity gives NaN.  Keys are used as stored (rotated
+ * already, if the model rotates them).
  *   q, out    device, [layer][seq][q head][row][d], fp32 or bf16, both the same; may not overlap
  *   n_rows    1 .. 16;  n_q_heads / n_kv_heads <= 8
  *   max_len   the longest sequence, as far as the host knows: it only sizes the split over the device, any length is served
@@ -456,7 +457,7 @@ spindlekv_status spindlekv_paged_attend(const spindlekv_page_pool* pool, const s
  * total = score and all else at -infinity.
  *   logits      device [n_seqs * n_beams] rows of `vocab` elements, `row_stride` elements apart, fp32 or bf16, any alignment of
  *               the rows that the element type allows
- *   score       device [n_seqs * n_beams] fp32
+ *   score       device [n_seqs * n_beams] fp32; with n_out = n_beams it may be `out_score` itself
  *   finished    device [n_seqs * n_beams] bytes (0: not finished), or NULL
  *   out_score   device out [n_seqs][n_out] fp32: total
  *   out_parent  device out [n_seqs][n_out]: row seq * n_beams + w, i.e. with n_out = n_beams the parents of spindlekv_pages_fork

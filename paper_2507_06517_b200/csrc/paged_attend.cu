@@ -179,8 +179,8 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + ring_bytes<D, NT>());    // [kAttWarps][2]
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + kAttWarps * 2);   // a wait gave up; and one for the waits after that
   uint2* sq = reinterpret_cast<uint2*>(bars + kAttWarps * 2 + 2);             // [NP][NT][KS][32]
-  float* sfac = reinterpret_cast<float*>(sq + NP * NT * KS * 32);       // [COLS] score factor
-  float* scorr = sfac + COLS;                                           // [COLS] and what the codes' offset adds to it
+  float* sfac = reinterpret_cast<float*>(sq + NP * NT * KS * 32);       // [COLS] factor of a score, NaN for an infinite query
+  float* scorr = sfac + COLS;                                           // [COLS] and what the codes' offset adds to the product before
   float* sm_m = scorr + COLS;                                            // [kAttWarps][COLS]
   float* sm_l = sm_m + kAttWarps * COLS;                                // [kAttWarps][COLS]
   int* warp_sums = reinterpret_cast<int*>(sm_l + kAttWarps * COLS);     // [33]
@@ -405,8 +405,8 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
         for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
       }
       if (lane == 0) {
-        sfac[col] = kOffset ? p.scale * down * 16777216.f : p.scale * down;
-        scorr[col] = kOffset ? p.scale * down * sum * 128.f : 0.f;
+        sfac[col] = amax < CUDART_INF_F ? p.scale * down : CUDART_NAN_F;
+        scorr[col] = kOffset ? sum * 128.f : 0.f;
       }
     }
     __syncthreads();
@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
         lim[t][i] = col < ncols ? len - p.n_rows + 1 + (p.n_rows == 1 ? 0 : (col0 + col) % p.n_rows) : 0;
       }
     float o[KS][NT][4], m[NT][2], l[NT][2];
-    float vref = 0.f;                   // one piece: O is in units of this, a power of two above every scale so far
+    float vref = 0.f;                   // O is in units of this, a power of two above every scale so far
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       m[t][0] = m[t][1] = -CUDART_INF_F;
@@ -503,7 +503,7 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) sc[x][t][i] = kOffset ? fmaf(sc[x][t][i], fac[t][i & 1], -corr[t][i & 1]) * ks_b[x] : sc[x][t][i] * (ks_b[x] * fac[t][i & 1]);
+          for (int x = 0; x < 2; ++x) sc[x][t][i] = (kOffset ? fmaf(sc[x][t][i], 16777216.f, -corr[t][i & 1]) : sc[x][t][i]) * (ks_b[x] * fac[t][i & 1]);
       }
       if (masked) {
 #pragma unroll
@@ -553,25 +553,22 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
       phase ^= 1;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        // one piece: a block's scale joins its weights, relative to the largest scale so far, unless it is much smaller (the weights
-        // would run out of fp16's range) or the block is masked; then, and for two pieces always, it is applied to the block's product
-        float ratio = vs_b[x];
-        bool joined = false;
-        if constexpr (NP == 1) {
-          if (vs_b[x] > vref) {                      // (not for a NaN)
-            const float to = __uint_as_float((__float_as_uint(vs_b[x]) & 0x7F800000u) + 0x00800000u);   // the next power of two
-            const float f = vref / to;
-            vref = to;
+        // a block's scale counts relative to the largest so far (in fp32 itself, large values would overflow before they are divided by
+        // the weights' sum).  One piece: it joins the weights, unless it is much smaller (the weights would run out of fp16's range) or
+        // the block is masked; then, and for two pieces always, it is applied to the block's product
+        if (vs_b[x] > vref) {                        // (not for a NaN)
+          const float to = __uint_as_float(min((__float_as_uint(vs_b[x]) & 0x7F800000u) + 0x00800000u, 0x7F000000u));   // the next power of two
+          const float f = vref / to;
+          vref = to;
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
+          for (int k = 0; k < KS; ++k)
 #pragma unroll
-              for (int t = 0; t < NT; ++t)
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[k][t][i] *= f;
-          }
-          ratio = vs_b[x] == 0.f ? 0.f : vs_b[x] / vref;
-          joined = !masked && ratio >= 0.00390625f;
+              for (int i = 0; i < 4; ++i) o[k][t][i] *= f;
         }
+        const float ratio = vs_b[x] == 0.f ? 0.f : vs_b[x] / vref;
+        const bool joined = NP == 1 && !masked && ratio >= 0.00390625f;
         const float wfac = joined ? ratio * kAttPScale : kAttPScale;
         uint2 pf[NT][NP];
 #pragma unroll
@@ -683,7 +680,7 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
           sm_l[warp * COLS + 8 * t + 2 * c + i] = l[t][i];
         }
       }
-    const float unit = (NP == 1 ? vref : 1.f) / kAttPScale;
+    const float unit = vref / kAttPScale;
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll

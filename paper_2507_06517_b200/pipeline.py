@@ -187,6 +187,10 @@ class SpindleKVPass:
             raise ValueError("the cache does not have the evicting layers' shape")
         if K.shape[0] != self.n_deep:
             K, V = K[self.n_shallow:], V[self.n_shallow:]
+        for name, t in (("K", K), ("V", V)):               # before anything is given back
+            cache._cache_rows(name, t, self.n_deep, self.cfg.n_kv_heads)
+            if t.shape[3] != self.max_len:
+                raise ValueError(f"{name}: {self.max_len} rows expected, got {t.shape[3]}")
         cache.resize(cache.no_tokens, stream=stream)
         cache.resize(self.kept_lens, stream=stream)
         cache.append(K, V, idx=self.keep_idx, idx_seq=self.max_len, max_new=int(self.k_ctx_host[self.n_shallow:].max()) + self.cfg.window,

@@ -122,6 +122,20 @@ def test_same_bits_in_a_graph_and_beside_another_call():
     assert all(torch.equal(p, q) for p, q in zip((b.score, b.parent, b.token), other))
 
 
+def test_scores_go_on_in_place():
+    # the loop of a beam search: the scores of a step are the next step's, in the same buffer
+    from paper_2507_06517_b200.pipeline import SpindleKVBeamSelect
+    select, plain = SpindleKVBeamSelect(6, 8, 20000), SpindleKVBeamSelect(6, 8, 20000)
+    select.score.zero_()
+    score = torch.zeros(48, device="cuda")
+    for step in range(8):
+        x = logits_of(48, 20000, torch.float32, step)
+        select.run(x, select.score.view(-1))
+        want = plain.run(x, score)
+        assert all(torch.equal(p, q) for p, q in zip((select.score, select.parent, select.token), want))
+        score = want[0].view(-1).clone()
+
+
 def test_workspace_needs_no_preparation_and_serves_other_shapes():
     from paper_2507_06517_b200 import binding as B
     shapes = ((4, 8, 40000, 16), (1, 2, 300, 3), (2, 16, 9000, 32), (4, 8, 40000, 16))

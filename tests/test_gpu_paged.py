@@ -283,6 +283,22 @@ def test_attention_with_tiny_and_huge_queries(dtype, size):
     check_attention(c, r, q, c.attend(q, scale=0.1 / size), dtype, scale=0.1 / size)
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("of_q,of_k,of_v", [(122, -120, 0), (-118, 116, 0), (0, 0, 118), (0, 0, -116)])
+def test_attention_of_numbers_near_the_ends_of_fp32(fmt, dtype, of_q, of_k, of_v):
+    # the scores and the results are ordinary numbers (or at least fp32 ones): no product or sum on the way may leave fp32's range
+    c = make(1, 1, 4, 1, 128, 8, 4, 64, fmt)
+    r = ref_of(c)
+    start = r.resize(np.array([[200]]))
+    c.resize(lens_t([[200]]))
+    K, V = rows((1, 1, 1, 200, 128), dtype, 1, 0.3) * 2.0 ** of_k, rows((1, 1, 1, 200, 128), dtype, 2, 0.3) * 2.0 ** of_v
+    c.append(K, V)
+    r.append(start, f64(K), f64(V))
+    q = rows((1, 1, 4, 1, 128), dtype, 5, 0.2) * 2.0 ** of_q
+    check_attention(c, r, q, c.attend(q, scale=0.02), dtype, scale=0.02)
+
+
 def test_attention_of_poisoned_blocks_reaches_only_rows_that_see_them():
     c = make(1, 2, 4, 2, 64, 16, 3, 16, "int8")
     fill(c, [[32, 32]], "f32", spread=0.3)
@@ -571,3 +587,30 @@ def test_evicted_prompt_decodes_from_the_paged_cache():
         check_attention(c, r, q, torch.cat(outs), "bf16")
     assert c.status() == 0
     same_state(c, r)
+
+
+def test_storing_a_prompt_refuses_before_it_gives_anything_back():
+    from gpu_util import generate, make_config, stack_layers, torch_dtype
+    from paper_2507_06517_b200 import synth
+    from paper_2507_06517_b200.pipeline import SpindleKVPagedCache, SpindleKVPass
+    wl = synth.Workload("paged", 3, 1, 8, 2, 128, "bf16", 32, (300, 300), 40, (0.05, 0.3), 4, "recency", budget_tokens=100.0, seed=4)
+    host = generate(wl)
+    p = SpindleKVPass(make_config(wl), wl.seq_lens, torch_dtype(wl))
+    K, V = (stack_layers(wl, host, [0, 1, 2], x) for x in "KV")
+    p.run(K, V, stack_layers(wl, host, [1, 2], "Q"))
+    c = SpindleKVPagedCache(2, 2, 8, 2, 128, 64, 12, 32, "int8")
+    p.store_paged(K, V, c)
+    r = ref_of(c)
+    for k, v in ((K[:, :1], V[:, :1]), (K[..., :200, :], V[..., :200, :]), (K[:1], V[:1]), (K, V[:, :, :1]), (K, V.cpu())):
+        with pytest.raises(ValueError):
+            p.store_paged(k, v, c)
+    with pytest.raises(ValueError):
+        p.store_paged(K, V, SpindleKVPagedCache(2, 3, 8, 2, 128, 64, 12, 32, "int8"))
+    same_state(c, r)
+    # once more over what it holds: the same content again
+    p.store_paged(K, V, c)
+    again = ref_of(c)
+    assert c.status() == 0 and np.array_equal(again.lens, r.lens)
+    for l, s in r.units():
+        for g in "kv":
+            assert np.array_equal(again.rows(g, l, s)[0], r.rows(g, l, s)[0])
