@@ -11,8 +11,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libspindlekv.so")
 
 SOURCES = ["api.cu", "evict.cu", "codebook.cu", "compact.cu", "sim_tc.cu", "win_tc.cu", "extend.cu", "noalloc.cu", "decode.cu",
-           "pages.cu", "paged_append.cu", "paged_attend.cu", "beam.cu"]
-HEADERS = ["args.cuh", "common.cuh", "paged.cuh", "simt_tile.cuh", "sm100_ptx.cuh"]
+           "pages.cu", "paged_append.cu", "paged_attend.cu", "paged_attend_tiles.cu", "beam.cu"]
+HEADERS = ["args.cuh", "common.cuh", "paged.cuh", "paged_attend.cuh", "simt_tile.cuh", "sm100_ptx.cuh"]
 
 
 def _nvcc() -> str:

@@ -25,44 +25,18 @@
 //
 // Measured (device time): 16384 tokens, 8 KV heads, 32 query heads 15.0 us, of which the loop is 5 at the copy rate and the rest set-up
 // (4.5), join (4) and launch; 8 sequences of 10000 on average 45 us (4.6 TB/s); 4 x 16384 tokens with 4 to 8 columns per KV head 33 to 36 us
-// (4.1 TB/s), 16 columns 44, 32 columns 66 (two column tiles and more have the SM to themselves, eight warps: latency, issue slots 39%
-// busy), 128 columns 185 (four passes); fp32 queries 1.1 to 1.5 times that.
+// (4.1 TB/s), 16 columns 44, with fp32 queries 37 to 54; 32 columns of fp32 queries 88 (two column tiles and more have the SM to themselves, eight
+// warps: latency), 128 columns 290 (four passes).  More than 16 bf16 columns of 128 elements take paged_attend_tiles.cu.
 #include <algorithm>
 
-#include <cuda_fp16.h>
-#include <math_constants.h>
-
-#include "paged.cuh"
-#include "sm100_ptx.cuh"
+#include "paged_attend.cuh"
 
 namespace skv {
 
-bool make_code_map(CUtensorMap* map, const void* codes, int head_dim, int rows, int n_pages);
-
 constexpr int kAttThreads = 256;
 constexpr int kAttWarps = kAttThreads / 32;
-constexpr int kAttMaxRuns = 592;       // thread blocks of a call: four on each of 148 SMs
-constexpr int kAttMaxCols = 32;        // (query head, row) columns of a unit
-constexpr float kAttLazy = 8.f;        // how far a score may exceed the running reference, in powers of two
-constexpr float kAttPScale = 128.f;    // p <= 2^8 times this stays inside fp16
-
-struct AttendParams {
-  Pool pool;
-  Table table;
-  View q, out;
-  int hn, n_rows, cols;      // query heads per KV head, new rows, columns in all
-  int groups;                // column groups of a (layer, seq, KV head): its units
-  int units_per;             // heads * groups
-  int per_shift;             // log2 of the blocks of a page
-  float scale;               // softmax scale * log2(e)
-  int whole_units;           // 1: every run is one unit, nothing is left to join
-  float* part;               // [2 * kAttMaxRuns][kAttMaxCols][d]: O of the parts of units that several runs share
-  float2* stat;              // [2 * kAttMaxRuns][kAttMaxCols]: their m and sum
-  int2* lead;                // [runs] the unit that a run is the first to continue and its number of parts; unit -1: none, -2: a wait gave up
-  uint32_t* hdr;             // status block of the workspace
-  long long wait_cycles;     // bound of a wait
-};
-
+constexpr int kAttCols = 32;            // columns of a part, at most
+constexpr int kSetUp = 6;              // places of a unit's beginning and end, in pairs of blocks
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint2 b) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -74,84 +48,16 @@ __device__ __forceinline__ void mma16816_first(float (&d)[4], const uint32_t (&a
                : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y), "f"(0.f));
 }
-// 2^x, to two units in the last place of fp32; results below the smallest normal number are 0
-__device__ __forceinline__ float pow2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 __device__ __forceinline__ float2 unpack_half2(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
 
-// N = 2 or 4 neighbouring elements
-template <int N>
-__device__ __forceinline__ void load_elements(const float* p, float (&x)[N]) {
-  if constexpr (N == 4) {
-    const float4 v = *reinterpret_cast<const float4*>(p);
-    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-  } else {
-    const float2 v = *reinterpret_cast<const float2*>(p);
-    x[0] = v.x; x[1] = v.y;
-  }
-}
-template <int N>
-__device__ __forceinline__ void load_elements(const __nv_bfloat16* p, float (&x)[N]) {
-  uint32_t w[N / 2];
-  if constexpr (N == 4) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
-    w[0] = v.x; w[1] = v.y;
-  } else {
-    w[0] = *reinterpret_cast<const uint32_t*>(p);
-  }
-#pragma unroll
-  for (int i = 0; i < N / 2; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-  }
-}
-
-// two of the four codes in w (bytes 0, 1 with HI = 0; 2, 3 with HI = 1) as two fp16 numbers
-template <int FMT, int HI>
-__device__ __forceinline__ uint32_t codes_to_half2(uint32_t w) {
-  if constexpr (FMT == SPINDLEKV_PAGED_INT8) {
-    // w holds code + 128: 1024 + that is an fp16 number whose low byte it is
-    const uint32_t x = __byte_perm(w, 0x64646464u, HI ? 0x4342 : 0x4140);
-    const __half2 off = __half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));   // 1152
-    const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&x), off);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  } else {
-    uint32_t v;
-    if constexpr (HI) asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, hi; }" : "=r"(v) : "r"(w));
-    else asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, lo; }" : "=r"(v) : "r"(w));
-    return v;
-  }
-}
 // the same, offset int8 codes as subnormal numbers
 template <int HI>
 __device__ __forceinline__ uint32_t offset_to_half2(uint32_t w) { return __byte_perm(w, 0u, HI ? 0x4342 : 0x4140); }
-template <int FMT>
-__device__ __forceinline__ uint32_t prepare_codes(uint32_t w) { return FMT == SPINDLEKV_PAGED_INT8 ? w ^ 0x80808080u : w; }
-// E4M3 codes of slots behind the last token may be its NaN patterns, whose product with a weight of 0 is not 0: a bit less, and
-// they are numbers
-__device__ __forceinline__ uint32_t without_nan(uint32_t w) { return w ^ ((((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u); }
-
-// The line: unit (ls, head, group) takes kSetUp places, which stand for looking up its pages, reading its queries and joining its
-// warps, and then one for each pair of blocks; all units of a (layer, seq) lie side by side.  Without those places a run with the ends
-// of two or three units in it finishes last.
-constexpr int kSetUp = 6;
-__device__ __forceinline__ int places_of(const AttendParams& p, int ls) {
-  const int len = unit_len(p.table, p.pool, ls);
-  return len ? (len + 2 * kPagedBlock - 1) / (2 * kPagedBlock) + kSetUp : 0;
-}
-
 template <int D, int NT>
 __host__ __device__ constexpr size_t ring_bytes() {   // the warps' results take the ring's place when a segment ends
   const size_t ring = (size_t)kAttWarps * 4 * kPagedBlock * D, results = (size_t)kAttWarps * 8 * NT * (D + 4) * 4;
@@ -209,78 +115,25 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
   uint8_t* ring = smem + warp * 2 * kSlot;   // K of a pair, V of a pair
   uint64_t* full = bars + warp * 2;          // the keys, the values have arrived
   uint32_t phase = 0;
-  // places of a (layer, seq) per unit, summed
-  int total = 0;
-  if (n_ls <= 32) {      // every warp for itself, the same values
-    const int n = lane < n_ls ? places_of(p, lane) : 0;
-    int upto = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int below = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += below;
-    }
-    if (lane < n_ls) prefix[lane] = upto - n;
-    total = __shfl_sync(0xffffffffu, upto, 31);
-    if (lane == 0) prefix[n_ls] = total;
-    __syncwarp();
-  } else {
-    for (int base = 0; base < n_ls; base += kAttThreads) {
-      const int ls = base + tid;
-      const int n = ls < n_ls ? places_of(p, ls) : 0;
-      int sum;
-      const int at = block_exclusive_scan(n, warp_sums, sum);
-      if (ls < n_ls) prefix[ls] = total + at;
-      total += sum;
-    }
-    if (tid == 0) prefix[n_ls] = total;
-    __syncthreads();
-  }
-  // run i has the places from all * i / runs (rounded down) on; runs without any are the last ones
-  const int all = total * p.units_per, runs = min((int)gridDim.x, max(all, 1));
-  const int share = all / runs, left = all - share * runs;
-  const float per_runs = 1.f / (float)runs, runs_per_place = (float)runs / (float)max(all, 1);
-  // left * i < 2^20 and runs < 2^10: the product is off by less than half of 1 / runs, so the quotient is exact
-  auto run_start = [&](int i) { return share * i + (int)(((float)(left * i) + 0.5f) * per_runs); };
-  auto run_of = [&](int place) {
-    int i = (int)((float)place * runs_per_place);
-    while (run_start(i) > place) --i;
-    while (run_start(i + 1) <= place) ++i;
-    return i;
-  };
+  const int total = line_prefix<2 * kPagedBlock, kSetUp>(p, prefix, warp_sums);
+  const Runs cut(total * p.units_per, (int)gridDim.x);
   int at, stop;
   if (p.whole_units) {
     const int e = blockIdx.x / p.units_per, u = blockIdx.x - e * p.units_per, places = prefix[e + 1] - prefix[e];
     at = prefix[e] * p.units_per + u * places;
     stop = at + places;
   } else {
-    at = run_start(blockIdx.x);
-    stop = (int)blockIdx.x < runs ? run_start(blockIdx.x + 1) : at;
+    at = cut.start(blockIdx.x);
+    stop = (int)blockIdx.x < cut.runs ? cut.start(blockIdx.x + 1) : at;
   }
   if (p.whole_units) {
     if (tid == 0 && blockIdx.x == 0) p.hdr[kHdrStatus] = SPINDLEKV_OK;
   } else if (tid == 0) {
     p.lead[blockIdx.x] = make_int2(-1, 0);
   }
-  // sequences without tokens give zeros
-  for (int e = blockIdx.x; e < n_ls; e += gridDim.x)
-    if (prefix[e + 1] == prefix[e]) {
-      const int layer = e / p.table.n_seqs, seq = e - layer * p.table.n_seqs, per_head = p.n_rows * D;
-      T* dst = reinterpret_cast<T*>(const_cast<void*>(p.out.ptr)) + (int64_t)layer * p.out.sl + (int64_t)seq * p.out.ss;
-      for (int i = tid; i < p.pool.heads * p.hn * per_head; i += kAttThreads) {
-        const int h = i / per_head, r = (i - h * per_head) / D, d = i % D;
-        dst[(int64_t)h * p.out.sh + (int64_t)r * p.out.st + d] = T(0.f);
-      }
-    }
+  zero_empty<T, D>(p, prefix);
   if (at >= stop) return;
-  int ls;
-  {   // the (layer, seq) that holds place `at`
-    int lo = 0, hi = n_ls - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (prefix[mid] * p.units_per <= at) lo = mid; else hi = mid - 1;
-    }
-    ls = lo;
-  }
+  int ls = unit_at(p, prefix, at);
   while (at < stop) {
     while (prefix[ls + 1] == prefix[ls] || prefix[ls + 1] * p.units_per <= at) ++ls;
     const int places = prefix[ls + 1] - prefix[ls], nb = places - kSetUp;
@@ -294,8 +147,8 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
     const int head = p.groups == 1 ? uh : uh / p.groups, group = uh - head * p.groups;
     if (tid == 0 && b0 > 0 && !p.whole_units) {
       // a unit's parts: of the run with its first pair, of the next one (which leads the join), and on to the one with its last
-      const int first = run_of(begin + kSetUp);
-      if (first == (int)blockIdx.x - 1) p.lead[blockIdx.x] = make_int2(ls * p.units_per + uh, run_of(begin + places - 1) - first + 1);
+      const int first = cut.of(begin + kSetUp);
+      if (first == (int)blockIdx.x - 1) p.lead[blockIdx.x] = make_int2(ls * p.units_per + uh, cut.of(begin + places - 1) - first + 1);
     }
     const int layer = ls / p.table.n_seqs, seq = ls - layer * p.table.n_seqs;
     const int len = unit_len(p.table, p.pool, ls);
@@ -697,7 +550,7 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
     __syncthreads();
     const bool whole = b0 == 0 && b1 == nb;
     // what is left for the join: a unit that began in an earlier run is this run's first, one that begins here and goes on its last
-    const int64_t place = (int64_t)(2 * blockIdx.x + (b0 == 0 ? 1 : 0)) * kAttMaxCols;
+    const int64_t place = (int64_t)(2 * blockIdx.x + (b0 == 0 ? 1 : 0)) * p.part_cols;
     for (int i = tid; i < ncols * (D / 4); i += kAttThreads) {
       const int col = i / (D / 4), d = (i - col * (D / 4)) * 4;
       float top = -CUDART_INF_F;
@@ -735,15 +588,16 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
   }
 }
 
-// Joins the parts of a unit: block (j, x) takes four columns of the unit that run j is the first to continue.  Four warps to a
-// column, each with every fourth run; the order of the sums is the order of the runs.
+// Joins the parts of a unit: block (j, x) takes 16 / TURNS columns of the unit that run j is the first to continue.  TURNS warps to a
+// column, each with every TURNS-th run; the order of the sums is the order of the runs.  Four for few columns, whose units are cut into many
+// parts; one for more than 16, of which there are many and in few parts.
 constexpr int kJoinThreads = 512;
 
-template <typename T, int D>
+template <typename T, int D, int TURNS>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(AttendParams p, int cols_per_unit) {
-  constexpr int E = D / 32;
-  __shared__ float so[4][4][D];
-  __shared__ float sden[4];
+  constexpr int E = D / 32, COLS = kJoinThreads / 32 / TURNS, PASS = 16 * TURNS, ST = (PASS + 31) / 32;
+  __shared__ float so[TURNS][COLS][D];
+  __shared__ float sden[COLS];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (blockIdx.x == 0 && blockIdx.y == 0) {
@@ -759,24 +613,26 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(AttendParams p
   const int ls = unit / p.units_per, uh = unit - ls * p.units_per, head = uh / p.groups, group = uh - head * p.groups;
   const int layer = ls / p.table.n_seqs, seq = ls - layer * p.table.n_seqs;
   const int col0 = group * cols_per_unit, ncols = min(cols_per_unit, p.cols - col0);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, which = warp & 3, turn = warp >> 2;
-  const int col = blockIdx.y * 4 + which;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, which = warp % COLS, turn = warp / COLS;
+  const int col = blockIdx.y * COLS + which;
   const bool mine = col < ncols;
-  auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * (run - 1) + 1 : 2 * (run - 1 + i)) * kAttMaxCols + col; };
+  auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * (run - 1) + 1 : 2 * (run - 1 + i)) * p.part_cols + col; };
   if (mine) {
     float num[E], den = 0.f, top = -CUDART_INF_F;
 #pragma unroll
     for (int e = 0; e < E; ++e) num[e] = 0.f;
-    // 64 parts at a time, 16 to a warp, all of them asked for at once; the weights are formed meanwhile
-    for (int i0 = 0; i0 < n; i0 += 64) {
+    // PASS parts at a time, 16 to a warp, all of them asked for at once; the weights are formed meanwhile
+    for (int i0 = 0; i0 < n; i0 += PASS) {
       float v[16][E];
 #pragma unroll
       for (int k = 0; k < 16; ++k)
-        if (i0 + 4 * k + turn < n) load_elements<E>(p.part + slot(i0 + 4 * k + turn) * D + lane * E, v[k]);
-      float2 st[2];
+        if (i0 + TURNS * k + turn < n) load_elements<E>(p.part + slot(i0 + TURNS * k + turn) * D + lane * E, v[k]);
+      float2 st[ST];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) st[h] = i0 + 32 * h + lane < n ? p.stat[slot(i0 + 32 * h + lane)] : make_float2(-CUDART_INF_F, 0.f);
-      float high = fmaxf(top, fmaxf(st[0].x, st[1].x));
+      for (int h = 0; h < ST; ++h) st[h] = 32 * h + lane < PASS && i0 + 32 * h + lane < n ? p.stat[slot(i0 + 32 * h + lane)] : make_float2(-CUDART_INF_F, 0.f);
+      float high = top;
+#pragma unroll
+      for (int h = 0; h < ST; ++h) high = fmaxf(high, st[h].x);
 #pragma unroll
       for (int o = 16; o >= 1; o >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
       const float old = top == high ? 1.f : pow2(top - high);
@@ -784,16 +640,16 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(AttendParams p
       den *= old;
 #pragma unroll
       for (int e = 0; e < E; ++e) num[e] *= old;
-      float f[2];
+      float f[ST];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < ST; ++h) {
         f[h] = st[h].x == top ? 1.f : pow2(st[h].x - top);
         den = fmaf(f[h], st[h].y, den);
       }
 #pragma unroll
       for (int k = 0; k < 16; ++k) {
-        const float w = __shfl_sync(0xffffffffu, f[k >> 3], (4 * k + turn) & 31);
-        if (i0 + 4 * k + turn < n) {
+        const float w = __shfl_sync(0xffffffffu, f[TURNS * k / 32], (TURNS * k + turn) & 31);
+        if (i0 + TURNS * k + turn < n) {
 #pragma unroll
           for (int e = 0; e < E; ++e) num[e] = fmaf(w, v[k][e], num[e]);
         }
@@ -814,7 +670,9 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(AttendParams p
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const int d = e * 32 + lane;
-    const float sum = so[0][which][d] + so[1][which][d] + so[2][which][d] + so[3][which][d];
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) sum += so[i][which][d];
     dst[d] = T(den == 0.f ? 0.f : sum / den);
   }
 }
@@ -834,10 +692,25 @@ static int resident_blocks(K kernel, size_t smem, int (&cache)[kMaxDevices], int
 
 static int column_tiles(int cols) { return cols <= 8 ? 1 : cols <= 16 ? 2 : 4; }
 
-constexpr size_t kPartRows = (size_t)2 * kAttMaxRuns * kAttMaxCols;
 
 size_t paged_workspace_bytes(const spindlekv_page_pool& pool) {
-  return kHeaderBytes + kPartRows * (pool.head_dim * sizeof(float) + sizeof(float2)) + kAttMaxRuns * sizeof(int2);
+  return kHeaderBytes + kAttPartRows * (pool.head_dim * sizeof(float) + sizeof(float2)) + kAttMaxRuns * sizeof(int2);
+}
+
+template <typename T, int D>
+static spindlekv_status launch_join(const AttendParams& p, int runs, int cols_per_unit, cudaStream_t st) {
+  const int cols = std::min(cols_per_unit, p.cols), per_block = cols <= 16 ? 4 : 16;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(runs, ceil_div(cols, per_block));
+  cfg.blockDim = dim3(kJoinThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  LaunchScope ls(KC_PAGED_ATTEND, st);
+  return cudaLaunchKernelEx(&cfg, per_block == 4 ? paged_join_kernel<T, D, 4> : paged_join_kernel<T, D, 1>, p, cols_per_unit) == cudaSuccess ? SPINDLEKV_OK : SPINDLEKV_CUDA;
 }
 
 template <typename T, int FMT, int D, int NT>
@@ -879,18 +752,21 @@ static spindlekv_status launch_attend(AttendParams& p, const CUtensorMap& kmap, 
     if (cudaLaunchKernelEx(&cfg, kernel, kmap, vmap, p) != cudaSuccess) return SPINDLEKV_CUDA;
   }
   if (p.whole_units) return SPINDLEKV_OK;
-  cfg.gridDim = dim3(runs, ceil_div(std::min(COLS, p.cols), 4));
-  cfg.blockDim = dim3(kJoinThreads);
-  cfg.dynamicSmemBytes = 0;
-  LaunchScope ls(KC_PAGED_ATTEND, st);
-  return cudaLaunchKernelEx(&cfg, paged_join_kernel<T, D>, p, COLS) == cudaSuccess ? SPINDLEKV_OK : SPINDLEKV_CUDA;
+  return launch_join<T, D>(p, runs, COLS, st);
 }
 
 template <typename T, int FMT, int D>
 static spindlekv_status launch_columns(AttendParams& p, int max_len, cudaStream_t st) {
+  if constexpr (sizeof(T) == 2 && D == 128) {
+    int runs = 0;
+    spindlekv_status status = SPINDLEKV_OK;
+    if (paged_attend_tiles(p, FMT, max_len, st, &runs, &status)) return status == SPINDLEKV_OK ? launch_join<T, D>(p, runs, p.part_cols, st) : status;
+  }
   CUtensorMap kmap, vmap;
   const int rows = p.pool.heads * p.pool.ps;
-  if (!make_code_map(&kmap, p.pool.kc, D, rows, p.pool.n_pages) || !make_code_map(&vmap, p.pool.vc, D, rows, p.pool.n_pages)) return SPINDLEKV_CUDA;
+  if (!make_code_map(&kmap, p.pool.kc, D, rows, p.pool.n_pages, kPagedBlock) || !make_code_map(&vmap, p.pool.vc, D, rows, p.pool.n_pages, kPagedBlock))
+    return SPINDLEKV_CUDA;
+  p.part_cols = kAttCols;
   const int nt = column_tiles(p.cols);
   p.groups = ceil_div(p.cols, 8 * nt);
   p.units_per = p.pool.heads * p.groups;
@@ -923,8 +799,8 @@ spindlekv_status paged_attend_impl(const spindlekv_page_pool& pool, const spindl
   p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kHeaderBytes);
   p.hdr = static_cast<uint32_t*>(ws);
   p.wait_cycles = current_tuning().mbar_wait_cycles;
-  p.stat = reinterpret_cast<float2*>(p.part + kPartRows * pool.head_dim);
-  p.lead = reinterpret_cast<int2*>(p.stat + kPartRows);
+  p.stat = reinterpret_cast<float2*>(p.part + kAttPartRows * pool.head_dim);
+  p.lead = reinterpret_cast<int2*>(p.stat + kAttPartRows);
   return q.dtype == SPINDLEKV_BF16 ? launch_format<__nv_bfloat16>(p, pool.format, max_len, st) : launch_format<float>(p, pool.format, max_len, st);
 }
 

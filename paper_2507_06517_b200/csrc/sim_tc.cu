@@ -733,13 +733,13 @@ bool make_query_map_bf16(CUtensorMap* map, const spindlekv_tensor& q, const spin
   return r == CUDA_SUCCESS;
 }
 
-// 8-bit codes [page][row][d] of a paged cache -> 3-D map (d, row, page), box d x 16 rows, swizzle as wide as a row
-bool make_code_map(CUtensorMap* map, const void* codes, int head_dim, int rows, int n_pages) {
+// 8-bit codes [page][row][d] of a paged cache -> 3-D map (d, row, page), box d x box_rows, swizzle as wide as a row
+bool make_code_map(CUtensorMap* map, const void* codes, int head_dim, int rows, int n_pages, int box_rows) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)rows, (cuuint64_t)n_pages};
   cuuint64_t strides[2] = {(cuuint64_t)head_dim, (cuuint64_t)head_dim * rows};
-  cuuint32_t box[3] = {(cuuint32_t)head_dim, SPINDLEKV_PAGED_BLOCK, 1};
+  cuuint32_t box[3] = {(cuuint32_t)head_dim, (cuuint32_t)box_rows, 1};
   cuuint32_t estr[3] = {1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,

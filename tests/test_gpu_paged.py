@@ -299,6 +299,92 @@ def test_attention_of_numbers_near_the_ends_of_fp32(fmt, dtype, of_q, of_k, of_v
     check_attention(c, r, q, c.attend(q, scale=0.02), dtype, scale=0.02)
 
 
+@pytest.mark.parametrize("fmt,ps", [("int8", 16), ("e4m3", 32), ("int8", 64), ("e4m3", 128)])
+@pytest.mark.parametrize("h,hn,n_rows", [(2, 6, 3), (1, 8, 4), (2, 7, 6), (1, 8, 8), (1, 7, 10), (2, 8, 16)])
+def test_attention_of_many_columns(fmt, ps, h, hn, n_rows):
+    # 18 to 128 columns, lengths around a tile's end and over many tiles, more units than runs and the reverse, whatever the hint
+    tiles = [[0, 1, 127, 128, 129, 511], [513, 5, 3000, 16, 640, 1100]]
+    c = make(2, 6, hn * h, h, 128, 6400 // ps + 12, 3200 // ps, ps, fmt)
+    r = fill(c, tiles, spread=0.3)
+    q = rows((2, 6, hn * h, n_rows, 128), "bf16", 77, 0.2)
+    first = None
+    for max_len in (600, 3000, 100000):
+        out = torch.full_like(q, 7.0)
+        c.attend(q, out=out, max_len=max_len)
+        check_attention(c, r, q, out, "bf16")
+        assert c.status() == 0
+        again = torch.full_like(q, 7.0)
+        c.attend(q, out=again, max_len=max_len)
+        assert torch.equal(out, again)
+        first = out if first is None else first
+    seen = r.lens[:, :, None] - n_rows + 1 + np.arange(n_rows)
+    assert (f64(first).transpose(0, 1, 3, 2, 4)[seen <= 0] == 0).all()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("rising", [False, True])
+def test_attention_of_many_columns_moves_its_references(fmt, rising):
+    # scores and values whose sizes rise, or fall, from block to block: every tile moves the running maximum, and the unit of the sums
+    c = make(1, 1, 8, 1, 128, 40, 36, 64, fmt)
+    n = 2000
+    r = ref_of(c)
+    start = r.resize(np.array([[n]]))
+    c.resize(lens_t([[n]]))
+    K, V = rows((1, 1, 1, n, 128), "bf16", 1, 0.1), rows((1, 1, 1, n, 128), "bf16", 2, 0.1)
+    size = torch.arange(n, device="cuda").div(64, rounding_mode="floor").float()
+    size = size if rising else size.max() - size
+    K = (K * 0.1 * size[:, None]).to(K.dtype)
+    V = (V * torch.exp2(size / 4)[:, None]).to(V.dtype)
+    c.append(K, V)
+    r.append(start, f64(K), f64(V))
+    q = rows((1, 1, 8, 4, 128), "bf16", 5, 0.2)
+    check_attention(c, r, q, c.attend(q), "bf16")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("of_q,of_k,of_v", [(122, -120, 0), (-118, 116, 0), (0, 0, 118), (0, 0, -116)])
+def test_attention_of_many_columns_near_the_ends_of_fp32(fmt, of_q, of_k, of_v):
+    c = make(1, 1, 8, 1, 128, 24, 12, 64, fmt)
+    r = ref_of(c)
+    start = r.resize(np.array([[700]]))
+    c.resize(lens_t([[700]]))
+    K, V = rows((1, 1, 1, 700, 128), "bf16", 1, 0.3) * 2.0 ** of_k, rows((1, 1, 1, 700, 128), "bf16", 2, 0.3) * 2.0 ** of_v
+    c.append(K, V)
+    r.append(start, f64(K), f64(V))
+    q = rows((1, 1, 8, 5, 128), "bf16", 5, 0.2) * 2.0 ** of_q
+    check_attention(c, r, q, c.attend(q, scale=0.02), "bf16", scale=0.02)
+
+
+def test_attention_of_many_columns_with_nan_infinities_and_missing_pages():
+    c = make(1, 3, 16, 2, 128, 100, 40, 32, "e4m3")
+    fill(c, [[900, 1001, 32]], "f32", spread=0.3)
+    r = ref_of(c)
+    start = r.resize(np.array([[901, 1002, 33]]))
+    c.resize(lens_t([[901, 1002, 33]]))
+    K, V = rows((1, 3, 2, 1, 128), "f32", 1), rows((1, 3, 2, 1, 128), "f32", 2)
+    K[0, 2, 1] = float("nan")
+    V[0, 0, 0] = float("inf")
+    c.append(K, V)
+    q = rows((1, 3, 16, 3, 128), "bf16", 3)
+    q[0, 1, 3, 1, 7] = float("nan")
+    q[0, 1, 9, 0, 100] = float("-inf")
+    c.pages[0, 1, 5] = -1
+    c.pages[0, 1, 6] = 100
+    got = f64(c.attend(q))
+    nan = np.isnan(got).all(-1)
+    want = np.zeros((1, 3, 16, 3), bool)
+    want[0, 2, 8:, 2] = want[0, 0, :8, 2] = True           # the last row alone sees a new token: blocks 56 and 2 begin with it
+    want[0, 1, 3, 1] = want[0, 1, 9, 0] = True
+    # sequence 0's new token is the 901st, in a block with four earlier ones: the rows that see these are lost as well
+    want[0, 0, :8] = True
+    assert np.array_equal(nan, want) and np.isfinite(got[~want]).all()
+    r.append(start, np.nan_to_num(f64(K)), np.where(np.isinf(f64(V)), 0, f64(V)))
+    r.pages[0, 1, 5:7] = -1
+    clean, mag, _ = r.attend(np.nan_to_num(f64(q), neginf=0.0))
+    # half a step of bf16, and less than that of the sum of weight * |value| for the weights
+    assert (np.abs(got - clean)[~want] <= (2.0 ** -8 * np.abs(clean) + 2.0 ** -8 * mag)[~want]).all()
+
+
 def test_attention_of_poisoned_blocks_reaches_only_rows_that_see_them():
     c = make(1, 2, 4, 2, 64, 16, 3, 16, "int8")
     fill(c, [[32, 32]], "f32", spread=0.3)
