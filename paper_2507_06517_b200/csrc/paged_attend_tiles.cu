@@ -10,7 +10,7 @@
 // running reference that moves when a score exceeds it by 8, block scales of V joined with the weights (relative to a power of two above
 // all scales so far) before their one rounding to fp16; m, the sums and O are fp32.
 //
-// Roles (one block per SM).  One warp asks for the codes (TMA, a page at a time, a ring of K and V tiles); four or eight widen them; two issue
+// Roles (one block per SM).  One warp asks for the codes (TMA, a page at a time, a ring of K and V tiles); four widen them; two issue
 // the products, one each, the keys' two tiles ahead of the values'; sixteen turn scores into weights: a thread has a token and a quarter of
 // the columns, so that only what happens rarely, a new reference, needs the other tokens.  A tile's scores are read before the weights of
 // the tile before are given away, because such a read waits for the products that are under way.
@@ -18,11 +18,12 @@
 // Split.  The line of all units' tiles is cut into equal runs, one per SM, and the parts of a unit are joined as for few columns.
 //
 // Measured (4 sequences x 16384 tokens, 8 KV heads, int8; beside it the kernel for few columns, which reads the codes once per 32 columns): 32
-// columns 53 us (64), 64 columns 77 (101), 128 columns 133 (179); 8 x 25000 tokens, 32 columns 98 us (117), i.e. 3.3 TB/s.  Bound by the
-// weights' warps: of 2400 cycles per tile at 32 columns (memory would allow 1450) they wait for 300; issue slots are 63% busy, the products
-// take 37 cycles per instruction (300 of 8 steps), widening 600 per tile of codes.
-// Tried: fewer and wider warps for the weights (eight: 60 us at 32 columns), two groups of them that take turns at the tiles (73), one thread
-// issuing both products (65), a box of 16 tokens per copy (65: 180 cycles per copy instruction).
+// columns 48 us (64), 64 columns 67 (101), 128 columns 117 (179); 6 x 26000 tokens, 32 columns 95 us (117), i.e. 3.4 TB/s.  Bound by the
+// weights' warps: of 2000 cycles per tile at 32 columns (memory would allow 1450) they wait for 500; issue slots are 63% busy, the products
+// take 45 cycles per instruction (360 of 8 steps), widening 600 per tile of codes.  A unit's beginning and end are 7 us, its first tile among them.
+// Tried: fewer and wider warps for the weights (eight: 60 us at 32 columns), two groups of them that take turns at the tiles (73), two tiles at a
+// time (53, as one at a time then), eight widening warps (50), one thread issuing both products (65), a box of 16 tokens per copy (180 cycles per
+// copy instruction).
 #include <algorithm>
 
 #include "paged_attend.cuh"
@@ -30,8 +31,9 @@
 namespace skv {
 
 constexpr int kTile = 128;             // tokens
-constexpr int kTileSetUp = 2;          // places of a unit's beginning and end
-constexpr int kSoftWarps = 16, kAskWarp = kSoftWarps, kScoreWarp = kAskWarp + 1, kValueWarp = kScoreWarp + 1, kWidenFirst = kValueWarp + 1;
+constexpr int kTileSetUp = 6;          // places of a unit's beginning and end, which take 7 us (2: 54 us for 4 x 16384 tokens and 32 columns, 4: 52.6, 6: 51.8)
+constexpr int kSoftWarps = 16, kWidenWarps = 4, kAskWarp = kSoftWarps, kScoreWarp = kAskWarp + 1, kValueWarp = kScoreWarp + 1, kWidenFirst = kValueWarp + 1;
+constexpr int kTilesThreads = 32 * (kWidenFirst + kWidenWarps);
 constexpr int kRawBytes = kTile * 128, kWideBytes = 2 * kRawBytes;
 
 __device__ __forceinline__ void warps_meet(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
@@ -41,10 +43,23 @@ __device__ __forceinline__ bool warps_any(int id, int threads, bool x) {
                : "=r"(y) : "r"((uint32_t)x), "r"(id), "r"(threads) : "memory");
   return y != 0;
 }
+// Eight values per lane -> each of the eight reduced over the warp's lanes; lane i gets the one of number reduced_by(i).  Half of the values
+// change hands at each of the first three steps: 9 shuffles in place of 40.
+__device__ __forceinline__ int reduced_by(int lane) { return (lane >> 2 & 4) | (lane >> 2 & 2) | (lane >> 2 & 1); }
+template <typename Op>
+__device__ __forceinline__ float reduce_eight(const float* v, int lane, Op op) {
+  float a[4], b[2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a[i] = op(lane & 16 ? v[i + 4] : v[i], __shfl_xor_sync(0xffffffffu, lane & 16 ? v[i] : v[i + 4], 16));
+#pragma unroll
+  for (int i = 0; i < 2; ++i) b[i] = op(lane & 8 ? a[i + 2] : a[i], __shfl_xor_sync(0xffffffffu, lane & 8 ? a[i] : a[i + 2], 8));
+  float c = op(lane & 4 ? b[1] : b[0], __shfl_xor_sync(0xffffffffu, lane & 4 ? b[0] : b[1], 4));
+  c = op(c, __shfl_xor_sync(0xffffffffu, c, 2));
+  return op(c, __shfl_xor_sync(0xffffffffu, c, 1));
+}
+
 template <int N>
 struct TilesSmem {
-  static constexpr int kWidenWarps = N == 32 ? 8 : 4;                       // (more would leave the others too few registers)
-  static constexpr int kThreads = 32 * (kWidenFirst + kWidenWarps);
   static constexpr int kK = 2, kV = N == 32 ? 2 : 1;                        // tiles of keys and of values in fp16, 32 KB each
   static constexpr int kRaw = N == 128 ? 3 : 4;                             // tiles of codes, 16 KB each
   static constexpr int kP = N == 128 ? 1 : 2;                               // buffers of weights; 32 columns each share rows of 64
@@ -67,7 +82,7 @@ static_assert(TilesSmem<32>::fm % 16 == 0 && TilesSmem<64>::fm % 16 == 0 && Tile
               TilesSmem<64>::bars % 1024 == 0 && TilesSmem<128>::bars % 1024 == 0, "alignment of what is read in 16 bytes, and of the tiles");
 
 template <int FMT, int N>
-__global__ void __launch_bounds__(TilesSmem<N>::kThreads, 1) paged_attend_tiles_kernel(const __grid_constant__ CUtensorMap kmap,
+__global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(const __grid_constant__ CUtensorMap kmap,
                                                                               const __grid_constant__ CUtensorMap vmap, AttendParams p) {
   using S = TilesSmem<N>;
   using T = __nv_bfloat16;
@@ -93,9 +108,9 @@ __global__ void __launch_bounds__(TilesSmem<N>::kThreads, 1) paged_attend_tiles_
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (tid == 0) {
-    for (int i = 0; i < RAW; ++i) { ptx::mbar_init(raw_full + i, 1); ptx::mbar_init(raw_empty + i, S::kWidenWarps); }
-    for (int i = 0; i < S::kK; ++i) { ptx::mbar_init(k_full + i, S::kWidenWarps); ptx::mbar_init(k_empty + i, 1); }
-    for (int i = 0; i < S::kV; ++i) { ptx::mbar_init(v_full + i, S::kWidenWarps); ptx::mbar_init(v_empty + i, 1); }
+    for (int i = 0; i < RAW; ++i) { ptx::mbar_init(raw_full + i, 1); ptx::mbar_init(raw_empty + i, kWidenWarps); }
+    for (int i = 0; i < S::kK; ++i) { ptx::mbar_init(k_full + i, kWidenWarps); ptx::mbar_init(k_empty + i, 1); }
+    for (int i = 0; i < S::kV; ++i) { ptx::mbar_init(v_full + i, kWidenWarps); ptx::mbar_init(v_empty + i, 1); }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(s_full + i, 1);
       ptx::mbar_init(s_empty + i, kSoftWarps);
@@ -201,7 +216,7 @@ __global__ void __launch_bounds__(TilesSmem<N>::kThreads, 1) paged_attend_tiles_
     // ---- codes -> fp16, in rows of 64 elements (two halves of d), 16-byte pieces swizzled as the products expect them.  Eight lanes take four
     // neighbouring pieces of the rows r and r ^ 5, which swizzling puts into different banks on both sides ----
     // this lane's row of eight, its first of four rows eight apart; piece: of the lower half of a row of codes, in bytes
-    const int r = (lane >> 3) ^ ((lane >> 2) & 1) * 5, first_row = (warp - kWidenFirst) * (kTile / S::kWidenWarps) * 128 + r * 128, xor_r = r << 4, piece = (lane & 3) << 4;
+    const int r = (lane >> 3) ^ ((lane >> 2) & 1) * 5, first_row = (warp - kWidenFirst) * (kTile / kWidenWarps) * 128 + r * 128, xor_r = r << 4, piece = (lane & 3) << 4;
     int item = 0, done[2] = {0, 0};
     segments([&](const Segment& g) {
       const int len = unit_len(p.table, p.pool, g.ls);
@@ -218,7 +233,7 @@ __global__ void __launch_bounds__(TilesSmem<N>::kThreads, 1) paged_attend_tiles_
             const bool clean = FMT == SPINDLEKV_PAGED_E4M3 && v && (holes[rs] || (n + 1) * kTile > len);
             const uint8_t* from = smem + S::raw + rs * kRawBytes + first_row;
             uint8_t* to = smem + S::wide + (ws + (v ? S::kK : 0)) * kWideBytes + first_row;
-            constexpr int kPieces = 32 / S::kWidenWarps;
+            constexpr int kPieces = 32 / kWidenWarps;
             uint4 raw[kPieces];
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) raw[j] = *reinterpret_cast<const uint4*>(from + (j >> 1) * 1024 + ((piece ^ ((j & 1) << 6)) ^ xor_r));
@@ -327,28 +342,37 @@ __global__ void __launch_bounds__(TilesSmem<N>::kThreads, 1) paged_attend_tiles_
       };
       const int blk0 = g.b0 * 8 + lane;            // this lane knows the scales of a block of four tiles, and looks up the next four's
       int page_next = page_of(g, blk0, len);
-      warps_meet(1 + kSoftWarps / 4, kSoftWarps * 32);              // nobody reads the columns' numbers of the segment before any more
-      // queries: a warp takes columns warp, warp + 8, ...; a lane four elements
-      for (int col = warp; col < N; col += kSoftWarps) {
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
-        const int gi = col / p.n_rows, r = col - gi * p.n_rows;
-        if (col < p.cols)
-          load_elements<4>(reinterpret_cast<const T*>(p.q.ptr) + (int64_t)layer * p.q.sl + (int64_t)seq * p.q.ss +
-                               (int64_t)(g.head * p.hn + gi) * p.q.sh + (int64_t)r * p.q.st + lane * 4, x);
-        float amax = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
+      // queries: a warp takes columns warp, warp + 16, ..., two at a time; a lane four elements
+#pragma unroll 1
+      for (int first = warp; first < N; first += 2 * kSoftWarps) {
+        float x[2][4];
 #pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-        // power of two that brings the largest element into [2^14, 2^15)
-        int e = 0;
-        if (amax > 0.f && amax < CUDART_INF_F) e = min(max(14 - ilogbf(amax), -126), 126);
-        const float up = __int_as_float((127 + e) << 23), down = __int_as_float((127 - e) << 23);
-        const int piece = (lane & 15) >> 1;
-        *reinterpret_cast<uint2*>(smem + S::q + (lane >> 4) * (N * 128) + col * 128 + ((piece ^ (col & 7)) << 4) + (lane & 1) * 8) =
-            make_uint2(pack_half2(x[0] * up, x[1] * up), pack_half2(x[2] * up, x[3] * up));
-        if (lane == 0) {
-          fm[col] = make_float2(amax < CUDART_INF_F ? p.scale * down : CUDART_NAN_F, 0.f);
-          top[col] = -CUDART_INF_F;
-          lim[col] = col < p.cols ? len - p.n_rows + 1 + r : 0;
+        for (int y = 0; y < 2; ++y) {
+          const int col = first + y * kSoftWarps, gi = col / p.n_rows, r = col - gi * p.n_rows;
+          x[y][0] = x[y][1] = x[y][2] = x[y][3] = 0.f;
+          if (col < p.cols)
+            load_elements<4>(reinterpret_cast<const T*>(p.q.ptr) + (int64_t)layer * p.q.sl + (int64_t)seq * p.q.ss +
+                                 (int64_t)(g.head * p.hn + gi) * p.q.sh + (int64_t)r * p.q.st + lane * 4, x[y]);
+        }
+        if (first == warp) warps_meet(1 + kSoftWarps / 4, kSoftWarps * 32);      // nobody reads the columns' numbers of the segment before any more
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int col = first + y * kSoftWarps;
+          float amax = fmaxf(fmaxf(fabsf(x[y][0]), fabsf(x[y][1])), fmaxf(fabsf(x[y][2]), fabsf(x[y][3])));
+#pragma unroll
+          for (int o = 16; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+          // power of two that brings the largest element into [2^14, 2^15)
+          int e = 0;
+          if (amax > 0.f && amax < CUDART_INF_F) e = min(max(14 - ilogbf(amax), -126), 126);
+          const float up = __int_as_float((127 + e) << 23), down = __int_as_float((127 - e) << 23);
+          const int piece = (lane & 15) >> 1;
+          *reinterpret_cast<uint2*>(smem + S::q + (lane >> 4) * (N * 128) + col * 128 + ((piece ^ (col & 7)) << 4) + (lane & 1) * 8) =
+              make_uint2(pack_half2(x[y][0] * up, x[y][1] * up), pack_half2(x[y][2] * up, x[y][3] * up));
+          if (lane == 0) {
+            fm[col] = make_float2(amax < CUDART_INF_F ? p.scale * down : CUDART_NAN_F, 0.f);
+            top[col] = -CUDART_INF_F;
+            lim[col] = col < p.cols ? len - p.n_rows + 1 + col % p.n_rows : 0;
+          }
         }
       }
       ptx::fence_proxy_async();
@@ -442,15 +466,8 @@ __global__ void __launch_bounds__(TilesSmem<N>::kThreads, 1) paged_attend_tiles_
               wait_values(tile - 1);
               __syncwarp();
               ptx::tc_fence_after();
-              float keep = 0.f;
-#pragma unroll
-              for (int c = 0; c < CW; ++c) {
-                float h = x[c];
-#pragma unroll
-                for (int o = 16; o >= 1; o >>= 1) h = fmaxf(h, __shfl_xor_sync(0xffffffffu, h, o));
-                if (lane == c) keep = h;
-              }
-              high[warp * 32 + lane] = keep;
+              const float highest = reduce_eight(x, lane, [](float a, float b) { return fmaxf(a, b); });
+              if ((lane & 3) == 0) high[warp * 32 + reduced_by(lane)] = highest;
               warps_meet(1 + wg, 128);
               if (quad == 0 && lane < CW) {
                 const float* hs = high + wg * 128 + lane;
@@ -509,20 +526,21 @@ __global__ void __launch_bounds__(TilesSmem<N>::kThreads, 1) paged_attend_tiles_
       ok = ptx::mbar_wait(pv_done + ((tile - 1) & 1), ((tile - 1) >> 1) & 1, abort_flag, p.wait_cycles) && ok;
       __syncwarp();
       ptx::tc_fence_after();
-      float keep = 0.f;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float v = l[c];
-#pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (lane == c) keep = v;
+      for (int c = 0; c < NC; c += 8) {
+        const float sum = reduce_eight(l + c, lane, [](float a, float b) { return a + b; });
+        if ((lane & 3) == 0) sums[warp * NC + c + reduced_by(lane)] = sum;
       }
-      if (lane < NC) sums[warp * NC + lane] = keep;
+      warps_meet(1 + wg, 128);
+      if (quad == 0 && lane < NC) {
+        float* of = sums + warp * NC + lane;
+        of[0] = of[0] + of[NC] + of[2 * NC] + of[3 * NC];
+      }
       warps_meet(1 + wg, 128);
       const bool whole = g.b0 == 0 && g.b1 == g.nb, write = ok && !*abort_flag;
       const int64_t place = (int64_t)(2 * blockIdx.x + (g.b0 == 0 ? 1 : 0)) * N;
       const float unit = vref / kAttPScale;
-      auto sum_of = [&](int c) { return sums[(wg * 4) * NC + c] + sums[(wg * 4 + 1) * NC + c] + sums[(wg * 4 + 2) * NC + c] + sums[(wg * 4 + 3) * NC + c]; };
+      const float* den_of = sums + wg * 4 * NC;
 #pragma unroll 1
       for (int c0 = 0; c0 < NC; c0 += CW) {
         uint32_t o[CW];
@@ -535,7 +553,7 @@ __global__ void __launch_bounds__(TilesSmem<N>::kThreads, 1) paged_attend_tiles_
             const float v = __uint_as_float(o[c]) * unit;
             if (whole) {
               const int gi = col / p.n_rows, r = col - gi * p.n_rows;
-              const float den = sum_of(c0 + c);
+              const float den = den_of[c0 + c];
               (reinterpret_cast<T*>(const_cast<void*>(p.out.ptr)) + (int64_t)layer * p.out.sl + (int64_t)seq * p.out.ss +
                (int64_t)(g.head * p.hn + gi) * p.out.sh + (int64_t)r * p.out.st)[mine] = T(den == 0.f ? 0.f : v / den);
             } else {
@@ -544,7 +562,7 @@ __global__ void __launch_bounds__(TilesSmem<N>::kThreads, 1) paged_attend_tiles_
           }
         }
       }
-      if (!whole && write && mine < NC && wg * NC + mine < p.cols) p.stat[place + wg * NC + mine] = make_float2(top[wg * NC + mine], sum_of(mine));
+      if (!whole && write && mine < NC && wg * NC + mine < p.cols) p.stat[place + wg * NC + mine] = make_float2(top[wg * NC + mine], den_of[mine]);
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(o_free);
@@ -582,7 +600,7 @@ static spindlekv_status launch_tiles(AttendParams& p, const CUtensorMap& kmap, c
   *runs = (int)std::min<int64_t>(std::min(resident[dev], kAttPartRows / (2 * N)), std::max<int64_t>(tiles, 1));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(*runs);
-  cfg.blockDim = dim3(TilesSmem<N>::kThreads);
+  cfg.blockDim = dim3(kTilesThreads);
   cfg.dynamicSmemBytes = TilesSmem<N>::bytes(p.table.n_layers * p.table.n_seqs);
   cfg.stream = st;
   cudaLaunchAttribute attr;
@@ -598,14 +616,18 @@ bool paged_attend_tiles(AttendParams& p, int format, int max_len, cudaStream_t s
   const int n_ls = p.table.n_layers * p.table.n_seqs, n = p.cols <= 32 ? 32 : p.cols <= 64 ? 64 : 128;
   const int64_t capacity = (int64_t)p.table.max_pages * p.pool.ps;
   const size_t smem = n == 32 ? TilesSmem<32>::bytes(n_ls) : n == 64 ? TilesSmem<64>::bytes(n_ls) : TilesSmem<128>::bytes(n_ls);
-  // up to 16 columns the other kernel is faster (16 columns, 4 x 16384 tokens: 44 us there, 52 here); a call of short units gets a block per
-  // unit there and no second kernel; for anything longer this one is faster, down to one sequence of 1000 tokens and two KV heads (14.6 us, 18.4)
-  if (p.cols <= 16 || p.cols > 128 || max_len <= 4 * kTile || smem > 227 * 1024) return false;
+  if (p.cols <= 16 || p.cols > 128 || smem > 227 * 1024) return false;   // (16 columns, 4 x 16384 tokens: 44 us in the other kernel, 50 here)
+  const int64_t units = (int64_t)n_ls * p.pool.heads, tiles = units * ((std::min<int64_t>(max_len, capacity) + kTile - 1) / kTile);
+  // Short units, if the other kernel has a block for each at once (4 sequences of 350 tokens, 8 KV heads: 15.7 us there with 32 columns, 16.1 with
+  // 64, 16.4 with 128; here 15.3, 21.4, 34.9.  32 sequences: 31, 61, 108 there; here 30, 43, 71)
+  if (max_len <= 4 * kTile && units * ceil_div(p.cols, 32) <= 148) return false;
+  // many columns over few tiles, which do not make up for the longer beginning and end (128 columns, one sequence of 1200 tokens: 27 us there, 31
+  // here; of 5000: 36 and 37; two of 5000: 48 and 42)
+  if (p.cols > 64 && tiles < 200) return false;
   p.groups = 1;
   p.units_per = p.pool.heads;
   if ((int64_t)n_ls * p.units_per * ((capacity + kTile - 1) / kTile + kTileSetUp) > 0x7FFFFFFF) return false;
   p.whole_units = 0;
-  const int64_t tiles = (int64_t)n_ls * p.units_per * ((std::min<int64_t>(max_len, capacity) + kTile - 1) / kTile);
   CUtensorMap kmap, vmap;
   const int rows = p.pool.heads * p.pool.ps;
   if (!make_code_map(&kmap, p.pool.kc, 128, rows, p.pool.n_pages, p.pool.ps) || !make_code_map(&vmap, p.pool.vc, 128, rows, p.pool.n_pages, p.pool.ps)) {
