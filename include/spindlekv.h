@@ -440,8 +440,9 @@ spindlekv_status spindlekv_paged_append(const spindlekv_page_pool* pool, const s
  *   ws        device scratch of spindlekv_paged_workspace_bytes bytes, 256-byte aligned, not to be shared by calls that may
  *             run at the same time
  * Sums and softmax statistics are fp32, in an order that the lengths, max_len and the device fix: the same call gives the same bits.
- * bf16 queries are multiplied as they are and the weights enter in 11 bits; fp32 queries and weights in 22.  The device status word of
- * `ws` (a bounded wait that gave up) is read with spindlekv_poll_status.
+ * bf16 queries are multiplied as they are and the weights enter in 11 bits (what weighs less than 2^-30 of the largest value fades
+ * out); fp32 queries and weights in 22.  The device status word of `ws` (a bounded wait that gave up) is read with
+ * spindlekv_poll_status.
  * UNSUPPORTED beyond 2^31 pairs of blocks in n_layers * n_seqs * n_kv_heads * max_pages * page_size: split the layers.
  */
 size_t spindlekv_paged_workspace_bytes(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t n_q_heads, int32_t n_rows);

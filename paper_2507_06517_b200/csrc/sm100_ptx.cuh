@@ -179,16 +179,7 @@ __device__ __forceinline__ void tmem_ld_32x8_sync(uint32_t taddr, uint32_t (&r)[
       : "r"(taddr)
       : "memory");
 }
-// 32 lanes x 16 consecutive fp32 columns written, and the wait for it.
-__device__ __forceinline__ void tmem_st_32x16_sync(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n\t"
-      "tcgen05.wait::st.sync.aligned;"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
+// 32 lanes x 8 consecutive fp32 columns written, and the wait for it.
 __device__ __forceinline__ void tmem_st_32x8_sync(uint32_t taddr, const uint32_t (&r)[8]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n\t"
