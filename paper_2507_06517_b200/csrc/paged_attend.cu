@@ -23,10 +23,10 @@
 // uneven the lengths are.  A unit that lies inside one run is finished there; of the others each run leaves (m, sum, O), which a second
 // kernel joins in the order of the runs.
 //
-// Measured (device time): 16384 tokens, 8 KV heads, 32 query heads 15.0 us, of which the loop is 5 at the copy rate and the rest set-up
+// Measured (device time): 16384 tokens, 8 KV heads, 32 query heads 14.6 us, of which the loop is 5 at the copy rate and the rest set-up
 // (4.5), join (4) and launch; 8 sequences of 10000 on average 45 us (4.6 TB/s); 4 x 16384 tokens with 4 to 8 columns per KV head 33 to 36 us
-// (4.1 TB/s), 16 columns 44, with fp32 queries 37 to 54; 32 columns of fp32 queries 88 (two column tiles and more have the SM to themselves, eight
-// warps: latency), 128 columns 290 (four passes).  More than 16 bf16 columns of 128 elements take paged_attend_tiles.cu.
+// (4.1 TB/s), 16 columns 43, with fp32 queries 36 to 52; 32 columns of fp32 queries 87 (two column tiles and more have the SM to themselves, eight
+// warps: latency), 128 columns 281 (four passes).  More than 16 bf16 columns of 128 elements take paged_attend_tiles.cu.
 #include <algorithm>
 
 #include "paged_attend.cuh"
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
         lim[t][i] = col < ncols ? len - p.n_rows + 1 + (p.n_rows == 1 ? 0 : (col0 + col) % p.n_rows) : 0;
       }
     float o[KS][NT][4], m[NT][2], l[NT][2];
-    float vref = 0.f;                   // O is in units of this, a power of two above every scale so far
+    float vinv = 0x1p126f;              // O is in units of 1 / vinv, a power of two that no scale so far exceeds
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       m[t][0] = m[t][1] = -CUDART_INF_F;
@@ -415,10 +415,12 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
         // a block's scale counts relative to the largest so far (in fp32 itself, large values would overflow before they are divided by
         // the weights' sum).  One piece: it joins the weights, unless it is much smaller (the weights would run out of fp16's range) or
         // the block is masked; then, and for two pieces always, it is applied to the block's product
-        if (vs_b[x] > vref) {                        // (not for a NaN)
-          const float to = __uint_as_float(min((__float_as_uint(vs_b[x]) & 0x7F800000u) + 0x00800000u, 0x7F000000u));   // the next power of two
-          const float f = vref / to;
-          vref = to;
+        float ratio = vs_b[x] * vinv;                // exact
+        if (ratio > 1.f) {                           // (not for a NaN)
+          const uint32_t to = min((__float_as_uint(vs_b[x]) & 0x7F800000u) + 0x00800000u, 0x7E800000u);   // the next power of two
+          const float now = __uint_as_float(0x7F000000u - to), f = now * __uint_as_float(0x7F000000u - __float_as_uint(vinv));
+          vinv = now;
+          ratio = vs_b[x] * vinv;
 #pragma unroll
           for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -426,7 +428,6 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
 #pragma unroll
               for (int i = 0; i < 4; ++i) o[k][t][i] *= f;
         }
-        const float ratio = vs_b[x] == 0.f ? 0.f : vs_b[x] / vref;
         const bool joined = NP == 1 && !masked && ratio >= 0.00390625f;
         const float wfac = joined ? ratio * kAttPScale : kAttPScale;
         uint2 pf[NT][NP];
@@ -539,7 +540,7 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
           sm_l[warp * COLS + 8 * t + 2 * c + i] = l[t][i];
         }
       }
-    const float unit = vref / kAttPScale;
+    const float unit = __uint_as_float(0x7F000000u - __float_as_uint(vinv)) / kAttPScale;
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll

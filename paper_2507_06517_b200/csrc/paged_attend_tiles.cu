@@ -616,7 +616,7 @@ bool paged_attend_tiles(AttendParams& p, int format, int max_len, cudaStream_t s
   const int n_ls = p.table.n_layers * p.table.n_seqs, n = p.cols <= 32 ? 32 : p.cols <= 64 ? 64 : 128;
   const int64_t capacity = (int64_t)p.table.max_pages * p.pool.ps;
   const size_t smem = n == 32 ? TilesSmem<32>::bytes(n_ls) : n == 64 ? TilesSmem<64>::bytes(n_ls) : TilesSmem<128>::bytes(n_ls);
-  if (p.cols <= 16 || p.cols > 128 || smem > 227 * 1024) return false;   // (16 columns, 4 x 16384 tokens: 44 us in the other kernel, 50 here)
+  if (p.cols <= 16 || p.cols > 128 || smem > 227 * 1024) return false;   // (16 columns, 4 x 16384 tokens: 43 us in the other kernel, 50 here)
   const int64_t units = (int64_t)n_ls * p.pool.heads, tiles = units * ((std::min<int64_t>(max_len, capacity) + kTile - 1) / kTile);
   // Short units, if the other kernel has a block for each at once (4 sequences of 350 tokens, 8 KV heads: 15.7 us there with 32 columns, 16.1 with
   // 64, 16.4 with 128; here 15.3, 21.4, 34.9.  32 sequences: 31, 61, 108 there; here 30, 43, 71)
