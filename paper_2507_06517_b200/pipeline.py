@@ -726,7 +726,8 @@ class SpindleKVPagedCache(_OnDevice):
 
 
 class SpindleKVBeamSelect(_OnDevice):
-    """Beam search's selection for batches of one shape: scratch and result buffers of ``spindlekv_beam_select``."""
+    """Beam search's selection for batches of one shape: scratch and result buffers of ``spindlekv_beam_select``.  All calls of one object
+    must be ordered: they share both."""
 
     def __init__(self, n_seqs: int, n_beams: int, vocab: int, n_out: Optional[int] = None, device="cuda"):
         self.n_seqs, self.n_beams, self.vocab, self.n_out = n_seqs, n_beams, vocab, n_beams if n_out is None else n_out

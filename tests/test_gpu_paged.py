@@ -495,6 +495,51 @@ def test_attention_over_a_pool_beyond_four_gigabytes():
     assert torch.equal(c.attend(q), got)
 
 
+def test_attention_of_many_columns_strides_streams_graphs_and_a_large_pool():
+    # pages at both ends of a pool whose byte offsets pass 32 bits; token-major queries with gaps; another stream; two graphs of one
+    # cache replayed in turn; one layer at a time
+    from paper_2507_06517_b200.pipeline import SpindleKVPagedCache, record_graph
+    n = (5 << 30) // (4 * 64 * 128)
+    c = SpindleKVPagedCache(2, 2, 32, 4, 128, n, 20, 64, "e4m3")
+    small = SpindleKVPagedCache(2, 2, 32, 4, 128, 80, 20, 64, "e4m3")
+    lens = [[1200, 77], [640, 1281 - 1]]
+    r = fill(small, lens, spread=0.3)
+    far = torch.randperm(80, generator=torch.Generator().manual_seed(1)).cuda()
+    far = torch.where(far % 2 == 0, far, n - 1 - far).int()        # page i of the small pool lies at far[i]
+    for big, little in zip(c.pool.tensors, small.pool.tensors):
+        big[far.long()] = little
+    c.pages.copy_(torch.where(small.pages >= 0, far[small.pages.clamp(min=0).long()], small.pages))
+    c.lens.copy_(small.lens)
+    wide = rows((2, 2, 5, 32, 2 * 128), "bf16", 4, 0.2)
+    q = wide[..., 128:].transpose(2, 3)                           # [L, B, Hq, rows, d]
+    held = torch.full((2, 2, 5, 32, 2 * 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = held[..., :128].transpose(2, 3)
+    c.attend(q, out=out)
+    check_attention(c, r, q, out, "bf16")
+    assert (held[..., 128:] == 7).all() and torch.equal(out, small.attend(q.contiguous()))
+    first = out.clone()
+    side = torch.cuda.Stream()
+    out.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    c.attend(q, out=out, stream=side)
+    side.synchronize()
+    assert torch.equal(out, first)
+    other = torch.zeros_like(first)
+    graphs = [record_graph(lambda: c.attend(q, out=out)), record_graph(lambda: c.attend(q, out=other, max_len=700))]
+    out.zero_()
+    for _ in range(3):
+        for g in graphs:
+            g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, first)
+    check_attention(c, r, q, other, "bf16")
+    for layer in range(2):
+        got = c.attend(q[layer:layer + 1], layer=layer, max_len=2000)
+        r1 = R.RefCache(r.codes["k"], r.codes["v"], r.scale["k"], r.scale["v"], r.ref, r.pages[layer:layer + 1], r.lens[layer:layer + 1], "e4m3")
+        check_attention(c, r1, q[layer:layer + 1], got, "bf16")
+    assert c.status() == 0
+
+
 # ---- pages -------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("fmt,ps,d,h", [("int8", 16, 64, 3), ("e4m3", 64, 128, 2)])
