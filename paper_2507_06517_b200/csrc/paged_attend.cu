@@ -23,7 +23,7 @@
 // uneven the lengths are.  A unit that lies inside one run is finished there; of the others each run leaves (m, sum, O), which a second
 // kernel joins in the order of the runs.
 //
-// Measured (device time): 16384 tokens, 8 KV heads, 32 query heads 14.6 us, of which the loop is 5 at the copy rate and the rest set-up
+// Measured (device time): 16384 tokens, 8 KV heads, 32 query heads 14.9 us, of which the loop is 5 at the copy rate and the rest set-up
 // (4.5), join (4) and launch; 8 sequences of 10000 on average 45 us (4.6 TB/s); 4 x 16384 tokens with 4 to 8 columns per KV head 33 to 36 us
 // (4.1 TB/s), 16 columns 43, with fp32 queries 36 to 52; 32 columns of fp32 queries 87 (two column tiles and more have the SM to themselves, eight
 // warps: latency), 128 columns 281 (four passes).  More than 16 bf16 columns of 128 elements take paged_attend_tiles.cu.
@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
         ks_b[x] = __shfl_sync(0xffffffffu, scales[x].x, n & 31);
         vs_b[x] = __shfl_sync(0xffffffffu, scales[x].y, n & 31);
       }
-      if (!ptx::mbar_wait(full, phase, abort_flag, p.wait_cycles)) {
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(full, phase, abort_flag, p.wait_cycles))) {      // the warp gives up as one
         owed = 3;
         break;
       }
@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int i = 0; i < 2; ++i) ref[t][i] = m[t][i] == -CUDART_INF_F ? 0.f : m[t][i];
-      if (!ptx::mbar_wait(full + 1, phase, abort_flag, p.wait_cycles)) {
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(full + 1, phase, abort_flag, p.wait_cycles))) {
         owed = more ? 6 : 2;
         break;
       }

@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
     int n = 0, seg = 0;
     bool ok = true;
     segments([&](const Segment& g) {
-      ok = ok && ptx::mbar_wait(q_full, seg & 1, abort_flag, p.wait_cycles);
+      ok = __all_sync(0xffffffffu, ok && ptx::mbar_wait(q_full, seg & 1, abort_flag, p.wait_cycles));      // the warp gives up as one
       for (int i = g.b0; i < g.b1 && ok; ++i) {
         const int slot = n % S::kK, sb = n & 1;
         ok = ptx::mbar_wait(k_full + slot, (n / S::kK) & 1, abort_flag, p.wait_cycles);
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
     int n = 0, seg = 0;
     bool ok = true;
     segments([&](const Segment& g) {
-      if (seg > 0) ok = ok && ptx::mbar_wait(o_free, (seg - 1) & 1, abort_flag, p.wait_cycles);
+      ok = __all_sync(0xffffffffu, ok && (seg == 0 || ptx::mbar_wait(o_free, (seg - 1) & 1, abort_flag, p.wait_cycles)));
       for (int i = g.b0; i < g.b1 && ok; ++i) {
         const int slot = n % S::kV, pb = n & 1;
         ok = ptx::mbar_wait(v_full + slot, (n / S::kV) & 1, abort_flag, p.wait_cycles);
