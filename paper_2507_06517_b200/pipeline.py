@@ -555,6 +555,15 @@ class _OnDevice:
     def _raw(self, stream) -> int:
         return B.raw_stream(self._index) if stream is None else B._stream(stream)
 
+    def _empty(self, shape, dtype, stream) -> torch.Tensor:
+        """Memory that is made within a call belongs to that call's stream: what the current stream still does with a block that the
+        allocator hands out again is in no order with ``stream``."""
+        raw = self._raw(stream)
+        if raw == B.raw_stream(self._index):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(torch.cuda.ExternalStream(raw, self.device) if raw else torch.cuda.default_stream(self.device)):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
     def _mine(self, name: str, t: torch.Tensor, dtype=None, shape=None) -> torch.Tensor:
         """``t``, if the library may be given its address as it is."""
         if t.device != self.device or (dtype is not None and t.dtype != dtype) or (shape is not None and t.shape != shape) or not t.is_contiguous():
@@ -571,8 +580,8 @@ def _device_of(device) -> torch.device:
 class SpindleKVPagedCache(_OnDevice):
     """A cache in 8 bits on pages: the pool, the page table of ``n_layers`` x ``n_seqs`` sequences, the scratch, and the calls on them.
     A step of decoding is ``resize(add=1)``, then for every layer ``append`` and ``attend``; a step of beam search ends with ``fork``.
-    ``max_pages`` bounds a sequence's pages, ``n_pages`` the pool's.  All calls of one object must be ordered (one stream, or
-    events): they share its scratch.  Buffers and call order only."""
+    ``max_pages`` bounds a sequence's pages, ``n_pages`` the pool's.  All calls of one object, its construction (on the stream current
+    then) included, must be ordered (one stream, or events): they share its scratch.  Buffers and call order only."""
 
     def __init__(self, n_layers: int, n_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int, n_pages: int, max_pages: int,
                  page_size: int = 64, fmt: str = "int8", device="cuda"):
@@ -615,7 +624,8 @@ class SpindleKVPagedCache(_OnDevice):
         self.n_live = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._tables = {}
         self._out: Dict[tuple, torch.Tensor] = {}
-        self.ws_attend = None
+        n = B.spindlekv_paged_workspace_bytes(self.pool, self.table, self.Hkv, 1)      # the same for every shape that is served
+        self.ws_attend = torch.zeros(n, dtype=torch.uint8, device=self.device)
 
     def _rows_of(self, layer: Optional[int]) -> B.PageTable:
         """The table of all layers, or of one."""
@@ -686,16 +696,15 @@ class SpindleKVPagedCache(_OnDevice):
         if out is None:
             held = self._out.get((shape, q.dtype))
             if held is None:
-                out = torch.empty(shape, dtype=q.dtype, device=self.device)
+                out = self._empty(shape, q.dtype, stream)
                 held = self._out[(shape, q.dtype)] = (out, self._cache_rows("out", out, table.n_layers, hq))
             out, od = held
         else:
             if out.shape != shape:
                 raise ValueError(f"out: {list(shape)} expected, got {list(out.shape)}")
             od = self._cache_rows("out", out, table.n_layers, hq)
-        if self.ws_attend is None:
-            need = B.spindlekv_paged_workspace_bytes(self.pool, self.table, self.Hkv, 1)      # the same for every shape that is served
-            self.ws_attend = torch.zeros(need, dtype=torch.uint8, device=self.device)
+        if self.ws_attend is None:       # given back by its owner: the kernels need no prepared scratch
+            self.ws_attend = self._empty((B.spindlekv_paged_workspace_bytes(self.pool, self.table, self.Hkv, 1),), torch.uint8, stream)
         B.spindlekv_paged_attend(self.pool, table, hq, shape[3], max_len or self.capacity, scale, qd, od, self.ws_attend, self._raw(stream))
         return out
 

@@ -745,3 +745,31 @@ def test_storing_a_prompt_refuses_before_it_gives_anything_back():
     for l, s in r.units():
         for g in "kv":
             assert np.array_equal(again.rows(g, l, s)[0], r.rows(g, l, s)[0])
+
+
+@pytest.mark.parametrize("n_rows", [1, 4])
+@pytest.mark.parametrize("given_back", [False, True])
+def test_first_attention_of_a_cache_on_a_stream_beside_a_busy_one(n_rows, given_back):
+    # the very first call goes to a side stream while the current one is far behind: nothing that the call needs may be in its queue
+    c = make(1, 2, 16, 2, 128, 400, 160, 32, "int8")
+    r = fill(c, [[5000, 3000]], spread=0.3)
+    q = rows((1, 2, 16, n_rows, 128), "bf16", 5, 0.2)
+    if given_back:
+        c.ws_attend = None
+    make(1, 1, 16, 2, 128, 4, 2, 32, "int8").attend(torch.zeros_like(q[:, :1]))        # kernels are loaded
+    scratch, side = torch.full((64 << 20,), 3.0, device="cuda"), torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.empty(64 << 20, dtype=torch.uint8, device="cuda"), torch.empty(1 << 18, dtype=torch.uint8, device="cuda")      # blocks to hand out
+    side.wait_stream(torch.cuda.current_stream())
+    free = torch.full((q.numel(),), 7.0, dtype=q.dtype, device="cuda")
+    for _ in range(100):
+        scratch.mul_(1.0001)
+    free.fill_(9.0)
+    del free                                   # a block that the current stream has still to write
+    out = c.attend(q, stream=side)
+    with torch.cuda.stream(side):
+        got = out.cpu()
+    torch.cuda.synchronize()
+    assert torch.equal(out.cpu(), got)         # and what it did afterwards changed nothing
+    check_attention(c, r, q, out, "bf16")
+    assert c.status() == 0

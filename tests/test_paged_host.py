@@ -133,3 +133,12 @@ def test_python_classes_refuse_what_does_not_fit():
         B.PageTable(z(1, 2, 3, dt=torch.int32), z(2, 1, dt=torch.int32))
     with pytest.raises(ValueError):
         B.PageTable(z(1, 2, 3), z(1, 2, dt=torch.int32))
+
+
+def test_a_cache_owns_its_scratch_before_its_first_call():
+    # made by a call, it would be filled on the current stream while the call's kernels run on another one
+    from paper_2507_06517_b200.pipeline import SpindleKVPagedCache
+    c = SpindleKVPagedCache(2, 3, 8, 2, 128, 64, 8, 64, device="cpu")
+    for ws, need in ((c.ws_attend, lib.spindlekv_paged_workspace_bytes(c.pool.c, c.table.c, 8, 1)),
+                     (c.ws_pages, lib.spindlekv_pages_workspace_bytes(c.pool.c, c.table.c))):
+        assert ws is not None and ws.nbytes == need > 0 and not ws.any()
