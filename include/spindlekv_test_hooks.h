@@ -26,9 +26,11 @@ enum {
                                            which an exact run can never exceed) */
   SPINDLEKV_TUNE_MBAR_WAIT_CYCLES = 2,  /* SM clock cycles after which a wait on a shared-memory barrier of the
                                            tensor-core kernels gives up */
-  SPINDLEKV_TUNE_SIM_BLOCK_PAIRS = 3    /* pairs of blocks the candidate-record similarity kernel runs on (default 0:
+  SPINDLEKV_TUNE_SIM_BLOCK_PAIRS = 3,   /* pairs of blocks the candidate-record similarity kernel runs on (default 0:
                                            as many as the device holds at once); fewer make every pair walk more
                                            (unit, row span) items one after the other */
+  SPINDLEKV_TUNE_PAGED_WITHHOLD = 4     /* number of the thread block of the paged attention kernels that does not ask for its
+                                           first keys and waits for them until its bound (default -1: no block) */
 };
 
 /* Sets one limit; value < 0 restores its default.  INVALID_ARG for an unknown key. */

@@ -200,6 +200,7 @@ struct Tuning {
   int round_cap;             // greedy rounds (never more than the sequence length)
   long long mbar_wait_cycles;
   int sim_block_pairs;       // pairs of blocks the candidate-record kernel runs on; 0: as many as the device holds
+  int paged_withhold;        // block of the paged attention kernels that waits for keys it has not asked for; -1: none
 };
 Tuning current_tuning();
 

@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
       }
     };
     if (n_it > 0) {
-      fetch(0, false, 0);
+      if ((int)blockIdx.x != p.withhold) fetch(0, false, 0);
       fetch(0, false, 1);
     }
     int owed = 0;                       // copies that a wait which gave up has left: 1 the keys', 2 the values', 4 the next keys'
@@ -799,7 +799,9 @@ spindlekv_status paged_attend_impl(const spindlekv_page_pool& pool, const spindl
   p.scale = (scale == 0.f ? 1.f / sqrtf((float)pool.head_dim) : scale) * 1.44269504088896340736f;
   p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kHeaderBytes);
   p.hdr = static_cast<uint32_t*>(ws);
-  p.wait_cycles = current_tuning().mbar_wait_cycles;
+  const Tuning tune = current_tuning();
+  p.wait_cycles = tune.mbar_wait_cycles;
+  p.withhold = tune.paged_withhold;
   p.stat = reinterpret_cast<float2*>(p.part + kAttPartRows * pool.head_dim);
   p.lead = reinterpret_cast<int2*>(p.stat + kAttPartRows);
   return q.dtype == SPINDLEKV_BF16 ? launch_format<__nv_bfloat16>(p, pool.format, max_len, st) : launch_format<float>(p, pool.format, max_len, st);

@@ -30,6 +30,7 @@ struct AttendParams {
   int2* lead;                // [runs] the unit that a run is the first to continue and its number of parts; unit -1: none, -2: a wait gave up
   uint32_t* hdr;             // status block of the workspace
   long long wait_cycles;     // bound of a wait
+  int withhold;              // for tests: the block that does not ask for its first keys; -1: none
 };
 
 // 2^x, to two units in the last place of fp32; results below the smallest normal number are 0

@@ -199,14 +199,15 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
           const int slot = item % RAW;
           ok = ok && __all_sync(0xffffffffu, ptx::mbar_wait(raw_empty + slot, ((item / RAW) & 1) ^ 1, abort_flag, p.wait_cycles));
           if (!ok) break;
+          const bool ask = item || (int)blockIdx.x != p.withhold;
           if (lane == 0) {
             holes[slot] = there < per;
             *n_asked = item + 1;
-            if (there) ptx::mbar_expect_tx(raw_full + slot, there * p.pool.ps * D);
-            else ptx::mbar_arrive(raw_full + slot);
+            if (ask && there) ptx::mbar_expect_tx(raw_full + slot, there * p.pool.ps * D);
+            else if (ask) ptx::mbar_arrive(raw_full + slot);
           }
           __syncwarp();
-          if (lane < per && in_pool(mine))
+          if (ask && lane < per && in_pool(mine))
             ptx::tma_load_3d(smem + S::raw + slot * kRawBytes + lane * p.pool.ps * D, v ? &vmap : &kmap, raw_full + slot, 0, g.head * p.pool.ps, mine);
           ++item;
         }

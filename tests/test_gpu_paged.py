@@ -773,3 +773,37 @@ def test_first_attention_of_a_cache_on_a_stream_beside_a_busy_one(n_rows, given_
     assert torch.equal(out.cpu(), got)         # and what it did afterwards changed nothing
     check_attention(c, r, q, out, "bf16")
     assert c.status() == 0
+
+
+@pytest.fixture
+def limits():
+    from paper_2507_06517_b200 import binding as B
+    yield B.spindlekv_set_tuning
+    for k in range(5):
+        B.spindlekv_set_tuning(k, -1)
+
+
+# which kernel serves a call: a block per unit, runs of the kernel for few columns (one, two and four column tiles), tiles of 32, 64, 128.
+# The hints make runs long enough that block 3 has tokens
+SHORT, LONG = [[40, 100, 33], [7, 0, 90]], [[9000, 700, 1], [0, 900, 8000]]
+GIVE_UP = [("bf16", 64, 2, 1, SHORT, 128), ("f32", 128, 4, 1, SHORT, 128), ("bf16", 128, 4, 1, LONG, 700), ("f32", 128, 8, 2, LONG, 700),
+           ("bf16", 64, 8, 4, LONG, 700), ("bf16", 128, 8, 4, LONG, 520), ("bf16", 128, 8, 8, LONG, 520), ("bf16", 128, 8, 16, LONG, 9000)]
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,d,hn,n_rows,lens,max_len", GIVE_UP)
+def test_a_wait_that_runs_out_comes_back_with_a_status(limits, dtype, d, hn, n_rows, lens, max_len, fmt):
+    # a block waits, with a short bound, for keys that nobody has asked for: the call returns and says so, and the next one is as ever
+    from paper_2507_06517_b200 import binding as B
+    c = make(2, 3, 2 * hn, 2, d, 700, 300, 32, fmt)
+    r = fill(c, lens, dtype, spread=0.3)
+    q = rows((2, 3, 2 * hn, n_rows, d), dtype, 5, 0.2)
+    limits(B.TUNE_MBAR_WAIT_CYCLES, 2_000_000)
+    limits(B.TUNE_PAGED_WITHHOLD, 3)
+    out = torch.full_like(q, 7.0)
+    c.attend(q, out=out, max_len=max_len)
+    assert c.status() == B.TIMEOUT
+    limits(B.TUNE_PAGED_WITHHOLD, -1)
+    c.attend(q, out=out, max_len=max_len)
+    assert c.status() == B.OK
+    check_attention(c, r, q, out, dtype)

@@ -142,3 +142,13 @@ def test_a_cache_owns_its_scratch_before_its_first_call():
     for ws, need in ((c.ws_attend, lib.spindlekv_paged_workspace_bytes(c.pool.c, c.table.c, 8, 1)),
                      (c.ws_pages, lib.spindlekv_pages_workspace_bytes(c.pool.c, c.table.c))):
         assert ws is not None and ws.nbytes == need > 0 and not ws.any()
+
+
+def test_the_hook_that_withholds_keys_can_be_set_and_restored():
+    assert B.spindlekv_get_tuning(B.TUNE_PAGED_WITHHOLD) == -1
+    try:
+        B.spindlekv_set_tuning(B.TUNE_PAGED_WITHHOLD, 3)
+        assert B.spindlekv_get_tuning(B.TUNE_PAGED_WITHHOLD) == 3
+    finally:
+        B.spindlekv_set_tuning(B.TUNE_PAGED_WITHHOLD, -1)
+    assert B.spindlekv_get_tuning(B.TUNE_PAGED_WITHHOLD) == -1
