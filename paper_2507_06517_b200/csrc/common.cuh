@@ -165,19 +165,42 @@ __device__ __forceinline__ int block_exclusive_scan(int v, int* warp_sums, int& 
 
 // ---- counting blocks that bring something to a common end -----------------------------------------------
 // A word in the workspace counts arrivals.  A call finds it at zero, because the last arrival of the call before put it back, or finds
-// something that is no count (upper 48 bits) and makes it one: the workspace needs no preparation.  The arriving thread calls this
-// after its block's writes and a __threadfence(); the last one gets true.
+// something that is no count (its upper bits are not the tag) and makes it one: the workspace needs no preparation.  Returns the word as it was
+// before this arrival; the lowest BITS bits are the count and what goes with it.
 constexpr unsigned long long kCountTag = 0x51BDC0F7A93Eull;
-__device__ __forceinline__ bool last_to_arrive(unsigned long long* word, int n) {
+template <int BITS>
+constexpr unsigned long long kNoArrivals = (kCountTag >> (BITS - 16)) << BITS;
+template <int BITS>
+__device__ __forceinline__ unsigned long long count_arrival(unsigned long long* word) {
   unsigned long long old = atomicAdd(word, 1ull);
-  while (old >> 16 != kCountTag) {
+  while (old >> BITS != kNoArrivals<BITS> >> BITS) {
     const unsigned long long now = *reinterpret_cast<volatile unsigned long long*>(word);
-    if (now >> 16 == kCountTag) old = atomicAdd(word, 1ull);
-    else if (atomicCAS(word, now, kCountTag << 16 | 1ull) == now) old = kCountTag << 16;
+    if (now >> BITS == kNoArrivals<BITS> >> BITS) old = atomicAdd(word, 1ull);
+    else if (atomicCAS(word, now, kNoArrivals<BITS> | 1ull) == now) old = kNoArrivals<BITS>;
   }
-  const bool last = (int)(old & 0xFFFFu) + 1 == n;
-  if (last) atomicExch(word, kCountTag << 16);
+  return old;
+}
+// The arriving thread calls this after its block's writes and a __threadfence(); the last of n < 2^16 gets true.
+__device__ __forceinline__ bool last_to_arrive(unsigned long long* word, int n) {
+  const bool last = (int)(count_arrival<16>(word) & 0xFFFFu) + 1 == n;
+  if (last) atomicExch(word, kNoArrivals<16>);
   return last;
+}
+// The same for arrivals that may bring a failure along, which is kept (bit 16) until the last one has arrived: 0 for all but the last, who gets
+// 1 when nobody failed and 2 otherwise.
+__device__ __forceinline__ int last_to_arrive(unsigned long long* word, int n, bool failed) {
+  if (failed) {
+    unsigned long long now = *reinterpret_cast<volatile unsigned long long*>(word);
+    while (now >> 24 != kNoArrivals<24> >> 24) {
+      atomicCAS(word, now, kNoArrivals<24>);
+      now = *reinterpret_cast<volatile unsigned long long*>(word);
+    }
+    atomicOr(word, 1ull << 16);
+  }
+  const unsigned long long old = count_arrival<24>(word);
+  if ((int)(old & 0xFFFFu) + 1 != n) return 0;
+  atomicExch(word, kNoArrivals<24>);
+  return old >> 16 & 1u ? 2 : 1;
 }
 
 // Per-device "done once" flags for host-side set-up (function attributes, occupancy queries): the

@@ -126,13 +126,19 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
     at = cut.start(blockIdx.x);
     stop = (int)blockIdx.x < cut.runs ? cut.start(blockIdx.x + 1) : at;
   }
-  if (p.whole_units) {
-    if (tid == 0 && blockIdx.x == 0) p.hdr[kHdrStatus] = SPINDLEKV_OK;
-  } else if (tid == 0) {
-    p.lead[blockIdx.x] = make_int2(-1, 0);
-  }
+  // With a block per unit there is no join to write the status word: the last block does, when it is known whether one has given up.  (The last
+  // warp asks, which has the least to do with a unit's result.)
+  auto settle = [&](bool gave_up) {
+    if (!p.whole_units || tid != kAttThreads - 32) return;
+    const int end = last_to_arrive(reinterpret_cast<unsigned long long*>(p.hdr + kHdrUnitsDone), (int)gridDim.x, gave_up);
+    if (end) p.hdr[kHdrStatus] = end == 1 ? SPINDLEKV_OK : SPINDLEKV_TIMEOUT;
+  };
+  if (!p.whole_units && tid == 0) p.lead[blockIdx.x] = make_int2(-1, 0);
   zero_empty<T, D>(p, prefix);
-  if (at >= stop) return;
+  if (at >= stop) {
+    settle(false);
+    return;
+  }
   int ls = unit_at(p, prefix, at);
   while (at < stop) {
     while (prefix[ls + 1] == prefix[ls] || prefix[ls + 1] * p.units_per <= at) ++ls;
@@ -523,10 +529,8 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
       if (owed & 1) ptx::mbar_wait(full, phase, abort_flag + 1, kDefaultMbarWaitCycles);
       if (owed & 2) ptx::mbar_wait(full + 1, phase, abort_flag + 1, kDefaultMbarWaitCycles);
       if (owed & 4) ptx::mbar_wait(full, phase ^ 1, abort_flag + 1, kDefaultMbarWaitCycles);
-      if (tid == 0) {
-        if (p.whole_units) atomicExch(&p.hdr[kHdrStatus], (uint32_t)SPINDLEKV_TIMEOUT);
-        else p.lead[blockIdx.x] = make_int2(-2, 0);
-      }
+      if (!p.whole_units && tid == 0) p.lead[blockIdx.x] = make_int2(-2, 0);
+      settle(true);
       return;
     }
 #pragma unroll
@@ -549,6 +553,7 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
         for (int i = 0; i < 2; ++i)   // elements d, d + 1 of column 2c + i
           *reinterpret_cast<float2*>(so + (warp * COLS + 8 * t + 2 * c + i) * OP + g * (D / 8) + 2 * k) = make_float2(o[k][t][i] * unit, o[k][t][i + 2] * unit);
     __syncthreads();
+    settle(false);
     const bool whole = b0 == 0 && b1 == nb;
     // what is left for the join: a unit that began in an earlier run is this run's first, one that begins here and goes on its last
     const int64_t place = (int64_t)(2 * blockIdx.x + (b0 == 0 ? 1 : 0)) * p.part_cols;

@@ -11,6 +11,7 @@ namespace skv {
 
 constexpr int kAttMaxRuns = 592;       // thread blocks of a call: four on each of 148 SMs
 constexpr int kAttPartRows = 2 * kAttMaxRuns * 32;   // rows of partial results: two parts of a run, up to 32 columns each (or 128 of a quarter of the runs)
+constexpr int kHdrUnitsDone = 16;      // words 16, 17 of the status block: units of a call that runs a block for each
 constexpr float kAttLazy = 8.f;        // how far a score may exceed the running reference, in powers of two
 constexpr float kAttPScale = 128.f;    // p <= 2^8 times this stays inside fp16
 

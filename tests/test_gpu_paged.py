@@ -807,3 +807,30 @@ def test_a_wait_that_runs_out_comes_back_with_a_status(limits, dtype, d, hn, n_r
     c.attend(q, out=out, max_len=max_len)
     assert c.status() == B.OK
     check_attention(c, r, q, out, dtype)
+
+
+def test_status_of_a_call_with_a_block_per_unit_is_the_last_blocks(limits):
+    # whichever block gives up, and whatever the workspace held: nobody's OK may cover it, and nothing of it stays
+    from paper_2507_06517_b200 import binding as B
+    from paper_2507_06517_b200.pipeline import record_graph
+    c = make(3, 20, 4, 2, 64, 3 * 20 * 8, 8, 16, "int8")
+    lens = np.random.default_rng(1).integers(0, 129, (3, 20))
+    lens[0, 0], lens[2, 19], lens[1, 3] = 5, 128, 0
+    r = fill(c, lens.tolist(), spread=0.3)
+    q = rows((3, 20, 4, 1, 64), "bf16", 5, 0.2)
+    limits(B.TUNE_MBAR_WAIT_CYCLES, 2_000_000)
+    for block in (119, 0):                     # the last unit's, and the first one's
+        limits(B.TUNE_PAGED_WITHHOLD, block)
+        c.ws_attend.random_(0, 256)
+        c.attend(q, max_len=128)
+        assert c.status() == B.TIMEOUT
+        limits(B.TUNE_PAGED_WITHHOLD, -1)
+        for _ in range(2):
+            check_attention(c, r, q, c.attend(q, max_len=128), "bf16")
+            assert c.status() == B.OK
+    graph = record_graph(lambda: c.attend(q, max_len=128))
+    for _ in range(3):
+        c.ws_attend.random_(0, 256)
+        graph.replay()
+        graph.replay()
+        assert c.status() == B.OK
