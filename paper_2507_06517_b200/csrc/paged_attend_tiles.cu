@@ -382,6 +382,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
       float2 sc = make_float2(0.f, 0.f), sc_next = scales_of(blk0, page_next);
       float vmost = 0.f;
       uint32_t missing = 0;
+      bool unset = true;                           // no token so far: the references say nothing yet
       float l[NC], vref = 0.f, vinv = 0.f;
 #pragma unroll
       for (int c = 0; c < NC; ++c) l[c] = 0.f;
@@ -416,7 +417,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
         const int block = (n & 3) * 8 + quad * 2 + (lane >> 4);
         const float ks = __shfl_sync(0xffffffffu, sc.x, block), vs = __shfl_sync(0xffffffffu, sc.y, block), vtop = __shfl_sync(0xffffffffu, vmost, block);
         const int t0 = (g.b0 + n) * kTile, t = t0 + mine;
-        const bool masked = (missing >> ((n & 3) * 8) & 0xFFu) || t0 + kTile > len - p.n_rows + 1;
+        const uint32_t absent = missing >> ((n & 3) * 8) & 0xFFu;     // blocks of the tile without a page
+        const bool masked = absent || t0 + kTile > len - p.n_rows + 1;
         // O is in units of a power of two above every scale so far
         const bool grows = vtop > vref;
         float vf = 1.f;
@@ -462,7 +464,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
             }
 #pragma unroll
             for (int c = 0; c < CW; ++c) most[c & 3] = fmaxf(most[c & 3], x[c]);
-            if (warps_any(1 + wg, 128, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) > kAttLazy || grows || n == 0)) {
+            if (warps_any(1 + wg, 128, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) > kAttLazy || grows || unset)) {
               // ---- new references for these columns: their largest score; what is summed so far moves along ----
               wait_values(tile - 1);
               __syncwarp();
@@ -515,6 +517,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
           for (int c = 0; c < CW; c += 8)
             *reinterpret_cast<uint4*>(row + (((piece + c / 8) ^ (mine & 7)) << 4)) = make_uint4(h[c / 2], h[c / 2 + 1], h[c / 2 + 2], h[c / 2 + 3]);
         }
+        unset = unset && absent == 0xFFu;
         ptx::fence_proxy_async();
         if (AHEAD && n + 1 < n_it) read_scores(tile + 1);
         ptx::tc_fence_before();

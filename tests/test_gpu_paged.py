@@ -834,3 +834,30 @@ def test_status_of_a_call_with_a_block_per_unit_is_the_last_blocks(limits):
         graph.replay()
         graph.replay()
         assert c.status() == B.OK
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("n_rows", [4, 8, 16])
+def test_attention_of_many_columns_that_begins_with_missing_pages(fmt, n_rows):
+    # scores near -200 (in powers of two): a column's reference is that of the tokens it sees, however many tiles of nothing come first
+    c = make(1, 12, 16, 2, 128, 12 * 50, 50, 64, fmt)
+    r = ref_of(c)
+    lens = 3200 - 37 * np.arange(12)[None]
+    start = r.resize(lens)
+    c.resize(lens_t(lens))
+    K, V = rows((1, 12, 2, 3200, 128), "bf16", 1, 0.1), rows((1, 12, 2, 3200, 128), "bf16", 2, 0.3)
+    K[..., 0] = -40
+    for s in range(12):
+        V[0, s, :, 128 * (s % 4):128 * (s % 4) + 128] = 0     # the first tile that is seen has a say in the weights' sum alone
+    c.append(K, V)
+    r.append(start, f64(K), f64(V))
+    for s in range(12):
+        c.pages[0, s, :2 * (s % 4)] = -1                      # none, one, two, three tiles at the front
+        c.pages[0, s, 8 + s:8 + s + s % 7] = 1 << 20          # and some inside, where a run may begin
+    c.pages[0, 11] = -1                                       # nothing at all
+    q = rows((1, 12, 16, n_rows, 128), "bf16", 5, 0.2)
+    q[..., 0] = 40
+    out = torch.full_like(q, 7.0)
+    c.attend(q, out=out)
+    check_attention(c, ref_of(c), q, out, "bf16")
+    assert (out[0, 11] == 0).all() and c.status() == 0
