@@ -440,8 +440,10 @@ spindlekv_status spindlekv_paged_append(const spindlekv_page_pool* pool, const s
  *   ws        device scratch of spindlekv_paged_workspace_bytes bytes, 256-byte aligned, not to be shared by calls that may
  *             run at the same time
  * Sums and softmax statistics are fp32, in an order that the lengths, max_len and the device fix: the same call gives the same bits.
- * bf16 queries are multiplied as they are and the weights enter in 11 bits (what weighs less than 2^-30 of the largest value fades
- * out); fp32 queries and weights in 22.  The device status word of `ws` (a bounded wait that gave up) is read with
+ * bf16 queries are multiplied as they are and the weights enter in 11 bits, to 2^-24 of the row's largest weight at worst (of two weights
+ * whose ratio is beyond 2^12 the smaller one loses bits); fp32 queries and weights in 22 bits, to 2^-32.  Values of any size that a row does not see,
+ * or whose weight is 0, leave the others as they are: block scales count in fp32, over 2^126 of range.  Sums of weight * value, relative to
+ * the row's largest weight, are held in fp32 and have to stay inside its range.  The device status word of `ws` (a bounded wait that gave up) is read with
  * spindlekv_poll_status.
  * UNSUPPORTED beyond 2^31 pairs of blocks in n_layers * n_seqs * n_kv_heads * max_pages * page_size: split the layers.
  */

@@ -8,7 +8,10 @@
 // so that K, V and P are stored the way they arise, token by token, and both products have 128 rows whatever the number of columns.
 // The numbers are those of the kernel for few columns: codes exact in fp16, queries scaled by a power of two (exact), p <= 2^8 by a
 // running reference that moves when a score exceeds it by 8, block scales of V joined with the weights (relative to a power of two above
-// all scales so far) before their one rounding to fp16; m, the sums and O are fp32.
+// all scales so far) before their one rounding to fp16; m, the sums and O are fp32.  Where a scale is less than 2^-8 of that power, the
+// weights would run out of fp16's range, for a value perhaps that has no weight or that a row does not even see.  Such a tile's values
+// are multiplied in groups of blocks of like scales (a block is a K step of the product), each relative to a power of two of its own and into
+// an accumulator of its own, which the weights' warps add to O in fp32.
 //
 // Roles (one block per SM).  One warp asks for the codes (TMA, a page at a time, a ring of K and V tiles); four widen them; two issue
 // the products, one each, the keys' two tiles ahead of the values'; sixteen turn scores into weights: a thread has a token and a quarter of
@@ -18,9 +21,11 @@
 // Split.  The line of all units' tiles is cut into equal runs, one per SM, and the parts of a unit are joined as for few columns.
 //
 // Measured (4 sequences x 16384 tokens, 8 KV heads, int8; beside it the kernel for few columns, which reads the codes once per 32 columns): 32
-// columns 48 us (64), 64 columns 67 (101), 128 columns 117 (179); 6 x 26000 tokens, 32 columns 95 us (117), i.e. 3.4 TB/s.  Bound by the
-// weights' warps: of 2000 cycles per tile at 32 columns (memory would allow 1450) they wait for 500; issue slots are 63% busy, the products
+// columns 50 us (64), 64 columns 76 (101), 128 columns 124 (179); 6 x 26000 tokens, 32 columns 105 us a call (117), i.e. 3.1 TB/s.  Bound by the
+// weights' warps: of 2000 cycles per tile at 32 columns (memory would allow 1450) they wait for 500; issue slots are 50% busy, the products
 // take 45 cycles per instruction (360 of 8 steps), widening 600 per tile of codes.  A unit's beginning and end are 7 us, its first tile among them.
+// The way out for uneven tiles costs the others registers (48.2, 71, 118.5 without it); with a block of 2^40 in front of every sequence, against which
+// all later tiles are uneven (one group each), 76, 103 and 150 us, with four sizes in turn (four groups) 141, 177 and 241.
 // Tried: fewer and wider warps for the weights (eight: 60 us at 32 columns), two groups of them that take turns at the tiles (73), two tiles at a
 // time (53, as one at a time then), eight widening warps (50), one thread issuing both products (65), a box of 16 tokens per copy (180 cycles per
 // copy instruction).
@@ -34,6 +39,7 @@ constexpr int kTile = 128;             // tokens
 constexpr int kTileSetUp = 6;          // places of a unit's beginning and end, which take 7 us (2: 54 us for 4 x 16384 tokens and 32 columns, 4: 52.6, 6: 51.8)
 constexpr int kSoftWarps = 16, kWidenWarps = 4, kAskWarp = kSoftWarps, kScoreWarp = kAskWarp + 1, kValueWarp = kScoreWarp + 1, kWidenFirst = kValueWarp + 1;
 constexpr int kTilesThreads = 32 * (kWidenFirst + kWidenWarps);
+constexpr float kTileEven = 0.00390625f;   // smallest scale, in units of the power of two above the largest, that joins the weights
 constexpr int kRawBytes = kTile * 128, kWideBytes = 2 * kRawBytes;
 
 __device__ __forceinline__ void warps_meet(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
@@ -65,9 +71,11 @@ struct TilesSmem {
   static constexpr int kP = N == 128 ? 1 : 2;                               // buffers of weights; 32 columns each share rows of 64
   static constexpr size_t wide = 0, raw = wide + (kK + kV) * kWideBytes, q = raw + kRaw * kRawBytes, p = q + N * 256;
   static constexpr size_t bars = p + (N == 32 ? 1 : kP * N / 64) * kRawBytes;
-  static constexpr int kBars = 2 * kRaw + 2 * kK + 2 * kV + 2 + 2 + 2 + 2 + 3;
-  static constexpr size_t words = bars + kBars * 8;                         // abort flags, TMEM address, flags of the raw slots
-  static constexpr size_t fm = (words + 16 * 4 + 15) / 16 * 16;             // [N] score factor and reference, read two at a time
+  static constexpr int kBars = 2 * kRaw + 2 * kK + 2 * kV + 2 + 2 + 2 + 2 + 5;
+  static constexpr size_t words = bars + kBars * 8;                         // abort flags, TMEM address, flags of the raw slots, bound of a wait
+  static constexpr size_t groups = (words + 16 * 4 + 15) / 16 * 16;         // [8]
+  static constexpr size_t counts = groups + 8 * 8;                          // [kSoftWarps] groups that a warp has read
+  static constexpr size_t fm = counts + kSoftWarps * 4;                     // [N] score factor and reference, read two at a time
   static constexpr size_t change = fm + N * 8;                              // [N] factor of what is summed, difference of the references
   static constexpr size_t top = change + N * 8;                             // [N] running maximum
   static constexpr size_t lim = top + N * 4;                                // [N] tokens that a column sees
@@ -81,6 +89,76 @@ struct TilesSmem {
 static_assert(TilesSmem<32>::fm % 16 == 0 && TilesSmem<64>::fm % 16 == 0 && TilesSmem<128>::fm % 16 == 0 && TilesSmem<32>::bars % 1024 == 0 &&
               TilesSmem<64>::bars % 1024 == 0 && TilesSmem<128>::bars % 1024 == 0, "alignment of what is read in 16 bytes, and of the tiles");
 
+// ---- uneven tiles (rare, and out of line so that the loop over the others has its registers to itself) ----
+// Lanes hold the V scales of the 32 blocks of four tiles.  A scale that is a number, or 0: zeros alone, NaN, no page
+__device__ __forceinline__ float number(float scale) { return scale > 0.f && scale < CUDART_INF_F ? scale : 0.f; }
+// the next power of two, and 1 / a power of two
+__device__ __forceinline__ float power_above(float x) { return __uint_as_float(min((__float_as_uint(x) & 0x7F800000u) + 0x00800000u, 0x7E800000u)); }
+__device__ __forceinline__ float inverse_power(float x) { return __uint_as_float(0x7F000000u - __float_as_uint(x)); }
+// The blocks among `left` that belong together: those within kTileEven of the power of two above the largest scale, and those without a number for
+// one, which any power serves
+__device__ __forceinline__ uint32_t next_group(float v, uint32_t left, float& power) {
+  power = power_above(__uint_as_float(__reduce_max_sync(0xffffffffu, left >> (threadIdx.x & 31) & 1 ? __float_as_uint(v) : 0u)));
+  return left & __ballot_sync(0xffffffffu, v == 0.f || v * inverse_power(power) >= kTileEven);
+}
+// 1 / the power of two of a block's group where its tile is uneven (`lows`: the blocks that are far below the tile's reference), `even` elsewhere; the
+// first thread of all writes the groups down, from tile `tile` on
+__device__ __noinline__ float group_blocks(float scale, uint32_t lows, float even, int tile, volatile uint64_t* table) {
+  const int lane = threadIdx.x & 31;
+  const float v = number(scale);
+  float mine = even;
+  for (int j = 0; j < 4; ++j) {
+    uint32_t left = lows >> (8 * j) & 0xFFu ? 0xFFu << (8 * j) : 0u;
+    uint64_t groups = 0;
+    for (int at = 0; left; at += 8) {
+      float power;
+      const uint32_t members = next_group(v, left, power);
+      if (members >> lane & 1) mine = inverse_power(power);
+      groups |= (uint64_t)(members >> (8 * j)) << at;
+      left &= ~members;
+    }
+    if (groups && threadIdx.x == 0) table[(tile + j) & 7] = groups;      // (entries that were cleared when their tiles were done)
+  }
+  return mine;
+}
+// Adds the groups' products to O, one after the other as they are done.  (What it needs it finds in shared memory: arguments would be kept in registers
+// by the loop that hardly ever calls.)
+template <int N>
+__device__ __noinline__ void add_groups(uint8_t* smem, float scale, float ref, int first, bool begins) {
+  using S = TilesSmem<N>;
+  constexpr int NC = N * 4 / kSoftWarps;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::words);
+  const long long wait_cycles = *reinterpret_cast<const long long*>(smem + S::words + 32);
+  uint64_t *done = reinterpret_cast<uint64_t*>(smem + S::bars) + S::kBars - 2, *read = done + 1;
+  int* number_done = reinterpret_cast<int*>(smem + S::counts) + warp;
+  const uint32_t to = reinterpret_cast<const uint32_t*>(smem + S::words)[2] + 2 * N + (warp >> 2) * NC + ((uint32_t)((warp & 3) * 32) << 16), from = to + N;
+  const float v = number(scale);
+  for (uint32_t left = 0xFFu << first; left; begins = false) {
+    float power;
+    left &= ~next_group(v, left, power);
+    const int turn = *number_done;
+    __syncwarp();
+    if (lane == 0) *number_done = turn + 1;
+    ptx::mbar_wait(done, turn & 1, abort_flag, wait_cycles);
+    __syncwarp();
+    ptx::tc_fence_after();
+    const float rel = power * inverse_power(ref);  // at most 1
+#pragma unroll 1
+    for (int c0 = 0; c0 < NC; c0 += 8) {
+      uint32_t x[8], o[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+      ptx::tmem_ld_32x8_sync(from + c0, x);
+      if (!begins) ptx::tmem_ld_32x8_sync(to + c0, o);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) o[c] = __float_as_uint(fmaf(__uint_as_float(x[c]), rel, __uint_as_float(o[c])));
+      ptx::tmem_st_32x8_sync(to + c0, o);
+    }
+    ptx::tc_fence_before();
+    __syncwarp();
+    if (left && lane == 0) ptx::mbar_arrive(read);
+  }
+}
+
 template <int FMT, int N>
 __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(const __grid_constant__ CUtensorMap kmap,
                                                                               const __grid_constant__ CUtensorMap vmap, AttendParams p) {
@@ -88,16 +166,19 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
   using T = __nv_bfloat16;
   constexpr int D = 128, NC = N * 4 / kSoftWarps, CW = 8, AHEAD = N < 128, RAW = S::kRaw, PB = S::kP;
   constexpr int kPNext = N == 32 ? 64 : N / 64 * kRawBytes;                 // bytes from one buffer of weights to the other
-  constexpr uint32_t kTmemCols = N == 32 ? 128 : N == 64 ? 256 : 512;        // two score buffers and O
+  constexpr uint32_t kTmemCols = 4 * N;                                     // two score buffers, O, and a group's product
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
   uint64_t* raw_full = reinterpret_cast<uint64_t*>(smem + S::bars);
   uint64_t *raw_empty = raw_full + RAW, *k_full = raw_empty + RAW, *k_empty = k_full + S::kK, *v_full = k_empty + S::kK, *v_empty = v_full + S::kV;
-  uint64_t *s_full = v_empty + S::kV, *s_empty = s_full + 2, *p_full = s_empty + 2, *pv_done = p_full + 2, *q_full = pv_done + 2, *o_free = q_full + 1, *drained = o_free + 1;
+  uint64_t *s_full = v_empty + S::kV, *s_empty = s_full + 2, *p_full = s_empty + 2, *pv_done = p_full + 2, *q_full = pv_done + 2, *o_free = q_full + 1, *drained = o_free + 1,
+           *group_done = drained + 1, *group_read = group_done + 1;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::words);   // a wait gave up; and one for the waits after that
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::words) + 2;
   volatile int* n_asked = reinterpret_cast<volatile int*>(smem + S::words) + 3;
   volatile int* holes = reinterpret_cast<volatile int*>(smem + S::words) + 4;    // [kRaw] blocks of the tile are missing
+  // [8] groups of the uneven ones among the last tiles: byte i holds the blocks of the i-th, 0 behind the last; 0 for an even tile
+  volatile uint64_t* groups = reinterpret_cast<volatile uint64_t*>(smem + S::groups);
   float2* fm = reinterpret_cast<float2*>(smem + S::fm);
   float2* change = reinterpret_cast<float2*>(smem + S::change);
   float* top = reinterpret_cast<float*>(smem + S::top);
@@ -120,9 +201,14 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
     ptx::mbar_init(q_full, kSoftWarps);
     ptx::mbar_init(o_free, kSoftWarps);
     ptx::mbar_init(drained, 2);
+    ptx::mbar_init(group_done, 1);
+    ptx::mbar_init(group_read, kSoftWarps);
     ptx::fence_barrier_init();
     abort_flag[0] = abort_flag[1] = 0;
     *n_asked = 0;
+    for (int i = 0; i < 8; ++i) groups[i] = 0;
+    for (int i = 0; i < kSoftWarps; ++i) reinterpret_cast<int*>(smem + S::counts)[i] = 0;
+    *reinterpret_cast<long long*>(smem + S::words + 32) = p.wait_cycles;
     ptx::prefetch_tensormap(&kmap);
     ptx::prefetch_tensormap(&vmap);
   }
@@ -144,7 +230,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
   }
   __syncthreads();
   ptx::tc_fence_after();
-  const uint32_t tmem = *tmem_slot, tmem_o = tmem + 2 * N;
+  const uint32_t tmem = *tmem_slot, tmem_o = tmem + 2 * N, tmem_group = tmem + 3 * N;
 
   // every role walks the same segments: tiles [b0, b1) of the nb of unit (ls, head), whose places begin at `begin`
   struct Segment { int ls, head, b0, b1, nb, begin, places; };
@@ -298,7 +384,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
     constexpr uint32_t idesc = ptx::idesc_f16_f32(D, N, true, true);
     const uint32_t issues = ptx::elect_one();
     const uint64_t sv = ptx::smem_desc_sw128_mn(ptx::smem_u32(smem + S::wide) + S::kK * kWideBytes, kRawBytes), sp = ptx::smem_desc_sw128_mn(ptx::smem_u32(smem + S::p), kRawBytes);
-    int n = 0, seg = 0;
+    int n = 0, seg = 0, read = 0;
     bool ok = true;
     segments([&](const Segment& g) {
       ok = __all_sync(0xffffffffu, ok && (seg == 0 || ptx::mbar_wait(o_free, (seg - 1) & 1, abort_flag, p.wait_cycles)));
@@ -309,8 +395,26 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
         if (!ok) break;
         ptx::tc_fence_after();
         const uint64_t a = sv + slot * (kWideBytes >> 4), b = sp + ((PB == 2 ? pb : 0) * kPNext >> 4);
+        uint64_t left = groups[n & 7];
+        if (__all_sync(0xffffffffu, left == 0)) {          // (a vote, so that the warp is seen to stay together)
 #pragma unroll
-        for (int k = 0; k < kTile / 16; ++k) ptx::umma_f16_elected(tmem_o, a + (k * 2048 >> 4), b + (k * 2048 >> 4), idesc, i == g.b0 && k == 0 ? 0u : 1u, issues);
+          for (int k = 0; k < kTile / 16; ++k) ptx::umma_f16_elected(tmem_o, a + (k * 2048 >> 4), b + (k * 2048 >> 4), idesc, i == g.b0 && k == 0 ? 0u : 1u, issues);
+        }
+        while (left) {
+          const uint32_t blocks = (uint32_t)left & 0xFFu;
+          left >>= 8;
+#pragma unroll 1
+          for (int k = 0; k < kTile / 16; ++k)
+            if (blocks >> k & 1) ptx::umma_f16_elected(tmem_group, a + (k * 2048 >> 4), b + (k * 2048 >> 4), idesc, blocks & ((1u << k) - 1u) ? 1u : 0u, issues);
+          if (issues) ptx::umma_commit(group_done);
+          __syncwarp();
+          if (left) {                    // (behind the last group the next tile's weights say that it has been read)
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait(group_read, read++ & 1, abort_flag, p.wait_cycles));
+            if (!ok) break;
+            ptx::tc_fence_after();
+          }
+        }
+        if (!ok) break;
         if (issues) {
           ptx::umma_commit(pv_done + pb);
           ptx::umma_commit(v_empty + slot);
@@ -380,10 +484,10 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
       warps_meet(1 + kSoftWarps / 4, kSoftWarps * 32);
       if (lane == 0) ptx::mbar_arrive(q_full);
       float2 sc = make_float2(0.f, 0.f), sc_next = scales_of(blk0, page_next);
-      float vmost = 0.f;
-      uint32_t missing = 0;
+      float power = 0.f, factor = 0.f;
+      uint32_t missing = 0, lows = 0;              // blocks without a page, and with a scale far below their tile's unit
       bool unset = true;                           // no token so far: the references say nothing yet
-      float l[NC], vref = 0.f, vinv = 0.f;
+      float l[NC], vref = 0.f;
 #pragma unroll
       for (int c = 0; c < NC; ++c) l[c] = 0.f;
       // scores of the next tile: read before this tile's weights are given away, since loads wait for the products that are under way.  (With 128
@@ -408,27 +512,31 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
         if ((n & 3) == 0) {
           sc = sc_next;
           missing = __ballot_sync(0xffffffffu, sc.x == -1.f);
-          vmost = sc.y;
+          // O is in units of a power of two above every scale so far: this lane's block's tile's, and the weights' factor
+          float most = fmaxf(sc.y, 0.f);
 #pragma unroll
-          for (int o = 1; o < 8; o <<= 1) vmost = fmaxf(vmost, __shfl_xor_sync(0xffffffffu, vmost, o));
+          for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+#pragma unroll
+          for (int o = 8; o < 32; o <<= 1) {
+            const float before = __shfl_up_sync(0xffffffffu, most, o);
+            if (lane >= o) most = fmaxf(most, before);
+          }
+          power = most > vref ? power_above(most) : vref;
+          float inv = inverse_power(power);
+          lows = __ballot_sync(0xffffffffu, number(sc.y) > 0.f && sc.y * inv < kTileEven);
+          if (lows) inv = group_blocks(sc.y, lows, inv, tile, groups);
+          factor = sc.y * inv * kAttPScale;
           page_next = page_of(g, blk0 + 8 * (n + 4), len);
         }
         if ((n & 3) == 1) sc_next = scales_of(blk0 + 8 * (n + 3), page_next);
         const int block = (n & 3) * 8 + quad * 2 + (lane >> 4);
-        const float ks = __shfl_sync(0xffffffffu, sc.x, block), vs = __shfl_sync(0xffffffffu, sc.y, block), vtop = __shfl_sync(0xffffffffu, vmost, block);
+        const float ks = __shfl_sync(0xffffffffu, sc.x, block), wfac = __shfl_sync(0xffffffffu, factor, block), vnow = __shfl_sync(0xffffffffu, power, block);
         const int t0 = (g.b0 + n) * kTile, t = t0 + mine;
         const uint32_t absent = missing >> ((n & 3) * 8) & 0xFFu;     // blocks of the tile without a page
         const bool masked = absent || t0 + kTile > len - p.n_rows + 1;
-        // O is in units of a power of two above every scale so far
-        const bool grows = vtop > vref;
-        float vf = 1.f;
-        if (grows) {
-          const uint32_t to = min((__float_as_uint(vtop) & 0x7F800000u) + 0x00800000u, 0x7E800000u);
-          vinv = __uint_as_float(0x7F000000u - to);              // 1 / 2^k, exactly
-          vf = vref * vinv;
-          vref = __uint_as_float(to);
-        }
-        const float wfac = vs * vinv * kAttPScale;
+        const bool grows = vnow > vref;
+        const float vf = vref * inverse_power(vnow);
+        vref = vnow;
         auto wait_values = [&](int t) {            // the values' product of tile t is done
           if (t >= 0) ok = ptx::mbar_wait(pv_done + (t & 1), (t >> 1) & 1, abort_flag, p.wait_cycles) && ok;
         };
@@ -524,6 +632,10 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
         __syncwarp();
         if (lane == 0) {
           ptx::mbar_arrive(p_full + (tile & 1));
+        }
+        if (lows >> ((n & 3) * 8) & 0xFFu) {
+          add_groups<N>(smem, sc.y, vref, (n & 3) * 8, n == 0);
+          if (tid == 0) groups[tile & 7] = 0;              // (read before the first product)
         }
       }
       // ---- the segment's result ----

@@ -861,3 +861,109 @@ def test_attention_of_many_columns_that_begins_with_missing_pages(fmt, n_rows):
     c.attend(q, out=out)
     check_attention(c, ref_of(c), q, out, "bf16")
     assert (out[0, 11] == 0).all() and c.status() == 0
+
+
+def check_rows(c, r, q, out, dtype):
+    """As ``check_attention``, row by row from what the row sees: |error| <= half a step of the output, plus, per token that has a weight at all
+    (2^-100 of the row's largest one: below that it adds nothing to a float64 sum either), its weight's relative error (2^-12 in one fp16
+    piece, 2^-22 in two; twice the score's) and half of fp16's smallest step.  That step is 2^-24, of a weight times 128 times the block's
+    scale in units of a power of two that is at most 2^8 (and the power's factor of two) above the scale where one piece holds both: 2^-23 of
+    the token's value; two pieces hold the weight alone: 2^-31.  Rows that see a block into which an infinity was written are NaN."""
+    got, x = f64(out), f64(q)
+    hn, n_rows = x.shape[2] // r.heads, x.shape[3]
+    half, weight, step = (2.0 ** -8, 2.0 ** -12, 2.0 ** -23) if dtype == "bf16" else (2.0 ** -24, 2.0 ** -22, 2.0 ** -31)
+    for l, s in r.units():
+        k, v = r.rows("k", l, s)[0], r.rows("v", l, s)[0]
+        for h in range(x.shape[2]):
+            kk, vv = k[h // hn], v[h // hn]
+            for i in range(n_rows):
+                n = max(kk.shape[0] - n_rows + 1 + i, 0)
+                if n == 0:
+                    assert (got[l, s, h, i] == 0).all()
+                    continue
+                if np.isnan(vv[:n]).any():
+                    assert np.isnan(got[l, s, h, i]).all()
+                    continue
+                y = kk[:n] @ x[l, s, h, i] / np.sqrt(c.d)
+                w = np.exp(y - y.max())
+                w /= w.sum()
+                has = w > 2.0 ** -100 * w.max()
+                want, mag = w @ vv[:n], w @ np.abs(vv[:n])
+                top = (np.abs(kk[:n][has]) @ np.abs(x[l, s, h, i])).max() / np.sqrt(c.d)
+                err = ((c.d + 16) * 2.0 ** -23 + (0 if dtype == "bf16" else 2.0 ** -22)) * top + 2.0 ** -20
+                bound = half * np.abs(want) + 1.01 * mag * (weight + 2 * err) + step * w.max() * np.abs(vv[:n][has]).sum(0)
+                assert np.isfinite(got[l, s, h, i]).all()
+                worst = (np.abs(got[l, s, h, i] - want) / np.maximum(bound, 1e-300)).max()
+                assert worst <= 1, (l, s, h, i, worst)
+
+
+UNEVEN = [("bf16", 128, 1, 1), ("bf16", 128, 8, 2), ("bf16", 128, 8, 4), ("bf16", 128, 8, 8), ("bf16", 128, 8, 16), ("bf16", 64, 1, 2), ("bf16", 64, 8, 4),
+          ("f32", 128, 1, 2), ("f32", 128, 8, 2), ("f32", 64, 8, 4)]
+
+
+def uneven_cache(fmt, d, dtype, n, n_seqs=8):
+    """Two KV heads and sequences enough for runs of several tiles.  Scores are small but for a query channel that tells tokens apart."""
+    c = make(1, n_seqs, None, 2, d, n_seqs * (n // 64 + 1), n // 64 + 1, 64, fmt)
+    r = ref_of(c)
+    start = r.resize(np.full((1, n_seqs), n))
+    c.resize(lens_t([[n] * n_seqs]))
+    return c, r, start, rows((1, n_seqs, 2, n, d), dtype, 1, 0.1) * 0.5, rows((1, n_seqs, 2, n, d), dtype, 2, 0.1)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,d,hn,n_rows", UNEVEN)
+def test_attention_is_untouched_by_a_large_value_that_has_no_weight(fmt, dtype, d, hn, n_rows):
+    # one token, of every size, whose score is far below all others, early and late; its neighbours' codes are zeros, all other blocks count
+    c, r, start, K, V = uneven_cache(fmt, d, dtype, 2500)
+    for s, (at, size) in enumerate([(3, 2.0 ** 12), (3, 2.0 ** 26), (130, 2.0 ** 40), (700, 2.0 ** 30), (1280, 2.0 ** 60), (2499, 2.0 ** 40), (5, 2.0 ** 100), (64, 2.0 ** -60)]):
+        V[0, s, :, at] *= size
+        if size > 1:
+            K[0, s, :, at] = 0
+            K[0, s, :, at, 0] = -30000
+    c.append(K, V)
+    r.append(start, f64(K), f64(V))
+    q = rows((1, 8, 2 * hn, n_rows, d), dtype, 5, 0.2)
+    q[..., 0] = q[..., 0].abs() + 1
+    out = c.attend(q, max_len=100000)
+    check_rows(c, r, q, out, dtype)
+    assert torch.equal(out.clone(), c.attend(q, max_len=100000)) and c.status() == 0
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,d,hn,n_rows", [x for x in UNEVEN if x[3] > 1])
+def test_attention_is_untouched_by_values_that_a_row_does_not_see(fmt, dtype, d, hn, n_rows):
+    # the newest token's value is large: rows before it are what they are without it
+    c, r, start, K, V = uneven_cache(fmt, d, dtype, 2500)
+    clean = V.clone()
+    for s in range(8):
+        V[0, s, :, -1] *= 2.0 ** (14 * s)
+    q = rows((1, 8, 2 * hn, n_rows, d), dtype, 5, 0.2)
+    c.append(K, V)
+    r.append(start, f64(K), f64(V))
+    check_rows(c, r, q, c.attend(q, max_len=100000), dtype)
+    # with the same codes where the rows look: a block of its own for the large value
+    keep = torch.full((1, 8), 2496, dtype=torch.int32, device="cuda")
+    c.append(K, clean, start=torch.zeros((1, 8), dtype=torch.int32, device="cuda"))
+    c.append(K[:, :, :, 2496:].contiguous(), torch.cat([clean[:, :, :, 2496:2499], V[:, :, :, 2499:]], 3), start=keep)
+    r = ref_of(c)
+    check_rows(c, r, q, c.attend(q, max_len=100000), dtype)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,d,hn,n_rows", UNEVEN)
+def test_attention_over_blocks_of_every_size(fmt, dtype, d, hn, n_rows):
+    # values of sizes from 2^-60 to 2^60, block by block, in patterns that repeat inside a tile, rise, fall, and leave blocks of zeros; the
+    # weight lies on one size of blocks after the other.  The last pattern rises beyond the types' range: infinities
+    c, r, start, K, V = uneven_cache(fmt, d, dtype, 2500)
+    block = torch.arange(2500, device="cuda") // 16
+    sizes = [block % 8 * 12 - 40, block % 2 * 20, block // 8 * 6 - 60, 60 - block // 8 * 6, block * 7919 % 120 - 60, block % 3 * -9, (block == 40) * 60, block % 157]
+    for s, e in enumerate(sizes):
+        V[0, s] = (V[0, s].float() * torch.exp2(e.float())[:, None]).to(V.dtype)
+        K[0, s, :, :, 0] = -(e.float() * (s % 3) * 0.5).to(K.dtype)      # the larger the value, the less it counts: not, a little, in full
+    V[0, 4, :, 160:192] = 0
+    V[0, 5, :, 0:128] = 0
+    c.append(K, V)
+    r.append(start, f64(K), f64(V))
+    q = rows((1, 8, 2 * hn, n_rows, d), dtype, 5, 0.2) * 0.3
+    q[..., 0] = 2 * np.sqrt(d) * np.log(2)                               # a score falls by s % 3 powers of two for every power of the value
+    check_rows(c, r, q, c.attend(q, max_len=100000), dtype)
