@@ -435,16 +435,17 @@ spindlekv_status spindlekv_paged_append(const spindlekv_page_pool* pool, const s
  * already, if the model rotates them).
  *   q, out    device, [layer][seq][q head][row][d], fp32 or bf16, both the same; may not overlap
  *   n_rows    1 .. 16;  n_q_heads / n_kv_heads <= 8
- *   max_len   the longest sequence, as far as the host knows: it only sizes the split over the device, any length is served
+ *   max_len   the longest sequence, as far as the host knows: it sizes the split over the device and chooses the kernel for it.  Any length is
+ *             served, a hint far from the truth more slowly
  *   scale     0: 1 / sqrt(head_dim)
  *   ws        device scratch of spindlekv_paged_workspace_bytes bytes, 256-byte aligned, not to be shared by calls that may
  *             run at the same time
- * Sums and softmax statistics are fp32, in an order that the lengths, max_len and the device fix: the same call gives the same bits.
- * bf16 queries are multiplied as they are and the weights enter in 11 bits, to 2^-24 of the row's largest weight at worst (of two weights
- * whose ratio is beyond 2^12 the smaller one loses bits); fp32 queries and weights in 22 bits, to 2^-32.  Values of any size that a row does not see,
- * or whose weight is 0, leave the others as they are: block scales count in fp32, over 2^126 of range.  Sums of weight * value, relative to
- * the row's largest weight, are held in fp32 and have to stay inside its range.  The device status word of `ws` (a bounded wait that gave up) is read with
- * spindlekv_poll_status.
+ * Sums and softmax statistics are fp32, in an order that the lengths, max_len and the device fix: the same call gives the same bits.  bf16
+ * queries are multiplied as they are (the roundings of a score of int8 keys are relative to sum |q_i| times their block's largest element), and
+ * the weights enter in 11 bits, to 2^-24 of the row's largest weight at worst (of two weights whose ratio is beyond 2^12 the smaller one loses
+ * bits); fp32 queries and weights in 22 bits, to 2^-32.  Values of any size that a row does not see, or whose weight is 0, leave the
+ * others as they are: block scales count in fp32, over 2^126 of range.  Sums of weight * value, relative to the row's largest weight, are held
+ * in fp32 and have to stay inside its range.  The device status word of `ws` (a bounded wait that gave up) is read with spindlekv_poll_status.
  * UNSUPPORTED beyond 2^31 pairs of blocks in n_layers * n_seqs * n_kv_heads * max_pages * page_size: split the layers.
  */
 size_t spindlekv_paged_workspace_bytes(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t n_q_heads, int32_t n_rows);

@@ -78,7 +78,10 @@ __global__ void __launch_bounds__(kAttThreads, NT >= 2 ? 1 : 2) paged_attend_ker
   constexpr int VW = D / 32;                      // words of a V row per lane
   constexpr int COLS = 8 * NT;
   // int8 keys under one query piece enter as (code + 128) 2^-24, a subnormal fp16 number, which saves a subtraction per two of them;
-  // the scores lose 128 times the query's sum.  The accumulator is three times larger then, too much for fp32 queries only
+  // the scores lose 128 times the query's sum.  The accumulator's roundings are then relative to sum |q_i| (|code_i| + 128) in place of
+  // sum |q_i code_i|: three times as much where codes fill their range, a hundred times where one outlier channel has set the block's
+  // scale and the other codes are small.  Against sum |q_i| times the block's largest key that is 2^-19 at most, below what bf16 results show
+  // for scores up to some hundreds; too much for fp32 queries
   constexpr bool kOffset = FMT == SPINDLEKV_PAGED_INT8 && NP == 1 && NT == 1;
   constexpr int OP = D + 4;                       // row pitch of the partial outputs in shared memory
   constexpr int kHalf = kPagedBlock * D;          // bytes of a block's K, or V

@@ -967,3 +967,31 @@ def test_attention_over_blocks_of_every_size(fmt, dtype, d, hn, n_rows):
     q = rows((1, 8, 2 * hn, n_rows, d), dtype, 5, 0.2) * 0.3
     q[..., 0] = 2 * np.sqrt(d) * np.log(2)                               # a score falls by s % 3 powers of two for every power of the value
     check_rows(c, r, q, c.attend(q, max_len=100000), dtype)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,d,hn,n_rows", UNEVEN + [("bf16", 64, 3, 1), ("bf16", 128, 8, 1), ("f32", 128, 8, 4)])
+def test_attention_over_keys_with_outlier_channels(fmt, dtype, d, hn, n_rows):
+    """Three channels forty times the size of the others, which the queries leave alone: most codes are small.  int8 keys may enter the products with
+    128 added and have it taken off again: the d + 16 roundings of a score (2^-23 each) are then relative to sum |q_i| (|k_i| + 128 steps of
+    the block's scale) in place of sum |q_i k_i|.  A weight is off by that and by 2^-20 of the power function, twice over, and by its own
+    rounding, to half of fp16's smallest step at worst (``check_rows``; the largest weight is at most 1); a bf16 result by 2^-8 of itself."""
+    c, r, start, K, V = uneven_cache(fmt, d, dtype, 1500, n_seqs=3)
+    K *= 2
+    K[..., [5, d // 2, d - 1]] *= 40
+    c.append(K, V)
+    r.append(start, f64(K), f64(V))
+    q = rows((1, 3, 2 * hn, n_rows, d), dtype, 5, 0.2)
+    q[..., [5, d // 2, d - 1]] = 0
+    got, x = f64(c.attend(q)), f64(q)
+    want, mag, top = r.attend(x)
+    steps = max(r.scale["k"][p].max() for l, s in r.units() for p in r.pages[l, s, :r.count(r.lens[l, s])])
+    offset = 128 * steps * np.abs(x).sum(-1) / np.sqrt(d) if fmt == "int8" else 0 * top
+    assert fmt != "int8" or (offset > 64 * top).any()
+    err = (d + 16) * 2.0 ** -23 * (top + offset) + (0 if dtype == "bf16" else 2.0 ** -22 * top) + 2.0 ** -20
+    half, weight, step = (2.0 ** -8, 2.0 ** -12, 2.0 ** -23) if dtype == "bf16" else (2.0 ** -24, 2.0 ** -22, 2.0 ** -31)
+    big = max(np.abs(r.rows("v", l, s)[0]).max() for l, s in r.units())
+    bound = half * np.abs(want) + 1.01 * mag * (weight + 2 * err[..., None]) + step * 1500 * big
+    assert (np.abs(got - want) <= bound).all()
+    # and far inside that where no bound says so: rounding errors of both signs
+    assert np.sqrt(((got - want) ** 2).mean() / (want ** 2).mean()) < (2.0 ** -8 if dtype == "bf16" else 2.0 ** -16)
