@@ -46,13 +46,6 @@ constexpr int kBeamKeep = 256;         // candidates of a slice beyond which onl
 constexpr int kBeamTies = 512;         // candidates of a tile beyond which those equal to the bound are read off in order
 constexpr float kLog2e = 1.44269504f;
 
-// 2^x, to two units in the last place of fp32; results below the smallest normal number are 0
-__device__ __forceinline__ float pow2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // a key whose unsigned order is the order of the value, then of falling index; never 0
 __device__ __forceinline__ unsigned long long key_of(float x, int i) {
   const uint32_t b = __float_as_uint(x + 0.f);               // -0 and 0 are one value

@@ -163,6 +163,13 @@ __device__ __forceinline__ int block_exclusive_scan(int v, int* warp_sums, int& 
   return res;
 }
 
+// 2^x, to two units in the last place of fp32; results below the smallest normal number are 0
+__device__ __forceinline__ float pow2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // ---- counting blocks that bring something to a common end -----------------------------------------------
 // A word in the workspace counts arrivals.  A call finds it at zero, because the last arrival of the call before put it back, or finds
 // something that is no count (its upper bits are not the tag) and makes it one: the workspace needs no preparation.  Returns the word as it was

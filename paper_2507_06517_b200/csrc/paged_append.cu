@@ -22,7 +22,7 @@
 
 namespace skv {
 
-struct AppendParams {
+struct PagedAppendParams {
   Pool pool;
   Table table;
   View K, V;
@@ -174,7 +174,7 @@ template <> struct Raw8<float> {
 constexpr int kAppendThreads = 256;
 
 template <typename T, int FMT, int D>
-__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(AppendParams p) {
+__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(PagedAppendParams p) {
   constexpr int LPR = D / 8;            // lanes of a row
   constexpr int RPI = 32 / LPR;         // rows side by side in a warp
   constexpr int NI = kPagedBlock / RPI;
@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(AppendPara
 }
 
 template <typename T, int FMT>
-static void launch_append(const AppendParams& p, cudaStream_t st) {
+static void launch_append(const PagedAppendParams& p, cudaStream_t st) {
   const dim3 grid((p.n_items + kAppendThreads / 32 - 1) / (kAppendThreads / 32), p.table.n_layers * p.table.n_seqs);   // at most 8192 units
   LaunchScope ls(KC_PAGED_APPEND, st);
   if (p.pool.d == 64) paged_append_kernel<T, FMT, 64><<<grid, kAppendThreads, 0, st>>>(p);
@@ -269,7 +269,7 @@ static void launch_append(const AppendParams& p, cudaStream_t st) {
 spindlekv_status paged_append_impl(const spindlekv_page_pool& pool, const spindlekv_page_table& table, const int32_t* start, int max_new,
                                    const spindlekv_tensor& K, const spindlekv_tensor& V, int n_rows, const int32_t* idx, int idx_len,
                                    int idx_seq, cudaStream_t st) {
-  AppendParams p;
+  PagedAppendParams p;
   p.pool = make_pool(pool);
   p.table = make_table(table);
   p.K = make_view(K);

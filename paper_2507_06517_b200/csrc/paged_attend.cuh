@@ -34,12 +34,6 @@ struct AttendParams {
   int withhold;              // for tests: the block that does not ask for its first keys; -1: none
 };
 
-// 2^x, to two units in the last place of fp32; results below the smallest normal number are 0
-__device__ __forceinline__ float pow2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);

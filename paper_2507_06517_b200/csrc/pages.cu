@@ -370,14 +370,14 @@ __global__ void __launch_bounds__(kCopyThreads, 6) fork_kernel(ForkParams p) {
 
 // ---- compact ---------------------------------------------------------------------------------------------------------
 
-struct CompactParams {
+struct PagesCompactParams {
   Pool pool;
   Table table;
   int32_t* n_live;
   PagesWs ws;
 };
 
-__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CompactParams p) {
+__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PagesCompactParams p) {
   let_dependents_start();
   __shared__ int warp_sums[33];
   const int n = p.pool.n_pages, tid = threadIdx.x, per = votes_per_lane(p.pool), lane = tid & 31;
@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CompactParam
 
 // Block b maps the entries of unit b, b + gridDim, ...; then all blocks copy.
 template <int D>
-__global__ void __launch_bounds__(kCopyThreads, 4) compact_kernel(CompactParams p) {
+__global__ void __launch_bounds__(kCopyThreads, 4) compact_kernel(PagesCompactParams p) {
   wait_for_plan();
   const int units = p.table.n_layers * p.table.n_seqs, live = p.ws.hdr[kHdrPagesLive];
   for (int u = blockIdx.x; u < units; u += gridDim.x) {
@@ -523,7 +523,7 @@ spindlekv_status pages_fork_impl(const spindlekv_page_pool& pool, const spindlek
 
 spindlekv_status pages_compact_impl(const spindlekv_page_pool& pool, const spindlekv_page_table& table, int32_t* n_live, void* ws,
                                     size_t ws_bytes, cudaStream_t st) {
-  CompactParams p{make_pool(pool), make_table(table), n_live, {}};
+  PagesCompactParams p{make_pool(pool), make_table(table), n_live, {}};
   const spindlekv_status s = pages_ws(pool, table, ws, ws_bytes, &p.ws);
   if (s != SPINDLEKV_OK) return s;
   const int sms = sm_count();

@@ -214,3 +214,16 @@ def test_decode_entry_points_check_their_arguments():
     assert lib.spindlekv_rope_table(128, 0, 10000.0, p, None) == B.INVALID_ARG
     assert lib.spindlekv_decode_workspace_bytes(C.byref(packed), 8, 2, 128) == 0
     assert lib.spindlekv_decode_workspace_bytes(C.byref(batch), 8, 2, 128) >= 4 * 130 * 4 * 2
+
+
+def test_no_struct_of_the_library_has_two_definitions():
+    # all files share one namespace, and a type with two definitions in it is undefined behaviour, whatever the linker makes of it
+    import glob
+    from paper_2507_06517_b200 import build
+    seen = {}
+    for path in sorted(glob.glob(os.path.join(build.CSRC, "*.cu")) + glob.glob(os.path.join(build.CSRC, "*.cuh"))):
+        with open(path) as f:
+            for name in re.findall(r"^struct (\w+)\s*\{", f.read(), re.M):
+                assert name not in seen, (name, seen[name], path)
+                seen[name] = path
+    assert len(seen) > 10
