@@ -461,7 +461,7 @@ spindlekv_status spindlekv_paged_attend(const spindlekv_page_pool* pool, const s
  * total = score and all else at -infinity.
  *   logits      device [n_seqs * n_beams] rows of `vocab` elements, `row_stride` elements apart, fp32 or bf16, any alignment of
  *               the rows that the element type allows
- *   score       device [n_seqs * n_beams] fp32; with n_out = n_beams it may be `out_score` itself
+ *   score       device [n_seqs * n_beams] fp32; with n_out = n_beams it may be `out_score` itself, else the two may not overlap
  *   finished    device [n_seqs * n_beams] bytes (0: not finished), or NULL
  *   out_score   device out [n_seqs][n_out] fp32: total
  *   out_parent  device out [n_seqs][n_out]: row seq * n_beams + w, i.e. with n_out = n_beams the parents of spindlekv_pages_fork

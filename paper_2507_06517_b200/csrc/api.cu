@@ -424,6 +424,9 @@ spindlekv_status spindlekv_beam_select(int32_t n_seqs, int32_t n_beams, int32_t 
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == SPINDLEKV_F32 ? 4 : 2)) return SPINDLEKV_INVALID_ARG;
   if (finished && (eos < 0 || eos >= vocab)) return SPINDLEKV_INVALID_ARG;
   if (!beam_size_ok(n_seqs, n_beams, vocab, n_out)) return SPINDLEKV_UNSUPPORTED;
+  // a sequence's totals are written while other sequences' scores are read
+  const uintptr_t in = reinterpret_cast<uintptr_t>(score), res = reinterpret_cast<uintptr_t>(out_score);
+  if (in < res + (size_t)n_seqs * n_out * 4 && res < in + (size_t)n_seqs * n_beams * 4 && !(in == res && n_out == n_beams)) return SPINDLEKV_INVALID_ARG;
   return beam_select_impl(n_seqs, n_beams, vocab, n_out, logits, dtype, row_stride, score, finished, eos, out_score, out_parent,
                           out_token, ws, ws_bytes, (cudaStream_t)stream);
 }

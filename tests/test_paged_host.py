@@ -152,3 +152,15 @@ def test_the_hook_that_withholds_keys_can_be_set_and_restored():
     finally:
         B.spindlekv_set_tuning(B.TUNE_PAGED_WITHHOLD, -1)
     assert B.spindlekv_get_tuning(B.TUNE_PAGED_WITHHOLD) == -1
+
+
+def test_beam_refuses_scores_that_its_results_would_overwrite():
+    # a sequence's results are written while others' scores are still read: only the same rows of the same buffer may be both
+    def call(score, out, n=2, w=4, k=4):
+        return lib.spindlekv_beam_select(n, w, 100, k, P, B.F32, 100, C.c_void_p(score), None, 0, C.c_void_p(out), P, P, P, 0, None)
+
+    assert call(4096, 4096) == B.WORKSPACE_TOO_SMALL            # in place: all is well but the workspace given here
+    for score, out, k in ((4096, 4100, 4), (4124, 4096, 4), (4096, 4096, 8), (4096, 4096, 2), (4096, 4124, 8), (4156, 4096, 8)):
+        assert call(score, out, k=k) == B.INVALID_ARG
+    for score, out, k in ((4096, 4128, 4), (4128, 4096, 4), (4160, 4096, 8)):
+        assert call(score, out, k=k) == B.WORKSPACE_TOO_SMALL   # side by side
