@@ -181,3 +181,9 @@ def test_refusals():
         sel.run(x, s, finished=torch.zeros(2, device="cuda"))
     with pytest.raises(TypeError):
         sel.run(x.half(), s)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,w,vocab,k", [(200, 4, 9001, 5), (1, 2, 400000, 32), (3000, 1, 40, 7)])
+def test_more_rows_than_blocks_and_long_rows(dtype, n, w, vocab, k):
+    check(logits_of(n * w, vocab, dtype, vocab), torch.zeros(n * w, device="cuda"), w, k)

@@ -995,3 +995,58 @@ def test_attention_over_keys_with_outlier_channels(fmt, dtype, d, hn, n_rows):
     assert (np.abs(got - want) <= bound).all()
     # and far inside that where no bound says so: rounding errors of both signs
     assert np.sqrt(((got - want) ** 2).mean() / (want ** 2).mean()) < (2.0 ** -8 if dtype == "bf16" else 2.0 ** -16)
+
+
+@pytest.mark.parametrize("n_rows,hn", [(3, 8), (7, 8), (16, 8)])
+@pytest.mark.parametrize("n_layers,n_seqs", [(3, 41), (1, 740)])
+def test_attention_of_many_columns_over_many_sequences(n_layers, n_seqs, n_rows, hn):
+    # more sequences than lanes, and than threads; many of them empty or shorter than the new rows
+    c = make(n_layers, n_seqs, hn, 1, 128, n_layers * n_seqs * 6, 22, 32, "int8")
+    rng = np.random.default_rng(n_seqs + n_rows)
+    lens = np.where(rng.random((n_layers, n_seqs)) < 0.4, 0, rng.integers(1, 60, (n_layers, n_seqs)))
+    lens[rng.random((n_layers, n_seqs)) < 0.08] = 290
+    lens[-1, -1] = 700
+    r = fill(c, lens.tolist(), spread=0.3)
+    q = rows((n_layers, n_seqs, hn, n_rows, 128), "bf16", 5, 0.2)
+    out = torch.full_like(q, 7.0)
+    c.attend(q, out=out)
+    check_attention(c, r, q, out, "bf16")
+    assert c.status() == 0
+
+
+def test_page_operators_over_a_large_pool():
+    # the planning block walks more than one stretch of 32768 pages: free pages, holes and live pages beyond the first
+    n = 70001
+    c = make(2, 5, 2, 1, 64, n, 300, 16, "int8")
+    rng = np.random.default_rng(3)
+    taken = np.sort(rng.choice(n, 69000, replace=False))
+    held = torch.zeros(n, dtype=torch.int32)
+    held[torch.from_numpy(taken)] = 1                     # pages that another table holds
+    c.page_ref.copy_(held)
+    r = fill(c, [[4800, 37, 0, 16, 1000], [3000, 1, 5, 700, 99]])
+    same_state(c, r)
+    c.page_ref.sub_(held.cuda())                          # that table is gone: holes everywhere
+    r = ref_of(c)
+    assert int(c.compact()) == r.compact()
+    same_state(c, r)
+    assert r.fork([0, 0, 1, 0, 4])
+    c.fork(lens_t([0, 0, 1, 0, 4]))
+    same_state(c, r)
+    for lens in ([[4790, 4800, 30, 100, 999], [0, 3000, 0, 2990, 105]], [[0] * 5] * 2):
+        start = r.resize(np.array(lens))
+        assert start is not None
+        c.resize(lens_t(lens))
+        assert c.status() == 0 and np.array_equal(c.start.cpu().numpy(), start)
+        for what in ("ref", "lens", "pages"):
+            assert np.array_equal(getattr(ref_of(c), what), getattr(r, what)), what
+
+
+def test_fork_of_as_many_sequences_as_there_may_be():
+    c = make(1, 1024, 2, 1, 64, 6000, 6, 16, "e4m3")
+    rng = np.random.default_rng(1)
+    r = fill(c, rng.integers(0, 60, (1, 1024)).tolist())
+    parent = rng.integers(-1, 1024, 1024)
+    assert r.fork(parent)
+    c.fork(lens_t(parent))
+    assert c.status() == 0
+    same_state(c, r)
