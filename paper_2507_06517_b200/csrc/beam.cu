@@ -11,8 +11,9 @@
 // The last block of a sequence to arrive joins its slices: log-sum-exp of the beams from the slices' pieces (added in double), totals in
 // double, and the same selection over the slices' lists, 2048 entries at a time beside the best so far.  (A second kernel for that cost
 // 2 us more, and 3 us on the host.)
-// Measured: 4 beams x 32000 bf16 logits 8.5 us (slices 3.5, join 4.5: latency); 128 rows x 128256 fp32 23.7 us, a tile 1.9 to 2.5, of which the
-// exponentials are 1; more and smaller slices repeat the search for a bound and take 25 to 28.
+// Measured: 4 beams x 32000 bf16 logits 8.7 us (slices 3.5, join 4.5: latency); 128 rows x 128256 fp32 27.2 us (23.9 when the 66 MB of logits
+// still lie in L2), a tile 1.9 to 2.5, of which the exponentials are 1: load, exponentials and block barriers follow one another, issue slots 22%
+// busy.  More and smaller slices repeat the search for a bound and take 25 to 28 (in L2).
 #include <algorithm>
 
 #include <math_constants.h>

@@ -11,8 +11,9 @@
 // byte is the code; only a warp in which some |r| reaches s/2 (one in fifty) takes the second look.
 // E4M3: s is a power of two, x / s exact, the conversion instruction rounds once.
 //
-// Bound by memory: 4 layers x 4 prompts of 6000 fp32 rows on average, 8 heads, 175 us (1.0 GB, 5.7 TB/s, 89% of a copy's rate); 16 layers x
-// 1000 bf16 rows picked by a list 17.8 us (87%); one token for each of 96 sequences 3.6 us, which is launch and latency.
+// Bound by memory: 4 layers x 4 prompts of 6000 fp32 rows on average, 8 heads, 177 us (1.0 GB, 5.7 TB/s, 88% of a copy's rate); 16 layers x
+// 1000 bf16 rows picked by a list 22.6 us (69%; 18.0 when the 67 MB of rows still lie in L2): list entry, then row, then the end of the warp.  One
+// token for each of 96 sequences 3.8 us on the device, which is launch and latency; a call from Python takes 14, the host's.
 #include <algorithm>
 
 #include <cuda_fp16.h>

@@ -23,10 +23,11 @@
 // uneven the lengths are.  A unit that lies inside one run is finished there; of the others each run leaves (m, sum, O), which a second
 // kernel joins in the order of the runs.
 //
-// Measured (device time): 16384 tokens, 8 KV heads, 32 query heads 14.9 us, of which the loop is 5 at the copy rate and the rest set-up
-// (4.5), join (4) and launch; 8 sequences of 10000 on average 45 us (4.6 TB/s); 4 x 16384 tokens with 4 to 8 columns per KV head 33 to 36 us
-// (4.1 TB/s), 16 columns 43, with fp32 queries 36 to 52; 32 columns of fp32 queries 87 (two column tiles and more have the SM to themselves, eight
-// warps: latency), 128 columns 281 (four passes).  More than 16 bf16 columns of 128 elements take paged_attend_tiles.cu.
+// Measured (device time): 16384 tokens, 8 KV heads, 32 query heads 15.0 us, of which the loop is 5 at the copy rate and the rest set-up
+// (4.5), join (4) and launch; 8 sequences of 2048 to 16384, 13000 on average (213 MB), 46.6 us (4.6 TB/s); 4 x 16384 tokens with 4 to 8 columns per KV
+// head 34 to 36 us (4.0 TB/s), 16 columns 41 to 44, with fp32 queries 37 to 54; 32 columns of fp32 queries 88 (E4M3) and 92 (int8) (two column tiles
+// and more have the SM to themselves, eight warps: latency), 128 columns 281 and 297 (four passes).  More than 16 bf16 columns of 128 elements take
+// paged_attend_tiles.cu.
 #include <algorithm>
 
 #include "paged_attend.cuh"
@@ -741,7 +742,7 @@ static spindlekv_status launch_attend(AttendParams& p, const CUtensorMap& kmap, 
   const int64_t line = (int64_t)n_ls * p.units_per * ceil_div((int)std::min<int64_t>(max_len, capacity), 2 * kPagedBlock);   // pairs
   if ((int64_t)n_ls * p.units_per * ((capacity + 2 * kPagedBlock - 1) / (2 * kPagedBlock) + kSetUp) > 0x7FFFFFFF) return SPINDLEKV_UNSUPPORTED;
   // Short units (two pairs per warp at most) gain nothing from being split: a block for each, and no second kernel (190 tokens, two KV
-  // heads: 4.6 us in place of 6.0).  Whatever the lengths turn out to be, both ways serve them
+  // heads: 5.4 us in place of 6.0).  Whatever the lengths turn out to be, both ways serve them
   const int64_t units = (int64_t)n_ls * p.units_per;
   p.whole_units = line <= units * 2 * kAttWarps && units <= 0xFFFF;
   const int runs = p.whole_units ? (int)units : (int)std::min<int64_t>(std::min(slots, kAttMaxRuns), std::max<int64_t>((line + kAttWarps - 1) / kAttWarps, 1));

@@ -21,7 +21,7 @@
 // Split.  The line of all units' tiles is cut into equal runs, one per SM, and the parts of a unit are joined as for few columns.
 //
 // Measured (4 sequences x 16384 tokens, 8 KV heads, int8; beside it the kernel for few columns, which reads the codes once per 32 columns): 32
-// columns 50 us (64), 64 columns 76 (101), 128 columns 124 (179); 6 x 26000 tokens, 32 columns 105 us a call (117), i.e. 3.1 TB/s.  Bound by the
+// columns 50 us (64), 64 columns 76 (101), 128 columns 124 (179); 6 x 26000 tokens, 32 columns 97 us (117), i.e. 3.4 TB/s.  Bound by the
 // weights' warps: of 2000 cycles per tile at 32 columns (memory would allow 1450) they wait for 500; issue slots are 50% busy, the products
 // take 45 cycles per instruction (360 of 8 steps), widening 600 per tile of codes.  A unit's beginning and end are 7 us, its first tile among them.
 // The way out for uneven tiles costs the others registers (48.2, 71, 118.5 without it); with a block of 2^40 in front of every sequence, against which
@@ -732,13 +732,13 @@ bool paged_attend_tiles(AttendParams& p, int format, int max_len, cudaStream_t s
   const int n_ls = p.table.n_layers * p.table.n_seqs, n = p.cols <= 32 ? 32 : p.cols <= 64 ? 64 : 128;
   const int64_t capacity = (int64_t)p.table.max_pages * p.pool.ps;
   const size_t smem = n == 32 ? TilesSmem<32>::bytes(n_ls) : n == 64 ? TilesSmem<64>::bytes(n_ls) : TilesSmem<128>::bytes(n_ls);
-  if (p.cols <= 16 || p.cols > 128 || smem > 227 * 1024) return false;   // (16 columns, 4 x 16384 tokens: 43 us in the other kernel, 50 here)
+  if (p.cols <= 16 || p.cols > 128 || smem > 227 * 1024) return false;   // (16 columns, 4 x 16384 tokens: 44 us in the other kernel, 51 here)
   const int64_t units = (int64_t)n_ls * p.pool.heads, tiles = units * ((std::min<int64_t>(max_len, capacity) + kTile - 1) / kTile);
   // Short units, if the other kernel has a block for each at once (4 sequences of 350 tokens, 8 KV heads: 15.7 us there with 32 columns, 16.1 with
-  // 64, 16.4 with 128; here 15.3, 21.4, 34.9.  32 sequences: 31, 61, 108 there; here 30, 43, 71)
+  // 64, 16.2 with 128; here 15.3, 22.2, 35.0.  32 sequences: 31, 60, 108 there; here 30, 45, 72)
   if (max_len <= 4 * kTile && units * ceil_div(p.cols, 32) <= 148) return false;
   // many columns over few tiles, which do not make up for the longer beginning and end (128 columns, one sequence of 1200 tokens: 27 us there, 31
-  // here; of 5000: 36 and 37; two of 5000: 48 and 42)
+  // here; of 5000: 36 and 37; two of 5000: 48 and 43)
   if (p.cols > 64 && tiles < 200) return false;
   p.groups = 1;
   p.units_per = p.pool.heads;
