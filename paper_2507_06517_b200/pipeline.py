@@ -684,7 +684,8 @@ class SpindleKVPagedCache(_OnDevice):
     def attend(self, q: torch.Tensor, out: Optional[torch.Tensor] = None, max_len: Optional[int] = None, scale: float = 0.0,
                layer: Optional[int] = None, stream=None) -> torch.Tensor:
         """Attention of the last ``rows`` tokens, ``q`` ``[n_layers or 1, n_seqs, H_q, rows, d]``.  Without ``out`` the result lies in a
-        buffer of this object that the next call of the same shape overwrites.  ``max_len`` (the longest sequence, the capacity by
+        buffer of this object that the next call of the same shape overwrites, another layer's too; a buffer per shape is kept as long as the
+        object, since recorded graphs write into them.  ``max_len`` (the longest sequence, the capacity by
         default) sizes the split and chooses the kernel: a cache with far more room than tokens is served faster with it."""
         if self._elsewhere():
             with torch.cuda.device(self.device):
