@@ -21,11 +21,11 @@
 // Split.  The line of all units' tiles is cut into equal runs, one per SM, and the parts of a unit are joined as for few columns.
 //
 // Measured (4 sequences x 16384 tokens, 8 KV heads, int8; beside it the kernel for few columns, which reads the codes once per 32 columns): 32
-// columns 50 us (64), 64 columns 76 (101), 128 columns 124 (179); 6 x 26000 tokens, 32 columns 97 us (117), i.e. 3.4 TB/s.  Bound by the
+// columns 49 us (64), 64 columns 73 (101), 128 columns 124 (179); 6 x 26000 tokens, 32 columns 97 us (117), i.e. 3.4 TB/s.  Bound by the
 // weights' warps: of 2000 cycles per tile at 32 columns (memory would allow 1450) they wait for 500; issue slots are 50% busy, the products
 // take 45 cycles per instruction (360 of 8 steps), widening 600 per tile of codes.  A unit's beginning and end are 7 us, its first tile among them.
 // The way out for uneven tiles costs the others registers (48.2, 71, 118.5 without it); with a block of 2^40 in front of every sequence, against which
-// all later tiles are uneven (one group each), 76, 103 and 150 us, with four sizes in turn (four groups) 141, 177 and 241.
+// all later tiles are uneven (one group each), 75, 100 and 145 us, with four sizes in turn (four groups) 140, 177 and 237.
 // Tried: fewer and wider warps for the weights (eight: 60 us at 32 columns), two groups of them that take turns at the tiles (73), two tiles at a
 // time (53, as one at a time then), eight widening warps (50), one thread issuing both products (65), a box of 16 tokens per copy (180 cycles per
 // copy instruction).
@@ -89,7 +89,7 @@ struct TilesSmem {
 static_assert(TilesSmem<32>::fm % 16 == 0 && TilesSmem<64>::fm % 16 == 0 && TilesSmem<128>::fm % 16 == 0 && TilesSmem<32>::bars % 1024 == 0 &&
               TilesSmem<64>::bars % 1024 == 0 && TilesSmem<128>::bars % 1024 == 0, "alignment of what is read in 16 bytes, and of the tiles");
 
-// ---- uneven tiles (rare, and out of line so that the loop over the others has its registers to itself) ----
+// ---- uneven tiles (rare; the loop over the others is to have its registers to itself) ----
 // Lanes hold the V scales of the 32 blocks of four tiles.  A scale that is a number, or 0: zeros alone, NaN, no page
 __device__ __forceinline__ float number(float scale) { return scale > 0.f && scale < CUDART_INF_F ? scale : 0.f; }
 // the next power of two, and 1 / a power of two
@@ -122,9 +122,9 @@ __device__ __noinline__ float group_blocks(float scale, uint32_t lows, float eve
   return mine;
 }
 // Adds the groups' products to O, one after the other as they are done.  (What it needs it finds in shared memory: arguments would be kept in registers
-// by the loop that hardly ever calls.)
+// by the loop that hardly ever comes here: 50.2 and 74.4 us with 32 and 64 columns in place of 49.5 and 72.7.)
 template <int N>
-__device__ __noinline__ void add_groups(uint8_t* smem, float scale, float ref, int first, bool begins) {
+__device__ __forceinline__ void add_groups(uint8_t* smem, float scale, float ref, int first, bool begins) {
   using S = TilesSmem<N>;
   constexpr int NC = N * 4 / kSoftWarps;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -627,15 +627,19 @@ __global__ void __launch_bounds__(kTilesThreads, 1) paged_attend_tiles_kernel(co
         }
         unset = unset && absent == 0xFFu;
         ptx::fence_proxy_async();
-        if (AHEAD && n + 1 < n_it) read_scores(tile + 1);
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          ptx::mbar_arrive(p_full + (tile & 1));
-        }
         if (lows >> ((n & 3) * 8) & 0xFFu) {
+          // (the next tile's scores are read afterwards: their registers are what the additions need)
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(p_full + (tile & 1));
           add_groups<N>(smem, sc.y, vref, (n & 3) * 8, n == 0);
           if (tid == 0) groups[tile & 7] = 0;              // (read before the first product)
+          if (AHEAD && n + 1 < n_it) read_scores(tile + 1);
+        } else {
+          if (AHEAD && n + 1 < n_it) read_scores(tile + 1);
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(p_full + (tile & 1));
         }
       }
       // ---- the segment's result ----
