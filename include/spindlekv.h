@@ -454,6 +454,30 @@ spindlekv_status spindlekv_paged_attend(const spindlekv_page_pool* pool, const s
                                         void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Causal attention of a prompt's rows over its keys and values.  `keys` describes K and V, `rows` q and out (NULL: the same tokens, the whole
+ * prompt); both have the same layers and sequences, each packed, padded (layer_lens) or of equal lengths as it likes.  The n_r rows of a sequence
+ * are the last ones of its n_k tokens: row i sees the keys 0 .. n_k - n_r + i.  For query head g of KV head j's group
+ *     out_i = softmax_t( q_i . K_t * scale ) V_t ,   lse_i = log sum_t exp( q_i . K_t * scale ) .
+ * A row that sees no key gives zeros and lse = -infinity.  Rows behind a sequence's last one, and columns of lse without a row, are left as they were.
+ *   q, K, V, out  device, fp32 or bf16, all the same; out shares memory with none of them
+ *   scale     >= 0; 0: 1 / sqrt(head_dim)
+ *   lse       device out, optional [n_layers][n_q_heads][T] with the T columns of `rows`
+ *   ws        device scratch of spindlekv_prompt_workspace_bytes bytes, 256-byte aligned, not to be shared by calls that may run at the same time; needs
+ *             no preparation
+ * Sums, softmax statistics and out are formed in fp32, in an order that the arguments and the lengths fix: the same call gives the same bits.  bf16: the
+ * weights are rounded to bf16 where they meet the values.  fp32: every factor enters in three pieces of 8 bits, six products of them; products below
+ * 2^-24 of the largest are left out.  Keys and values that a row does not see do not reach it, not even if they are NaN or infinite; of those that it
+ * sees, a NaN or an infinity leaves a NaN or an infinity.  A wait that gave up shows in the status word of `ws` (spindlekv_poll_status).
+ * UNSUPPORTED: layer_lens per head, more than 128 query heads per KV head, 65535 (layer, sequence) pairs, tensors that repeat memory (a stride of 0
+ * where there is more than one).
+ */
+size_t spindlekv_prompt_workspace_bytes(const spindlekv_batch* keys, const spindlekv_batch* rows, int32_t n_q_heads, int32_t n_kv_heads,
+                                        int32_t head_dim, int32_t dtype);
+spindlekv_status spindlekv_prompt_attend(const spindlekv_batch* keys, const spindlekv_batch* rows, int32_t n_q_heads, int32_t n_kv_heads,
+                                         int32_t head_dim, float scale, spindlekv_tensor q, spindlekv_tensor K, spindlekv_tensor V,
+                                         spindlekv_tensor out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Beam search's selection: among the continuations (beam w, token t) of a sequence the n_out with the largest
  *     total = score[w] + logits[w][t] - log sum_u exp(logits[w][u]) ,
  * best first, ties to the lower w * vocab + t.  The totals are formed and compared in double precision from a log-sum-exp
@@ -497,7 +521,7 @@ int64_t spindlekv_launch_count(int32_t reset);
  * spindlekv_timing_read synchronises the recorded events and returns, for kernel class `which`
  * (0 window-score, 1 top-k, 2 norms, 3 similarity, 4 neighbour lists, 5 greedy cover, 6 entry numbering, 7 gather,
  * 8 the bit-matrix pass of the similarity kernel over units that overflowed their record pool, 9 decode attention,
- * 10 paged attention, 11 paged append, 12 page tables and page copies, 13 beam selection),
+ * 10 paged attention, 11 paged append, 12 page tables and page copies, 13 beam selection, 14 prompt attention, 15 logits),
  * the summed milliseconds and the number of launches since the last spindlekv_timing_enable call.
  */
 void spindlekv_timing_enable(int32_t on);

@@ -22,7 +22,7 @@ WS_EVICT, WS_CODEBOOK = 0, 1
 PAGED_INT8, PAGED_E4M3 = 0, 1
 PAGED_BLOCK = 16
 KERNEL_CLASSES = ("window_score", "topk", "norms", "similarity", "degree", "greedy", "finalise", "gather",
-                  "similarity_fallback", "decode", "paged_attend", "paged_append", "pages", "beam")
+                  "similarity_fallback", "decode", "paged_attend", "paged_append", "pages", "beam", "prompt", "logits")
 
 
 class SpindleKVError(RuntimeError):
@@ -127,6 +127,11 @@ def _load() -> C.CDLL:
     lib.spindlekv_paged_attend.restype = C.c_int32
     lib.spindlekv_paged_attend.argtypes = [pool, table, C.c_int32, C.c_int32, C.c_int32, C.c_float, _Tensor, _Tensor, C.c_void_p,
                                            C.c_size_t, C.c_void_p]
+    lib.spindlekv_prompt_workspace_bytes.restype = C.c_size_t
+    lib.spindlekv_prompt_workspace_bytes.argtypes = [C.POINTER(_Batch), C.POINTER(_Batch)] + [C.c_int32] * 4
+    lib.spindlekv_prompt_attend.restype = C.c_int32
+    lib.spindlekv_prompt_attend.argtypes = [C.POINTER(_Batch), C.POINTER(_Batch), C.c_int32, C.c_int32, C.c_int32, C.c_float, _Tensor, _Tensor, _Tensor, _Tensor,
+                                            C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.spindlekv_beam_workspace_bytes.restype = C.c_size_t
     lib.spindlekv_beam_workspace_bytes.argtypes = [C.c_int32] * 4
     lib.spindlekv_beam_select.restype = C.c_int32
@@ -454,6 +459,19 @@ def spindlekv_paged_attend(pool: PagePool, table: PageTable, n_q_heads: int, n_r
                            out: _Tensor, ws: torch.Tensor, stream=None) -> None:
     _check(_lib.spindlekv_paged_attend(pool.c, table.c, n_q_heads, n_rows, max_len, scale, q, out, _ptr(ws), _bytes(ws), _stream(stream)),
            "spindlekv_paged_attend")
+
+
+def spindlekv_prompt_workspace_bytes(keys: Batch, rows: Optional[Batch], n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int) -> int:
+    kk, rr = keys.c(), None if rows is None else rows.c()
+    return int(_lib.spindlekv_prompt_workspace_bytes(kk, rr, n_q_heads, n_kv_heads, head_dim, dtype))
+
+
+def spindlekv_prompt_attend(keys: Batch, rows: Optional[Batch], n_q_heads: int, n_kv_heads: int, head_dim: int, scale: float, q: _Tensor, K: _Tensor, V: _Tensor,
+                            out: _Tensor, lse: Optional[torch.Tensor], ws: torch.Tensor, stream=None) -> None:
+    """``lse``: ``[n_layers, n_q_heads, T]`` fp32 or None.  ``rows`` None: every token is a row."""
+    kk, rr = (None if b is None else b if isinstance(b, _Batch) else b.c() for b in (keys, rows))
+    _check(_lib.spindlekv_prompt_attend(kk, rr, n_q_heads, n_kv_heads, head_dim, scale, q, K, V, out, _ptr(lse), _ptr(ws), _bytes(ws), _stream(stream)),
+           "spindlekv_prompt_attend")
 
 
 def spindlekv_beam_workspace_bytes(n_seqs: int, n_beams: int, vocab: int, n_out: int) -> int:

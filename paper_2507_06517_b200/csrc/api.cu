@@ -73,6 +73,11 @@ spindlekv_status beam_select_impl(int n_seqs, int n_beams, int vocab, int k, con
                                   const float* score, const uint8_t* finished, int eos, float* out_score, int32_t* out_parent,
                                   int32_t* out_token, void* ws, size_t ws_bytes, cudaStream_t st);
 
+size_t prompt_workspace_bytes(const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int n_kv_heads, int head_dim, int dtype);
+spindlekv_status prompt_attend_impl(const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int n_kv_heads, int head_dim, float scale,
+                                    const spindlekv_tensor& q, const spindlekv_tensor& k, const spindlekv_tensor& v, const spindlekv_tensor& out, float* lse, void* ws,
+                                    size_t ws_bytes, cudaStream_t st);
+
 spindlekv_status selftest_mbarrier_impl(uint32_t* hdr, long long wait_cycles, cudaStream_t st);
 
 // ---- limits that tests may tighten --------------------------------------------------------------
@@ -429,6 +434,39 @@ spindlekv_status spindlekv_beam_select(int32_t n_seqs, int32_t n_beams, int32_t 
   if (in < res + (size_t)n_seqs * n_out * 4 && res < in + (size_t)n_seqs * n_beams * 4 && !(in == res && n_out == n_beams)) return SPINDLEKV_INVALID_ARG;
   return beam_select_impl(n_seqs, n_beams, vocab, n_out, logits, dtype, row_stride, score, finished, eos, out_score, out_parent,
                           out_token, ws, ws_bytes, (cudaStream_t)stream);
+}
+
+static spindlekv_status prompt_shape_status(const spindlekv_batch* keys, const spindlekv_batch* rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                            int32_t dtype) {
+  if (!batch_ok(keys, 0) || !batch_ok(rows, 0)) return SPINDLEKV_INVALID_ARG;
+  if (keys->n_layers != rows->n_layers || keys->n_seqs != rows->n_seqs) return SPINDLEKV_INVALID_ARG;
+  if (n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads) return SPINDLEKV_INVALID_ARG;
+  if (dtype != SPINDLEKV_F32 && dtype != SPINDLEKV_BF16) return SPINDLEKV_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return SPINDLEKV_UNSUPPORTED;
+  if (n_q_heads / n_kv_heads > 128 || keys->layer_lens_heads || rows->layer_lens_heads) return SPINDLEKV_UNSUPPORTED;
+  if ((int64_t)rows->n_layers * rows->n_seqs > 65535 || n_kv_heads > 1024) return SPINDLEKV_UNSUPPORTED;
+  if (keys->max_len > (1 << 30) || rows->max_len > (1 << 30)) return SPINDLEKV_UNSUPPORTED;   // positions and their differences are 32-bit
+  return SPINDLEKV_OK;
+}
+
+size_t spindlekv_prompt_workspace_bytes(const spindlekv_batch* keys, const spindlekv_batch* rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                        int32_t dtype) {
+  if (!rows) rows = keys;
+  if (prompt_shape_status(keys, rows, n_q_heads, n_kv_heads, head_dim, dtype) != SPINDLEKV_OK) return 0;
+  return prompt_workspace_bytes(*keys, *rows, n_q_heads, n_kv_heads, head_dim, dtype);
+}
+
+spindlekv_status spindlekv_prompt_attend(const spindlekv_batch* keys, const spindlekv_batch* rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float scale,
+                                         spindlekv_tensor q, spindlekv_tensor k, spindlekv_tensor v, spindlekv_tensor out, float* lse, void* ws, size_t ws_bytes,
+                                         void* stream) {
+  if (!rows) rows = keys;
+  const spindlekv_status ps = prompt_shape_status(keys, rows, n_q_heads, n_kv_heads, head_dim, q.dtype);
+  if (ps != SPINDLEKV_OK) return ps;
+  if (!tensor_ok(q) || !tensor_ok(k) || !tensor_ok(v) || !tensor_ok(out) || !ws_ok(ws)) return SPINDLEKV_INVALID_ARG;
+  if (!(scale >= 0.f && scale < INFINITY) || reinterpret_cast<uintptr_t>(lse) % 4) return SPINDLEKV_INVALID_ARG;
+  if (out.ptr == q.ptr || out.ptr == k.ptr || out.ptr == v.ptr) return SPINDLEKV_INVALID_ARG;
+  if (k.dtype != q.dtype || v.dtype != q.dtype || out.dtype != q.dtype) return SPINDLEKV_UNSUPPORTED;
+  return prompt_attend_impl(*keys, *rows, n_q_heads, n_kv_heads, head_dim, scale, q, k, v, out, lse, ws, ws_bytes, (cudaStream_t)stream);
 }
 
 spindlekv_status spindlekv_poll_status(const void* ws, int32_t* device_status, int32_t* detail) {

@@ -1,0 +1,600 @@
+// Causal attention of a prompt's rows over its keys and values, bf16, grouped heads.
+//
+// Row i of n_r over n_k keys sees the first n_k - n_r + i + 1 of them:  O_i = sum_j p_ij V_j / sum_j p_ij,  p_ij = 2^(c q_i.k_j - m_i).
+//
+// A tile of 128 rows holds 128 / hn positions of all hn query heads of a KV head, so that keys and values are read once for the group and the
+// triangle that is computed for nothing shrinks with the positions of a tile; a block has two tiles and walks 128 keys at a time:
+//     S_w [128 rows x 128 keys] = Q_w K^T      both operands in shared memory, d contiguous
+//     O_w [128 rows x d]       += P_w V        P_w in tensor memory, where S_w was; V read transposed
+// Tensor memory: S_0, S_1, O_0, O_1.
+//
+// Roles: two warpgroups turn scores into weights, a thread for each row of their tile; one warp asks for Q, K and V (TMA); one issues the
+// products.  While one tile's weights are formed the products of the other run.  The reference m of a row moves only when a score exceeds
+// it by 2^8 (then O is multiplied by the row's thread: the products that wrote it are done when the scores that follow them are).
+// Sums and references are fp32; the weights enter the second product in bf16, where values are, to half a step of 2^-8: as much as the result's
+// own rounding, and independent from key to key.
+//
+// Values that a row does not see are multiplied by 0, which does nothing unless they are NaN or infinite.  A result that is NaN though its sum
+// is not says so, and its item is done again, with the tiles that hide keys from some row multiplied by hand.
+#include <algorithm>
+
+#include "args.cuh"
+#include "prompt_attend.cuh"
+
+namespace skv {
+
+// Three warpgroups of 168 registers a thread; the two with rows take 208 and leave the third 88 (2 x 208 + 88 = 3 x 168).
+constexpr int kPromptThreads = 384, kAskRole = 8, kIssueRole = 9;
+constexpr int kPromptItemSlots = 4;
+
+template <int D>
+struct PromptSmem {
+  static constexpr int kTile = kPromptRows * D * 2;                // bytes of a tile of rows, keys or values
+  static constexpr int kHalf = kPromptRows * 128;                  // of its 64 elements side by side
+  static constexpr int kRing = D == 128 ? 5 : 8;
+  static constexpr int q = 0, ring = 2 * kTile, bars = ring + kRing * kTile;
+  static constexpr int kBars = 2 * kRing + 2 + 2 * 4 + 2 * kPromptItemSlots + 1;
+  static constexpr int words = bars + kBars * 8;                   // abort flags [2], TMEM address, redo at all, [4] copies that were asked for
+  static constexpr int items = (words + 32 + 15) / 16 * 16;
+  static constexpr int redo = items + kPromptItemSlots * (int)sizeof(PromptItem);
+  static constexpr int bytes = 1024 + redo + kPromptMaxItems / 8;
+};
+static_assert(PromptSmem<128>::bytes <= 227 * 1024, "shared memory");
+
+// a x b + c of two numbers at a time
+__device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
+  unsigned long long x, y, z, r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(b.x), "f"(b.y));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(z) : "f"(c.x), "f"(c.y));
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+  float2 o;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(o.x), "=f"(o.y) : "l"(r));
+  return o;
+}
+__device__ __forceinline__ float2 add_pair(float2 a, float2 b) {
+  unsigned long long x, y, r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(b.x), "f"(b.y));
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+  float2 o;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(o.x), "=f"(o.y) : "l"(r));
+  return o;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// What masked tiles give to 32 elements of a row, key by key: the tiles whose values are not all numbers.  Rare
+template <int D>
+__device__ __noinline__ void add_by_hand(const PromptParams& p, const PromptItem& it, int layer, int seq, int head, int pos, int from, int to, float ref, int d0,
+                                         float (&o)[32]) {
+  const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q.ptr) + row_offset(p.q, p.rows, layer, seq, it.base_r, head, pos);
+  for (int j = from; j < to; ++j) {
+    const __nv_bfloat16* k = reinterpret_cast<const __nv_bfloat16*>(p.k.ptr) + row_offset(p.k, p.keys, layer, seq, it.base_k, it.head, j);
+    const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.v.ptr) + row_offset(p.v, p.keys, layer, seq, it.base_k, it.head, j) + d0;
+    float s = 0.f;
+    for (int d = 0; d < D; d += 8) {
+      float a[8], b[8];
+      load8(q + d, a);
+      load8(k + d, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s = fmaf(a[i], b[i], s);
+    }
+    const float w = pow2(fmaf(s, p.scale, -ref));
+#pragma unroll
+    for (int d = 0; d < 32; d += 8) {
+      float b[8];
+      load8(v + d, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[d + i] = fmaf(w, b[i], o[d + i]);
+    }
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+                                                                          const __grid_constant__ CUtensorMap vmap, const __grid_constant__ PromptParams p) {
+  using S = PromptSmem<D>;
+  using T = __nv_bfloat16;
+  constexpr int KT = 128, RING = S::kRing, SLOTS = kPromptItemSlots;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint64_t* kv_full = reinterpret_cast<uint64_t*>(smem + S::bars);
+  uint64_t *kv_empty = kv_full + RING, *q_full = kv_empty + RING, *q_empty = q_full + 1, *s_full = q_empty + 1, *p_full = s_full + 2, *o_full = p_full + 2,
+           *o_empty = o_full + 2, *item_full = o_empty + 2, *item_empty = item_full + SLOTS, *drained = item_empty + SLOTS;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::words);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::words) + 2;
+  volatile int* any_redo = reinterpret_cast<volatile int*>(smem + S::words) + 3;
+  volatile int* asked = reinterpret_cast<volatile int*>(smem + S::words) + 4;    // keys or values, rows
+  PromptItem* items = reinterpret_cast<PromptItem*>(smem + S::items);
+  uint32_t* redo = reinterpret_cast<uint32_t*>(smem + S::redo);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if (tid == 0) {
+    for (int i = 0; i < RING; ++i) { ptx::mbar_init(kv_full + i, 1); ptx::mbar_init(kv_empty + i, 1); }
+    ptx::mbar_init(q_full, 1);
+    ptx::mbar_init(q_empty, 1);
+    for (int w = 0; w < 2; ++w) {
+      ptx::mbar_init(s_full + w, 1);
+      ptx::mbar_init(p_full + w, 4);
+      ptx::mbar_init(o_full + w, 1);
+      ptx::mbar_init(o_empty + w, 4);
+    }
+    for (int i = 0; i < SLOTS; ++i) { ptx::mbar_init(item_full + i, 1); ptx::mbar_init(item_empty + i, 9); }
+    ptx::mbar_init(drained, 1);
+    ptx::fence_barrier_init();
+    abort_flag[0] = abort_flag[1] = 0;
+    *any_redo = 0;
+    asked[0] = asked[1] = 0;
+    ptx::prefetch_tensormap(&qmap);
+    ptx::prefetch_tensormap(&kmap);
+    ptx::prefetch_tensormap(&vmap);
+  }
+  for (int i = tid; i < kPromptMaxItems / 32; i += kPromptThreads) redo[i] = 0;
+  // rows that no copy fills (hn does not divide 128) hold zeros
+  for (int i = p.pt * p.hn * 8 + tid; i < kPromptRows * 8; i += kPromptThreads)
+    for (int h = 0; h < 2 * D / 64; ++h) *reinterpret_cast<uint4*>(smem + S::q + h * S::kHalf + i * 16) = make_uint4(0, 0, 0, 0);
+  ptx::fence_proxy_async();
+  if (warp == kIssueRole) {
+    ptx::tmem_alloc(tmem_slot, 512);
+    ptx::tmem_relinquish();
+    ptx::tc_fence_before();
+  }
+  // up to here nothing was read or written that an earlier kernel of the stream knows of
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = *tmem_slot, tmem_o = tmem + 256;
+
+  auto wait = [&](uint64_t* bar, int phase) { return ptx::mbar_wait(bar, phase & 1, abort_flag, p.wait_cycles); };
+  int item_no = 0;                        // items so far, both passes' and the ends of passes
+  // what the other roles do with an item; false: the pass is over
+  auto next_item = [&](PromptItem& it, bool& ok) {
+    const int slot = item_no % SLOTS;
+    ok = __all_sync(0xffffffffu, wait(item_full + slot, item_no / SLOTS));
+    if (!ok) return false;
+    it = items[slot];
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(item_empty + slot);
+    ++item_no;
+    return it.ls >= 0;
+  };
+  bool ok = true;
+  int n_kv = 0, n_q = 0;                  // ring slots and row tiles so far (asking and issuing role)
+  // All roles meet at the end of a pass; the second one is for items that have to be done again.  One answer for all
+  auto again = [&]() {
+    __syncthreads();
+    return __syncthreads_and(*any_redo && !*abort_flag) != 0;
+  };
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    int n_s = 0, n_o = 0;                 // scores and results so far
+    for (int pass = 0; pass == 0 || (pass == 1 && again()); ++pass) {
+      const int w = warp >> 2, row = (warp & 3) * 32 + lane;
+      const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tmem + w * 128 + lanes, to = tmem_o + w * D + lanes;
+      PromptItem it;
+      while (ok && next_item(it, ok)) {
+        const PromptTiles<2, KT> tiles(p, it);
+        const int layer = it.ls / p.rows.n_seqs, seq = it.ls - layer * p.rows.n_seqs;
+        const int within = row / p.hn, head = it.head * p.hn + row - within * p.hn, pos = it.blk * p.per_item + w * p.pt + within;
+        const bool there = within < p.pt && pos < it.n_r;
+        const int n = tiles.count[w], sees = there ? seen_by(pos, it.n_r, it.n_k) : 0x7FFFFFFF;
+        float m = -CUDART_INF_F, l = 0.f;
+        for (int j = 0; j < n; ++j) {
+          ok = wait(s_full + w, n_s++) && ok;
+          __syncwarp();
+          ptx::tc_fence_after();
+          uint32_t s[4][32];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(ts + c * 32, s[c]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) ptx::tmem_ld_wait(s[c]);
+          if (j >= tiles.even[w]) {
+            const int left = sees - (tiles.first + j) * KT;
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+              if (c >= left) s[c >> 5][c & 31] = 0xFF800000u;
+          }
+          float top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+          for (int c = 0; c < 128; c += 2) top[(c >> 1) & 3] = fmaxf(fmaxf(top[(c >> 1) & 3], __uint_as_float(s[c >> 5][c & 31])), __uint_as_float(s[c >> 5][(c & 31) + 1]));
+          const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale;
+          if (j == 0) {
+            m = high;
+          } else if (__any_sync(0xffffffffu, high > m + kPromptLazy)) {
+            const float now = fmaxf(m, high), f = now == m ? 1.f : pow2(m - now);
+            m = now;
+            l *= f;
+            if (!it.careful || tiles.even[w] > 0) {
+#pragma unroll 1
+              for (int c = 0; c < D; c += 32) {
+                uint32_t o[32];
+                ptx::tmem_ld_32x32_sync(to + c, o);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                ptx::tmem_st_32x32(to + c, o);
+              }
+            }
+          }
+          const float ref = m == -CUDART_INF_F ? 0.f : m;
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t h[16];
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              float2 x = fma_pair(make_float2(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1])), make_float2(p.scale, p.scale), make_float2(-ref, -ref));
+              x.x = pow2(x.x);
+              x.y = pow2(x.y);
+              sum[(i >> 1) & 1] = add_pair(sum[(i >> 1) & 1], x);
+              h[i >> 1] = pack_bf16(x.x, x.y);
+            }
+            ptx::tmem_st_32x16(ts + c * 16, h);
+          }
+          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+          ptx::tmem_st_wait();
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(p_full + w);
+        }
+        // ---- the item's result ----
+        if (n > 0) ok = wait(o_full + w, n_o++) && ok;
+        __syncwarp();
+        ptx::tc_fence_after();
+        const bool write = there && ok && !*abort_flag;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int64_t number = row_number(p, layer, seq, it.base_r, head, pos);
+        T* dst = reinterpret_cast<T*>(const_cast<void*>(p.out.ptr)) + row_offset(p.out, p.rows, layer, seq, it.base_r, head, pos);
+        bool odd = false;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          if (n > 0) {
+            __syncwarp();
+            ptx::tmem_ld_32x32_sync(to + c, o);
+          }
+          float x[32];
+#pragma unroll
+          for (int i = 0; i < 32; ++i) x[i] = n > 0 && (!it.careful || tiles.even[w] > 0) ? __uint_as_float(o[i]) : 0.f;
+          if (it.careful && there && n > tiles.even[w]) {
+            float y[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) y[i] = x[i];
+            add_by_hand<D>(p, it, layer, seq, head, pos, (tiles.first + tiles.even[w]) * KT, min(sees, (tiles.first + n) * KT), m == -CUDART_INF_F ? 0.f : m, c, y);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] = y[i];
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i) odd |= x[i] != x[i];
+          if (!write) continue;
+          if (p.splits > 1) {
+            float* part = p.part + ((int64_t)it.split * p.rows.n_layers * p.rows.total_len * (p.heads * p.hn) + number) * D + c;
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(part + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8)
+              *reinterpret_cast<uint4*>(dst + c + i) = make_uint4(pack_bf16(x[i] * inv, x[i + 1] * inv), pack_bf16(x[i + 2] * inv, x[i + 3] * inv),
+                                                                  pack_bf16(x[i + 4] * inv, x[i + 5] * inv), pack_bf16(x[i + 6] * inv, x[i + 7] * inv));
+          }
+        }
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (n > 0 && lane == 0) ptx::mbar_arrive(o_empty + w);
+        if (write) {
+          if (p.splits > 1) p.stat[(int64_t)it.split * p.rows.n_layers * p.rows.total_len * (p.heads * p.hn) + number] = make_float2(m, l);
+          else put_lse(p, number, m, l);
+          // (only what is hidden from a row can make its result NaN where its sum is a number; what it sees does so again)
+          if (odd && !it.careful && l == l) {
+            atomicOr(redo + (it.number >> 5), 1u << (it.number & 31));
+            *any_redo = 1;
+          }
+        }
+        ok = __all_sync(0xffffffffu, ok);
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == kAskRole) {
+      const PromptList list(p);
+      for (int pass = 0; pass == 0 || (pass == 1 && again()); ++pass) {
+      for (int k = 0; ok; ++k) {
+        while (pass && k < kPromptMaxItems && !(redo[k >> 5] >> (k & 31) & 1u)) ++k;
+        PromptItem it = {};
+        it.ls = -1;
+        if (k < kPromptMaxItems) it = list.item(p, k);
+        it.careful = pass;
+        const int slot = item_no % SLOTS;
+        ok = __all_sync(0xffffffffu, wait(item_empty + slot, item_no / SLOTS + 1));
+        if (!ok) break;
+        if (lane == 0) {
+          items[slot] = it;
+          ptx::mbar_arrive(item_full + slot);
+        }
+        __syncwarp();
+        ++item_no;
+        if (it.ls < 0) break;
+        const PromptTiles<2, KT> tiles(p, it);
+        if (tiles.most == 0) continue;
+        const int layer = it.ls / p.rows.n_seqs, seq = it.ls - layer * p.rows.n_seqs;
+        ok = __all_sync(0xffffffffu, wait(q_empty, n_q + 1));
+        if (!ok) break;
+        if (lane == 0) {
+          const int box = p.pt * p.hn * 128;
+          ptx::mbar_expect_tx(q_full, ((tiles.count[0] > 0) + (tiles.count[1] > 0)) * (D / 64) * box);
+#pragma unroll
+          for (int w = 0; w < 2; ++w)
+            if (tiles.count[w] > 0)
+              for (int h = 0; h < D / 64; ++h)
+                ptx::tma_load_5d(smem + S::q + w * S::kTile + h * S::kHalf, &qmap, q_full, h * 64, it.head * p.hn, it.base_r + it.blk * p.per_item + w * p.pt,
+                                 p.rows.cu ? 0 : seq, layer);
+          asked[1] = n_q + 1;
+        }
+        __syncwarp();
+        ++n_q;
+        for (int i = 0; i < 2 * tiles.most; ++i) {         // K and V in turn
+          const int at = n_kv % RING;
+          ok = __all_sync(0xffffffffu, wait(kv_empty + at, n_kv / RING + 1));
+          if (!ok) break;
+          if (lane == 0) {
+            if (n_kv || (int)blockIdx.x != p.withhold) {
+              ptx::mbar_expect_tx(kv_full + at, S::kTile);
+              for (int h = 0; h < D / 64; ++h)
+                ptx::tma_load_5d(smem + S::ring + at * S::kTile + h * S::kHalf, i & 1 ? &vmap : &kmap, kv_full + at, h * 64, it.base_k + (tiles.first + (i >> 1)) * KT, it.head,
+                                 p.keys.cu ? 0 : seq, layer);
+            }
+            asked[0] = n_kv + 1;
+          }
+          __syncwarp();
+          ++n_kv;
+        }
+      }
+      }
+    } else if (warp == kIssueRole) {
+      int n_s[2] = {0, 0}, n_o[2] = {0, 0};      // scores and results so far, by tile
+      for (int pass = 0; pass == 0 || (pass == 1 && again()); ++pass) {
+      constexpr uint32_t idesc_s = ptx::idesc_bf16_f32(128, KT), idesc_o = ptx::idesc_bf16_f32(128, D) | (1u << 16);
+      const uint32_t issues = ptx::elect_one();
+      const uint64_t dq = ptx::smem_desc_sw128(ptx::smem_u32(smem + S::q)), dk = ptx::smem_desc_sw128(ptx::smem_u32(smem + S::ring)),
+                     dv = ptx::smem_desc_sw128_mn(ptx::smem_u32(smem + S::ring), S::kHalf);
+      PromptItem it;
+      while (ok && next_item(it, ok)) {
+        const PromptTiles<2, KT> tiles(p, it);
+        if (tiles.most == 0) continue;
+        auto scores = [&](int w, int at) {
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t step = ((k >> 2) * S::kHalf + (k & 3) * 32) >> 4;
+            ptx::umma_f16_elected(tmem + w * 128, dq + (w * S::kTile >> 4) + step, dk + (at * S::kTile >> 4) + step, idesc_s, k ? 1u : 0u, issues);
+          }
+          if (issues) ptx::umma_commit(s_full + w);
+          __syncwarp();
+        };
+        auto release = [&](uint64_t* bar) {
+          if (issues) ptx::umma_commit(bar);
+          __syncwarp();
+        };
+        ok = wait(q_full, n_q++);
+        int at = n_kv % RING;
+        ok = __all_sync(0xffffffffu, wait(kv_full + at, n_kv / RING) && ok);
+        if (!ok) break;
+        ptx::tc_fence_after();
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+          if (tiles.count[w] > 0) scores(w, at);
+        release(kv_empty + at);
+        ++n_kv;
+        if (tiles.most == 1) release(q_empty);
+        for (int j = 0; j < tiles.most && ok; ++j) {
+          const int av = n_kv % RING, ak = (n_kv + 1) % RING;
+          const bool more = j + 1 < tiles.most;
+          ok = wait(kv_full + av, n_kv / RING);
+          if (more) ok = wait(kv_full + ak, (n_kv + 1) / RING) && ok;
+          ok = __all_sync(0xffffffffu, ok);
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            if (j >= tiles.count[w] || !ok) continue;
+            if (j == 0) ok = wait(o_empty + w, n_o[w]++ + 1);
+            ok = __all_sync(0xffffffffu, wait(p_full + w, n_s[w]++) && ok);
+            if (!ok) continue;
+            ptx::tc_fence_after();
+            if (!it.careful || j < tiles.even[w]) {
+#pragma unroll
+              for (int k = 0; k < KT / 16; ++k)
+                ptx::umma_bf16_ts_elected(tmem_o + w * D, tmem + w * 128 + k * 8, dv + (av * S::kTile >> 4) + (k * 2048 >> 4), idesc_o, j == 0 && k == 0 ? 0u : 1u, issues);
+            }
+            if (j + 1 < tiles.count[w]) scores(w, ak);
+            else release(o_full + w);
+          }
+          if (!ok) break;
+          release(kv_empty + av);
+          if (more) release(kv_empty + ak);
+          if (j + 2 == tiles.most) release(q_empty);
+          n_kv += more ? 2 : 1;
+        }
+      }
+      }
+    } else {
+      again();
+    }
+  }
+  __syncwarp();
+  if (warp == kIssueRole) {
+    if (ptx::elect_one()) ptx::umma_commit(drained);
+    __syncwarp();
+    // all products are done, and with them their arrivals, before the block goes; after a wait that gave up so are the copies that were still on
+    // their way (within the default bound)
+    ptx::mbar_wait(drained, 0, abort_flag + 1, kDefaultMbarWaitCycles);
+    __syncwarp();
+    if (lane == 0 && *abort_flag) {
+      const int held = (int)blockIdx.x == p.withhold ? 1 : 0;        // (a copy that was never asked for)
+      for (int i = max(asked[0] - RING, held); i < asked[0]; ++i) ptx::mbar_wait(kv_full + i % RING, (i / RING) & 1, abort_flag + 1, kDefaultMbarWaitCycles);
+      if (asked[1] > 0) ptx::mbar_wait(q_full, (asked[1] - 1) & 1, abort_flag + 1, kDefaultMbarWaitCycles);
+    }
+    __syncwarp();
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(tmem, 512);
+  }
+  __syncthreads();
+  if (tid == 0) prompt_settle(p, *abort_flag != 0);
+}
+
+// Joins the parts of a row: a warp for each (layer, column, query head).
+template <typename T, int D>
+__global__ void __launch_bounds__(256) prompt_join_kernel(const __grid_constant__ PromptParams p) {
+  constexpr int E = D / 32;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int hq = p.heads * p.hn, lane = threadIdx.x & 31;
+  const int64_t rows = (int64_t)p.rows.n_layers * p.rows.total_len * hq, number = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (number >= rows) return;
+  const int64_t lt = number / hq;
+  const int head = (int)(number - lt * hq), layer = (int)(lt / p.rows.total_len), col = (int)(lt - (int64_t)layer * p.rows.total_len);
+  int seq, pos;
+  if (p.rows.cu) {                       // the sequence that holds the column
+    int lo = 0, hi = p.rows.n_seqs - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (p.rows.cu[mid + 1] > col) hi = mid; else lo = mid + 1;
+    }
+    seq = lo;
+  } else {
+    seq = col / p.rows.max_len;
+  }
+  const Span r = span_of(p.rows, layer, seq);
+  pos = p.rows.cu ? col - r.base : col - seq * p.rows.max_len;
+  if (pos < 0 || pos >= r.len) return;
+  float top = -CUDART_INF_F, den = 0.f, num[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) num[e] = 0.f;
+  for (int z0 = 0; z0 < p.splits; z0 += 32) {
+    const float2 st = z0 + lane < p.splits ? p.stat[(int64_t)(z0 + lane) * rows + number] : make_float2(-CUDART_INF_F, 0.f);
+    float high = fmaxf(top, st.x);
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
+    const float was = top == high ? 1.f : pow2(top - high);
+    top = high;
+    const float f = st.y == 0.f ? 0.f : st.x == top ? 1.f : pow2(st.x - top);
+    float d = f * st.y;
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+    den = fmaf(den, was, d);
+#pragma unroll
+    for (int e = 0; e < E; ++e) num[e] *= was;
+    const int n = min(32, p.splits - z0);
+#pragma unroll 8
+    for (int z = 0; z < n; ++z) {
+      const float w = __shfl_sync(0xffffffffu, f, z);
+      if (__shfl_sync(0xffffffffu, st.y, z) == 0.f) continue;      // no key: nothing was written
+      const float* part = p.part + ((int64_t)(z0 + z) * rows + number) * D + lane * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) num[e] = fmaf(w, part[e], num[e]);
+    }
+  }
+  T* dst = reinterpret_cast<T*>(const_cast<void*>(p.out.ptr)) + row_offset(p.out, p.rows, layer, seq, r.base, head, pos) + lane * E;
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+#pragma unroll
+  for (int e = 0; e < E; ++e) dst[e] = T(num[e] * inv);
+  if (lane == 0) put_lse(p, number, top, den);
+}
+
+// ---- host ----------------------------------------------------------------------------------------
+
+bool make_tensor_map_bf16(CUtensorMap* map, const spindlekv_tensor& t, const spindlekv_batch& b, int n_heads, int head_dim, int box_rows);
+bool make_rows_map_bf16(CUtensorMap* map, const spindlekv_tensor& t, const spindlekv_batch& b, int n_heads, int head_dim, int box_heads, int box_rows);
+bool sim_tc_available();
+
+constexpr int kPromptSms = 148;
+// the most items of a call, by what the host knows
+static int64_t prompt_items(const spindlekv_batch& rows, int heads, int per_item) {
+  const int64_t blocks = rows.cu_seqlens ? (int64_t)rows.total_len / per_item + rows.n_seqs : (int64_t)rows.n_seqs * ((rows.max_len + per_item - 1) / per_item);
+  return blocks * rows.n_layers * heads;
+}
+// Parts that the keys are cut into: as many as bring the items to one for each SM, of two tiles of keys at least
+static int prompt_splits(const spindlekv_batch& keys, const spindlekv_batch& rows, int heads, int per_item) {
+  const int64_t items = prompt_items(rows, heads, per_item);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(kPromptSms / items, keys.max_len / 256));
+}
+static int prompt_per_item(int hn, int dtype) { return (dtype == SPINDLEKV_BF16 ? 2 : 1) * (kPromptRows / hn); }
+
+size_t prompt_workspace_bytes(const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int n_kv_heads, int head_dim, int dtype) {
+  const int splits = prompt_splits(keys, rows, n_kv_heads, prompt_per_item(n_q_heads / n_kv_heads, dtype));
+  const size_t numbers = (size_t)rows.n_layers * rows.total_len * n_q_heads;
+  return kHeaderBytes + (splits > 1 ? align_up(splits * numbers * (head_dim * sizeof(float) + sizeof(float2)), 256) : 0);
+}
+
+template <typename K, typename... A>
+static spindlekv_status launch_after(K kernel, int64_t blocks, int threads, size_t smem, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  LaunchScope ls(KC_PROMPT, st);
+  return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? SPINDLEKV_OK : SPINDLEKV_CUDA;
+}
+
+template <int D>
+static spindlekv_status launch_prompt(const CUtensorMap& qmap, const CUtensorMap& kmap, const CUtensorMap& vmap, const PromptParams& p, int64_t blocks, cudaStream_t st) {
+  static PerDeviceOnce once;
+  const int dev = PerDeviceOnce::current();
+  if (dev < 0) return SPINDLEKV_CUDA;
+  if (!once.done[dev]) {
+    if (cudaFuncSetAttribute(prompt_attend_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptSmem<D>::bytes) != cudaSuccess) return SPINDLEKV_CUDA;
+    once.done[dev] = true;
+  }
+  const spindlekv_status s = launch_after(prompt_attend_kernel<D>, blocks, kPromptThreads, PromptSmem<D>::bytes, st, qmap, kmap, vmap, p);
+  if (s != SPINDLEKV_OK || p.splits == 1) return s;
+  const int64_t rows = (int64_t)p.rows.n_layers * p.rows.total_len * p.heads * p.hn;
+  return launch_after(prompt_join_kernel<__nv_bfloat16, D>, (rows + 7) / 8, 256, 0, st, p);
+}
+
+spindlekv_status prompt_attend_impl(const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int n_kv_heads, int head_dim, float scale,
+                                    const spindlekv_tensor& q, const spindlekv_tensor& k, const spindlekv_tensor& v, const spindlekv_tensor& out, float* lse, void* ws,
+                                    size_t ws_bytes, cudaStream_t st) {
+  if (ws_bytes < prompt_workspace_bytes(keys, rows, n_q_heads, n_kv_heads, head_dim, q.dtype)) return SPINDLEKV_WORKSPACE_TOO_SMALL;
+  if (!sim_tc_available()) return SPINDLEKV_UNSUPPORTED;
+  PromptParams p;
+  p.keys = make_batch(keys);
+  p.rows = make_batch(rows);
+  p.q = make_view(q);
+  p.k = make_view(k);
+  p.v = make_view(v);
+  p.out = make_view(out);
+  p.heads = n_kv_heads;
+  p.hn = n_q_heads / n_kv_heads;
+  p.pt = kPromptRows / p.hn;
+  p.per_item = prompt_per_item(p.hn, q.dtype);
+  p.max_blocks = ceil_div(rows.max_len, p.per_item);
+  p.splits = prompt_splits(keys, rows, n_kv_heads, p.per_item);
+  p.scale = (scale == 0.f ? 1.f / sqrtf((float)head_dim) : scale) * 1.44269504088896340736f;
+  p.lse = lse;
+  const size_t numbers = (size_t)rows.n_layers * rows.total_len * n_q_heads;
+  p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kHeaderBytes);
+  p.stat = reinterpret_cast<float2*>(p.part + p.splits * numbers * head_dim);
+  p.hdr = static_cast<uint32_t*>(ws);
+  const Tuning tune = current_tuning();
+  p.wait_cycles = tune.mbar_wait_cycles;
+  p.withhold = tune.paged_withhold;
+  const int64_t items = prompt_items(rows, n_kv_heads, p.per_item) * p.splits;
+  // one block per SM; more only where a block's list of items would not do
+  const int64_t blocks = std::min(items, std::max<int64_t>(kPromptSms, (items + kPromptMaxItems - 1) / kPromptMaxItems));
+  if (blocks > 65535) return SPINDLEKV_UNSUPPORTED;
+  if (q.dtype != SPINDLEKV_BF16) return SPINDLEKV_UNSUPPORTED;
+  CUtensorMap qmap, kmap, vmap;
+  if (!make_rows_map_bf16(&qmap, q, rows, n_q_heads, head_dim, p.hn, p.pt) || !make_tensor_map_bf16(&kmap, k, keys, n_kv_heads, head_dim, 128) ||
+      !make_tensor_map_bf16(&vmap, v, keys, n_kv_heads, head_dim, 128))
+    return SPINDLEKV_UNSUPPORTED;
+  return head_dim == 64 ? launch_prompt<64>(qmap, kmap, vmap, p, blocks, st) : launch_prompt<128>(qmap, kmap, vmap, p, blocks, st);
+}
+
+}  // namespace skv

@@ -1,0 +1,174 @@
+// What the kernels of the prompt's attention share: parameters, lengths, the list of work items, the join of split keys.
+#pragma once
+
+#include <math_constants.h>
+
+#include "common.cuh"
+#include "sm100_ptx.cuh"
+
+namespace skv {
+
+constexpr int kPromptRows = 128;          // rows of a tile: (position, query head of the group), heads next to one another
+constexpr int kPromptMaxItems = 4096;     // items of a block, at most: one bit each for those that are done again
+constexpr int kPromptHdrDone = 16;        // words 16, 17 of the status block: blocks that have arrived
+constexpr float kPromptLazy = 8.f;        // how far a score may exceed the running reference, in powers of two
+
+struct PromptParams {
+  Batch keys, rows;
+  View q, k, v, out;         // (q, k, v as the caller has them)
+  int heads, hn;             // KV heads, query heads of each
+  int pt;                    // positions of a row tile: 128 / hn, rounded down
+  int per_item;              // positions of an item
+  int max_blocks;            // items of the longest sequence, a head and a split
+  int splits;                // parts that the keys of an item are cut into
+  float scale;               // softmax scale * log2(e)
+  float* lse;                // [layer][query head][T], or null
+  float* part;               // [splits][layer][T][query head][d] and
+  float2* stat;              // [splits][layer][T][query head]: O, reference and sum of a part
+  uint32_t* hdr;
+  long long wait_cycles;
+  int withhold;              // for tests: the block that does not ask for its first keys; -1: none
+};
+
+// rows of (layer, seq): the first one's number in a packed tensor (0 in a padded one) and how many there are, never outside the tensor
+struct Span { int base, len; };
+__device__ __forceinline__ Span span_of(const Batch& b, int layer, int s) {
+  if (b.cu) {
+    const int base = min(max(b.cu[s], 0), b.total_len);
+    return {base, max(0, min(min(b.cu[s + 1], b.total_len) - base, b.max_len))};
+  }
+  return {0, b.ll ? max(0, min(b.ll[layer * b.n_seqs + s], b.max_len)) : b.max_len};
+}
+// keys that row i of n_r sees among n_k
+__device__ __forceinline__ int seen_by(int i, int n_r, int n_k) { return max(0, n_k - n_r + i + 1); }
+
+// One item: `per_item` positions of a (layer, seq) and KV head, and a part of the keys that they see.
+struct PromptItem {
+  int ls, head, blk, split;   // ls -1: no more of them
+  int n_r, n_k, base_r, base_k;
+  int careful, number, pad[2];
+};
+
+// Items in falling order of their block's number, which is nearly that of their work: all sequences' last positions first.  A warp finds item
+// `i` by the number of blocks with a number of b or more, which falls with b.
+struct PromptList {
+  int nb[4];                  // blocks of (layer, seq) lane, lane + 32, ... where there are up to 128
+  int n_ls, all;
+  __device__ __forceinline__ static int blocks_of(const PromptParams& p, int ls) {
+    const int layer = ls / p.rows.n_seqs;
+    return (span_of(p.rows, layer, ls - layer * p.rows.n_seqs).len + p.per_item - 1) / p.per_item;
+  }
+  __device__ __forceinline__ int count(const PromptParams& p, int b) const {       // blocks with the number b or a larger one
+    const int lane = threadIdx.x & 31;
+    int n = 0;
+    if (n_ls <= 128) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) n += max(nb[i] - b, 0);
+    } else {
+      for (int ls = lane; ls < n_ls; ls += 32) n += max(blocks_of(p, ls) - b, 0);
+    }
+    return __reduce_add_sync(0xffffffffu, n);
+  }
+  __device__ __forceinline__ PromptList(const PromptParams& p) {
+    const int lane = threadIdx.x & 31;
+    n_ls = p.rows.n_layers * p.rows.n_seqs;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) nb[i] = n_ls <= 128 && lane + 32 * i < n_ls ? blocks_of(p, lane + 32 * i) : 0;
+    all = count(p, 0);
+  }
+  // The block's k-th item, or one with ls = -1; every other round goes backwards, so that no block gets the longest of all rounds
+  __device__ __forceinline__ PromptItem item(const PromptParams& p, int k) const {
+    const int lane = threadIdx.x & 31;
+    PromptItem it = {};
+    it.ls = -1;
+    const long long i = (long long)k * gridDim.x + ((k & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    const int per = p.heads * p.splits;
+    if (i >= (long long)all * per) return it;
+    const int q = (int)(i / per), inner = (int)(i - (long long)q * per);
+    int lo = 0, hi = p.max_blocks - 1, above = 0;          // the largest b with more than q blocks of that number or more; `above`: those of b + 1 or more
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1, c = count(p, mid);
+      if (c > q) lo = mid;
+      else { hi = mid - 1; above = c; }
+    }
+    int rank = q - above, found = -1;
+    for (int first = 0; first < n_ls && found < 0; first += 32) {
+      const int ls = first + lane;
+      int n = 0;
+      if (n_ls <= 128) n = first == 0 ? nb[0] : first == 32 ? nb[1] : first == 64 ? nb[2] : nb[3];
+      else if (ls < n_ls) n = blocks_of(p, ls);
+      uint32_t has = __ballot_sync(0xffffffffu, n > lo);
+      if (rank >= __popc(has)) {
+        rank -= __popc(has);
+        continue;
+      }
+      while (rank-- > 0) has &= has - 1;
+      found = first + __ffs(has) - 1;
+    }
+    if (found < 0) return it;
+    const int layer = found / p.rows.n_seqs, s = found - layer * p.rows.n_seqs;
+    const Span r = span_of(p.rows, layer, s), n = span_of(p.keys, layer, s);
+    it.ls = found;
+    it.blk = lo;
+    it.head = inner / p.splits;
+    it.split = inner - it.head * p.splits;
+    it.n_r = r.len;
+    it.n_k = n.len;
+    it.base_r = r.base;
+    it.base_k = n.base;
+    it.number = k;
+    return it;
+  }
+};
+
+// Tiles of KT keys that an item's row tiles have: [first, first + count[w]) for row tile w, of which the last ones, from `even[w]` of them on, hide keys
+// from some row
+template <int NT, int KT>
+struct PromptTiles {
+  int first, count[NT], even[NT], most;
+  __device__ __forceinline__ PromptTiles(const PromptParams& p, const PromptItem& it) {
+    int n[NT], all = 0;
+#pragma unroll
+    for (int w = 0; w < NT; ++w) {
+      const int from = it.blk * p.per_item + w * p.pt, last = min(from + p.pt, it.n_r) - 1;
+      n[w] = last >= from ? (seen_by(last, it.n_r, it.n_k) + KT - 1) / KT : 0;
+      even[w] = last >= from ? seen_by(from, it.n_r, it.n_k) / KT : 0;
+      all = max(all, n[w]);
+    }
+    first = (int)((long long)all * it.split / p.splits);
+    const int end = (int)((long long)all * (it.split + 1) / p.splits);
+    most = 0;
+#pragma unroll
+    for (int w = 0; w < NT; ++w) {
+      count[w] = max(0, min(end, n[w]) - first);
+      even[w] = max(0, min(min(end, even[w]) - first, count[w]));
+      most = max(most, count[w]);
+    }
+  }
+};
+
+// element of (layer, seq, query head, position) of a tensor of rows
+__device__ __forceinline__ int64_t row_offset(const View& v, const Batch& b, int layer, int s, int base, int head, int pos) {
+  return (int64_t)layer * v.sl + (b.cu ? 0 : (int64_t)s * v.ss) + (int64_t)head * v.sh + (int64_t)(base + pos) * v.st;
+}
+// (layer, T column, query head) as one number
+__device__ __forceinline__ int64_t row_number(const PromptParams& p, int layer, int s, int base, int head, int pos) {
+  const int64_t col = p.rows.cu ? (int64_t)base + pos : (int64_t)s * p.rows.max_len + pos;
+  return ((int64_t)layer * p.rows.total_len + col) * (p.heads * p.hn) + head;
+}
+__device__ __forceinline__ void put_lse(const PromptParams& p, int64_t number, float m, float l) {
+  if (!p.lse) return;
+  const int hq = p.heads * p.hn;
+  const int64_t lt = number / hq, layer = lt / p.rows.total_len;
+  const float lse = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * 0.69314718055994530942f;
+  p.lse[(layer * hq + (number - lt * hq)) * p.rows.total_len + (lt - layer * p.rows.total_len)] = lse;
+}
+
+// the last block of a call leaves the status word
+__device__ __forceinline__ void prompt_settle(const PromptParams& p, bool failed) {
+  __threadfence();
+  const int last = last_to_arrive(reinterpret_cast<unsigned long long*>(p.hdr + kPromptHdrDone), gridDim.x, failed);
+  if (last) p.hdr[kHdrStatus] = last == 2 ? SPINDLEKV_TIMEOUT : SPINDLEKV_OK;
+}
+
+}  // namespace skv

@@ -733,6 +733,27 @@ bool make_query_map_bf16(CUtensorMap* map, const spindlekv_tensor& q, const spin
   return r == CUDA_SUCCESS;
 }
 
+// bf16 rows [layer][seq][head][token][d] -> 5-D map (d, head, token, seq, layer): one box is 64 elements of `box_heads` heads next to one another
+// at each of `box_rows` positions
+bool make_rows_map_bf16(CUtensorMap* map, const spindlekv_tensor& t, const spindlekv_batch& b, int n_heads, int head_dim, int box_heads, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const bool packed = b.cu_seqlens != nullptr;
+  auto bytes = [](int64_t elems) { return (cuuint64_t)(elems > 0 ? elems : 8) * 2; };
+  const int64_t st_el[5] = {1, t.stride_head, t.stride_tok, packed ? t.stride_tok : t.stride_seq, t.stride_layer};
+  cuuint64_t dims[5] = {(cuuint64_t)head_dim, (cuuint64_t)n_heads, (cuuint64_t)(packed ? b.total_len : b.max_len), (cuuint64_t)(packed ? 1 : b.n_seqs),
+                        (cuuint64_t)b.n_layers};
+  cuuint64_t strides[4];
+  for (int i = 1; i < 5; ++i) {
+    if (dims[i] > 1 && st_el[i] <= 0) return false;
+    strides[i - 1] = bytes(st_el[i]);
+  }
+  cuuint32_t box[5] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows, 1, 1};
+  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, t.ptr, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // 8-bit codes [page][row][d] of a paged cache -> 3-D map (d, row, page), box d x box_rows, swizzle as wide as a row
 bool make_code_map(CUtensorMap* map, const void* codes, int head_dim, int rows, int n_pages, int box_rows) {
   EncodeTiledFn fn = encode_fn();

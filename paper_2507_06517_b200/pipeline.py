@@ -555,14 +555,14 @@ class _OnDevice:
     def _raw(self, stream) -> int:
         return B.raw_stream(self._index) if stream is None else B._stream(stream)
 
-    def _empty(self, shape, dtype, stream) -> torch.Tensor:
+    def _empty(self, shape, dtype, stream, zero: bool = False) -> torch.Tensor:
         """Memory that is made within a call belongs to that call's stream: what the current stream still does with a block that the
         allocator hands out again is in no order with ``stream``."""
-        raw = self._raw(stream)
+        raw, make = self._raw(stream), torch.zeros if zero else torch.empty
         if raw == B.raw_stream(self._index):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return make(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(torch.cuda.ExternalStream(raw, self.device) if raw else torch.cuda.default_stream(self.device)):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return make(shape, dtype=dtype, device=self.device)
 
     def _mine(self, name: str, t: torch.Tensor, dtype=None, shape=None) -> torch.Tensor:
         """``t``, if the library may be given its address as it is."""
@@ -733,6 +733,59 @@ class SpindleKVPagedCache(_OnDevice):
                 return self.status()
         st = B.spindlekv_poll_status(self.ws_pages)[0]
         return B.spindlekv_poll_status(self.ws_attend)[0] if st == B.OK and self.ws_attend is not None else st
+
+
+class SpindleKVPromptAttention(_OnDevice):
+    """Causal attention of a prompt batch, or of the last rows of one: scratch of ``spindlekv_prompt_attend`` for batches of one shape.  ``keys`` describes
+    K and V, ``rows`` the queries (every token by default).  Tensors are ``[L, B, H, N, d]``, or packed ``[L, T, H, d]`` where their batch has
+    ``cu_seqlens``.  All calls of one object must be ordered: they share the scratch."""
+
+    def __init__(self, keys: B.Batch, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, rows: Optional[B.Batch] = None, device="cuda"):
+        self.keys, self.rows, self.Hq, self.Hkv, self.d, self.dtype = keys, rows or keys, n_q_heads, n_kv_heads, head_dim, dtype
+        self.device = dev = _device_of(device)
+        self._index = dev.index
+        codes = {torch.float32: B.F32, torch.bfloat16: B.BF16}
+        if dtype not in codes:
+            raise TypeError(f"unsupported dtype {dtype}")
+        for b in (self.keys, self.rows):
+            for t, n in ((b.cu_seqlens, b.n_seqs + 1), (b.layer_lens, b.n_layers * b.n_seqs)):
+                if t is not None and (t.device != dev or t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n):
+                    raise ValueError(f"lengths: {n} contiguous int32 on {dev} expected, got {t.dtype} {list(t.shape)} on {t.device}")
+        n = B.spindlekv_prompt_workspace_bytes(self.keys, self.rows, n_q_heads, n_kv_heads, head_dim, codes[dtype])
+        if n == 0:
+            raise ValueError(f"unsupported attention: {n_q_heads} query heads, {n_kv_heads} KV heads of {head_dim}, {self.keys}, {self.rows}")
+        self.ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        self._c = self.keys.c(), self.rows.c()
+
+    def _rows_of(self, name: str, t: torch.Tensor, b: B.Batch, heads: int) -> B._Tensor:
+        shape, strides = t.shape, t.stride()
+        want = (b.n_layers, b.total_len, heads, self.d) if b.cu_seqlens is not None else (b.n_layers, b.n_seqs, heads, b.max_len, self.d)
+        if shape != want or strides[-1] != 1 or t.dtype != self.dtype or t.device != self.device:
+            raise ValueError(f"{name}: {list(want)} {self.dtype} on {self.device} expected, rows contiguous, got {list(shape)} {t.dtype} on {t.device}")
+        if b.cu_seqlens is not None:
+            return B._Tensor(t.data_ptr(), B._dtype_code(t), strides[0], 0, strides[2], strides[1])
+        return B._Tensor(t.data_ptr(), B._dtype_code(t), strides[0], strides[1], strides[2], strides[3])
+
+    def run(self, q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, scale: float = 0.0,
+            stream=None) -> torch.Tensor:
+        """``out`` (made by the call by default: zeros behind a sequence's rows) and ``lse`` ``[L, H_q, T]`` fp32, if given, are written; returns ``out``."""
+        if self._elsewhere():
+            with torch.cuda.device(self.device):
+                return self.run(q, K, V, out, lse, scale, stream)
+        qd, kd, vd = self._rows_of("q", q, self.rows, self.Hq), self._rows_of("K", K, self.keys, self.Hkv), self._rows_of("V", V, self.keys, self.Hkv)
+        if out is None:
+            out = self._empty(q.shape, q.dtype, stream, zero=self.rows.cu_seqlens is not None or self.rows.layer_lens is not None)
+        if lse is not None:
+            self._mine("lse", lse, torch.float32, (self.rows.n_layers, self.Hq, self.rows.total_len))
+        B.spindlekv_prompt_attend(self._c[0], self._c[1], self.Hq, self.Hkv, self.d, scale, qd, kd, vd, self._rows_of("out", out, self.rows, self.Hq), lse, self.ws,
+                                  self._raw(stream))
+        return out
+
+    def status(self) -> int:
+        """Status word of the last call (synchronises the device)."""
+        torch.cuda.synchronize(self.device)
+        with torch.cuda.device(self.device):
+            return B.spindlekv_poll_status(self.ws)[0]
 
 
 class SpindleKVBeamSelect(_OnDevice):

@@ -1,0 +1,185 @@
+"""Attention of prompts on the GPU against float64."""
+import math
+
+import pytest
+import torch
+
+import prompt_ref as R
+from paper_2507_06517_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+TYPES = [BF]
+
+
+def batch(lens, packed, n_layers=1, room=0):
+    """A batch of these lengths: packed, padded, or (all alike) of equal lengths."""
+    if packed:
+        cu = torch.tensor([0] + lens).cumsum(0).int().cuda()
+        return B.Batch(n_layers, len(lens), max(max(lens), 1), max(sum(lens) + room, max(lens), 1), cu)
+    most = max(max(lens), 1) + room
+    ll = None if min(lens) == most else torch.tensor([lens] * n_layers, dtype=torch.int32).cuda()
+    return B.Batch(n_layers, len(lens), most, len(lens) * most, None, ll)
+
+
+def tensor_of(b, heads, d, dtype, gen, size=1.0):
+    shape = (b.n_layers, b.total_len, heads, d) if b.cu_seqlens is not None else (b.n_layers, b.n_seqs, heads, b.max_len, d)
+    return (torch.randn(shape, generator=gen, device="cuda") * size).to(dtype)
+
+
+def make(lens, rows, hq, h, d, dtype, packed=False, n_layers=1, room=0, seed=0, size=1.0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    keys, rws = batch(lens, packed, n_layers, room), batch(rows or lens, packed, n_layers, room)
+    return keys, rws, tensor_of(rws, hq, d, dtype, gen, size), tensor_of(keys, h, d, dtype, gen), tensor_of(keys, h, d, dtype, gen)
+
+
+def attend(keys, rows, q, k, v, scale=0.0, fill=7.0):
+    from paper_2507_06517_b200.pipeline import SpindleKVPromptAttention
+    a = SpindleKVPromptAttention(keys, q.shape[2], k.shape[2], q.shape[-1], q.dtype, rows=rows)
+    a.ws.fill_(0xA5)                                       # needs no preparation
+    out = torch.full_like(q, fill)
+    lse = torch.full((rows.n_layers, q.shape[2], rows.total_len), fill, device="cuda")
+    a.run(q, k, v, out=out, lse=lse, scale=scale)
+    assert a.status() == B.OK
+    return out, lse
+
+
+def check(keys, rows, q, k, v, scale=0.0):
+    out, lse = attend(keys, rows, q, k, v, scale)
+    want, want_lse, bound = R.attend(q, k, v, keys, rows, scale)
+    there = ~want_lse.isnan()
+    row = ~want.isnan()
+    assert (out[~row] == 7.0).all() and (lse[~there] == 7.0).all()                          # nothing behind the last rows
+    off = (out.double() - want).abs()[row]
+    assert out[row].isfinite().all()
+    assert (off <= bound[row]).all(), (off / bound[row].clamp(min=1e-300)).max()
+    empty = want_lse == -math.inf
+    assert (lse[empty] == -math.inf).all()
+    ok = there & ~empty
+    assert ((lse.double() - want_lse).abs()[ok] <= 1e-4 * (1 + want_lse.abs()[ok])).all()
+    return out, lse
+
+
+SHAPES = [  # lengths, rows (None: all), query heads, KV heads, d
+    ([1], None, 1, 1, 64), ([1], None, 4, 2, 128), ([2], None, 8, 1, 128), ([127], None, 2, 2, 64), ([128], None, 2, 2, 128), ([129], None, 4, 4, 128),
+    ([190], None, 4, 2, 64), ([257], None, 3, 1, 128), ([300], None, 7, 1, 128), ([515], None, 10, 2, 64), ([700], None, 16, 2, 128), ([1000], None, 5, 5, 128),
+    ([2049], None, 8, 8, 128), ([333], None, 64, 1, 128), ([90], None, 128, 1, 64), ([150], None, 100, 1, 128),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens,rows,hq,h,d", SHAPES)
+def test_one_prompt(lens, rows, hq, h, d, dtype):
+    check(*make(lens, rows, hq, h, d, dtype, seed=lens[0]))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("packed,room", [(True, 0), (False, 0), (True, 37), (False, 50)])
+@pytest.mark.parametrize("hq,h,d,layers", [(8, 2, 128, 1), (6, 2, 64, 2)])
+def test_batches_of_uneven_prompts(packed, room, hq, h, d, layers, dtype):
+    check(*make([130, 1, 0, 700, 64, 255, 0, 33], None, hq, h, d, dtype, packed, layers, room, seed=3))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens,rows", [([5000], [1]), ([3000, 17, 1], [1, 1, 1]), ([4097, 100], [33, 5]), ([2000], [300]), ([900, 64, 3], [20, 64, 0]), ([40000], [2])])
+@pytest.mark.parametrize("packed", [True, False])
+def test_last_rows_of_long_prompts(lens, rows, packed, dtype):
+    check(*make(lens, rows, 8, 2, 128, dtype, packed, seed=5))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_that_see_nothing(dtype):
+    # more rows than keys: the first ones see none
+    check(*make([3, 0, 500], [10, 4, 700], 4, 2, 64, dtype, False, seed=6))
+    check(*make([0], [5], 4, 2, 128, dtype, False, seed=6))
+    check(*make([2], [300], 4, 1, 128, dtype, True, seed=6))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_short_sequences(dtype):
+    gen = torch.Generator().manual_seed(1)
+    lens = torch.randint(0, 40, (300,), generator=gen).tolist()
+    check(*make(lens, None, 4, 2, 64, dtype, True, seed=8))
+    check(*make(lens[:150], None, 4, 2, 128, dtype, False, 2, seed=8))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_scores_of_every_size(dtype):
+    # references that move late, and by much; scores all alike; a scale of one's own
+    keys, rows, q, k, v = make([900], None, 4, 2, 128, dtype, seed=9, size=6.0)
+    ramp = torch.linspace(0.1, 4.0, 900, device="cuda")[:, None]
+    check(keys, rows, q, (k * ramp).to(dtype), v)
+    check(keys, rows, q, (k * ramp.flip(0)).to(dtype), v, scale=0.3)
+    check(keys, rows, torch.zeros_like(q), k, v)
+    check(keys, rows, q, k, v, scale=1e-6)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens,rows,packed", [([300, 200], None, False), ([300, 200], None, True), ([3000], [5], False)])
+def test_what_a_row_does_not_see_may_be_anything(lens, rows, packed, dtype):
+    keys, rws, q, k, v = make(lens, rows, 4, 2, 128, dtype, packed, room=60, seed=11)
+    clean = check(keys, rws, q, k, v)
+    # behind the sequences
+    for t in (k, v):
+        if packed:
+            t[:, sum(lens):] = math.nan
+            t[:, sum(lens) + 20:] = math.inf
+        else:
+            for s, n in enumerate(lens):
+                t[:, s, :, n:] = math.inf if s else math.nan
+    check(keys, rws, q, k, v)
+    # the last key: only the last row sees it
+    last = (0, sum(lens) - 1) if packed else (0, len(lens) - 1, slice(None), lens[-1] - 1)
+    k[last], v[last] = math.nan, math.inf
+    out, lse = attend(keys, rws, q, k, v)
+    n_r = (rows or lens)[-1]
+    out_s = out[0, -60 - n_r:-60 or None] if packed else out[0, -1].transpose(0, 1)[:n_r]
+    was_s = clean[0][0, -60 - n_r:-60 or None] if packed else clean[0][0, -1].transpose(0, 1)[:n_r]
+    assert out_s[-1].isnan().all()
+    assert out_s[:-1].isfinite().all()
+    assert ((out_s[:-1] - was_s[:-1]).abs() <= 2 * torch.finfo(dtype).eps * (1 + was_s[:-1].abs())).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_values_that_are_not_numbers_show_where_they_are_seen(dtype):
+    keys, rows, q, k, v = make([1000], None, 2, 1, 64, dtype, seed=12)
+    want, _ = attend(keys, rows, q, k, v)
+    v[0, 0, 0, 400, 7] = math.nan
+    v[0, 0, 0, 700, 9] = -math.inf
+    out, lse = attend(keys, rows, q, k, v)
+    assert lse.isfinite().all()
+    bad = ~out[0, 0].isfinite()                                # [heads, rows, d]
+    seen = torch.zeros_like(bad)
+    seen[:, 400:, 7] = True
+    seen[:, 700:, 9] = True
+    assert torch.equal(bad, seen)
+    assert ((out[0, 0] - want[0, 0]).abs()[~bad] <= 2 * torch.finfo(dtype).eps * (1 + want[0, 0].abs()[~bad])).all()
+    v.fill_(math.nan)                                          # and all of them
+    assert attend(keys, rows, q, k, v)[0].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_strides_streams_graphs_and_repeats(dtype):
+    from paper_2507_06517_b200.pipeline import SpindleKVPromptAttention, record_graph
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    n, hq, h, d = 450, 8, 2, 128
+    keys = batch([n, n], False)
+    wide = torch.randn((1, 2, n, hq + 2 * h, d), generator=gen, device="cuda").to(dtype)    # a fused projection's rows: [token][q, k, v heads]
+    q, k, v = (wide[:, :, :, a:b].transpose(2, 3) for a, b in ((0, hq), (hq, hq + h), (hq + h, hq + 2 * h)))
+    first = check(keys, keys, q, k, v)
+    assert all(torch.equal(a, b) for a, b in zip(first, attend(keys, keys, q.contiguous(), k.contiguous(), v.contiguous())))
+    out = torch.full((1, 2, n, hq, d), 7.0, dtype=dtype, device="cuda").transpose(2, 3)
+    a = SpindleKVPromptAttention(keys, hq, h, d, dtype)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    a.run(q, k, v, out=out, stream=side)
+    side.synchronize()
+    assert torch.equal(out, first[0])
+    graph = record_graph(lambda: a.run(q, k, v, out=out))
+    wide.copy_(wide.flip(2))
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, attend(keys, keys, q, k, v)[0])
+    assert a.status() == B.OK
