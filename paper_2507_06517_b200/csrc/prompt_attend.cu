@@ -41,59 +41,6 @@ struct PromptSmem {
 };
 static_assert(PromptSmem<128>::bytes <= 227 * 1024, "shared memory");
 
-// a x b + c of two numbers at a time
-__device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
-  unsigned long long x, y, z, r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
-  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(b.x), "f"(b.y));
-  asm("mov.b64 %0, {%1, %2};" : "=l"(z) : "f"(c.x), "f"(c.y));
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
-  float2 o;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(o.x), "=f"(o.y) : "l"(r));
-  return o;
-}
-__device__ __forceinline__ float2 add_pair(float2 a, float2 b) {
-  unsigned long long x, y, r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
-  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(b.x), "f"(b.y));
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
-  float2 o;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(o.x), "=f"(o.y) : "l"(r));
-  return o;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-
-// What masked tiles give to 32 elements of a row, key by key: the tiles whose values are not all numbers.  Rare
-template <int D>
-__device__ __noinline__ void add_by_hand(const PromptParams& p, const PromptItem& it, int layer, int seq, int head, int pos, int from, int to, float ref, int d0,
-                                         float (&o)[32]) {
-  const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q.ptr) + row_offset(p.q, p.rows, layer, seq, it.base_r, head, pos);
-  for (int j = from; j < to; ++j) {
-    const __nv_bfloat16* k = reinterpret_cast<const __nv_bfloat16*>(p.k.ptr) + row_offset(p.k, p.keys, layer, seq, it.base_k, it.head, j);
-    const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.v.ptr) + row_offset(p.v, p.keys, layer, seq, it.base_k, it.head, j) + d0;
-    float s = 0.f;
-    for (int d = 0; d < D; d += 8) {
-      float a[8], b[8];
-      load8(q + d, a);
-      load8(k + d, b);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s = fmaf(a[i], b[i], s);
-    }
-    const float w = pow2(fmaf(s, p.scale, -ref));
-#pragma unroll
-    for (int d = 0; d < 32; d += 8) {
-      float b[8];
-      load8(v + d, b);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[d + i] = fmaf(w, b[i], o[d + i]);
-    }
-  }
-}
-
 template <int D>
 __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                                                                           const __grid_constant__ CUtensorMap vmap, const __grid_constant__ PromptParams p) {
@@ -264,7 +211,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
             float y[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) y[i] = x[i];
-            add_by_hand<D>(p, it, layer, seq, head, pos, (tiles.first + tiles.even[w]) * KT, min(sees, (tiles.first + n) * KT), m == -CUDART_INF_F ? 0.f : m, c, y);
+            add_by_hand<T, D>(p, it, layer, seq, head, pos, (tiles.first + tiles.even[w]) * KT, min(sees, (tiles.first + n) * KT), m == -CUDART_INF_F ? 0.f : m, c, y);
 #pragma unroll
             for (int i = 0; i < 32; ++i) x[i] = y[i];
           }
@@ -443,69 +390,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
   if (tid == 0) prompt_settle(p, *abort_flag != 0);
 }
 
-// Joins the parts of a row: a warp for each (layer, column, query head).
-template <typename T, int D>
-__global__ void __launch_bounds__(256) prompt_join_kernel(const __grid_constant__ PromptParams p) {
-  constexpr int E = D / 32;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int hq = p.heads * p.hn, lane = threadIdx.x & 31;
-  const int64_t rows = (int64_t)p.rows.n_layers * p.rows.total_len * hq, number = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (number >= rows) return;
-  const int64_t lt = number / hq;
-  const int head = (int)(number - lt * hq), layer = (int)(lt / p.rows.total_len), col = (int)(lt - (int64_t)layer * p.rows.total_len);
-  int seq, pos;
-  if (p.rows.cu) {                       // the sequence that holds the column
-    int lo = 0, hi = p.rows.n_seqs - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (p.rows.cu[mid + 1] > col) hi = mid; else lo = mid + 1;
-    }
-    seq = lo;
-  } else {
-    seq = col / p.rows.max_len;
-  }
-  const Span r = span_of(p.rows, layer, seq);
-  pos = p.rows.cu ? col - r.base : col - seq * p.rows.max_len;
-  if (pos < 0 || pos >= r.len) return;
-  float top = -CUDART_INF_F, den = 0.f, num[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) num[e] = 0.f;
-  for (int z0 = 0; z0 < p.splits; z0 += 32) {
-    const float2 st = z0 + lane < p.splits ? p.stat[(int64_t)(z0 + lane) * rows + number] : make_float2(-CUDART_INF_F, 0.f);
-    float high = fmaxf(top, st.x);
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
-    const float was = top == high ? 1.f : pow2(top - high);
-    top = high;
-    const float f = st.y == 0.f ? 0.f : st.x == top ? 1.f : pow2(st.x - top);
-    float d = f * st.y;
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-    den = fmaf(den, was, d);
-#pragma unroll
-    for (int e = 0; e < E; ++e) num[e] *= was;
-    const int n = min(32, p.splits - z0);
-#pragma unroll 8
-    for (int z = 0; z < n; ++z) {
-      const float w = __shfl_sync(0xffffffffu, f, z);
-      if (__shfl_sync(0xffffffffu, st.y, z) == 0.f) continue;      // no key: nothing was written
-      const float* part = p.part + ((int64_t)(z0 + z) * rows + number) * D + lane * E;
-#pragma unroll
-      for (int e = 0; e < E; ++e) num[e] = fmaf(w, part[e], num[e]);
-    }
-  }
-  T* dst = reinterpret_cast<T*>(const_cast<void*>(p.out.ptr)) + row_offset(p.out, p.rows, layer, seq, r.base, head, pos) + lane * E;
-  const float inv = den == 0.f ? 0.f : 1.f / den;
-#pragma unroll
-  for (int e = 0; e < E; ++e) dst[e] = T(num[e] * inv);
-  if (lane == 0) put_lse(p, number, top, den);
-}
-
 // ---- host ----------------------------------------------------------------------------------------
 
-bool make_tensor_map_bf16(CUtensorMap* map, const spindlekv_tensor& t, const spindlekv_batch& b, int n_heads, int head_dim, int box_rows);
-bool make_rows_map_bf16(CUtensorMap* map, const spindlekv_tensor& t, const spindlekv_batch& b, int n_heads, int head_dim, int box_heads, int box_rows);
 bool sim_tc_available();
 
 constexpr int kPromptSms = 148;
@@ -524,23 +410,8 @@ static int prompt_per_item(int hn, int dtype) { return (dtype == SPINDLEKV_BF16 
 size_t prompt_workspace_bytes(const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int n_kv_heads, int head_dim, int dtype) {
   const int splits = prompt_splits(keys, rows, n_kv_heads, prompt_per_item(n_q_heads / n_kv_heads, dtype));
   const size_t numbers = (size_t)rows.n_layers * rows.total_len * n_q_heads;
-  return kHeaderBytes + (splits > 1 ? align_up(splits * numbers * (head_dim * sizeof(float) + sizeof(float2)), 256) : 0);
-}
-
-template <typename K, typename... A>
-static spindlekv_status launch_after(K kernel, int64_t blocks, int threads, size_t smem, cudaStream_t st, const A&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)blocks);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  LaunchScope ls(KC_PROMPT, st);
-  return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? SPINDLEKV_OK : SPINDLEKV_CUDA;
+  return kHeaderBytes + (splits > 1 ? align_up(splits * numbers * (head_dim * sizeof(float) + sizeof(float2)), 256) : 0) +
+         (dtype == SPINDLEKV_F32 ? prompt_pieces_bytes(keys, rows, n_q_heads, n_kv_heads, head_dim) : 0);
 }
 
 template <int D>
@@ -553,9 +424,7 @@ static spindlekv_status launch_prompt(const CUtensorMap& qmap, const CUtensorMap
     once.done[dev] = true;
   }
   const spindlekv_status s = launch_after(prompt_attend_kernel<D>, blocks, kPromptThreads, PromptSmem<D>::bytes, st, qmap, kmap, vmap, p);
-  if (s != SPINDLEKV_OK || p.splits == 1) return s;
-  const int64_t rows = (int64_t)p.rows.n_layers * p.rows.total_len * p.heads * p.hn;
-  return launch_after(prompt_join_kernel<__nv_bfloat16, D>, (rows + 7) / 8, 256, 0, st, p);
+  return s == SPINDLEKV_OK ? launch_prompt_join<__nv_bfloat16, D>(p, st) : s;
 }
 
 spindlekv_status prompt_attend_impl(const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int n_kv_heads, int head_dim, float scale,
@@ -589,7 +458,10 @@ spindlekv_status prompt_attend_impl(const spindlekv_batch& keys, const spindlekv
   // one block per SM; more only where a block's list of items would not do
   const int64_t blocks = std::min(items, std::max<int64_t>(kPromptSms, (items + kPromptMaxItems - 1) / kPromptMaxItems));
   if (blocks > 65535) return SPINDLEKV_UNSUPPORTED;
-  if (q.dtype != SPINDLEKV_BF16) return SPINDLEKV_UNSUPPORTED;
+  if (q.dtype == SPINDLEKV_F32) {
+    const size_t parts = p.splits > 1 ? align_up(p.splits * numbers * (head_dim * sizeof(float) + sizeof(float2)), 256) : 0;
+    return prompt_attend_f32(p, keys, rows, n_q_heads, head_dim, static_cast<uint8_t*>(ws) + kHeaderBytes + parts, blocks, st);
+  }
   CUtensorMap qmap, kmap, vmap;
   if (!make_rows_map_bf16(&qmap, q, rows, n_q_heads, head_dim, p.hn, p.pt) || !make_tensor_map_bf16(&kmap, k, keys, n_kv_heads, head_dim, 128) ||
       !make_tensor_map_bf16(&vmap, v, keys, n_kv_heads, head_dim, 128))

@@ -1,6 +1,7 @@
 // What the kernels of the prompt's attention share: parameters, lengths, the list of work items, the join of split keys.
 #pragma once
 
+#include <math.h>
 #include <math_constants.h>
 
 #include "common.cuh"
@@ -170,5 +171,152 @@ __device__ __forceinline__ void prompt_settle(const PromptParams& p, bool failed
   const int last = last_to_arrive(reinterpret_cast<unsigned long long*>(p.hdr + kPromptHdrDone), gridDim.x, failed);
   if (last) p.hdr[kHdrStatus] = last == 2 ? SPINDLEKV_TIMEOUT : SPINDLEKV_OK;
 }
+
+// a x b + c of two numbers at a time
+__device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
+  unsigned long long x, y, z, r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(b.x), "f"(b.y));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(z) : "f"(c.x), "f"(c.y));
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+  float2 o;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(o.x), "=f"(o.y) : "l"(r));
+  return o;
+}
+__device__ __forceinline__ float2 add_pair(float2 a, float2 b) {
+  unsigned long long x, y, r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(b.x), "f"(b.y));
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+  float2 o;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(o.x), "=f"(o.y) : "l"(r));
+  return o;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// What masked tiles give to 32 elements of a row, key by key: the tiles whose values are not all numbers.  Rare
+template <typename T, int D>
+__device__ __noinline__ void add_by_hand(const PromptParams& p, const PromptItem& it, int layer, int seq, int head, int pos, int from, int to, float ref, int d0,
+                                         float (&o)[32]) {
+  const T* q = reinterpret_cast<const T*>(p.q.ptr) + row_offset(p.q, p.rows, layer, seq, it.base_r, head, pos);
+  for (int j = from; j < to; ++j) {
+    const T* k = reinterpret_cast<const T*>(p.k.ptr) + row_offset(p.k, p.keys, layer, seq, it.base_k, it.head, j);
+    const T* v = reinterpret_cast<const T*>(p.v.ptr) + row_offset(p.v, p.keys, layer, seq, it.base_k, it.head, j) + d0;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int d = 0; d < D; d += 8) {
+      float a[8], b[8];
+      load8(q + d, a);
+      load8(k + d, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] = fmaf(a[i], b[i], s[i]);
+    }
+    const float w = pow2(fmaf(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])), p.scale, -ref));
+#pragma unroll
+    for (int d = 0; d < 32; d += 8) {
+      float b[8];
+      load8(v + d, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[d + i] = fmaf(w, b[i], o[d + i]);
+    }
+  }
+}
+
+// Joins the parts of a row: a warp for each (layer, column, query head).
+template <typename T, int D>
+__global__ void __launch_bounds__(256) prompt_join_kernel(const __grid_constant__ PromptParams p) {
+  constexpr int E = D / 32;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int hq = p.heads * p.hn, lane = threadIdx.x & 31;
+  const int64_t rows = (int64_t)p.rows.n_layers * p.rows.total_len * hq, number = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (number >= rows) return;
+  const int64_t lt = number / hq;
+  const int head = (int)(number - lt * hq), layer = (int)(lt / p.rows.total_len), col = (int)(lt - (int64_t)layer * p.rows.total_len);
+  int seq, pos;
+  if (p.rows.cu) {                       // the sequence that holds the column
+    int lo = 0, hi = p.rows.n_seqs - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (p.rows.cu[mid + 1] > col) hi = mid; else lo = mid + 1;
+    }
+    seq = lo;
+  } else {
+    seq = col / p.rows.max_len;
+  }
+  const Span r = span_of(p.rows, layer, seq);
+  pos = p.rows.cu ? col - r.base : col - seq * p.rows.max_len;
+  if (pos < 0 || pos >= r.len) return;
+  float top = -CUDART_INF_F, den = 0.f, num[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) num[e] = 0.f;
+  for (int z0 = 0; z0 < p.splits; z0 += 32) {
+    const float2 st = z0 + lane < p.splits ? p.stat[(int64_t)(z0 + lane) * rows + number] : make_float2(-CUDART_INF_F, 0.f);
+    float high = fmaxf(top, st.x);
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
+    const float was = top == high ? 1.f : pow2(top - high);
+    top = high;
+    const float f = st.y == 0.f ? 0.f : st.x == top ? 1.f : pow2(st.x - top);
+    float d = f * st.y;
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+    den = fmaf(den, was, d);
+#pragma unroll
+    for (int e = 0; e < E; ++e) num[e] *= was;
+    const int n = min(32, p.splits - z0);
+#pragma unroll 8
+    for (int z = 0; z < n; ++z) {
+      const float w = __shfl_sync(0xffffffffu, f, z);
+      if (__shfl_sync(0xffffffffu, st.y, z) == 0.f) continue;      // no key: nothing was written
+      const float* part = p.part + ((int64_t)(z0 + z) * rows + number) * D + lane * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) num[e] = fmaf(w, part[e], num[e]);
+    }
+  }
+  T* dst = reinterpret_cast<T*>(const_cast<void*>(p.out.ptr)) + row_offset(p.out, p.rows, layer, seq, r.base, head, pos) + lane * E;
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+#pragma unroll
+  for (int e = 0; e < E; ++e) dst[e] = T(num[e] * inv);
+  if (lane == 0) put_lse(p, number, top, den);
+}
+
+// ---- host ----------------------------------------------------------------------------------------
+
+// Launches a kernel that waits by itself for the one before it on the stream
+template <typename K, typename... A>
+spindlekv_status launch_after(K kernel, int64_t blocks, int threads, size_t smem, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  LaunchScope ls(KC_PROMPT, st);
+  return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? SPINDLEKV_OK : SPINDLEKV_CUDA;
+}
+
+// behind the attention itself: joins the parts, if there are any
+template <typename T, int D>
+spindlekv_status launch_prompt_join(const PromptParams& p, cudaStream_t st) {
+  if (p.splits == 1) return SPINDLEKV_OK;
+  const int64_t rows = (int64_t)p.rows.n_layers * p.rows.total_len * p.heads * p.hn;
+  return launch_after(prompt_join_kernel<T, D>, (rows + 7) / 8, 256, 0, st, p);
+}
+
+bool make_rows_map_bf16(CUtensorMap* map, const spindlekv_tensor& t, const spindlekv_batch& b, int n_heads, int head_dim, int box_heads, int box_rows);
+bool make_tensor_map_bf16(CUtensorMap* map, const spindlekv_tensor& t, const spindlekv_batch& b, int n_heads, int head_dim, int box_rows);
+
+// fp32: bytes of the pieces, and the call with `pieces` to put them into
+size_t prompt_pieces_bytes(const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int n_kv_heads, int head_dim);
+spindlekv_status prompt_attend_f32(const PromptParams& p, const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int head_dim, void* pieces,
+                                   int64_t blocks, cudaStream_t st);
 
 }  // namespace skv

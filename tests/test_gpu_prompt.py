@@ -10,7 +10,7 @@ from paper_2507_06517_b200 import binding as B
 pytestmark = pytest.mark.gpu
 
 BF, F32 = torch.bfloat16, torch.float32
-TYPES = [BF]
+TYPES = [BF, F32]
 
 
 def batch(lens, packed, n_layers=1, room=0):
@@ -119,7 +119,8 @@ def test_scores_of_every_size(dtype):
 @pytest.mark.parametrize("lens,rows,packed", [([300, 200], None, False), ([300, 200], None, True), ([3000], [5], False)])
 def test_what_a_row_does_not_see_may_be_anything(lens, rows, packed, dtype):
     keys, rws, q, k, v = make(lens, rows, 4, 2, 128, dtype, packed, room=60, seed=11)
-    clean = check(keys, rws, q, k, v)
+    check(keys, rws, q, k, v)
+    want, _, bound = R.attend(q, k, v, keys, rws)
     # behind the sequences
     for t in (k, v):
         if packed:
@@ -134,17 +135,18 @@ def test_what_a_row_does_not_see_may_be_anything(lens, rows, packed, dtype):
     k[last], v[last] = math.nan, math.inf
     out, lse = attend(keys, rws, q, k, v)
     n_r = (rows or lens)[-1]
-    out_s = out[0, -60 - n_r:-60 or None] if packed else out[0, -1].transpose(0, 1)[:n_r]
-    was_s = clean[0][0, -60 - n_r:-60 or None] if packed else clean[0][0, -1].transpose(0, 1)[:n_r]
-    assert out_s[-1].isnan().all()
-    assert out_s[:-1].isfinite().all()
-    assert ((out_s[:-1] - was_s[:-1]).abs() <= 2 * torch.finfo(dtype).eps * (1 + was_s[:-1].abs())).all()
+    got, want, bound = (x[0, -60 - n_r:-60] if packed else x[0, -1].transpose(0, 1)[:n_r] for x in (out, want, bound))
+    assert got[-1].isnan().all()
+    assert got[:-1].isfinite().all()
+    assert ((got.double() - want).abs()[:-1] <= bound[:-1]).all()
 
 
 @pytest.mark.parametrize("dtype", TYPES)
 def test_values_that_are_not_numbers_show_where_they_are_seen(dtype):
     keys, rows, q, k, v = make([1000], None, 2, 1, 64, dtype, seed=12)
-    want, _ = attend(keys, rows, q, k, v)
+    # what does not see them is the formula's, to the formula's bound: tiles that are done by hand add d / 8 + 3 products to a score and 128 to a
+    # result one after the other, 19 and 128 steps of 2^-24 where the bound counts 28 and 375 (bf16: 8 and 62, and half a step of 2^-8 beside them)
+    want, bound = (x[0, 0] for x in R.attend(q, k, v, keys, rows)[::2])
     v[0, 0, 0, 400, 7] = math.nan
     v[0, 0, 0, 700, 9] = -math.inf
     out, lse = attend(keys, rows, q, k, v)
@@ -154,7 +156,7 @@ def test_values_that_are_not_numbers_show_where_they_are_seen(dtype):
     seen[:, 400:, 7] = True
     seen[:, 700:, 9] = True
     assert torch.equal(bad, seen)
-    assert ((out[0, 0] - want[0, 0]).abs()[~bad] <= 2 * torch.finfo(dtype).eps * (1 + want[0, 0].abs()[~bad])).all()
+    assert ((out[0, 0].double() - want).abs()[~bad] <= bound[~bad]).all()
     v.fill_(math.nan)                                          # and all of them
     assert attend(keys, rows, q, k, v)[0].isnan().all()
 
