@@ -26,14 +26,15 @@ namespace skv {
 // Three warpgroups of 168 registers a thread; the two with rows take 208 and leave the third 88 (2 x 208 + 88 = 3 x 168).
 constexpr int kPromptThreads = 384, kAskRole = 8, kIssueRole = 9;
 constexpr int kPromptItemSlots = 4;
+constexpr int kPart = 96;                 // keys of a tile whose weights the second product starts with
 
 template <int D>
 struct PromptSmem {
   static constexpr int kTile = kPromptRows * D * 2;                // bytes of a tile of rows, keys or values
   static constexpr int kHalf = kPromptRows * 128;                  // of its 64 elements side by side
-  static constexpr int kRing = D == 128 ? 5 : 8;
-  static constexpr int q = 0, ring = 2 * kTile, bars = ring + kRing * kTile;
-  static constexpr int kBars = 2 * kRing + 2 + 2 * 4 + 2 * kPromptItemSlots + 1;
+  static constexpr int kRing = D == 128 ? 4 : 6;
+  static constexpr int q = 0, ring = 2 * kTile, stage = ring + kRing * kTile, bars = stage + 8 * 4096;      // stage: 4 KB for each warp with rows
+  static constexpr int kBars = 2 * kRing + 2 + 2 * 5 + 2 * kPromptItemSlots + 1;
   static constexpr int words = bars + kBars * 8;                   // abort flags [2], TMEM address, redo at all, [4] copies that were asked for
   static constexpr int items = (words + 32 + 15) / 16 * 16;
   static constexpr int redo = items + kPromptItemSlots * (int)sizeof(PromptItem);
@@ -51,7 +52,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
   uint8_t* smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
   uint64_t* kv_full = reinterpret_cast<uint64_t*>(smem + S::bars);
   uint64_t *kv_empty = kv_full + RING, *q_full = kv_empty + RING, *q_empty = q_full + 1, *s_full = q_empty + 1, *p_full = s_full + 2, *o_full = p_full + 2,
-           *o_empty = o_full + 2, *item_full = o_empty + 2, *item_empty = item_full + SLOTS, *drained = item_empty + SLOTS;
+           *o_empty = o_full + 2, *p_part = o_empty + 2, *item_full = p_part + 2, *item_empty = item_full + SLOTS, *drained = item_empty + SLOTS;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::words);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::words) + 2;
   volatile int* any_redo = reinterpret_cast<volatile int*>(smem + S::words) + 3;
@@ -66,6 +67,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
     ptx::mbar_init(q_empty, 1);
     for (int w = 0; w < 2; ++w) {
       ptx::mbar_init(s_full + w, 1);
+      ptx::mbar_init(p_part + w, 4);
       ptx::mbar_init(p_full + w, 4);
       ptx::mbar_init(o_full + w, 1);
       ptx::mbar_init(o_empty + w, 4);
@@ -122,6 +124,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
     int n_s = 0, n_o = 0;                 // scores and results so far
     for (int pass = 0; pass == 0 || (pass == 1 && again()); ++pass) {
       const int w = warp >> 2, row = (warp & 3) * 32 + lane;
+      uint8_t* stage = smem + S::stage + warp * 4096;
       const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tmem + w * 128 + lanes, to = tmem_o + w * D + lanes;
       PromptItem it;
       while (ok && next_item(it, ok)) {
@@ -148,8 +151,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
           }
           float top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-          for (int c = 0; c < 128; c += 2) top[(c >> 1) & 3] = fmaxf(fmaxf(top[(c >> 1) & 3], __uint_as_float(s[c >> 5][c & 31])), __uint_as_float(s[c >> 5][(c & 31) + 1]));
-          const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale;
+          for (int c = 0; c < 128; c += 2) top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(s[c >> 5][c & 31]), __uint_as_float(s[c >> 5][(c & 31) + 1]));
+          const float high = max3(max3(top[0], top[1], top[2]), top[3], top[3]) * p.scale;
+          if (!(high < CUDART_INF_F)) l = CUDART_NAN_F;      // (and so it stays)
           if (j == 0) {
             m = high;
           } else if (__any_sync(0xffffffffu, high > m + kPromptLazy)) {
@@ -175,12 +179,22 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
               float2 x = fma_pair(make_float2(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1])), make_float2(p.scale, p.scale), make_float2(-ref, -ref));
-              x.x = pow2(x.x);
-              x.y = pow2(x.y);
+              if ((i & 7) == 6) {
+                x = pow2_pair(x);
+              } else {
+                x.x = pow2(x.x);
+                x.y = pow2(x.y);
+              }
               sum[(i >> 1) & 1] = add_pair(sum[(i >> 1) & 1], x);
               h[i >> 1] = pack_bf16(x.x, x.y);
             }
             ptx::tmem_st_32x16(ts + c * 16, h);
+            if (c == kPart / 32 - 1) {
+              ptx::tmem_st_wait();
+              ptx::tc_fence_before();
+              __syncwarp();
+              if (lane == 0) ptx::mbar_arrive(p_part + w);
+            }
           }
           l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
           ptx::tmem_st_wait();
@@ -192,48 +206,52 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
         if (n > 0) ok = wait(o_full + w, n_o++) && ok;
         __syncwarp();
         ptx::tc_fence_after();
+        if (it.careful && n > tiles.even[w])
+          add_by_hand<T, D>(p, it, to, tiles.even[w] == 0, head, there ? pos : 0, (tiles.first + tiles.even[w]) * KT, there ? min(sees, (tiles.first + n) * KT) : 0,
+                            m == -CUDART_INF_F ? 0.f : m);
         const bool write = there && ok && !*abort_flag;
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        const int64_t number = row_number(p, layer, seq, it.base_r, head, pos);
-        T* dst = reinterpret_cast<T*>(const_cast<void*>(p.out.ptr)) + row_offset(p.out, p.rows, layer, seq, it.base_r, head, pos);
+        const int64_t number = row_number(p, layer, seq, it.base_r, head, pos), parts = (int64_t)it.split * p.rows.n_layers * p.rows.total_len * (p.heads * p.hn);
+        const int64_t at = !write ? -1 : p.splits > 1 ? (parts + number) * D * 4 : row_offset(p.out, p.rows, layer, seq, it.base_r, head, pos) * 2;
+        uint8_t* base = reinterpret_cast<uint8_t*>(p.splits > 1 ? p.part : const_cast<void*>(p.out.ptr));
         bool odd = false;
 #pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          uint32_t o[32];
-          if (n > 0) {
-            __syncwarp();
-            ptx::tmem_ld_32x32_sync(to + c, o);
-          }
-          float x[32];
+        for (int c = 0; c < D; c += 64) {
+          float x[64];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) x[i] = n > 0 && (!it.careful || tiles.even[w] > 0) ? __uint_as_float(o[i]) : 0.f;
-          if (it.careful && there && n > tiles.even[w]) {
-            float y[32];
+          for (int i = 0; i < 64; i += 32) {
+            uint32_t o[32];
+            if (n > 0) {
+              __syncwarp();
+              ptx::tmem_ld_32x32_sync(to + c + i, o);
+            }
 #pragma unroll
-            for (int i = 0; i < 32; ++i) y[i] = x[i];
-            add_by_hand<T, D>(p, it, layer, seq, head, pos, (tiles.first + tiles.even[w]) * KT, min(sees, (tiles.first + n) * KT), m == -CUDART_INF_F ? 0.f : m, c, y);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = y[i];
+            for (int e = 0; e < 32; ++e) x[i + e] = n > 0 ? __uint_as_float(o[e]) : 0.f;
           }
 #pragma unroll
-          for (int i = 0; i < 32; ++i) odd |= x[i] != x[i];
-          if (!write) continue;
+          for (int e = 0; e < 64; ++e) odd |= x[e] != x[e];
+          uint4 h[8];
           if (p.splits > 1) {
-            float* part = p.part + ((int64_t)it.split * p.rows.n_layers * p.rows.total_len * (p.heads * p.hn) + number) * D + c;
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(part + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+            for (int i = 0; i < 64; i += 32) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                h[e] = make_uint4(__float_as_uint(x[i + 4 * e]), __float_as_uint(x[i + 4 * e + 1]), __float_as_uint(x[i + 4 * e + 2]), __float_as_uint(x[i + 4 * e + 3]));
+              put_rows(stage, h, base + (c + i) * 4, at);
+            }
           } else {
 #pragma unroll
-            for (int i = 0; i < 32; i += 8)
-              *reinterpret_cast<uint4*>(dst + c + i) = make_uint4(pack_bf16(x[i] * inv, x[i + 1] * inv), pack_bf16(x[i + 2] * inv, x[i + 3] * inv),
-                                                                  pack_bf16(x[i + 4] * inv, x[i + 5] * inv), pack_bf16(x[i + 6] * inv, x[i + 7] * inv));
+            for (int e = 0; e < 8; ++e)
+              h[e] = make_uint4(pack_bf16(x[8 * e] * inv, x[8 * e + 1] * inv), pack_bf16(x[8 * e + 2] * inv, x[8 * e + 3] * inv),
+                                pack_bf16(x[8 * e + 4] * inv, x[8 * e + 5] * inv), pack_bf16(x[8 * e + 6] * inv, x[8 * e + 7] * inv));
+            put_rows(stage, h, base + c * 2, at);
           }
         }
         ptx::tc_fence_before();
         __syncwarp();
         if (n > 0 && lane == 0) ptx::mbar_arrive(o_empty + w);
         if (write) {
-          if (p.splits > 1) p.stat[(int64_t)it.split * p.rows.n_layers * p.rows.total_len * (p.heads * p.hn) + number] = make_float2(m, l);
+          if (p.splits > 1) p.stat[parts + number] = make_float2(m, l);
           else put_lse(p, number, m, l);
           // (only what is hidden from a row can make its result NaN where its sum is a number; what it sees does so again)
           if (odd && !it.careful && l == l) {
@@ -346,14 +364,18 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
           for (int w = 0; w < 2; ++w) {
             if (j >= tiles.count[w] || !ok) continue;
             if (j == 0) ok = wait(o_empty + w, n_o[w]++ + 1);
+            auto values = [&](int k0, int k1) {      // of 16 keys each
+              ptx::tc_fence_after();
+              if (it.careful && j >= tiles.even[w]) return;
+#pragma unroll
+              for (int k = k0; k < k1; ++k)
+                ptx::umma_bf16_ts_elected(tmem_o + w * D, tmem + w * 128 + k * 8, dv + (av * S::kTile >> 4) + (k * 2048 >> 4), idesc_o, j == 0 && k == 0 ? 0u : 1u, issues);
+            };
+            ok = __all_sync(0xffffffffu, wait(p_part + w, n_s[w]) && ok);
+            if (ok) values(0, kPart / 16);
             ok = __all_sync(0xffffffffu, wait(p_full + w, n_s[w]++) && ok);
             if (!ok) continue;
-            ptx::tc_fence_after();
-            if (!it.careful || j < tiles.even[w]) {
-#pragma unroll
-              for (int k = 0; k < KT / 16; ++k)
-                ptx::umma_bf16_ts_elected(tmem_o + w * D, tmem + w * 128 + k * 8, dv + (av * S::kTile >> 4) + (k * 2048 >> 4), idesc_o, j == 0 && k == 0 ? 0u : 1u, issues);
-            }
+            values(kPart / 16, KT / 16);
             if (j + 1 < tiles.count[w]) scores(w, ak);
             else release(o_full + w);
           }

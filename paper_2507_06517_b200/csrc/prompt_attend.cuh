@@ -198,31 +198,85 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
-// What masked tiles give to 32 elements of a row, key by key: the tiles whose values are not all numbers.  Rare
-template <typename T, int D>
-__device__ __noinline__ void add_by_hand(const PromptParams& p, const PromptItem& it, int layer, int seq, int head, int pos, int from, int to, float ref, int d0,
-                                         float (&o)[32]) {
-  const T* q = reinterpret_cast<const T*>(p.q.ptr) + row_offset(p.q, p.rows, layer, seq, it.base_r, head, pos);
-  for (int j = from; j < to; ++j) {
-    const T* k = reinterpret_cast<const T*>(p.k.ptr) + row_offset(p.k, p.keys, layer, seq, it.base_k, it.head, j);
-    const T* v = reinterpret_cast<const T*>(p.v.ptr) + row_offset(p.v, p.keys, layer, seq, it.base_k, it.head, j) + d0;
-    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int d = 0; d < D; d += 8) {
-      float a[8], b[8];
-      load8(q + d, a);
-      load8(k + d, b);
+// The largest of three; NaN if one of them is
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// 2^x of two numbers without the special function unit: x = n + f, |f| <= 1/2, 2^f by a polynomial of degree 4 fitted to the least relative error
+// (2.7e-6 in fp32), n added to the exponent.  0 below 2^-126; not for NaN or infinity.
+__device__ __forceinline__ float2 pow2_pair(float2 x) {
+  const float2 magic = make_float2(12582912.f, 12582912.f), t = add_pair(x, magic);        // n in the low bits
+  const float2 n = add_pair(t, make_float2(-12582912.f, -12582912.f)), f = fma_pair(n, make_float2(-1.f, -1.f), x);
+  float2 y = make_float2(0.009570101902682773f, 0.009570101902682773f);
+  y = fma_pair(y, f, make_float2(0.05591786031871889f, 0.05591786031871889f));
+  y = fma_pair(y, f, make_float2(0.2402474482807297f, 0.2402474482807297f));
+  y = fma_pair(y, f, make_float2(0.6931218147368134f, 0.6931218147368134f));
+  y = fma_pair(y, f, make_float2(0.9999992614456492f, 0.9999992614456492f));
+  y.x = x.x < -126.f ? 0.f : __uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23));
+  y.y = x.y < -126.f ? 0.f : __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23));
+  return y;
+}
+// 128 bytes of a warp's 32 rows, a row in each lane, to memory: through shared memory, so that a store covers four rows and not a piece of each.
+// `row`: where a lane's row lies behind `base`, in bytes; negative: nowhere
+__device__ __forceinline__ void put_rows(uint8_t* stage, const uint4 (&piece)[8], uint8_t* base, int64_t row) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[i] = fmaf(a[i], b[i], s[i]);
-    }
-    const float w = pow2(fmaf(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])), p.scale, -ref));
+  for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(stage + lane * 128 + ((i ^ (lane & 7)) << 4)) = piece[i];
+  __syncwarp();
 #pragma unroll
-    for (int d = 0; d < 32; d += 8) {
-      float b[8];
-      load8(v + d, b);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o[d + i] = fmaf(w, b[i], o[d + i]);
-    }
+  for (int i = 0; i < 8; ++i) {
+    const int r = i * 4 + (lane >> 3);
+    const int64_t at = __shfl_sync(0xffffffffu, row, r);
+    const uint4 x = *reinterpret_cast<const uint4*>(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+    if (at >= 0) *reinterpret_cast<uint4*>(base + at + (lane & 7) * 16) = x;
   }
+  __syncwarp();
+}
+
+// What a row's tiles that hide keys from some row give to O in tensor memory (`o_tmem`: this warp's lanes), key by key: the keys [from, to) of a row,
+// none for to <= from.  `begins`: O holds nothing yet.  Rare, and so a function of its own that costs the others no registers
+template <typename T, int D>
+__device__ __noinline__ void add_by_hand(const PromptParams& p, const PromptItem& it, uint32_t o_tmem, bool begins, int head, int pos, int from, int to, float ref) {
+  const int layer = it.ls / p.rows.n_seqs, seq = it.ls - layer * p.rows.n_seqs;
+  const T* q = reinterpret_cast<const T*>(p.q.ptr) + row_offset(p.q, p.rows, layer, seq, it.base_r, head, pos);
+#pragma unroll 1
+  for (int c = 0; c < D; c += 32) {
+    uint32_t o[32];
+    __syncwarp();
+    ptx::tmem_ld_32x32_sync(o_tmem + c, o);
+    float x[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = begins ? 0.f : __uint_as_float(o[i]);
+#pragma unroll 1
+    for (int j = from; j < to; ++j) {
+      const T* k = reinterpret_cast<const T*>(p.k.ptr) + row_offset(p.k, p.keys, layer, seq, it.base_k, it.head, j);
+      const T* v = reinterpret_cast<const T*>(p.v.ptr) + row_offset(p.v, p.keys, layer, seq, it.base_k, it.head, j) + c;
+      float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int d = 0; d < D; d += 8) {
+        float a[8], b[8];
+        load8(q + d, a);
+        load8(k + d, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = fmaf(a[i], b[i], s[i]);
+      }
+      const float w = pow2(fmaf(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])), p.scale, -ref));
+#pragma unroll
+      for (int d = 0; d < 32; d += 8) {
+        float b[8];
+        load8(v + d, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[d + i] = fmaf(w, b[i], x[d + i]);
+      }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(x[i]);
+    ptx::tmem_st_32x32(o_tmem + c, o);
+  }
+  ptx::tmem_st_wait();
 }
 
 // Joins the parts of a row: a warp for each (layer, column, query head).

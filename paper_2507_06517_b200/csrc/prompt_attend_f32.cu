@@ -27,7 +27,7 @@ struct ExactSmem {
   static constexpr int kQHalf = kPromptRows * 128, kQPiece = D / 64 * kQHalf;
   static constexpr int kHalf = kExactKeys * 128, kPiece = D / 64 * kHalf, kSlot = kPieces * kPiece;
   static constexpr int kRing = D == 128 ? 1 : 2;                             // slots of keys, and of values
-  static constexpr int q = 0, k = kPieces * kQPiece, v = k + kRing * kSlot, bars = v + kRing * kSlot;
+  static constexpr int q = 0, k = kPieces * kQPiece, v = k + kRing * kSlot, stage = v + kRing * kSlot, bars = stage + 4 * 4096;
   static constexpr int kBars = 4 * kRing + 2 + 2 + 1 + 2 + 2 + 2 * kExactSlots + 1;
   static constexpr int words = bars + kBars * 8;
   static constexpr int items = (words + 32 + 15) / 16 * 16;
@@ -380,10 +380,16 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
         if (n > 0) ok = wait(o_full, n_o++) && ok;
         __syncwarp();
         ptx::tc_fence_after();
+        if (it.careful && n > tiles.even[0])
+          add_by_hand<T, D>(p, it, to, tiles.even[0] == 0, head, there ? pos : 0, (tiles.first + tiles.even[0]) * KT, there ? min(sees, (tiles.first + n) * KT) : 0,
+                            m == -CUDART_INF_F ? 0.f : m);
         const bool write = there && ok && !*abort_flag;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const int64_t number = row_number(p, layer, seq, it.base_r, head, pos);
-        T* dst = reinterpret_cast<T*>(const_cast<void*>(p.out.ptr)) + row_offset(p.out, p.rows, layer, seq, it.base_r, head, pos);
+        const int64_t parts = (int64_t)it.split * p.rows.n_layers * p.rows.total_len * (p.heads * p.hn);
+        const int64_t at = !write ? -1 : (p.splits > 1 ? (parts + number) * D : row_offset(p.out, p.rows, layer, seq, it.base_r, head, pos)) * 4;
+        uint8_t* base = reinterpret_cast<uint8_t*>(p.splits > 1 ? p.part : const_cast<void*>(p.out.ptr));
+        const float f = p.splits > 1 ? 1.f : inv;
         bool odd = false;
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
@@ -394,28 +400,20 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
           }
           float x[32];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) x[i] = n > 0 && (!it.careful || tiles.even[0] > 0) ? __uint_as_float(o[i]) : 0.f;
-          if (it.careful && there && n > tiles.even[0]) {
-            float y[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) y[i] = x[i];
-            add_by_hand<T, D>(p, it, layer, seq, head, pos, (tiles.first + tiles.even[0]) * KT, min(sees, (tiles.first + n) * KT), m == -CUDART_INF_F ? 0.f : m, c, y);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = y[i];
-          }
+          for (int i = 0; i < 32; ++i) x[i] = n > 0 ? __uint_as_float(o[i]) : 0.f;
 #pragma unroll
           for (int i = 0; i < 32; ++i) odd |= x[i] != x[i];
-          if (!write) continue;
-          float* to_row = p.splits > 1 ? p.part + ((int64_t)it.split * p.rows.n_layers * p.rows.total_len * (p.heads * p.hn) + number) * D + c : dst + c;
-          const float f = p.splits > 1 ? 1.f : inv;
+          uint4 h[8];
 #pragma unroll
-          for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(to_row + i) = make_float4(x[i] * f, x[i + 1] * f, x[i + 2] * f, x[i + 3] * f);
+          for (int e = 0; e < 8; ++e)
+            h[e] = make_uint4(__float_as_uint(x[4 * e] * f), __float_as_uint(x[4 * e + 1] * f), __float_as_uint(x[4 * e + 2] * f), __float_as_uint(x[4 * e + 3] * f));
+          put_rows(smem + S::stage + warp * 4096, h, base + c * 4, at);
         }
         ptx::tc_fence_before();
         __syncwarp();
         if (n > 0 && lane == 0) ptx::mbar_arrive(o_empty);
         if (write) {
-          if (p.splits > 1) p.stat[(int64_t)it.split * p.rows.n_layers * p.rows.total_len * (p.heads * p.hn) + number] = make_float2(m, l);
+          if (p.splits > 1) p.stat[parts + number] = make_float2(m, l);
           else put_lse(p, number, m, l);
           if (odd && !it.careful && l == l) {
             atomicOr(redo + (it.number >> 5), 1u << (it.number & 31));
