@@ -59,7 +59,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
   volatile int* asked = reinterpret_cast<volatile int*>(smem + S::words) + 4;    // keys or values, rows
   PromptItem* items = reinterpret_cast<PromptItem*>(smem + S::items);
   uint32_t* redo = reinterpret_cast<uint32_t*>(smem + S::redo);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // (broadcasts, here and where products are issued, say that a value is the whole warp's: descriptors are then formed where the products take them from)
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
   if (tid == 0) {
     for (int i = 0; i < RING; ++i) { ptx::mbar_init(kv_full + i, 1); ptx::mbar_init(kv_empty + i, 1); }
@@ -97,7 +98,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   __syncthreads();
   ptx::tc_fence_after();
-  const uint32_t tmem = *tmem_slot, tmem_o = tmem + 256;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0), tmem_o = tmem + 256;
 
   auto wait = [&](uint64_t* bar, int phase) { return ptx::mbar_wait(bar, phase & 1, abort_flag, p.wait_cycles); };
   int item_no = 0;                        // items so far, both passes' and the ends of passes
@@ -126,32 +127,46 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
       const int w = warp >> 2, row = (warp & 3) * 32 + lane;
       uint8_t* stage = smem + S::stage + warp * 4096;
       const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tmem + w * 128 + lanes, to = tmem_o + w * D + lanes;
-      PromptItem it;
-      while (ok && next_item(it, ok)) {
-        const PromptTiles<2, KT> tiles(p, it);
-        const int layer = it.ls / p.rows.n_seqs, seq = it.ls - layer * p.rows.n_seqs;
-        const int within = row / p.hn, head = it.head * p.hn + row - within * p.hn, pos = it.blk * p.per_item + w * p.pt + within;
-        const bool there = within < p.pt && pos < it.n_r;
-        const int n = tiles.count[w], sees = there ? seen_by(pos, it.n_r, it.n_k) : 0x7FFFFFFF;
+      while (ok) {
+        // The item stays in its slot until its result is written: registers are short here
+        const int slot = item_no % SLOTS;
+        ok = __all_sync(0xffffffffu, wait(item_full + slot, item_no / SLOTS));
+        if (!ok) break;
+        const PromptItem* held = items + slot;
+        ++item_no;
+        if (held->ls < 0) {
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(item_empty + slot);
+          break;
+        }
+        int n, first, even, sees;
+        bool careful;
+        {
+          const PromptItem it = *held;
+          const PromptTiles<2, KT> tiles(p, it);
+          const int within = row / p.hn, pos = it.blk * p.per_item + w * p.pt + within;
+          n = w ? tiles.count[1] : tiles.count[0];
+          even = w ? tiles.even[1] : tiles.even[0];
+          first = tiles.first;
+          careful = it.careful != 0;
+          sees = within < p.pt && pos < it.n_r ? seen_by(pos, it.n_r, it.n_k) : 0x7FFFFFFF;
+        }
         float m = -CUDART_INF_F, l = 0.f;
         for (int j = 0; j < n; ++j) {
           ok = wait(s_full + w, n_s++) && ok;
           __syncwarp();
           ptx::tc_fence_after();
-          uint32_t s[4][32];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(ts + c * 32, s[c]);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) ptx::tmem_ld_wait(s[c]);
-          if (j >= tiles.even[w]) {
-            const int left = sees - (tiles.first + j) * KT;
+          uint32_t s[128];
+          ptx::tmem_ld_32x128_sync(ts, s);
+          if (j >= even) {
+            const int left = sees - (first + j) * KT;
 #pragma unroll
             for (int c = 0; c < 128; ++c)
-              if (c >= left) s[c >> 5][c & 31] = 0xFF800000u;
+              if (c >= left) s[c] = 0xFF800000u;
           }
           float top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-          for (int c = 0; c < 128; c += 2) top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(s[c >> 5][c & 31]), __uint_as_float(s[c >> 5][(c & 31) + 1]));
+          for (int c = 0; c < 128; c += 2) top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
           const float high = max3(max3(top[0], top[1], top[2]), top[3], top[3]) * p.scale;
           if (!(high < CUDART_INF_F)) l = CUDART_NAN_F;      // (and so it stays)
           if (j == 0) {
@@ -160,14 +175,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
             const float now = fmaxf(m, high), f = now == m ? 1.f : pow2(m - now);
             m = now;
             l *= f;
-            if (!it.careful || tiles.even[w] > 0) {
+            if (!careful || even > 0) {
 #pragma unroll 1
-              for (int c = 0; c < D; c += 32) {
-                uint32_t o[32];
-                ptx::tmem_ld_32x32_sync(to + c, o);
+              for (int c = 0; c < D; c += 8) {
+                uint32_t o[8];
+                ptx::tmem_ld_32x8_sync(to + c, o);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                ptx::tmem_st_32x32(to + c, o);
+                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                ptx::tmem_st_32x8_sync(to + c, o);
               }
             }
           }
@@ -178,13 +193,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
             uint32_t h[16];
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
-              float2 x = fma_pair(make_float2(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1])), make_float2(p.scale, p.scale), make_float2(-ref, -ref));
-              if ((i & 7) == 6) {
-                x = pow2_pair(x);
-              } else {
-                x.x = pow2(x.x);
-                x.y = pow2(x.y);
-              }
+              float2 x = fma_pair(make_float2(__uint_as_float(s[c * 32 + i]), __uint_as_float(s[c * 32 + i + 1])), make_float2(p.scale, p.scale), make_float2(-ref, -ref));
+              x.x = pow2(x.x);
+              x.y = pow2(x.y);
               sum[(i >> 1) & 1] = add_pair(sum[(i >> 1) & 1], x);
               h[i >> 1] = pack_bf16(x.x, x.y);
             }
@@ -203,12 +214,17 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
           if (lane == 0) ptx::mbar_arrive(p_full + w);
         }
         // ---- the item's result ----
+        const PromptItem it = *held;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(item_empty + slot);
+        const int layer = it.ls / p.rows.n_seqs, seq = it.ls - layer * p.rows.n_seqs;
+        const int within = row / p.hn, head = it.head * p.hn + row - within * p.hn, pos = it.blk * p.per_item + w * p.pt + within;
+        const bool there = sees != 0x7FFFFFFF;
         if (n > 0) ok = wait(o_full + w, n_o++) && ok;
         __syncwarp();
         ptx::tc_fence_after();
-        if (it.careful && n > tiles.even[w])
-          add_by_hand<T, D>(p, it, to, tiles.even[w] == 0, head, there ? pos : 0, (tiles.first + tiles.even[w]) * KT, there ? min(sees, (tiles.first + n) * KT) : 0,
-                            m == -CUDART_INF_F ? 0.f : m);
+        if (careful && n > even)
+          add_by_hand<T, D>(p, it, to, 0, D, even == 0, head, there ? pos : 0, (first + even) * KT, there ? min(sees, (first + n) * KT) : 0, m == -CUDART_INF_F ? 0.f : m);
         const bool write = there && ok && !*abort_flag;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const int64_t number = row_number(p, layer, seq, it.base_r, head, pos), parts = (int64_t)it.split * p.rows.n_layers * p.rows.total_len * (p.heads * p.hn);
@@ -328,8 +344,18 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
                      dv = ptx::smem_desc_sw128_mn(ptx::smem_u32(smem + S::ring), S::kHalf);
       PromptItem it;
       while (ok && next_item(it, ok)) {
-        const PromptTiles<2, KT> tiles(p, it);
-        if (tiles.most == 0) continue;
+        int most, count[2], even[2];
+        {
+          const PromptTiles<2, KT> tiles(p, it);
+          auto all = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+          most = all(tiles.most);
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            count[w] = all(tiles.count[w]);
+            even[w] = all(it.careful ? tiles.even[w] : tiles.count[w]);      // tiles whose values are multiplied here
+          }
+        }
+        if (most == 0) continue;
         auto scores = [&](int w, int at) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
@@ -350,23 +376,23 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
         ptx::tc_fence_after();
 #pragma unroll
         for (int w = 0; w < 2; ++w)
-          if (tiles.count[w] > 0) scores(w, at);
+          if (count[w] > 0) scores(w, at);
         release(kv_empty + at);
         ++n_kv;
-        if (tiles.most == 1) release(q_empty);
-        for (int j = 0; j < tiles.most && ok; ++j) {
+        if (most == 1) release(q_empty);
+        for (int j = 0; j < most && ok; ++j) {
           const int av = n_kv % RING, ak = (n_kv + 1) % RING;
-          const bool more = j + 1 < tiles.most;
+          const bool more = j + 1 < most;
           ok = wait(kv_full + av, n_kv / RING);
           if (more) ok = wait(kv_full + ak, (n_kv + 1) / RING) && ok;
           ok = __all_sync(0xffffffffu, ok);
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
-            if (j >= tiles.count[w] || !ok) continue;
+            if (j >= count[w] || !ok) continue;
             if (j == 0) ok = wait(o_empty + w, n_o[w]++ + 1);
             auto values = [&](int k0, int k1) {      // of 16 keys each
               ptx::tc_fence_after();
-              if (it.careful && j >= tiles.even[w]) return;
+              if (j >= even[w]) return;
 #pragma unroll
               for (int k = k0; k < k1; ++k)
                 ptx::umma_bf16_ts_elected(tmem_o + w * D, tmem + w * 128 + k * 8, dv + (av * S::kTile >> 4) + (k * 2048 >> 4), idesc_o, j == 0 && k == 0 ? 0u : 1u, issues);
@@ -376,13 +402,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
             ok = __all_sync(0xffffffffu, wait(p_full + w, n_s[w]++) && ok);
             if (!ok) continue;
             values(kPart / 16, KT / 16);
-            if (j + 1 < tiles.count[w]) scores(w, ak);
+            if (j + 1 < count[w]) scores(w, ak);
             else release(o_full + w);
           }
           if (!ok) break;
           release(kv_empty + av);
           if (more) release(kv_empty + ak);
-          if (j + 2 == tiles.most) release(q_empty);
+          if (j + 2 == most) release(q_empty);
           n_kv += more ? 2 : 1;
         }
       }
@@ -391,7 +417,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
       again();
     }
   }
-  __syncwarp();
+  __syncthreads();                        // nobody reads the tensor memory any more
   if (warp == kIssueRole) {
     if (ptx::elect_one()) ptx::umma_commit(drained);
     __syncwarp();

@@ -204,45 +204,35 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// 2^x of two numbers without the special function unit: x = n + f, |f| <= 1/2, 2^f by a polynomial of degree 4 fitted to the least relative error
-// (2.7e-6 in fp32), n added to the exponent.  0 below 2^-126; not for NaN or infinity.
-__device__ __forceinline__ float2 pow2_pair(float2 x) {
-  const float2 magic = make_float2(12582912.f, 12582912.f), t = add_pair(x, magic);        // n in the low bits
-  const float2 n = add_pair(t, make_float2(-12582912.f, -12582912.f)), f = fma_pair(n, make_float2(-1.f, -1.f), x);
-  float2 y = make_float2(0.009570101902682773f, 0.009570101902682773f);
-  y = fma_pair(y, f, make_float2(0.05591786031871889f, 0.05591786031871889f));
-  y = fma_pair(y, f, make_float2(0.2402474482807297f, 0.2402474482807297f));
-  y = fma_pair(y, f, make_float2(0.6931218147368134f, 0.6931218147368134f));
-  y = fma_pair(y, f, make_float2(0.9999992614456492f, 0.9999992614456492f));
-  y.x = x.x < -126.f ? 0.f : __uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23));
-  y.y = x.y < -126.f ? 0.f : __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23));
-  return y;
-}
-// 128 bytes of a warp's 32 rows, a row in each lane, to memory: through shared memory, so that a store covers four rows and not a piece of each.
+// NP x 16 bytes of a warp's 32 rows, a row in each lane, to memory: through shared memory, so that a store covers whole pieces of few rows.
 // `row`: where a lane's row lies behind `base`, in bytes; negative: nowhere
-__device__ __forceinline__ void put_rows(uint8_t* stage, const uint4 (&piece)[8], uint8_t* base, int64_t row) {
+template <int NP>
+__device__ __forceinline__ void put_rows(uint8_t* stage, const uint4 (&piece)[NP], uint8_t* base, int64_t row) {
+  constexpr int kRows = 32 / NP;         // of a store
   const int lane = threadIdx.x & 31;
+  // (rows that share banks take different places for a piece)
+  auto place = [](int r, int i) { return r * (NP * 16) + ((i ^ (NP == 8 ? r : r >> 1) & (NP - 1)) << 4); };
 #pragma unroll
-  for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(stage + lane * 128 + ((i ^ (lane & 7)) << 4)) = piece[i];
+  for (int i = 0; i < NP; ++i) *reinterpret_cast<uint4*>(stage + place(lane, i)) = piece[i];
   __syncwarp();
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = i * 4 + (lane >> 3);
+  for (int i = 0; i < NP; ++i) {
+    const int r = i * kRows + lane / NP;
     const int64_t at = __shfl_sync(0xffffffffu, row, r);
-    const uint4 x = *reinterpret_cast<const uint4*>(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
-    if (at >= 0) *reinterpret_cast<uint4*>(base + at + (lane & 7) * 16) = x;
+    const uint4 x = *reinterpret_cast<const uint4*>(stage + place(r, lane % NP));
+    if (at >= 0) *reinterpret_cast<uint4*>(base + at + (lane % NP) * 16) = x;
   }
   __syncwarp();
 }
 
-// What a row's tiles that hide keys from some row give to O in tensor memory (`o_tmem`: this warp's lanes), key by key: the keys [from, to) of a row,
-// none for to <= from.  `begins`: O holds nothing yet.  Rare, and so a function of its own that costs the others no registers
+// What a row's tiles that hide keys from some row give to the elements [c0, c1) of O in tensor memory (`o_tmem`: this warp's lanes), key by key: the keys
+// [from, to) of a row, none for to <= from.  `begins`: O holds nothing yet.  Rare, and so a function of its own that costs the others no registers
 template <typename T, int D>
-__device__ __noinline__ void add_by_hand(const PromptParams& p, const PromptItem& it, uint32_t o_tmem, bool begins, int head, int pos, int from, int to, float ref) {
+__device__ __noinline__ void add_by_hand(const PromptParams& p, const PromptItem& it, uint32_t o_tmem, int c0, int c1, bool begins, int head, int pos, int from, int to, float ref) {
   const int layer = it.ls / p.rows.n_seqs, seq = it.ls - layer * p.rows.n_seqs;
   const T* q = reinterpret_cast<const T*>(p.q.ptr) + row_offset(p.q, p.rows, layer, seq, it.base_r, head, pos);
 #pragma unroll 1
-  for (int c = 0; c < D; c += 32) {
+  for (int c = c0; c < c1; c += 32) {
     uint32_t o[32];
     __syncwarp();
     ptx::tmem_ld_32x32_sync(o_tmem + c, o);

@@ -314,20 +314,17 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
           ok = wait(s_full + (n_kv & 1), n_kv >> 1) && ok;
           __syncwarp();
           ptx::tc_fence_after();
-          uint32_t s[2][32];
-#pragma unroll
-          for (int c = 0; c < 2; ++c) ptx::tmem_ld_32x32(tmem + (n_kv & 1) * KT + lanes + c * 32, s[c]);
-#pragma unroll
-          for (int c = 0; c < 2; ++c) ptx::tmem_ld_wait(s[c]);
+          uint32_t s[KT];
+          ptx::tmem_ld_32x64_sync(tmem + (n_kv & 1) * KT + lanes, s);
           if (j >= tiles.even[0]) {
             const int left = sees - (tiles.first + j) * KT;
 #pragma unroll
             for (int c = 0; c < KT; ++c)
-              if (c >= left) s[c >> 5][c & 31] = 0xFF800000u;
+              if (c >= left) s[c] = 0xFF800000u;
           }
           float top[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-          for (int c = 0; c < KT; ++c) top[c & 3] = fmaxf(top[c & 3], __uint_as_float(s[c >> 5][c & 31]));
+          for (int c = 0; c < KT; ++c) top[c & 3] = fmaxf(top[c & 3], __uint_as_float(s[c]));
           const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale;
           if (j == 0) {
             m = high;
@@ -360,7 +357,7 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
               uint32_t a[2][kPieces];
 #pragma unroll
               for (int u = 0; u < 2; ++u) {
-                const float x = pow2(fmaf(__uint_as_float(s[c][i + u]), p.scale, -ref));
+                const float x = pow2(fmaf(__uint_as_float(s[c * 32 + i + u]), p.scale, -ref));
                 sum[u] += x;
                 pieces_of(x, a[u][0], a[u][1], a[u][2]);
               }
@@ -381,7 +378,7 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
         __syncwarp();
         ptx::tc_fence_after();
         if (it.careful && n > tiles.even[0])
-          add_by_hand<T, D>(p, it, to, tiles.even[0] == 0, head, there ? pos : 0, (tiles.first + tiles.even[0]) * KT, there ? min(sees, (tiles.first + n) * KT) : 0,
+          add_by_hand<T, D>(p, it, to, 0, D, tiles.even[0] == 0, head, there ? pos : 0, (tiles.first + tiles.even[0]) * KT, there ? min(sees, (tiles.first + n) * KT) : 0,
                             m == -CUDART_INF_F ? 0.f : m);
         const bool write = there && ok && !*abort_flag;
         const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -424,7 +421,7 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
       }
     }
   }
-  __syncwarp();
+  __syncthreads();                        // nobody reads the tensor memory any more
   if (warp == kExactIssue) {
     if (ptx::elect_one()) ptx::umma_commit(drained);
     __syncwarp();
