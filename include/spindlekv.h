@@ -428,6 +428,25 @@ spindlekv_status spindlekv_paged_append(const spindlekv_page_pool* pool, const s
                                         int32_t idx_len, int32_t idx_seq, void* stream);
 
 /*
+ * spindlekv_paged_append of rows that their position's rotation turns on the way (spindlekv_rope_table: elements i and i + head_dim / 2 by the angle of
+ * pair i).  Row r of a sequence stands at position first_pos[layer][seq] + r, wherever it goes in the cache: what eviction kept takes the
+ * positions that it had in the prompt.  V is not rotated.
+ *   rope_table, table_positions  as for spindlekv_decode_attend, 16-byte aligned; a row whose position lies outside the table turns into NaN
+ *   first_pos  device [n_layers][n_seqs], or NULL: start with rows in order, 0 with a list
+ *   K_out      rotated keys [layer][seq][kv head][row][d], or ptr NULL: none.  May be K itself
+ *   n_q_heads, Q, Q_out  0, or queries [layer][seq][q head][row][d] of the same rows, which are rotated alike and go nowhere else.  Q_out may be Q itself
+ * K_out and Q_out hold rows 0 .. lens - start - 1 (none of n_rows and above); those behind are left as they were, and so are all of a sequence that is
+ * skipped.  A key's row is written even where its page is missing.  With `idx` both must be absent (lists differ from head to head).
+ * The rotation is formed in fp32, its two products and their sum each rounded by itself, and then rounded to the rows' type: codes, scales and rows
+ * are those of rotating first and appending the result, bit for bit.
+ */
+spindlekv_status spindlekv_paged_append_rotated(const spindlekv_page_pool* pool, const spindlekv_page_table* table, const int32_t* start,
+                                                int32_t max_new, spindlekv_tensor K, spindlekv_tensor V, int32_t n_rows, const int32_t* idx,
+                                                int32_t idx_len, int32_t idx_seq, const void* rope_table, int32_t table_positions,
+                                                const int32_t* first_pos, spindlekv_tensor K_out, int32_t n_q_heads, spindlekv_tensor Q,
+                                                spindlekv_tensor Q_out, void* stream);
+
+/*
  * Attention of the newest tokens over the paged cache.  The n_rows query rows of a sequence are its last n_rows tokens, already
  * appended: row r sees the tokens 0 .. lens - n_rows + r.  For KV head j and query head g of its group
  *     out_r = softmax_t( q_r . K_t * scale ) V_t ,
@@ -476,6 +495,39 @@ size_t spindlekv_prompt_workspace_bytes(const spindlekv_batch* keys, const spind
 spindlekv_status spindlekv_prompt_attend(const spindlekv_batch* keys, const spindlekv_batch* rows, int32_t n_q_heads, int32_t n_kv_heads,
                                          int32_t head_dim, float scale, spindlekv_tensor q, spindlekv_tensor K, spindlekv_tensor V,
                                          spindlekv_tensor out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Logits ahead of a selection.  For token t of a row, with n_t its occurrences among the generated tokens of the history (those from n_prompt on)
+ * and s_t whether the history has it at all,
+ *     z = s_t ? (x > 0 ? x / repetition : x * repetition) : x
+ *     z = n_t > 0 ? z - (frequency * n_t + presence) : z
+ *     z = z + each bias of t, in the list's order
+ *     z = allowed_t ? z : -infinity
+ * in fp32, each operation rounded by itself, and at the end to the logits' type.  A token that is not allowed is -infinity whatever its logit is.
+ */
+typedef struct {
+  const int32_t* history;        /* device [n_rows], rows history_stride apart, or NULL: no penalties; tokens outside the vocabulary are passed over */
+  int64_t history_stride;
+  int32_t max_history;           /* tokens of a row at most */
+  const int32_t* history_lens;   /* device [n_rows], clamped to max_history; NULL: max_history for all */
+  const int32_t* n_prompt;       /* device [n_rows]; NULL: 0 */
+  const float* repetition;       /* device [n_rows], > 0; NULL: 1 */
+  const float* presence;         /* device [n_rows]; NULL: 0 */
+  const float* frequency;        /* device [n_rows]; NULL: 0 */
+  int32_t n_bias;                /* biases of a row */
+  const int32_t* bias_token;     /* device [n_rows][n_bias]; outside the vocabulary: none */
+  const float* bias_value;       /* device [n_rows][n_bias] */
+  const uint32_t* allowed;       /* device, bit t % 32 of word t / 32, rows allowed_stride words apart (0: one for all rows); NULL: every token */
+  int64_t allowed_stride;
+} spindlekv_logit_rules;
+
+/*
+ *   logits, out  device [n_rows] rows of `vocab` elements, row_stride and out_stride elements apart, fp32 or bf16, any alignment that the type allows;
+ *                out may be logits itself (same stride), else they may not overlap
+ * n_rows < 2^16, vocab <= 2^30.
+ */
+spindlekv_status spindlekv_logits_adjust(int32_t n_rows, int32_t vocab, const void* logits, int32_t dtype, int64_t row_stride,
+                                         const spindlekv_logit_rules* rules, void* out, int64_t out_stride, void* stream);
 
 /*
  * Beam search's selection: among the continuations (beam w, token t) of a sequence the n_out with the largest

@@ -59,6 +59,12 @@ class _PageTable(C.Structure):
     _fields_ = [("pages", C.c_void_p), ("lens", C.c_void_p), ("n_layers", C.c_int32), ("n_seqs", C.c_int32), ("max_pages", C.c_int32)]
 
 
+class _LogitRules(C.Structure):
+    _fields_ = [("history", C.c_void_p), ("history_stride", C.c_int64), ("max_history", C.c_int32), ("history_lens", C.c_void_p), ("n_prompt", C.c_void_p),
+                ("repetition", C.c_void_p), ("presence", C.c_void_p), ("frequency", C.c_void_p), ("n_bias", C.c_int32), ("bias_token", C.c_void_p),
+                ("bias_value", C.c_void_p), ("allowed", C.c_void_p), ("allowed_stride", C.c_int64)]
+
+
 def _load() -> C.CDLL:
     path = _build.LIB
     if not os.path.exists(path):
@@ -122,6 +128,11 @@ def _load() -> C.CDLL:
     lib.spindlekv_paged_append.restype = C.c_int32
     lib.spindlekv_paged_append.argtypes = [pool, table, C.c_void_p, C.c_int32, _Tensor, _Tensor, C.c_int32, C.c_void_p, C.c_int32,
                                            C.c_int32, C.c_void_p]
+    lib.spindlekv_paged_append_rotated.restype = C.c_int32
+    lib.spindlekv_paged_append_rotated.argtypes = [pool, table, C.c_void_p, C.c_int32, _Tensor, _Tensor, C.c_int32, C.c_void_p, C.c_int32, C.c_int32,
+                                                   C.c_void_p, C.c_int32, C.c_void_p, _Tensor, C.c_int32, _Tensor, _Tensor, C.c_void_p]
+    lib.spindlekv_logits_adjust.restype = C.c_int32
+    lib.spindlekv_logits_adjust.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_int64, C.POINTER(_LogitRules), C.c_void_p, C.c_int64, C.c_void_p]
     lib.spindlekv_paged_workspace_bytes.restype = C.c_size_t
     lib.spindlekv_paged_workspace_bytes.argtypes = [pool, table, C.c_int32, C.c_int32]
     lib.spindlekv_paged_attend.restype = C.c_int32
@@ -451,6 +462,18 @@ def spindlekv_paged_append(pool: PagePool, table: PageTable, start: torch.Tensor
                                        idx_seq, _stream(stream)), "spindlekv_paged_append")
 
 
+NO_TENSOR = _Tensor(None, F32, 0, 0, 0, 0)
+
+
+def spindlekv_paged_append_rotated(pool: PagePool, table: PageTable, start: torch.Tensor, max_new: int, K: _Tensor, V: _Tensor, n_rows: int, rope_table: torch.Tensor,
+                                   first_pos: Optional[torch.Tensor] = None, K_out: _Tensor = NO_TENSOR, n_q_heads: int = 0, Q: _Tensor = NO_TENSOR,
+                                   Q_out: _Tensor = NO_TENSOR, idx: Optional[torch.Tensor] = None, idx_seq: int = 0, stream=None) -> None:
+    """``rope_table``: ``[n_positions, head_dim/2, 2]`` fp32; ``idx`` as for ``spindlekv_paged_append``."""
+    _check(_lib.spindlekv_paged_append_rotated(pool.c, table.c, _ptr(start), max_new, K, V, n_rows, _ptr(idx), 0 if idx is None else idx.shape[-1], idx_seq,
+                                               _ptr(rope_table), rope_table.shape[0], _ptr(first_pos), K_out, n_q_heads, Q, Q_out, _stream(stream)),
+           "spindlekv_paged_append_rotated")
+
+
 def spindlekv_paged_workspace_bytes(pool: PagePool, table: PageTable, n_q_heads: int, n_rows: int) -> int:
     return int(_lib.spindlekv_paged_workspace_bytes(pool.c, table.c, n_q_heads, n_rows))
 
@@ -459,6 +482,12 @@ def spindlekv_paged_attend(pool: PagePool, table: PageTable, n_q_heads: int, n_r
                            out: _Tensor, ws: torch.Tensor, stream=None) -> None:
     _check(_lib.spindlekv_paged_attend(pool.c, table.c, n_q_heads, n_rows, max_len, scale, q, out, _ptr(ws), _bytes(ws), _stream(stream)),
            "spindlekv_paged_attend")
+
+
+def spindlekv_logits_adjust(logits: torch.Tensor, out: torch.Tensor, rules: _LogitRules, stream=None) -> None:
+    """``logits``, ``out``: ``[n_rows, vocab]`` with any row stride, the rows contiguous."""
+    _check(_lib.spindlekv_logits_adjust(logits.shape[0], logits.shape[1], _ptr(logits), _dtype_code(logits), logits.stride(0), rules, _ptr(out), out.stride(0),
+                                        _stream(stream)), "spindlekv_logits_adjust")
 
 
 def spindlekv_prompt_workspace_bytes(keys: Batch, rows: Optional[Batch], n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int) -> int:

@@ -73,6 +73,12 @@ spindlekv_status beam_select_impl(int n_seqs, int n_beams, int vocab, int k, con
                                   const float* score, const uint8_t* finished, int eos, float* out_score, int32_t* out_parent,
                                   int32_t* out_token, void* ws, size_t ws_bytes, cudaStream_t st);
 
+spindlekv_status paged_append_rotated_impl(const spindlekv_page_pool& pool, const spindlekv_page_table& table, const int32_t* start, int max_new,
+                                           const spindlekv_tensor& K, const spindlekv_tensor& V, int n_rows, const int32_t* idx, int idx_len, int idx_seq,
+                                           const void* rope, int positions, const int32_t* first_pos, const spindlekv_tensor& K_out, int n_q_heads,
+                                           const spindlekv_tensor& Q, const spindlekv_tensor& Q_out, cudaStream_t st);
+spindlekv_status logits_adjust_impl(int n_rows, int vocab, const void* logits, int dtype, int64_t row_stride, const spindlekv_logit_rules& rules, void* out,
+                                    int64_t out_stride, cudaStream_t st);
 size_t prompt_workspace_bytes(const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int n_kv_heads, int head_dim, int dtype);
 spindlekv_status prompt_attend_impl(const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int n_kv_heads, int head_dim, float scale,
                                     const spindlekv_tensor& q, const spindlekv_tensor& k, const spindlekv_tensor& v, const spindlekv_tensor& out, float* lse, void* ws,
@@ -382,6 +388,31 @@ spindlekv_status spindlekv_paged_append(const spindlekv_page_pool* pool, const s
   return paged_append_impl(*pool, *table, start, max_new, K, V, n_rows, idx, idx_len, idx_seq, (cudaStream_t)stream);
 }
 
+// the same rows, or rows somewhere else
+static bool rows_out_ok(const spindlekv_tensor& in, const spindlekv_tensor& out) {
+  if (!tensor_ok(out)) return false;
+  return out.ptr != in.ptr || (out.stride_layer == in.stride_layer && out.stride_seq == in.stride_seq && out.stride_head == in.stride_head && out.stride_tok == in.stride_tok);
+}
+
+spindlekv_status spindlekv_paged_append_rotated(const spindlekv_page_pool* pool, const spindlekv_page_table* table, const int32_t* start,
+                                                int32_t max_new, spindlekv_tensor K, spindlekv_tensor V, int32_t n_rows, const int32_t* idx, int32_t idx_len,
+                                                int32_t idx_seq, const void* rope_table, int32_t table_positions, const int32_t* first_pos,
+                                                spindlekv_tensor K_out, int32_t n_q_heads, spindlekv_tensor Q, spindlekv_tensor Q_out, void* stream) {
+  const spindlekv_status ps = pool_table_status(pool, table);
+  if (ps != SPINDLEKV_OK) return ps;
+  if (!start || max_new <= 0 || n_rows <= 0 || !tensor_ok(K) || !tensor_ok(V)) return SPINDLEKV_INVALID_ARG;
+  if (!rope_table || reinterpret_cast<uintptr_t>(rope_table) % 16 || table_positions <= 0) return SPINDLEKV_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(start) | reinterpret_cast<uintptr_t>(idx) | reinterpret_cast<uintptr_t>(first_pos)) % 4) return SPINDLEKV_INVALID_ARG;
+  if (idx && (idx_seq < max_new || (int64_t)table->n_seqs * idx_seq > idx_len)) return SPINDLEKV_INVALID_ARG;
+  if (idx && (K_out.ptr || n_q_heads)) return SPINDLEKV_INVALID_ARG;      // a list may name a row for some heads only
+  if (n_q_heads < 0 || (K_out.ptr && !rows_out_ok(K, K_out)) || (n_q_heads && (!tensor_ok(Q) || !rows_out_ok(Q, Q_out)))) return SPINDLEKV_INVALID_ARG;
+  if (K.ptr == V.ptr && K_out.ptr == K.ptr) return SPINDLEKV_INVALID_ARG;
+  if (K.dtype != V.dtype || (K_out.ptr && K_out.dtype != K.dtype) || (n_q_heads && (Q.dtype != K.dtype || Q_out.dtype != K.dtype))) return SPINDLEKV_UNSUPPORTED;
+  if (n_q_heads > 65536) return SPINDLEKV_UNSUPPORTED;
+  return paged_append_rotated_impl(*pool, *table, start, max_new, K, V, n_rows, idx, idx_len, idx_seq, rope_table, table_positions, first_pos, K_out, n_q_heads, Q, Q_out,
+                                   (cudaStream_t)stream);
+}
+
 static spindlekv_status paged_shape_status(const spindlekv_page_pool* pool, const spindlekv_page_table* table, int32_t n_q_heads, int32_t n_rows) {
   const spindlekv_status ps = pool_table_status(pool, table);
   if (ps != SPINDLEKV_OK) return ps;
@@ -434,6 +465,25 @@ spindlekv_status spindlekv_beam_select(int32_t n_seqs, int32_t n_beams, int32_t 
   if (in < res + (size_t)n_seqs * n_out * 4 && res < in + (size_t)n_seqs * n_beams * 4 && !(in == res && n_out == n_beams)) return SPINDLEKV_INVALID_ARG;
   return beam_select_impl(n_seqs, n_beams, vocab, n_out, logits, dtype, row_stride, score, finished, eos, out_score, out_parent,
                           out_token, ws, ws_bytes, (cudaStream_t)stream);
+}
+
+spindlekv_status spindlekv_logits_adjust(int32_t n_rows, int32_t vocab, const void* logits, int32_t dtype, int64_t row_stride, const spindlekv_logit_rules* rules,
+                                         void* out, int64_t out_stride, void* stream) {
+  if (n_rows <= 0 || vocab <= 0 || !logits || !out || !rules || row_stride < 0) return SPINDLEKV_INVALID_ARG;
+  if (dtype != SPINDLEKV_F32 && dtype != SPINDLEKV_BF16) return SPINDLEKV_INVALID_ARG;
+  const uintptr_t size = dtype == SPINDLEKV_F32 ? 4 : 2;
+  if ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(out)) % size) return SPINDLEKV_INVALID_ARG;
+  if (n_rows > 1 && out_stride < vocab) return SPINDLEKV_INVALID_ARG;                                   // rows would write over one another
+  if (logits == out && n_rows > 1 && row_stride != out_stride) return SPINDLEKV_INVALID_ARG;
+  const spindlekv_logit_rules& r = *rules;
+  if (r.max_history < 0 || r.n_bias < 0 || r.history_stride < 0 || r.allowed_stride < 0) return SPINDLEKV_INVALID_ARG;
+  if (!r.history && (r.repetition || r.presence || r.frequency || r.n_prompt || r.history_lens)) return SPINDLEKV_INVALID_ARG;      // penalties of nothing
+  if (r.n_bias && (!r.bias_token || !r.bias_value)) return SPINDLEKV_INVALID_ARG;
+  const void* words[] = {r.history, r.history_lens, r.n_prompt, r.repetition, r.presence, r.frequency, r.bias_token, r.bias_value, r.allowed};
+  for (const void* w : words)
+    if (reinterpret_cast<uintptr_t>(w) % 4) return SPINDLEKV_INVALID_ARG;
+  if (n_rows > 65535 || vocab > (1 << 30)) return SPINDLEKV_UNSUPPORTED;
+  return logits_adjust_impl(n_rows, vocab, logits, dtype, row_stride, r, out, out_stride, (cudaStream_t)stream);
 }
 
 static spindlekv_status prompt_shape_status(const spindlekv_batch* keys, const spindlekv_batch* rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,

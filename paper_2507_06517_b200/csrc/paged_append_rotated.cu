@@ -1,0 +1,277 @@
+// Rows -> codes of the 8-bit paged cache with the position's rotation on the way, and rotated queries beside them.
+//
+// Elements i and i + d/2 of a row at position t become  x_i c - x_(i+d/2) s  and  x_(i+d/2) c + x_i s  with the table's cosine and sine of (t, i): four
+// products, a difference and a sum, each rounded to fp32 by itself, then the row's own type, as if the rotated row had been stored; codes are those of
+// that row.  So the result is the same, bit for bit, as rotating first and appending then, without the rotated rows' way through memory.
+//
+// A lane holds four neighbouring elements of either half of a row, so that a pair never leaves its lane; 16 lanes (d = 128) or 8 (d = 64) make a row.
+// Keys and values: a warp per (layer, sequence, KV head, block of 16 tokens, K or V), as in the append without rotation.  The warps of a thread block
+// are the heads of the same tokens, whose table rows (512 bytes each, twice a bf16 row) then come from the first-level cache.  Queries: a warp takes 16
+// tokens of eight heads and keeps a token's cosines and sines for all of them.
+//
+#include <algorithm>
+
+#include "paged_rounding.cuh"
+
+namespace skv {
+
+struct RotateParams {
+  Pool pool;
+  Table table;
+  View K, V, K_out, Q, Q_out;
+  const int32_t *start, *idx, *first_pos;
+  const float2* rope;        // [positions][d / 2]
+  int positions;
+  int idx_len, idx_seq, max_new, n_rows, n_blocks, q_heads, q_groups, q_chunks;
+  int per_shift, page_shift;
+  unsigned n_kv, n_items;    // warps of a unit: for keys and values, and in all
+};
+
+constexpr int kRotateThreads = 256, kRotateHeads = 8;      // query heads of a warp
+
+// four elements of either half of a row (plain loads: the rotated rows may take the rows' place)
+__device__ __forceinline__ void load_pairs(const float* p, int half, float (&x)[8]) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + half);
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+  x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load_pairs(const __nv_bfloat16* p, int half, float (&x)[8]) {
+  const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(p + half);
+  const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void store_pairs(float* p, int half, const float (&x)[8]) {
+  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  *reinterpret_cast<float4*>(p + half) = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void store_pairs(__nv_bfloat16* p, int half, const float (&x)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+  *reinterpret_cast<uint2*>(p + half) = make_uint2(w[2], w[3]);
+}
+__device__ __forceinline__ float as_stored(float x, const float*) { return x; }
+__device__ __forceinline__ float as_stored(float x, const __nv_bfloat16*) { return __bfloat162float(__float2bfloat16_rn(x)); }
+
+// cosines and sines of four pairs at a position; NaN outside the table
+__device__ __forceinline__ void load_turn(const RotateParams& p, long long pos, int col, int half, float2 (&t)[4]) {
+  if (pos >= 0 && pos < p.positions) {
+    const float4* at = reinterpret_cast<const float4*>(p.rope + pos * half + col);
+    const float4 a = __ldg(at), b = __ldg(at + 1);
+    t[0] = make_float2(a.x, a.y); t[1] = make_float2(a.z, a.w);
+    t[2] = make_float2(b.x, b.y); t[3] = make_float2(b.z, b.w);
+  } else {
+    const float nan = __uint_as_float(0x7FC00000u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = make_float2(nan, nan);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void turn(float (&x)[8], const float2 (&t)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float a = x[i], b = x[i + 4];
+    x[i] = as_stored(__fsub_rn(__fmul_rn(a, t[i].x), __fmul_rn(b, t[i].y)), static_cast<const T*>(nullptr));
+    x[i + 4] = as_stored(__fadd_rn(__fmul_rn(b, t[i].x), __fmul_rn(a, t[i].y)), static_cast<const T*>(nullptr));
+  }
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void rotate_queries(const RotateParams& p, int layer, int s, int u, unsigned item, int start, int n_new) {
+  constexpr int LPR = D / 8, RPI = 32 / LPR, NI = kPagedBlock / RPI, HALF = D / 2;
+  const int lane = threadIdx.x & 31, sub = lane / LPR, col = (lane % LPR) * 4;
+  const int chunk = (int)(item / (unsigned)p.q_groups), group = (int)(item - (unsigned)chunk * p.q_groups);
+  const int r0 = chunk * kPagedBlock, h0 = group * kRotateHeads, heads = min(kRotateHeads, p.q_heads - h0);
+  if (r0 >= n_new) return;
+  const T* from = reinterpret_cast<const T*>(p.Q.ptr) + (int64_t)layer * p.Q.sl + (int64_t)s * p.Q.ss + (int64_t)h0 * p.Q.sh + col;
+  T* to = reinterpret_cast<T*>(const_cast<void*>(p.Q_out.ptr)) + (int64_t)layer * p.Q_out.sl + (int64_t)s * p.Q_out.ss + (int64_t)h0 * p.Q_out.sh + col;
+  const long long first = p.first_pos ? p.first_pos[u] : start;
+#pragma unroll 2
+  for (int i = 0; i < NI; ++i) {
+    const int r = r0 + i * RPI + sub;
+    if (r0 + i * RPI >= n_new) break;
+    if (r >= n_new) continue;
+    float2 t[4];
+    load_turn(p, first + r, col, HALF, t);
+    float x[kRotateHeads][8];
+#pragma unroll
+    for (int h = 0; h < kRotateHeads; ++h)
+      if (h < heads) load_pairs(from + (int64_t)h * p.Q.sh + (int64_t)r * p.Q.st, HALF, x[h]);
+#pragma unroll
+    for (int h = 0; h < kRotateHeads; ++h)
+      if (h < heads) {
+        turn<T>(x[h], t);
+        store_pairs(to + (int64_t)h * p.Q_out.sh + (int64_t)r * p.Q_out.st, HALF, x[h]);
+      }
+  }
+}
+
+template <typename T, int FMT, int D>
+__global__ void __launch_bounds__(kRotateThreads) paged_append_rotated_kernel(const __grid_constant__ RotateParams p) {
+  constexpr int LPR = D / 8, RPI = 32 / LPR, NI = kPagedBlock / RPI, HALF = D / 2;
+  const unsigned item = blockIdx.x * (kRotateThreads / 32) + (threadIdx.x >> 5);
+  if (item >= p.n_items) return;
+  const int lane = threadIdx.x & 31, u = blockIdx.y;
+  const int layer = u / p.table.n_seqs, s = u - layer * p.table.n_seqs;
+  const int start = p.start[u];
+  if (start < 0) return;
+  const int end = (int)min((long long)unit_len(p.table, p.pool, u), (long long)start + p.max_new);
+  if (start >= end) return;
+  if (item >= p.n_kv) return rotate_queries<T, D>(p, layer, s, u, item - p.n_kv, start, min(end - start, p.n_rows));
+  const int rel = (int)(item / (2u * p.pool.heads)), rest = (int)(item - (unsigned)rel * 2u * p.pool.heads), head = rest >> 1;
+  const bool is_v = (rest & 1) != 0;
+  const int blk = start / kPagedBlock + rel, t0 = blk * kPagedBlock;
+  if (t0 >= end) return;
+  const int page = p.table.pages[(int64_t)u * p.table.max_pages + (t0 >> p.page_shift)];
+  const bool in_pool = page >= 0 && page < p.pool.n_pages;
+  const bool keeps = !is_v && p.K_out.ptr;
+  if (!in_pool && !keeps) return;
+  const int64_t slab = (((int64_t)(in_pool ? page : 0) * p.pool.heads + head) << p.per_shift) + (blk & ((1 << p.per_shift) - 1));
+  const int sub = lane / LPR, col = (lane % LPR) * 4;
+  uint8_t* codes = (is_v ? p.pool.vc : p.pool.kc) + slab * (kPagedBlock * D) + col;
+  float* scale = (is_v ? p.pool.vs : p.pool.ks) + slab;
+  const View src = is_v ? p.V : p.K;
+  const T* rows = reinterpret_cast<const T*>(src.ptr) + (int64_t)layer * src.sl + (int64_t)s * src.ss + (int64_t)head * src.sh + col;
+  const int first = max(start - t0, 0), last = min(end - t0, kPagedBlock);       // new slots of the block: [first, last)
+  int my_row = -1;
+  if (lane >= first && lane < last) {
+    const int i = t0 + lane - start;
+    my_row = i;
+    if (p.idx) my_row = p.idx[((int64_t)layer * p.pool.heads + head) * p.idx_len + (int64_t)s * p.idx_seq + i];
+    if (my_row < 0 || my_row >= p.n_rows) my_row = -1;
+  }
+  const long long at0 = p.first_pos ? p.first_pos[u] : p.idx ? 0 : start;
+  const float was = first > 0 && in_pool ? *scale : 0.f;
+  float x[NI][8];
+  float2 most = make_float2(0.f, 0.f);       // the largest magnitude; and NaN if there is a NaN or an infinity
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int row = __shfl_sync(0xffffffffu, my_row, i * RPI + sub);
+    if (row >= 0) {
+      load_pairs(rows + (int64_t)row * src.st, HALF, x[i]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
+    }
+  }
+  if (!is_v) {
+    // four rows' cosines and sines at a time
+#pragma unroll
+    for (int g = 0; g < NI; g += 4) {
+      float2 t[4][4];
+      int row[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        row[i] = __shfl_sync(0xffffffffu, my_row, (g + i) * RPI + sub);
+        if (row[i] >= 0) load_turn(p, at0 + row[i], col, HALF, t[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (row[i] >= 0) {
+          turn<T>(x[g + i], t[i]);
+          if (keeps)
+            store_pairs(reinterpret_cast<T*>(const_cast<void*>(p.K_out.ptr)) + (int64_t)layer * p.K_out.sl + (int64_t)s * p.K_out.ss + (int64_t)head * p.K_out.sh +
+                            (int64_t)row[i] * p.K_out.st + col, HALF, x[g + i]);
+        }
+    }
+  }
+  if (!in_pool) return;
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      most.x = fmaxf(most.x, fabsf(x[i][e]));
+      most.y = fmaf(x[i][e], 0.f, most.y);
+    }
+  const uint32_t amax = __reduce_max_sync(0xffffffffu, most.y == 0.f ? __float_as_uint(most.x) : 0x7FC00000u);
+  const bool poisoned = amax >= 0x7F800000u || !(was < __uint_as_float(0x7F800000u));
+  const float sc = poisoned ? __uint_as_float(0x7FC00000u) : fmaxf(was, scale_of<FMT>(amax));
+  __syncwarp();                              // every lane has read the old scale
+  if (lane == 0) *scale = sc;
+  const bool empty = poisoned || sc == 0.f;
+  const float inv = empty ? 0.f : __fdiv_rn(1.f, sc);
+  auto put = [&](int slot, uint2 c) {
+    *reinterpret_cast<uint32_t*>(codes + slot * D) = c.x;
+    *reinterpret_cast<uint32_t*>(codes + slot * D + HALF) = c.y;
+  };
+  if (first > 0 && sc != was) {              // earlier tokens of the block move to the larger scale (NaN: to codes of zero)
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int slot = i * RPI + sub;
+      if (slot < first) {
+        const uint2 old = make_uint2(*reinterpret_cast<const uint32_t*>(codes + slot * D), *reinterpret_cast<const uint32_t*>(codes + slot * D + HALF));
+        put(slot, empty ? make_uint2(0, 0) : recode8<FMT>(old, was, sc));
+      }
+    }
+  }
+  float worst = 0.f;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int slot = i * RPI + sub;
+    if (slot >= first && slot < last) put(slot, empty ? make_uint2(0, 0) : encode8<FMT>(x[i], sc, inv, worst));
+  }
+  if (FMT == SPINDLEKV_PAGED_INT8 && !empty && worst >= 0.5f * sc) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int slot = i * RPI + sub;
+      if (slot >= first && slot < last) put(slot, encode8_exactly(x[i], sc, inv));
+    }
+  }
+}
+
+template <typename T, int FMT>
+static void launch_rotated(const RotateParams& p, cudaStream_t st) {
+  const dim3 grid((p.n_items + kRotateThreads / 32 - 1) / (kRotateThreads / 32), p.table.n_layers * p.table.n_seqs);
+  LaunchScope ls(KC_PAGED_APPEND, st);
+  if (p.pool.d == 64) paged_append_rotated_kernel<T, FMT, 64><<<grid, kRotateThreads, 0, st>>>(p);
+  else paged_append_rotated_kernel<T, FMT, 128><<<grid, kRotateThreads, 0, st>>>(p);
+}
+
+spindlekv_status paged_append_rotated_impl(const spindlekv_page_pool& pool, const spindlekv_page_table& table, const int32_t* start, int max_new,
+                                           const spindlekv_tensor& K, const spindlekv_tensor& V, int n_rows, const int32_t* idx, int idx_len, int idx_seq,
+                                           const void* rope, int positions, const int32_t* first_pos, const spindlekv_tensor& K_out, int n_q_heads,
+                                           const spindlekv_tensor& Q, const spindlekv_tensor& Q_out, cudaStream_t st) {
+  RotateParams p;
+  p.pool = make_pool(pool);
+  p.table = make_table(table);
+  p.K = make_view(K);
+  p.V = make_view(V);
+  p.K_out = make_view(K_out);
+  p.Q = make_view(Q);
+  p.Q_out = make_view(Q_out);
+  p.start = start;
+  p.idx = idx;
+  p.first_pos = first_pos;
+  p.rope = static_cast<const float2*>(rope);
+  p.positions = positions;
+  p.idx_len = idx_len;
+  p.idx_seq = idx_seq;
+  p.max_new = (int)std::min<int64_t>(max_new, (int64_t)table.max_pages * pool.page_size);      // no sequence can take more than its table row holds
+  p.n_rows = n_rows;
+  p.n_blocks = (int)(((int64_t)p.max_new + kPagedBlock - 2) / kPagedBlock) + 1;
+  p.q_heads = n_q_heads;
+  p.q_groups = ceil_div(n_q_heads, kRotateHeads);
+  p.q_chunks = ceil_div(std::min(p.max_new, n_rows), kPagedBlock);
+  const int64_t kv = 2ll * pool.n_kv_heads * p.n_blocks, items = kv + (int64_t)p.q_groups * p.q_chunks;
+  if (items > 0x7FFFFFFF) return SPINDLEKV_UNSUPPORTED;
+  p.n_kv = (unsigned)kv;
+  p.n_items = (unsigned)items;
+  p.page_shift = pool.page_size == 16 ? 4 : pool.page_size == 32 ? 5 : pool.page_size == 64 ? 6 : 7;
+  p.per_shift = p.page_shift - 4;
+  const bool bf = K.dtype == SPINDLEKV_BF16, i8 = pool.format == SPINDLEKV_PAGED_INT8;
+  if (bf && i8) launch_rotated<__nv_bfloat16, SPINDLEKV_PAGED_INT8>(p, st);
+  else if (bf) launch_rotated<__nv_bfloat16, SPINDLEKV_PAGED_E4M3>(p, st);
+  else if (i8) launch_rotated<float, SPINDLEKV_PAGED_INT8>(p, st);
+  else launch_rotated<float, SPINDLEKV_PAGED_E4M3>(p, st);
+  return cudaGetLastError() == cudaSuccess ? SPINDLEKV_OK : SPINDLEKV_CUDA;
+}
+
+}  // namespace skv

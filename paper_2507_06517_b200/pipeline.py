@@ -177,10 +177,11 @@ class SpindleKVPass:
             cur.wait_stream(sE)
         cur.wait_stream(sV)
 
-    def store_paged(self, K: torch.Tensor, V: torch.Tensor, cache: "SpindleKVPagedCache", stream=None) -> None:
+    def store_paged(self, K: torch.Tensor, V: torch.Tensor, cache: "SpindleKVPagedCache", stream=None, rope_table: Optional[torch.Tensor] = None) -> None:
         """What the last eviction kept of ``K`` and ``V`` (every layer's, or the evicting layers' alone) becomes the content of
         ``cache``, whose layers are the evicting ones; what it held is given back.  The kept rows go from the prompt's tensors into
-        the pages in one step.  Equal-length batches."""
+        the pages in one step; with ``rope_table`` (``[n_positions, d/2, 2]``) the keys are rotated on the way, each by the position that it had in
+        the prompt.  Equal-length batches."""
         if self.packed:
             raise ValueError("store_paged needs sequences of equal length")
         if (cache.n_layers, cache.n_seqs, cache.Hkv, cache.d) != (self.n_deep, self.n_seqs, self.cfg.n_kv_heads, self.cfg.head_dim):
@@ -193,8 +194,11 @@ class SpindleKVPass:
                 raise ValueError(f"{name}: {self.max_len} rows expected, got {t.shape[3]}")
         cache.resize(cache.no_tokens, stream=stream)
         cache.resize(self.kept_lens, stream=stream)
-        cache.append(K, V, idx=self.keep_idx, idx_seq=self.max_len, max_new=int(self.k_ctx_host[self.n_shallow:].max()) + self.cfg.window,
-                     stream=stream)
+        most = int(self.k_ctx_host[self.n_shallow:].max()) + self.cfg.window
+        if rope_table is None:
+            cache.append(K, V, idx=self.keep_idx, idx_seq=self.max_len, max_new=most, stream=stream)
+        else:
+            cache.append_rotated(K, V, rope_table, idx=self.keep_idx, idx_seq=self.max_len, max_new=most, stream=stream)
 
     # -- the same pass fed from host memory ----------------------------------------------------
     def host_outputs(self) -> Dict[str, torch.Tensor]:
@@ -681,6 +685,57 @@ class SpindleKVPagedCache(_OnDevice):
         k, v = self._cache_rows("K", K, n_l, self.Hkv), self._cache_rows("V", V, n_l, self.Hkv)
         B.spindlekv_paged_append(self.pool, table, start, max_new, k, v, K.shape[3], idx, idx_seq or 0, self._raw(stream))
 
+    def append_rotated(self, K: torch.Tensor, V: torch.Tensor, rope_table: torch.Tensor, start: Optional[torch.Tensor] = None,
+                       first_pos: Optional[torch.Tensor] = None, idx: Optional[torch.Tensor] = None, idx_seq: Optional[int] = None, max_new: Optional[int] = None,
+                       K_out: Optional[torch.Tensor] = None, Q: Optional[torch.Tensor] = None, Q_out: Optional[torch.Tensor] = None, layer: Optional[int] = None,
+                       stream=None) -> Optional[torch.Tensor]:
+        """``append`` of keys that ``rope_table`` (``[n_positions, d/2, 2]`` fp32, ``spindlekv_rope_table``) rotates on the way: row ``r`` of a sequence by
+        position ``first_pos + r`` (``first_pos`` ``[n_layers or 1, n_seqs]`` int32; ``start`` by default, 0 with ``idx``).  ``K_out``, if given, gets the rotated
+        keys (it may be ``K``); queries ``Q`` ``[n_layers or 1, n_seqs, H_q, rows, d]`` of the same rows are rotated alike into ``Q_out`` (it may be ``Q``; by
+        default a new tensor, zeros behind the new rows), which is returned."""
+        if self._elsewhere():
+            with torch.cuda.device(self.device):
+                return self.append_rotated(K, V, rope_table, start, first_pos, idx, idx_seq, max_new, K_out, Q, Q_out, layer, stream)
+        table = self._rows_of(layer)
+        n_l = table.n_layers
+        start = self.start if start is None else start
+        if layer is not None and start.shape[0] == self.n_layers:
+            start = start[layer:layer + 1]
+        if layer is not None and first_pos is not None and first_pos.shape[0] == self.n_layers:
+            first_pos = first_pos[layer:layer + 1]
+        self._mine("start", start, torch.int32, (n_l, self.n_seqs))
+        if first_pos is not None:
+            self._mine("first_pos", first_pos, torch.int32, (n_l, self.n_seqs))
+        self._mine("rope_table", rope_table, torch.float32)
+        if rope_table.dim() != 3 or rope_table.shape[1:] != (self.d // 2, 2):
+            raise ValueError(f"rope_table: [positions, {self.d // 2}, 2] expected, got {list(rope_table.shape)}")
+        n_rows = K.shape[3] if K.dim() == 5 else -1
+        if idx is not None:
+            self._mine("idx", idx, torch.int32)
+            if idx.dim() != 3 or idx.shape[0] != n_l or idx.shape[1] != self.Hkv:
+                raise ValueError(f"idx: [{n_l}, {self.Hkv}, n_seqs * idx_seq] expected, got {list(idx.shape)}")
+            idx_seq = idx.shape[2] // self.n_seqs if idx_seq is None else idx_seq
+        if max_new is None:
+            max_new = n_rows if idx is None else idx_seq
+        rows = {"K": self._cache_rows("K", K, n_l, self.Hkv), "V": self._cache_rows("V", V, n_l, self.Hkv), "K_out": B.NO_TENSOR, "Q": B.NO_TENSOR, "Q_out": B.NO_TENSOR}
+        hq, same = 0, [("V", V)]
+        if K_out is not None:
+            rows["K_out"] = self._cache_rows("K_out", K_out, n_l, self.Hkv)
+            same.append(("K_out", K_out))
+        if Q is not None:
+            hq = Q.shape[2] if Q.dim() == 5 else 0
+            rows["Q"] = self._cache_rows("Q", Q, n_l, hq)
+            if Q_out is None:
+                Q_out = self._empty(Q.shape, Q.dtype, stream, zero=True)
+            rows["Q_out"] = self._cache_rows("Q_out", Q_out, n_l, hq)
+            same += [("Q", Q), ("Q_out", Q_out)]
+        for name, t in same:
+            if t.shape[3] != n_rows:
+                raise ValueError(f"{name}: {n_rows} rows expected as in K, got {t.shape[3]}")
+        B.spindlekv_paged_append_rotated(self.pool, table, start, max_new, rows["K"], rows["V"], n_rows, rope_table, first_pos, rows["K_out"], hq, rows["Q"],
+                                         rows["Q_out"], idx, idx_seq or 0, self._raw(stream))
+        return Q_out
+
     def attend(self, q: torch.Tensor, out: Optional[torch.Tensor] = None, max_len: Optional[int] = None, scale: float = 0.0,
                layer: Optional[int] = None, stream=None) -> torch.Tensor:
         """Attention of the last ``rows`` tokens, ``q`` ``[n_layers or 1, n_seqs, H_q, rows, d]``.  Without ``out`` the result lies in a
@@ -786,6 +841,69 @@ class SpindleKVPromptAttention(_OnDevice):
         torch.cuda.synchronize(self.device)
         with torch.cuda.device(self.device):
             return B.spindlekv_poll_status(self.ws)[0]
+
+
+class SpindleKVLogits(_OnDevice):
+    """Penalties for repeated tokens, biases and masks of allowed tokens (``spindlekv_logits_adjust``) for ``n_rows`` rows of logits over ``vocab`` tokens, e.g. the
+    beams of ``SpindleKVBeamSelect``.  No scratch: calls of one object need no order among themselves."""
+
+    def __init__(self, n_rows: int, vocab: int, device="cuda"):
+        if not (0 < n_rows < 65536 and 0 < vocab <= 1 << 30):
+            raise ValueError(f"unsupported logits: {n_rows} rows, vocabulary {vocab}")
+        self.n_rows, self.vocab = n_rows, vocab
+        self.device = _device_of(device)
+        self._index = self.device.index
+
+    def _logits(self, name: str, t: torch.Tensor, dtype=None) -> torch.Tensor:
+        if t.shape != (self.n_rows, self.vocab) or (self.vocab > 1 and t.stride(1) != 1) or t.device != self.device or (dtype is not None and t.dtype != dtype):
+            raise ValueError(f"{name}: [{self.n_rows}, {self.vocab}] {dtype or ''} on {self.device} expected, rows contiguous, got {list(t.shape)} {t.dtype} on {t.device}")
+        return t
+
+    def adjust(self, logits: torch.Tensor, out: Optional[torch.Tensor] = None, history: Optional[torch.Tensor] = None, history_lens: Optional[torch.Tensor] = None,
+               n_prompt: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
+               frequency: Optional[torch.Tensor] = None, bias_token: Optional[torch.Tensor] = None, bias_value: Optional[torch.Tensor] = None,
+               allowed: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """``history`` ``[n_rows, n]`` int32 (any row stride) with ``history_lens`` tokens each, of which the first ``n_prompt`` are the prompt's; ``repetition``,
+        ``presence``, ``frequency`` fp32 ``[n_rows]``; ``bias_token`` int32 and ``bias_value`` fp32 ``[n_rows, n]``; ``allowed`` int32 or uint32 ``[n_rows or 1,
+        ceil(vocab / 32)]``, a bit per token, the lowest first.  Returns ``out`` (``logits`` itself, in place, by default)."""
+        if self._elsewhere():
+            with torch.cuda.device(self.device):
+                return self.adjust(logits, out, history, history_lens, n_prompt, repetition, presence, frequency, bias_token, bias_value, allowed, stream)
+        n = self.n_rows
+        self._logits("logits", logits)
+        out = logits if out is None else self._logits("out", out, logits.dtype)
+        r = B._LogitRules()
+        if history is not None:
+            if history.dim() != 2 or history.shape[0] != n or (history.shape[1] > 1 and history.stride(1) != 1) or history.dtype != torch.int32 or history.device != self.device:
+                raise ValueError(f"history: [{n}, tokens] int32 on {self.device} expected, rows contiguous, got {list(history.shape)} {history.dtype} on {history.device}")
+            if history.shape[1]:
+                r.history, r.history_stride, r.max_history = history.data_ptr(), history.stride(0), history.shape[1]
+        for name, t, dtype in (("history_lens", history_lens, torch.int32), ("n_prompt", n_prompt, torch.int32), ("repetition", repetition, torch.float32),
+                               ("presence", presence, torch.float32), ("frequency", frequency, torch.float32)):
+            if t is None:
+                continue
+            if history is None:
+                raise ValueError(f"{name} without a history")
+            self._mine(name, t, dtype, (n,))
+            if r.history:
+                setattr(r, name, t.data_ptr())
+        if (bias_token is None) != (bias_value is None):
+            raise ValueError("bias_token and bias_value belong together")
+        if bias_token is not None:
+            if bias_token.dim() != 2 or bias_token.shape[0] != n:
+                raise ValueError(f"bias_token: [{n}, biases] expected, got {list(bias_token.shape)}")
+            self._mine("bias_token", bias_token, torch.int32)
+            self._mine("bias_value", bias_value, torch.float32, bias_token.shape)
+            if bias_token.shape[1]:
+                r.n_bias, r.bias_token, r.bias_value = bias_token.shape[1], bias_token.data_ptr(), bias_value.data_ptr()
+        if allowed is not None:
+            words = (self.vocab + 31) // 32
+            if allowed.dtype not in (torch.int32, torch.uint32) or allowed.dim() != 2 or allowed.shape[0] not in (1, n) or allowed.shape[1] != words:
+                raise ValueError(f"allowed: [{n} or 1, {words}] int32 or uint32 expected, got {list(allowed.shape)} {allowed.dtype}")
+            self._mine("allowed", allowed)
+            r.allowed, r.allowed_stride = allowed.data_ptr(), words if allowed.shape[0] == n else 0
+        B.spindlekv_logits_adjust(logits, out, r, self._raw(stream))
+        return out
 
 
 class SpindleKVBeamSelect(_OnDevice):
