@@ -8,7 +8,7 @@
 // all in fp32, each operation rounded by itself, and once more to the logits' type.
 //
 // A thread block takes a slice of a row: it counts the history's tokens that fall into the slice in shared memory (whole numbers, so that no order
-// shows), marks the biased ones, and then streams the slice, where a word of counts tells the few tokens that change from the many that do not.
+// shows), marks the biased ones, which it does one by one, and then streams the slice, where a word of counts tells the few tokens that change from the many that do not.
 //
 #include <algorithm>
 
@@ -29,34 +29,41 @@ struct LogitsParams {
 constexpr int kLogitsThreads = 512, kLogitsMaxSlice = 16384;
 constexpr uint32_t kBiased = 1u << 31, kInPrompt = 1u << 30, kCountBits = kInPrompt - 1;
 
-template <typename T>
-__device__ __forceinline__ float adjusted(const LogitsParams& p, int row, int t, float x, uint32_t word, bool allowed, float rep, float presence, float frequency) {
-  if (!allowed) return -CUDART_INF_F;
-  if (word == 0u) return x;
-  float z = x;
-  if (word & ~kBiased) z = x > 0.f ? __fdiv_rn(x, rep) : __fmul_rn(x, rep);
+// penalties of a token that the history has
+__device__ __forceinline__ float penalised(float x, uint32_t word, float rep, float presence, float frequency) {
+  if ((word & ~kBiased) == 0u) return x;
+  float z = x > 0.f ? __fdiv_rn(x, rep) : __fmul_rn(x, rep);
   const uint32_t n = word & kCountBits;
   if (n) z = __fsub_rn(z, __fadd_rn(__fmul_rn(frequency, (float)n), presence));
-  if (word & kBiased) {
-    const int32_t* tok = p.r.bias_token + (int64_t)row * p.r.n_bias;
-    for (int i = 0; i < p.r.n_bias; ++i)
-      if (__ldg(tok + i) == t) z = __fadd_rn(z, __ldg(p.r.bias_value + (int64_t)row * p.r.n_bias + i));
-  }
   return z;
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kLogitsThreads) logits_adjust_kernel(const __grid_constant__ LogitsParams p) {
-  constexpr int E = 16 / sizeof(T);        // elements of 16 bytes
-  extern __shared__ uint32_t words[];
+__global__ void __launch_bounds__(kLogitsThreads, 2) logits_adjust_kernel(const __grid_constant__ LogitsParams p) {
+  constexpr int E = 16 / sizeof(T), V = kLogitsMaxSlice / E / kLogitsThreads;        // elements of 16 bytes; a thread's pieces of 16 bytes
+  extern __shared__ uint4 shared[];
+  uint32_t* words = reinterpret_cast<uint32_t*>(shared);
+  __shared__ uint32_t mask[kLogitsMaxSlice / 32 + 1];
   const int row = blockIdx.y, lo = blockIdx.x * p.slice, hi = min(lo + p.slice, p.vocab), tid = threadIdx.x;
   const T* in = reinterpret_cast<const T*>(p.in) + (int64_t)row * p.in_stride;
   T* out = reinterpret_cast<T*>(p.out) + (int64_t)row * p.out_stride;
-  const uint32_t* allowed = p.r.allowed ? p.r.allowed + (int64_t)row * p.r.allowed_stride : nullptr;
+  // 16 bytes at a time where both rows lie alike, the elements before and behind one by one.  They are asked for first, and come while the history is counted
+  const int off = (int)(reinterpret_cast<uintptr_t>(in + lo) % 16 / sizeof(T));
+  const bool alike = reinterpret_cast<uintptr_t>(in + lo) % 16 == reinterpret_cast<uintptr_t>(out + lo) % 16;
+  const int first = alike ? min(hi, lo + (off ? E - off : 0)) : hi, vectors = (hi - first) / E, last = first + vectors * E;
+  uint4 raw[V];
+#pragma unroll
+  for (int a = 0; a < V; ++a) {
+    const int v = tid + a * kLogitsThreads;
+    raw[a] = v < vectors ? *reinterpret_cast<const uint4*>(in + first + v * E) : make_uint4(0u, 0u, 0u, 0u);
+  }
+  const bool counts = p.r.history || p.r.n_bias > 0, masked = p.r.allowed != nullptr;
+  const uint32_t* allowed = p.r.allowed + (int64_t)row * p.r.allowed_stride + lo / 32;
+  if (masked)
+    for (int i = tid; i < (hi - lo + 31) / 32; i += kLogitsThreads) mask[i] = __ldg(allowed + i);
   float rep = 1.f, presence = 0.f, frequency = 0.f;
-  const bool counts = p.r.history || p.r.n_bias > 0;
   if (counts) {
-    for (int i = tid; i < hi - lo; i += kLogitsThreads) words[i] = 0u;
+    for (int i = tid; i < (hi - lo + 3) / 4; i += kLogitsThreads) shared[i] = make_uint4(0u, 0u, 0u, 0u);
     __syncthreads();
     if (p.r.history) {
       if (p.r.repetition) rep = __ldg(p.r.repetition + row);
@@ -65,12 +72,28 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_adjust_kernel(const __g
       const int32_t* h = p.r.history + (int64_t)row * p.r.history_stride;
       const int n = p.r.history_lens ? min(max(__ldg(p.r.history_lens + row), 0), p.r.max_history) : p.r.max_history;
       const int prompt = p.r.n_prompt ? __ldg(p.r.n_prompt + row) : 0;
-#pragma unroll 8
-      for (int i = tid; i < n; i += kLogitsThreads) {
-        const int t = __ldg(h + i);
-        if (t >= lo && t < hi) {
-          if (i >= prompt) atomicAdd(words + (t - lo), 1u);
-          else atomicOr(words + (t - lo), kInPrompt);
+      auto count = [&](int i, int t) {
+        if (t < lo || t >= hi) return;
+        if (i >= prompt) atomicAdd(words + (t - lo), 1u);
+        else atomicOr(words + (t - lo), kInPrompt);
+      };
+      // 16 bytes at a time from where they begin, and four of those asked for together (one by one: 80 us in place of 53 for 128 rows of up to 16384 tokens)
+      const int head = min(n, (int)((16 - reinterpret_cast<uintptr_t>(h) % 16) % 16 / 4)), quads = (n - head) / 4;
+      const int4* h4 = reinterpret_cast<const int4*>(h + head);
+      if (tid < head) count(tid, __ldg(h + tid));
+      for (int i = head + 4 * quads + tid; i < n; i += kLogitsThreads) count(i, __ldg(h + i));
+#pragma unroll 1
+      for (int q0 = tid; q0 < quads; q0 += 4 * kLogitsThreads) {
+        int4 t[4];
+#pragma unroll
+        for (int a = 0; a < 4; ++a) t[a] = q0 + a * kLogitsThreads < quads ? __ldg(h4 + q0 + a * kLogitsThreads) : make_int4(-1, -1, -1, -1);
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const int i = head + 4 * (q0 + a * kLogitsThreads);
+          count(i, t[a].x);
+          count(i + 1, t[a].y);
+          count(i + 2, t[a].z);
+          count(i + 3, t[a].w);
         }
       }
     }
@@ -78,36 +101,37 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_adjust_kernel(const __g
       const int t = __ldg(p.r.bias_token + (int64_t)row * p.r.n_bias + i);
       if (t >= lo && t < hi) atomicOr(words + (t - lo), kBiased);
     }
-    __syncthreads();
   }
+  if (counts || masked) __syncthreads();
+  auto is_allowed = [&](int t) { return !masked || (mask[(t - lo) >> 5] >> ((t - lo) & 31) & 1u); };
   auto one = [&](int t) {
-    const bool ok = !allowed || (__ldg(allowed + (t >> 5)) >> (t & 31) & 1u);
-    out[t] = T(adjusted<T>(p, row, t, to_f32(in[t]), counts ? words[t - lo] : 0u, ok, rep, presence, frequency));
+    const uint32_t word = counts ? words[t - lo] : 0u;
+    if (word & kBiased) return;
+    out[t] = T(is_allowed(t) ? penalised(to_f32(in[t]), word, rep, presence, frequency) : -CUDART_INF_F);
   };
-  // 16 bytes at a time where both rows lie alike; the elements before and behind one by one
-  const int off = (int)(reinterpret_cast<uintptr_t>(in + lo) % 16 / sizeof(T));
-  const bool alike = reinterpret_cast<uintptr_t>(in + lo) % 16 == reinterpret_cast<uintptr_t>(out + lo) % 16;
-  const int first = alike ? min(hi, lo + (off ? E - off : 0)) : hi, vectors = (hi - first) / E, last = first + vectors * E;
   for (int t = lo + tid; t < first; t += kLogitsThreads) one(t);
   for (int t = last + tid; t < hi; t += kLogitsThreads) one(t);
-#pragma unroll 4
-  for (int v = tid; v < vectors; v += kLogitsThreads) {
-    const int t = first + v * E;
-    const uint4 raw = *reinterpret_cast<const uint4*>(in + t);
-    uint32_t bits = ~0u;
-    if (allowed) {
-      const int w = t >> 5, s = t & 31;
-      bits = __ldg(allowed + w) >> s;
-      if (s > 32 - E) bits |= __ldg(allowed + w + 1) << (32 - s);
-    }
-    float x[E];
-    uint32_t word[E], any = 0u;
+  const bool even = (first - lo) % 4 == 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      word[e] = counts ? words[t - lo + e] : 0u;
-      any |= word[e];
+  for (int a = 0; a < V; ++a) {
+    const int v = tid + a * kLogitsThreads, t = first + v * E, i = t - lo;
+    if (v >= vectors) break;
+    uint32_t word[E], any = 0u, bits = ~0u;
+    if (masked) bits = __funnelshift_r(mask[i >> 5], mask[(i >> 5) + 1], i & 31);      // (the word behind the slice's last is there, and its bits are not used)
+    if (counts) {
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        const uint32_t* from = words + i + e;
+        if (even) {
+          const uint4 w = *reinterpret_cast<const uint4*>(from);
+          word[e] = w.x; word[e + 1] = w.y; word[e + 2] = w.z; word[e + 3] = w.w;
+        } else {
+          word[e] = from[0]; word[e + 1] = from[1]; word[e + 2] = from[2]; word[e + 3] = from[3];
+        }
+        any |= word[e] | word[e + 1] | word[e + 2] | word[e + 3];
+      }
     }
-    const uint32_t r4[4] = {raw.x, raw.y, raw.z, raw.w};
+    const uint32_t r4[4] = {raw[a].x, raw[a].y, raw[a].z, raw[a].w};
     uint32_t o4[4];
     if (any == 0u) {
       // nothing but the mask
@@ -119,11 +143,18 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_adjust_kernel(const __g
         for (int e = 0; e < 4; ++e) o4[e] = (bits >> (2 * e) & 1u ? r4[e] & 0xFFFFu : 0xFF80u) | (bits >> (2 * e + 1) & 1u ? r4[e] & 0xFFFF0000u : 0xFF800000u);
       }
     } else {
+      float x[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         if constexpr (sizeof(T) == 4) x[e] = __uint_as_float(r4[e]);
         else x[e] = __uint_as_float(e & 1 ? r4[e / 2] & 0xFFFF0000u : r4[e / 2] << 16);
-        x[e] = adjusted<T>(p, row, t + e, x[e], word[e], bits >> e & 1u, rep, presence, frequency);
+        x[e] = bits >> e & 1u ? penalised(x[e], word[e], rep, presence, frequency) : -CUDART_INF_F;
+      }
+      if (any & kBiased) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (!(word[e] & kBiased)) out[t + e] = T(x[e]);
+        continue;
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -136,6 +167,27 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_adjust_kernel(const __g
       }
     }
     *reinterpret_cast<uint4*>(out + t) = make_uint4(o4[0], o4[1], o4[2], o4[3]);
+  }
+  // A biased token is the warp's alone that has its first bias: the others have passed it over.  The lanes look through the list together
+  const int warp = tid >> 5, lane = tid & 31;
+  for (int i = warp; i < p.r.n_bias; i += kLogitsThreads / 32) {
+    const int32_t* tok = p.r.bias_token + (int64_t)row * p.r.n_bias;
+    const float* val = p.r.bias_value + (int64_t)row * p.r.n_bias;
+    const int t = __ldg(tok + i);
+    if (t < lo || t >= hi) continue;
+    float z = penalised(to_f32(in[t]), words[t - lo], rep, presence, frequency);
+    bool mine = true;
+    for (int j0 = 0; j0 < p.r.n_bias && mine; j0 += 32) {
+      const bool same = j0 + lane < p.r.n_bias && __ldg(tok + j0 + lane) == t;
+      const float v = same ? __ldg(val + j0 + lane) : 0.f;
+      for (uint32_t left = __ballot_sync(0xffffffffu, same); left; left &= left - 1) {
+        const int k = __ffs(left) - 1;
+        mine = mine && j0 + k >= i;
+        z = __fadd_rn(z, __shfl_sync(0xffffffffu, v, k));
+      }
+    }
+    __syncwarp();
+    if (mine && lane == 0) out[t] = T(is_allowed(t) ? z : -CUDART_INF_F);
   }
 }
 
@@ -152,7 +204,7 @@ spindlekv_status logits_adjust_impl(int n_rows, int vocab, const void* logits, i
   const int64_t wanted = std::max<int64_t>(1, 4 * 148 / n_rows);
   const int64_t slice = std::min<int64_t>(kLogitsMaxSlice, std::max<int64_t>(2048, (vocab + wanted - 1) / wanted));
   p.slice = (int)((slice + 1023) / 1024 * 1024);
-  const size_t smem = rules.history || rules.n_bias > 0 ? (size_t)std::min(p.slice, vocab) * 4 : 0;
+  const size_t smem = rules.history || rules.n_bias > 0 ? (size_t)std::min(p.slice, (vocab + 3) / 4 * 4) * 4 : 0;
   static PerDeviceOnce once;
   const int dev = PerDeviceOnce::current();
   if (dev < 0) return SPINDLEKV_CUDA;

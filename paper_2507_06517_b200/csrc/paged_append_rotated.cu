@@ -29,37 +29,58 @@ struct RotateParams {
 
 constexpr int kRotateThreads = 256, kRotateHeads = 8;      // query heads of a warp
 
-// four elements of either half of a row (plain loads: the rotated rows may take the rows' place)
-__device__ __forceinline__ void load_pairs(const float* p, int half, float (&x)[8]) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + half);
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-  x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-__device__ __forceinline__ void load_pairs(const __nv_bfloat16* p, int half, float (&x)[8]) {
-  const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(p + half);
-  const uint32_t w[4] = {a.x, a.y, b.x, b.y};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+// Four elements of either half of a row, as they lie in memory (plain loads: the rotated rows may take the rows' place)
+template <typename T> struct Pairs;
+template <> struct Pairs<float> {
+  float x[8];
+  __device__ __forceinline__ void load(const float* p, int half) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + half);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
   }
-}
-__device__ __forceinline__ void store_pairs(float* p, int half, const float (&x)[8]) {
-  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-  *reinterpret_cast<float4*>(p + half) = make_float4(x[4], x[5], x[6], x[7]);
-}
-__device__ __forceinline__ void store_pairs(__nv_bfloat16* p, int half, const float (&x)[8]) {
+  __device__ __forceinline__ void store(float* p, int half) const {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4*>(p + half) = make_float4(x[4], x[5], x[6], x[7]);
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = 0.f;
+  }
+  __device__ __forceinline__ void floats(float (&y)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = x[i];
+  }
+  __device__ __forceinline__ void set(const float (&y)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = y[i];
+  }
+};
+template <> struct Pairs<__nv_bfloat16> {
   uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int half) {
+    const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(p + half);
+    w[0] = a.x; w[1] = a.y; w[2] = b.x; w[3] = b.y;
   }
-  *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-  *reinterpret_cast<uint2*>(p + half) = make_uint2(w[2], w[3]);
-}
-__device__ __forceinline__ float as_stored(float x, const float*) { return x; }
-__device__ __forceinline__ float as_stored(float x, const __nv_bfloat16*) { return __bfloat162float(__float2bfloat16_rn(x)); }
+  __device__ __forceinline__ void store(__nv_bfloat16* p, int half) const {
+    *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    *reinterpret_cast<uint2*>(p + half) = make_uint2(w[2], w[3]);
+  }
+  __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0u; }
+  __device__ __forceinline__ void floats(float (&y)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y[2 * i] = __uint_as_float(w[i] << 16);
+      y[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  __device__ __forceinline__ void set(const float (&y)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+  }
+};
 
 // cosines and sines of four pairs at a position; NaN outside the table
 __device__ __forceinline__ void load_turn(const RotateParams& p, long long pos, int col, int half, float2 (&t)[4]) {
@@ -75,13 +96,16 @@ __device__ __forceinline__ void load_turn(const RotateParams& p, long long pos, 
   }
 }
 template <typename T>
-__device__ __forceinline__ void turn(float (&x)[8], const float2 (&t)[4]) {
+__device__ __forceinline__ void turn(Pairs<T>& row, const float2 (&t)[4]) {
+  float x[8];
+  row.floats(x);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float a = x[i], b = x[i + 4];
-    x[i] = as_stored(__fsub_rn(__fmul_rn(a, t[i].x), __fmul_rn(b, t[i].y)), static_cast<const T*>(nullptr));
-    x[i + 4] = as_stored(__fadd_rn(__fmul_rn(b, t[i].x), __fmul_rn(a, t[i].y)), static_cast<const T*>(nullptr));
+    x[i] = __fsub_rn(__fmul_rn(a, t[i].x), __fmul_rn(b, t[i].y));
+    x[i + 4] = __fadd_rn(__fmul_rn(b, t[i].x), __fmul_rn(a, t[i].y));
   }
+  row.set(x);
 }
 
 template <typename T, int D>
@@ -94,28 +118,28 @@ __device__ __forceinline__ void rotate_queries(const RotateParams& p, int layer,
   const T* from = reinterpret_cast<const T*>(p.Q.ptr) + (int64_t)layer * p.Q.sl + (int64_t)s * p.Q.ss + (int64_t)h0 * p.Q.sh + col;
   T* to = reinterpret_cast<T*>(const_cast<void*>(p.Q_out.ptr)) + (int64_t)layer * p.Q_out.sl + (int64_t)s * p.Q_out.ss + (int64_t)h0 * p.Q_out.sh + col;
   const long long first = p.first_pos ? p.first_pos[u] : start;
-#pragma unroll 2
+#pragma unroll 1
   for (int i = 0; i < NI; ++i) {
     const int r = r0 + i * RPI + sub;
     if (r0 + i * RPI >= n_new) break;
     if (r >= n_new) continue;
     float2 t[4];
     load_turn(p, first + r, col, HALF, t);
-    float x[kRotateHeads][8];
+    Pairs<T> x[kRotateHeads];
 #pragma unroll
     for (int h = 0; h < kRotateHeads; ++h)
-      if (h < heads) load_pairs(from + (int64_t)h * p.Q.sh + (int64_t)r * p.Q.st, HALF, x[h]);
+      if (h < heads) x[h].load(from + (int64_t)h * p.Q.sh + (int64_t)r * p.Q.st, HALF);
 #pragma unroll
     for (int h = 0; h < kRotateHeads; ++h)
       if (h < heads) {
-        turn<T>(x[h], t);
-        store_pairs(to + (int64_t)h * p.Q_out.sh + (int64_t)r * p.Q_out.st, HALF, x[h]);
+        turn(x[h], t);
+        x[h].store(to + (int64_t)h * p.Q_out.sh + (int64_t)r * p.Q_out.st, HALF);
       }
   }
 }
 
 template <typename T, int FMT, int D>
-__global__ void __launch_bounds__(kRotateThreads) paged_append_rotated_kernel(const __grid_constant__ RotateParams p) {
+__global__ void __launch_bounds__(kRotateThreads, sizeof(T) == 2 ? 3 : 2) paged_append_rotated_kernel(const __grid_constant__ RotateParams p) {
   constexpr int LPR = D / 8, RPI = 32 / LPR, NI = kPagedBlock / RPI, HALF = D / 2;
   const unsigned item = blockIdx.x * (kRotateThreads / 32) + (threadIdx.x >> 5);
   if (item >= p.n_items) return;
@@ -150,47 +174,49 @@ __global__ void __launch_bounds__(kRotateThreads) paged_append_rotated_kernel(co
   }
   const long long at0 = p.first_pos ? p.first_pos[u] : p.idx ? 0 : start;
   const float was = first > 0 && in_pool ? *scale : 0.f;
-  float x[NI][8];
+  Pairs<T> x[NI];
   float2 most = make_float2(0.f, 0.f);       // the largest magnitude; and NaN if there is a NaN or an infinity
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const int row = __shfl_sync(0xffffffffu, my_row, i * RPI + sub);
     if (row >= 0) {
-      load_pairs(rows + (int64_t)row * src.st, HALF, x[i]);
+      x[i].load(rows + (int64_t)row * src.st, HALF);
     } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
+      x[i].zero();
     }
   }
   if (!is_v) {
-    // four rows' cosines and sines at a time
+    // two rows' cosines and sines at a time
 #pragma unroll
-    for (int g = 0; g < NI; g += 4) {
-      float2 t[4][4];
-      int row[4];
+    for (int g = 0; g < NI; g += 2) {
+      float2 t[2][4];
+      int row[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 2; ++i) {
         row[i] = __shfl_sync(0xffffffffu, my_row, (g + i) * RPI + sub);
         if (row[i] >= 0) load_turn(p, at0 + row[i], col, HALF, t[i]);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 2; ++i)
         if (row[i] >= 0) {
-          turn<T>(x[g + i], t[i]);
+          turn(x[g + i], t[i]);
           if (keeps)
-            store_pairs(reinterpret_cast<T*>(const_cast<void*>(p.K_out.ptr)) + (int64_t)layer * p.K_out.sl + (int64_t)s * p.K_out.ss + (int64_t)head * p.K_out.sh +
-                            (int64_t)row[i] * p.K_out.st + col, HALF, x[g + i]);
+            x[g + i].store(reinterpret_cast<T*>(const_cast<void*>(p.K_out.ptr)) + (int64_t)layer * p.K_out.sl + (int64_t)s * p.K_out.ss + (int64_t)head * p.K_out.sh +
+                               (int64_t)row[i] * p.K_out.st + col, HALF);
         }
     }
   }
   if (!in_pool) return;
 #pragma unroll
-  for (int i = 0; i < NI; ++i)
+  for (int i = 0; i < NI; ++i) {
+    float f[8];
+    x[i].floats(f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      most.x = fmaxf(most.x, fabsf(x[i][e]));
-      most.y = fmaf(x[i][e], 0.f, most.y);
+      most.x = fmaxf(most.x, fabsf(f[e]));
+      most.y = fmaf(f[e], 0.f, most.y);
     }
+  }
   const uint32_t amax = __reduce_max_sync(0xffffffffu, most.y == 0.f ? __float_as_uint(most.x) : 0x7FC00000u);
   const bool poisoned = amax >= 0x7F800000u || !(was < __uint_as_float(0x7F800000u));
   const float sc = poisoned ? __uint_as_float(0x7FC00000u) : fmaxf(was, scale_of<FMT>(amax));
@@ -216,13 +242,21 @@ __global__ void __launch_bounds__(kRotateThreads) paged_append_rotated_kernel(co
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const int slot = i * RPI + sub;
-    if (slot >= first && slot < last) put(slot, empty ? make_uint2(0, 0) : encode8<FMT>(x[i], sc, inv, worst));
+    if (slot >= first && slot < last) {
+      float f[8];
+      x[i].floats(f);
+      put(slot, empty ? make_uint2(0, 0) : encode8<FMT>(f, sc, inv, worst));
+    }
   }
   if (FMT == SPINDLEKV_PAGED_INT8 && !empty && worst >= 0.5f * sc) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int slot = i * RPI + sub;
-      if (slot >= first && slot < last) put(slot, encode8_exactly(x[i], sc, inv));
+      if (slot >= first && slot < last) {
+        float f[8];
+        x[i].floats(f);
+        put(slot, encode8_exactly(f, sc, inv));
+      }
     }
   }
 }
