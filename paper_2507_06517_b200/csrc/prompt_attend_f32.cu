@@ -10,6 +10,9 @@
 // for bf16, with one row tile of 128 (position, head) rows and 64 keys at a time: their pieces fill the shared memory.  The scores of the next keys are
 // multiplied while this one's weights are formed: two buffers of scores and of weights in tensor memory.
 //     tensor memory: S [2][64 columns], P [2][3 pieces][32 columns], O [d columns]
+// The accumulator cuts off what it adds, always towards zero; over the products of thousands of keys that would be 2^-17 of the result (8.6e-6 at 4000
+// tokens).  So O holds one tile at a time, whose largest product comes last, and a warpgroup of its own adds the tiles up in its registers, rounding as
+// usual (7e-7).
 // Bound by the products: 6 x (128 x 64 x d) x 2 for 64 keys.
 #include <algorithm>
 
@@ -18,7 +21,9 @@
 
 namespace skv {
 
-constexpr int kExactThreads = 192, kExactAsk = 4, kExactIssue = 5, kExactKeys = 64;
+// warps 0-3: scores to weights, 4-7: sums of the tiles
+constexpr int kExactThreads = 320, kExactAsk = 8, kExactIssue = 9, kExactKeys = 64;
+constexpr int kExactFactors = 4;          // tiles whose factors of what is summed are kept: one that is read, and those that may be ahead of it
 constexpr int kExactSlots = 4;            // of the list of items
 constexpr int kPieces = 3;
 
@@ -27,8 +32,9 @@ struct ExactSmem {
   static constexpr int kQHalf = kPromptRows * 128, kQPiece = D / 64 * kQHalf;
   static constexpr int kHalf = kExactKeys * 128, kPiece = D / 64 * kHalf, kSlot = kPieces * kPiece;
   static constexpr int kRing = D == 128 ? 1 : 2;                             // slots of keys, and of values
-  static constexpr int q = 0, k = kPieces * kQPiece, v = k + kRing * kSlot, stage = v + kRing * kSlot, bars = stage + 4 * 4096;
-  static constexpr int kBars = 4 * kRing + 2 + 2 + 1 + 2 + 2 + 2 * kExactSlots + 1;
+  static constexpr int q = 0, k = kPieces * kQPiece, v = k + kRing * kSlot, stage = v + kRing * kSlot, factors = stage + 4 * 4096, stats = factors + kExactFactors * kPromptRows * 4,
+                       bars = stats + kPromptRows * 8;
+  static constexpr int kBars = 4 * kRing + 2 + 2 + 1 + 2 + 1 + 2 + 2 * kExactSlots + 1;
   static constexpr int words = bars + kBars * 8;
   static constexpr int items = (words + 32 + 15) / 16 * 16;
   static constexpr int redo = items + kExactSlots * (int)sizeof(PromptItem);
@@ -109,7 +115,7 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
   uint8_t* smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
   uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + S::bars);
   uint64_t *k_empty = k_full + RING, *v_full = k_empty + RING, *v_empty = v_full + RING, *q_full = v_empty + RING, *q_empty = q_full + 1, *s_full = q_empty + 1,
-           *pv_done = s_full + 2, *p_full = pv_done + 1, *o_full = p_full + 2, *o_empty = o_full + 1, *item_full = o_empty + 1, *item_empty = item_full + SLOTS,
+           *pv_done = s_full + 2, *p_full = pv_done + 1, *o_read = p_full + 2, *l_full = o_read + 1, *l_empty = l_full + 1, *item_full = l_empty + 1, *item_empty = item_full + SLOTS,
            *drained = item_empty + SLOTS;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::words);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + S::words) + 2;
@@ -117,7 +123,9 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
   volatile int* asked = reinterpret_cast<volatile int*>(smem + S::words) + 4;    // keys, rows, values
   PromptItem* items = reinterpret_cast<PromptItem*>(smem + S::items);
   uint32_t* redo = reinterpret_cast<uint32_t*>(smem + S::redo);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  float* factors = reinterpret_cast<float*>(smem + S::factors);
+  float2* stats = reinterpret_cast<float2*>(smem + S::stats);
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
   if (tid == 0) {
     for (int i = 0; i < RING; ++i) {
@@ -133,9 +141,10 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
       ptx::mbar_init(p_full + i, 4);          // (two: a warp may be done with the next tile's weights before another is with this one's)
     }
     ptx::mbar_init(pv_done, 1);
-    ptx::mbar_init(o_full, 1);
-    ptx::mbar_init(o_empty, 4);
-    for (int i = 0; i < SLOTS; ++i) { ptx::mbar_init(item_full + i, 1); ptx::mbar_init(item_empty + i, 5); }
+    ptx::mbar_init(o_read, 4);
+    ptx::mbar_init(l_full, 4);
+    ptx::mbar_init(l_empty, 4);
+    for (int i = 0; i < SLOTS; ++i) { ptx::mbar_init(item_full + i, 1); ptx::mbar_init(item_empty + i, 9); }
     ptx::mbar_init(drained, 1);
     ptx::fence_barrier_init();
     abort_flag[0] = abort_flag[1] = 0;
@@ -159,7 +168,7 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   __syncthreads();
   ptx::tc_fence_after();
-  const uint32_t tmem = *tmem_slot, tmem_p = tmem + 128, tmem_o = tmem + 384;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0), tmem_p = tmem + 128, tmem_o = tmem + 384;
 
   auto wait = [&](uint64_t* bar, int phase) { return ptx::mbar_wait(bar, phase & 1, abort_flag, p.wait_cycles); };
   int item_no = 0;
@@ -244,12 +253,16 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
     const uint32_t issues = ptx::elect_one();
     const uint64_t dq = ptx::smem_desc_sw128(ptx::smem_u32(smem + S::q)), dk = ptx::smem_desc_sw128(ptx::smem_u32(smem + S::k)),
                    dv = ptx::smem_desc_sw128_mn(ptx::smem_u32(smem + S::v), S::kHalf);
-    int n_o = 0;
     for (int pass = 0; pass == 0 || (pass == 1 && again()); ++pass) {
       PromptItem it;
       while (ok && next_item(it, ok)) {
-        const PromptTiles<1, KT> tiles(p, it);
-        if (tiles.most == 0) continue;
+        int most, even;
+        {
+          const PromptTiles<1, KT> tiles(p, it);
+          most = __shfl_sync(0xffffffffu, tiles.most, 0);
+          even = __shfl_sync(0xffffffffu, it.careful ? tiles.even[0] : tiles.most, 0);      // tiles whose values are multiplied here
+        }
+        if (most == 0) continue;
         auto release = [&](uint64_t* bar) {
           if (issues) ptx::umma_commit(bar);
           __syncwarp();
@@ -271,42 +284,41 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
         ok = __all_sync(0xffffffffu, wait(q_full, n_q++));
         if (!ok) break;
         scores(n_kv);
-        if (tiles.most == 1) release(q_empty);
-        for (int j = 0; j < tiles.most && ok; ++j, ++n_kv) {
-          if (j + 1 < tiles.most) {
+        if (most == 1) release(q_empty);
+        for (int j = 0; j < most && ok; ++j, ++n_kv) {
+          if (j + 1 < most) {
             scores(n_kv + 1);
-            if (j + 2 == tiles.most) release(q_empty);
+            if (j + 2 == most) release(q_empty);
           }
           const int at = n_kv % RING;
-          if (j == 0) ok = wait(o_empty, n_o++ + 1) && ok;
           ok = wait(v_full + at, n_kv / RING) && ok;
+          ok = wait(o_read, n_kv + 1) && ok;               // the tile before has been read
           ok = __all_sync(0xffffffffu, wait(p_full + (n_kv & 1), n_kv >> 1) && ok);
           if (!ok) break;
           ptx::tc_fence_after();
-          if (!it.careful || j < tiles.even[0]) {
+          if (j < even) {
 #pragma unroll
             for (int x = 0; x < kProducts; ++x)
 #pragma unroll
               for (int k = 0; k < KT / 16; ++k)
                 ptx::umma_bf16_ts_elected(tmem_o, tmem_p + (n_kv & 1) * 96 + kFirst[x] * 32 + k * 8, dv + ((at * S::kSlot + kSecond[x] * S::kPiece + k * 2048) >> 4), idesc_o,
-                                          j == 0 && x == 0 && k == 0 ? 0u : 1u, issues);
+                                          x == 0 && k == 0 ? 0u : 1u, issues);
           }
           release(v_empty + at);
           release(pv_done);
-          if (j + 1 == tiles.most) release(o_full);
         }
       }
     }
-  } else {
+  } else if (warp < 4) {
+    // ---- scores -> weights: a thread has a row ----
     const int row = warp * 32 + lane;
-    const uint32_t lanes = (uint32_t)(warp * 32) << 16, to = tmem_o + lanes;
-    int n_o = 0;
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    int n_items = 0;
     for (int pass = 0; pass == 0 || (pass == 1 && again()); ++pass) {
       PromptItem it;
       while (ok && next_item(it, ok)) {
         const PromptTiles<1, KT> tiles(p, it);
-        const int layer = it.ls / p.rows.n_seqs, seq = it.ls - layer * p.rows.n_seqs;
-        const int within = row / p.hn, head = it.head * p.hn + row - within * p.hn, pos = it.blk * p.per_item + within;
+        const int within = row / p.hn, pos = it.blk * p.per_item + within;
         const bool there = within < p.pt && pos < it.n_r;
         const int n = tiles.count[0], sees = there ? seen_by(pos, it.n_r, it.n_k) : 0x7FFFFFFF;
         float m = -CUDART_INF_F, l = 0.f;
@@ -326,26 +338,15 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
 #pragma unroll
           for (int c = 0; c < KT; ++c) top[c & 3] = fmaxf(top[c & 3], __uint_as_float(s[c]));
           const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale;
+          float f = 1.f;                       // of what is summed so far
           if (j == 0) {
             m = high;
-          } else if (__any_sync(0xffffffffu, high > m + kPromptLazy)) {
-            const float now = fmaxf(m, high), f = now == m ? 1.f : pow2(m - now);
-            m = now;
+          } else if (high > m + kPromptLazy) {
+            f = pow2(m - high);
+            m = high;
             l *= f;
-            if (!it.careful || tiles.even[0] > 0) {
-              ok = wait(pv_done, n_kv - 1) && ok;          // (it is at most one behind)
-              __syncwarp();
-              ptx::tc_fence_after();
-#pragma unroll 1
-              for (int c = 0; c < D; c += 32) {
-                uint32_t o[32];
-                ptx::tmem_ld_32x32_sync(to + c, o);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                ptx::tmem_st_32x32(to + c, o);
-              }
-            }
           }
+          factors[(n_kv % kExactFactors) * kPromptRows + row] = f;
           const float ref = m == -CUDART_INF_F ? 0.f : m;
           float sum[2] = {0.f, 0.f};
           const uint32_t tp = tmem_p + (n_kv & 1) * 96 + lanes;
@@ -373,13 +374,74 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(p_full + (n_kv & 1));
         }
-        // ---- the item's result ----
-        if (n > 0) ok = wait(o_full, n_o++) && ok;
+        ok = wait(l_empty, n_items++ + 1) && ok;
+        stats[row] = make_float2(m, l);
         __syncwarp();
-        ptx::tc_fence_after();
-        if (it.careful && n > tiles.even[0])
-          add_by_hand<T, D>(p, it, to, 0, D, tiles.even[0] == 0, head, there ? pos : 0, (tiles.first + tiles.even[0]) * KT, there ? min(sees, (tiles.first + n) * KT) : 0,
-                            m == -CUDART_INF_F ? 0.f : m);
+        if (lane == 0) ptx::mbar_arrive(l_full);
+        ok = __all_sync(0xffffffffu, ok);
+      }
+    }
+  } else {
+    // ---- the tiles' products are summed, and the result leaves: a thread has a row ----
+    const int row = (warp - 4) * 32 + lane;
+    const uint32_t to = tmem_o + ((uint32_t)((warp - 4) * 32) << 16);
+    int n_items = 0;
+    float o[D];
+    auto read = [&](auto&& each) {
+#pragma unroll
+      for (int c = 0; c < D; c += 16) {
+        uint32_t x[16];
+        ptx::tmem_ld_32x16_sync(to + c, x);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) each(c + i, __uint_as_float(x[i]));
+      }
+    };
+    for (int pass = 0; pass == 0 || (pass == 1 && again()); ++pass) {
+      PromptItem it;
+      while (ok && next_item(it, ok)) {
+        const PromptTiles<1, KT> tiles(p, it);
+        const int layer = it.ls / p.rows.n_seqs, seq = it.ls - layer * p.rows.n_seqs;
+        const int within = row / p.hn, head = it.head * p.hn + row - within * p.hn, pos = it.blk * p.per_item + within;
+        const bool there = within < p.pt && pos < it.n_r, by_hand = it.careful && tiles.count[0] > tiles.even[0];
+        const int n = tiles.count[0];
+#pragma unroll
+        for (int i = 0; i < D; ++i) o[i] = 0.f;
+        for (int j = 0; j < n; ++j, ++n_kv) {
+          ok = wait(pv_done, n_kv) && ok;
+          __syncwarp();
+          ptx::tc_fence_after();
+          const float f = factors[(n_kv % kExactFactors) * kPromptRows + row];
+          if (!by_hand || j < tiles.even[0]) {
+            read([&](int i, float x) { o[i] = fmaf(o[i], f, x); });
+          } else {
+#pragma unroll
+            for (int i = 0; i < D; ++i) o[i] *= f;
+          }
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0 && !(by_hand && j + 1 == n)) ptx::mbar_arrive(o_read);
+        }
+        ok = wait(l_full, n_items++) && ok;
+        const float m = stats[row].x, l = stats[row].y;
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(l_empty);
+        if (by_hand) {                         // by way of the tensor memory, which is this item's until its last tile counts as read
+#pragma unroll
+          for (int c = 0; c < D; c += 16) {
+            uint32_t x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(o[c + i]);
+            ptx::tmem_st_32x16(to + c, x);
+          }
+          ptx::tmem_st_wait();
+          const int sees = there ? seen_by(pos, it.n_r, it.n_k) : 0;
+          add_by_hand<T, D>(p, it, to, 0, D, false, head, there ? pos : 0, (tiles.first + tiles.even[0]) * KT, min(sees, (tiles.first + n) * KT), m == -CUDART_INF_F ? 0.f : m);
+          __syncwarp();
+          read([&](int i, float x) { o[i] = x; });
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(o_read);
+        }
         const bool write = there && ok && !*abort_flag;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const int64_t number = row_number(p, layer, seq, it.base_r, head, pos);
@@ -388,27 +450,17 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
         uint8_t* base = reinterpret_cast<uint8_t*>(p.splits > 1 ? p.part : const_cast<void*>(p.out.ptr));
         const float f = p.splits > 1 ? 1.f : inv;
         bool odd = false;
-#pragma unroll 1
+#pragma unroll
         for (int c = 0; c < D; c += 32) {
-          uint32_t o[32];
-          if (n > 0) {
-            __syncwarp();
-            ptx::tmem_ld_32x32_sync(to + c, o);
-          }
-          float x[32];
-#pragma unroll
-          for (int i = 0; i < 32; ++i) x[i] = n > 0 ? __uint_as_float(o[i]) : 0.f;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) odd |= x[i] != x[i];
           uint4 h[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            h[e] = make_uint4(__float_as_uint(x[4 * e] * f), __float_as_uint(x[4 * e + 1] * f), __float_as_uint(x[4 * e + 2] * f), __float_as_uint(x[4 * e + 3] * f));
-          put_rows(smem + S::stage + warp * 4096, h, base + c * 4, at);
+          for (int e = 0; e < 8; ++e) {
+            const float* x = o + c + 4 * e;
+            odd |= x[0] != x[0] || x[1] != x[1] || x[2] != x[2] || x[3] != x[3];
+            h[e] = make_uint4(__float_as_uint(x[0] * f), __float_as_uint(x[1] * f), __float_as_uint(x[2] * f), __float_as_uint(x[3] * f));
+          }
+          put_rows(smem + S::stage + (warp - 4) * 4096, h, base + c * 4, at);
         }
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (n > 0 && lane == 0) ptx::mbar_arrive(o_empty);
         if (write) {
           if (p.splits > 1) p.stat[parts + number] = make_float2(m, l);
           else put_lse(p, number, m, l);
