@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
         if (n > 0 && lane == 0) ptx::mbar_arrive(o_empty + w);
         if (write) {
           if (p.splits > 1) p.stat[parts + number] = make_float2(m, l);
-          else put_lse(p, number, m, l);
+          else put_lse(p, layer, column_of(p, seq, it.base_r, pos), head, m, l);
           // (only what is hidden from a row can make its result NaN where its sum is a number; what it sees does so again)
           if (odd && !it.careful && l == l) {
             atomicOr(redo + (it.number >> 5), 1u << (it.number & 31));
@@ -414,6 +414,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
       }
       }
     } else {
+      if (tid == kPromptThreads - 1) prompt_begins(p);
       again();
     }
   }
@@ -434,8 +435,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem, 512);
   }
-  __syncthreads();
-  if (tid == 0) prompt_settle(p, *abort_flag != 0);
+  if (tid == 0 && *abort_flag) prompt_failed(p);
 }
 
 // ---- host ----------------------------------------------------------------------------------------

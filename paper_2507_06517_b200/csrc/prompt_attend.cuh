@@ -53,28 +53,29 @@ struct PromptItem {
 // Items in falling order of their block's number, which is nearly that of their work: all sequences' last positions first.  A warp finds item
 // `i` by the number of blocks with a number of b or more, which falls with b.
 struct PromptList {
-  int nb[4];                  // blocks of (layer, seq) lane, lane + 32, ... where there are up to 128
+  Span rows, keys;            // of (layer, seq) lane, where there are up to 32
   int n_ls, all;
-  __device__ __forceinline__ static int blocks_of(const PromptParams& p, int ls) {
-    const int layer = ls / p.rows.n_seqs;
-    return (span_of(p.rows, layer, ls - layer * p.rows.n_seqs).len + p.per_item - 1) / p.per_item;
+  __device__ __forceinline__ static Span span_at(const Batch& b, int ls) {
+    const int layer = ls / b.n_seqs;
+    return span_of(b, layer, ls - layer * b.n_seqs);
   }
-  __device__ __forceinline__ int count(const PromptParams& p, int b) const {       // blocks with the number b or a larger one
-    const int lane = threadIdx.x & 31;
+  __device__ __forceinline__ int blocks_of(const PromptParams& p, int ls) const {       // with up to 32: of this lane's
+    if (n_ls <= 32) return (rows.len + p.per_item - 1) / p.per_item;
+    return ls < n_ls ? (span_at(p.rows, ls).len + p.per_item - 1) / p.per_item : 0;
+  }
+  __device__ __forceinline__ int count(const PromptParams& p, int b) const {            // blocks with the number b or a larger one
     int n = 0;
-    if (n_ls <= 128) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) n += max(nb[i] - b, 0);
-    } else {
-      for (int ls = lane; ls < n_ls; ls += 32) n += max(blocks_of(p, ls) - b, 0);
-    }
+    for (int ls = threadIdx.x & 31; ls < (n_ls + 31) / 32 * 32; ls += 32) n += max(blocks_of(p, ls) - b, 0);
     return __reduce_add_sync(0xffffffffu, n);
   }
   __device__ __forceinline__ PromptList(const PromptParams& p) {
     const int lane = threadIdx.x & 31;
     n_ls = p.rows.n_layers * p.rows.n_seqs;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) nb[i] = n_ls <= 128 && lane + 32 * i < n_ls ? blocks_of(p, lane + 32 * i) : 0;
+    rows = keys = {0, 0};
+    if (n_ls <= 32 && lane < n_ls) {
+      rows = span_at(p.rows, lane);
+      keys = span_at(p.keys, lane);
+    }
     all = count(p, 0);
   }
   // The block's k-th item, or one with ls = -1; every other round goes backwards, so that no block gets the longest of all rounds
@@ -85,7 +86,7 @@ struct PromptList {
     const long long i = (long long)k * gridDim.x + ((k & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
     const int per = p.heads * p.splits;
     if (i >= (long long)all * per) return it;
-    const int q = (int)(i / per), inner = (int)(i - (long long)q * per);
+    const int q = i <= 0x7FFFFFFF ? (int)i / per : (int)(i / per), inner = (int)(i - (long long)q * per);
     int lo = 0, hi = p.max_blocks - 1, above = 0;          // the largest b with more than q blocks of that number or more; `above`: those of b + 1 or more
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1, c = count(p, mid);
@@ -94,11 +95,7 @@ struct PromptList {
     }
     int rank = q - above, found = -1;
     for (int first = 0; first < n_ls && found < 0; first += 32) {
-      const int ls = first + lane;
-      int n = 0;
-      if (n_ls <= 128) n = first == 0 ? nb[0] : first == 32 ? nb[1] : first == 64 ? nb[2] : nb[3];
-      else if (ls < n_ls) n = blocks_of(p, ls);
-      uint32_t has = __ballot_sync(0xffffffffu, n > lo);
+      uint32_t has = __ballot_sync(0xffffffffu, blocks_of(p, first + lane) > lo);
       if (rank >= __popc(has)) {
         rank -= __popc(has);
         continue;
@@ -107,16 +104,22 @@ struct PromptList {
       found = first + __ffs(has) - 1;
     }
     if (found < 0) return it;
-    const int layer = found / p.rows.n_seqs, s = found - layer * p.rows.n_seqs;
-    const Span r = span_of(p.rows, layer, s), n = span_of(p.keys, layer, s);
     it.ls = found;
     it.blk = lo;
     it.head = inner / p.splits;
     it.split = inner - it.head * p.splits;
-    it.n_r = r.len;
-    it.n_k = n.len;
-    it.base_r = r.base;
-    it.base_k = n.base;
+    if (n_ls <= 32) {
+      it.n_r = __shfl_sync(0xffffffffu, rows.len, found);
+      it.n_k = __shfl_sync(0xffffffffu, keys.len, found);
+      it.base_r = __shfl_sync(0xffffffffu, rows.base, found);
+      it.base_k = __shfl_sync(0xffffffffu, keys.base, found);
+    } else {
+      const Span r = span_at(p.rows, found), n = span_at(p.keys, found);
+      it.n_r = r.len;
+      it.n_k = n.len;
+      it.base_r = r.base;
+      it.base_k = n.base;
+    }
     it.number = k;
     return it;
   }
@@ -152,24 +155,39 @@ struct PromptTiles {
 __device__ __forceinline__ int64_t row_offset(const View& v, const Batch& b, int layer, int s, int base, int head, int pos) {
   return (int64_t)layer * v.sl + (b.cu ? 0 : (int64_t)s * v.ss) + (int64_t)head * v.sh + (int64_t)(base + pos) * v.st;
 }
-// (layer, T column, query head) as one number
+// (layer, T column, query head) as one number, and its place in lse
+__device__ __forceinline__ int column_of(const PromptParams& p, int s, int base, int pos) { return p.rows.cu ? base + pos : s * p.rows.max_len + pos; }
 __device__ __forceinline__ int64_t row_number(const PromptParams& p, int layer, int s, int base, int head, int pos) {
-  const int64_t col = p.rows.cu ? (int64_t)base + pos : (int64_t)s * p.rows.max_len + pos;
-  return ((int64_t)layer * p.rows.total_len + col) * (p.heads * p.hn) + head;
+  return ((int64_t)layer * p.rows.total_len + column_of(p, s, base, pos)) * (p.heads * p.hn) + head;
 }
-__device__ __forceinline__ void put_lse(const PromptParams& p, int64_t number, float m, float l) {
-  if (!p.lse) return;
-  const int hq = p.heads * p.hn;
-  const int64_t lt = number / hq, layer = lt / p.rows.total_len;
-  const float lse = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * 0.69314718055994530942f;
-  p.lse[(layer * hq + (number - lt * hq)) * p.rows.total_len + (lt - layer * p.rows.total_len)] = lse;
+__device__ __forceinline__ void put_lse(const PromptParams& p, int layer, int col, int head, float m, float l) {
+  if (p.lse) p.lse[((int64_t)layer * (p.heads * p.hn) + head) * p.rows.total_len + col] = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * 0.69314718055994530942f;
 }
 
-// the last block of a call leaves the status word
-__device__ __forceinline__ void prompt_settle(const PromptParams& p, bool failed) {
+// The status word.  Blocks are counted as they begin, which nobody waits for; the last one writes OK.  A block that fails says so to the last one to begin,
+// or, if that has been, in the status word itself: the word is written before the count starts again from zero.
+__device__ __forceinline__ void prompt_begins(const PromptParams& p) {        // one thread
+  unsigned long long* word = reinterpret_cast<unsigned long long*>(p.hdr + kPromptHdrDone);
+  const unsigned long long was = count_arrival<24>(word);
+  if ((int)(was & 0xFFFFu) + 1 != (int)gridDim.x) return;
+  // (a failure that comes in now changes the word, and is seen)
+  for (unsigned long long now = was + 1;;) {
+    *reinterpret_cast<volatile uint32_t*>(p.hdr + kHdrStatus) = now >> 16 & 1u ? SPINDLEKV_TIMEOUT : SPINDLEKV_OK;
+    __threadfence();
+    const unsigned long long seen = atomicCAS(word, now, kNoArrivals<24>);
+    if (seen == now) return;
+    now = seen;
+  }
+}
+__device__ __forceinline__ void prompt_failed(const PromptParams& p) {        // one thread, after its block has been counted
+  unsigned long long* word = reinterpret_cast<unsigned long long*>(p.hdr + kPromptHdrDone);
+  for (unsigned long long now = *reinterpret_cast<volatile unsigned long long*>(word); now >> 24 == kNoArrivals<24> >> 24 && (now & 0xFFFFu);) {
+    const unsigned long long seen = atomicCAS(word, now, now | 1ull << 16);
+    if (seen == now) return;
+    now = seen;
+  }
   __threadfence();
-  const int last = last_to_arrive(reinterpret_cast<unsigned long long*>(p.hdr + kPromptHdrDone), gridDim.x, failed);
-  if (last) p.hdr[kHdrStatus] = last == 2 ? SPINDLEKV_TIMEOUT : SPINDLEKV_OK;
+  *reinterpret_cast<volatile uint32_t*>(p.hdr + kHdrStatus) = SPINDLEKV_TIMEOUT;
 }
 
 // a x b + c of two numbers at a time
@@ -325,7 +343,7 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const __grid_constant_
   const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
   for (int e = 0; e < E; ++e) dst[e] = T(num[e] * inv);
-  if (lane == 0) put_lse(p, number, top, den);
+  if (lane == 0) put_lse(p, layer, col, head, top, den);
 }
 
 // ---- host ----------------------------------------------------------------------------------------

@@ -385,6 +385,8 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
     // ---- the tiles' products are summed, and the result leaves: a thread has a row ----
     const int row = (warp - 4) * 32 + lane;
     const uint32_t to = tmem_o + ((uint32_t)((warp - 4) * 32) << 16);
+    if (tid == 4 * 32) prompt_begins(p);
+    __syncwarp();
     int n_items = 0;
     float o[D];
     auto read = [&](auto&& each) {
@@ -463,7 +465,7 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
         }
         if (write) {
           if (p.splits > 1) p.stat[parts + number] = make_float2(m, l);
-          else put_lse(p, number, m, l);
+          else put_lse(p, layer, column_of(p, seq, it.base_r, pos), head, m, l);
           if (odd && !it.careful && l == l) {
             atomicOr(redo + (it.number >> 5), 1u << (it.number & 31));
             *any_redo = 1;
@@ -490,8 +492,7 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem, 512);
   }
-  __syncthreads();
-  if (tid == 0) prompt_settle(p, *abort_flag != 0);
+  if (tid == 0 && *abort_flag) prompt_failed(p);
 }
 
 // ---- host ----------------------------------------------------------------------------------------

@@ -185,3 +185,38 @@ def test_strides_streams_graphs_and_repeats(dtype):
     torch.cuda.synchronize()
     assert torch.equal(out, attend(keys, keys, q, k, v)[0])
     assert a.status() == B.OK
+
+
+@pytest.fixture
+def limits():
+    yield B.spindlekv_set_tuning
+    for key in (B.TUNE_MBAR_WAIT_CYCLES, B.TUNE_PAGED_WITHHOLD):
+        B.spindlekv_set_tuning(key, -1)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens,rows,blocks", [([300, 200, 90], None, (0, 3, 5)), ([3000], [3], (0, 7))])
+def test_a_wait_that_gives_up_shows_in_the_status_and_leaves_nothing_behind(lens, rows, blocks, dtype, limits):
+    from paper_2507_06517_b200.pipeline import SpindleKVPromptAttention, record_graph
+    keys, rws, q, k, v = make(lens, rows, 4, 2, 128, dtype, True, seed=21)
+    a = SpindleKVPromptAttention(keys, 4, 2, 128, dtype, rows=rws)
+    want, _, bound = R.attend(q, k, v, keys, rws)
+    out = torch.zeros_like(q)
+    for block in blocks:                                   # whichever block gives up, and whatever the scratch held
+        a.ws.random_(0, 256)
+        limits(B.TUNE_MBAR_WAIT_CYCLES, 2_000_000)
+        limits(B.TUNE_PAGED_WITHHOLD, block)
+        a.run(q, k, v, out=out)
+        assert a.status() == B.TIMEOUT
+        limits(B.TUNE_MBAR_WAIT_CYCLES, -1)
+        limits(B.TUNE_PAGED_WITHHOLD, -1)
+        for _ in range(2):
+            a.run(q, k, v, out=out)
+            assert a.status() == B.OK
+            assert ((out.double() - want).abs() <= bound).all()
+    graph = record_graph(lambda: a.run(q, k, v, out=out))
+    for _ in range(3):
+        a.ws.random_(0, 256)
+        graph.replay()
+        graph.replay()
+        assert a.status() == B.OK
