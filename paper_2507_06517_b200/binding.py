@@ -498,8 +498,11 @@ def spindlekv_prompt_workspace_bytes(keys: Batch, rows: Optional[Batch], n_q_hea
 def spindlekv_prompt_attend(keys: Batch, rows: Optional[Batch], n_q_heads: int, n_kv_heads: int, head_dim: int, scale: float, q: _Tensor, K: _Tensor, V: _Tensor,
                             out: _Tensor, lse: Optional[torch.Tensor], ws: torch.Tensor, stream=None) -> None:
     """``lse``: ``[n_layers, n_q_heads, T]`` fp32 or None.  ``rows`` None: every token is a row."""
-    kk, rr = (None if b is None else b if isinstance(b, _Batch) else b.c() for b in (keys, rows))
-    _check(_lib.spindlekv_prompt_attend(kk, rr, n_q_heads, n_kv_heads, head_dim, scale, q, K, V, out, _ptr(lse), _ptr(ws), _bytes(ws), _stream(stream)),
+    if isinstance(keys, Batch):
+        keys = keys.c()
+    if isinstance(rows, Batch):
+        rows = rows.c()
+    _check(_lib.spindlekv_prompt_attend(keys, rows, n_q_heads, n_kv_heads, head_dim, scale, q, K, V, out, _ptr(lse), _ptr(ws), _bytes(ws), _stream(stream)),
            "spindlekv_prompt_attend")
 
 

@@ -186,24 +186,29 @@ __global__ void __launch_bounds__(kRotateThreads, sizeof(T) == 2 ? 3 : 2) paged_
     }
   }
   if (!is_v) {
-    // two rows' cosines and sines at a time
-#pragma unroll
-    for (int g = 0; g < NI; g += 2) {
-      float2 t[2][4];
-      int row[2];
+    // two rows' cosines and sines at a time, the next two's asked for before these are used
+    float2 t[2][2][4];
+    auto ask = [&](int g) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        row[i] = __shfl_sync(0xffffffffu, my_row, (g + i) * RPI + sub);
-        if (row[i] >= 0) load_turn(p, at0 + row[i], col, HALF, t[i]);
+        const int row = __shfl_sync(0xffffffffu, my_row, (g + i) * RPI + sub);
+        if (row >= 0) load_turn(p, at0 + row, col, HALF, t[(g >> 1) & 1][i]);
       }
+    };
+    ask(0);
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (row[i] >= 0) {
-          turn(x[g + i], t[i]);
+    for (int g = 0; g < NI; g += 2) {
+      if (g + 2 < NI) ask(g + 2);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = __shfl_sync(0xffffffffu, my_row, (g + i) * RPI + sub);
+        if (row >= 0) {
+          turn(x[g + i], t[(g >> 1) & 1][i]);
           if (keeps)
             x[g + i].store(reinterpret_cast<T*>(const_cast<void*>(p.K_out.ptr)) + (int64_t)layer * p.K_out.sl + (int64_t)s * p.K_out.ss + (int64_t)head * p.K_out.sh +
-                               (int64_t)row[i] * p.K_out.st + col, HALF);
+                               (int64_t)row * p.K_out.st + col, HALF);
         }
+      }
     }
   }
   if (!in_pool) return;

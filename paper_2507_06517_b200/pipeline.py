@@ -550,6 +550,10 @@ class SpindleKVDecodeAttention:
         return self.out
 
 
+def _layout(t: Optional[torch.Tensor]):
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
+
+
 class _OnDevice:
     """Calls go to the current device and stream; ``_elsewhere`` says that the owner's device has to be made current first."""
 
@@ -627,6 +631,7 @@ class SpindleKVPagedCache(_OnDevice):
         self.no_tokens = torch.zeros((self.n_layers, self.n_seqs), dtype=torch.int32, device=self.device)
         self.n_live = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._tables = {}
+        self._rotated = (None, None)                       # layouts of the last append_rotated, and what follows from them
         self._out: Dict[tuple, torch.Tensor] = {}
         n = B.spindlekv_paged_workspace_bytes(self.pool, self.table, self.Hkv, 1)      # the same for every shape that is served
         self.ws_attend = torch.zeros(n, dtype=torch.uint8, device=self.device)
@@ -693,48 +698,53 @@ class SpindleKVPagedCache(_OnDevice):
         position ``first_pos + r`` (``first_pos`` ``[n_layers or 1, n_seqs]`` int32; ``start`` by default, 0 with ``idx``).  ``K_out``, if given, gets the rotated
         keys (it may be ``K``); queries ``Q`` ``[n_layers or 1, n_seqs, H_q, rows, d]`` of the same rows are rotated alike into ``Q_out`` (it may be ``Q``; by
         default a new tensor, zeros behind the new rows), which is returned."""
-        if self._elsewhere():
+        if B.current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self.append_rotated(K, V, rope_table, start, first_pos, idx, idx_seq, max_new, K_out, Q, Q_out, layer, stream)
-        table = self._rows_of(layer)
-        n_l = table.n_layers
+        table = self.table if layer is None else self._rows_of(layer)
         start = self.start if start is None else start
-        if layer is not None and start.shape[0] == self.n_layers:
-            start = start[layer:layer + 1]
-        if layer is not None and first_pos is not None and first_pos.shape[0] == self.n_layers:
-            first_pos = first_pos[layer:layer + 1]
+        if layer is not None:
+            start, first_pos = (t[layer:layer + 1] if t is not None and t.shape[0] == self.n_layers else t for t in (start, first_pos))
+        if Q is not None and Q_out is None:
+            Q_out = self._empty(Q.shape, Q.dtype, stream, zero=True)
+        # arguments laid out as those of the last call have been looked over
+        layouts = (layer is None, _layout(K), _layout(V), _layout(rope_table), _layout(start), _layout(first_pos), _layout(idx), _layout(K_out), _layout(Q), _layout(Q_out))
+        if layouts != self._rotated[0]:
+            self._rotated = (layouts, self._look_over_rotated(table.n_layers, K, V, rope_table, start, first_pos, idx, K_out, Q, Q_out))
+        kd, vd, kod, qd, qod, hq, n_rows = self._rotated[1]
+        kd.ptr, vd.ptr = K.data_ptr(), V.data_ptr()
+        if K_out is not None:
+            kod.ptr = K_out.data_ptr()
+        if Q is not None:
+            qd.ptr, qod.ptr = Q.data_ptr(), Q_out.data_ptr()
+        if idx is not None and idx_seq is None:
+            idx_seq = idx.shape[2] // self.n_seqs
+        if max_new is None:
+            max_new = n_rows if idx is None else idx_seq
+        B.spindlekv_paged_append_rotated(self.pool, table, start, max_new, kd, vd, n_rows, rope_table, first_pos, kod, hq, qd, qod, idx, idx_seq or 0, self._raw(stream))
+        return Q_out
+
+    def _look_over_rotated(self, n_l, K, V, rope_table, start, first_pos, idx, K_out, Q, Q_out):
+        """Checks of ``append_rotated``; descriptors of its rows, the query heads and the rows of each."""
         self._mine("start", start, torch.int32, (n_l, self.n_seqs))
         if first_pos is not None:
             self._mine("first_pos", first_pos, torch.int32, (n_l, self.n_seqs))
         self._mine("rope_table", rope_table, torch.float32)
         if rope_table.dim() != 3 or rope_table.shape[1:] != (self.d // 2, 2):
             raise ValueError(f"rope_table: [positions, {self.d // 2}, 2] expected, got {list(rope_table.shape)}")
-        n_rows = K.shape[3] if K.dim() == 5 else -1
         if idx is not None:
             self._mine("idx", idx, torch.int32)
             if idx.dim() != 3 or idx.shape[0] != n_l or idx.shape[1] != self.Hkv:
                 raise ValueError(f"idx: [{n_l}, {self.Hkv}, n_seqs * idx_seq] expected, got {list(idx.shape)}")
-            idx_seq = idx.shape[2] // self.n_seqs if idx_seq is None else idx_seq
-        if max_new is None:
-            max_new = n_rows if idx is None else idx_seq
-        rows = {"K": self._cache_rows("K", K, n_l, self.Hkv), "V": self._cache_rows("V", V, n_l, self.Hkv), "K_out": B.NO_TENSOR, "Q": B.NO_TENSOR, "Q_out": B.NO_TENSOR}
-        hq, same = 0, [("V", V)]
-        if K_out is not None:
-            rows["K_out"] = self._cache_rows("K_out", K_out, n_l, self.Hkv)
-            same.append(("K_out", K_out))
-        if Q is not None:
-            hq = Q.shape[2] if Q.dim() == 5 else 0
-            rows["Q"] = self._cache_rows("Q", Q, n_l, hq)
-            if Q_out is None:
-                Q_out = self._empty(Q.shape, Q.dtype, stream, zero=True)
-            rows["Q_out"] = self._cache_rows("Q_out", Q_out, n_l, hq)
-            same += [("Q", Q), ("Q_out", Q_out)]
-        for name, t in same:
-            if t.shape[3] != n_rows:
-                raise ValueError(f"{name}: {n_rows} rows expected as in K, got {t.shape[3]}")
-        B.spindlekv_paged_append_rotated(self.pool, table, start, max_new, rows["K"], rows["V"], n_rows, rope_table, first_pos, rows["K_out"], hq, rows["Q"],
-                                         rows["Q_out"], idx, idx_seq or 0, self._raw(stream))
-        return Q_out
+        if Q is None and Q_out is not None:
+            raise ValueError("Q_out without Q")
+        hq = 0 if Q is None else Q.shape[2] if Q.dim() == 5 else -1
+        out = []
+        for name, t, heads in (("K", K, self.Hkv), ("V", V, self.Hkv), ("K_out", K_out, self.Hkv), ("Q", Q, hq), ("Q_out", Q_out, hq)):
+            out.append(B.NO_TENSOR if t is None else self._cache_rows(name, t, n_l, heads))
+            if t is not None and t.shape[3] != K.shape[3]:
+                raise ValueError(f"{name}: {K.shape[3]} rows expected as in K, got {t.shape[3]}")
+        return (*out, hq, K.shape[3])
 
     def attend(self, q: torch.Tensor, out: Optional[torch.Tensor] = None, max_len: Optional[int] = None, scale: float = 0.0,
                layer: Optional[int] = None, stream=None) -> torch.Tensor:
@@ -811,6 +821,7 @@ class SpindleKVPromptAttention(_OnDevice):
             raise ValueError(f"unsupported attention: {n_q_heads} query heads, {n_kv_heads} KV heads of {head_dim}, {self.keys}, {self.rows}")
         self.ws = torch.empty(n, dtype=torch.uint8, device=dev)
         self._c = self.keys.c(), self.rows.c()
+        self._seen = (None, None)                          # layouts of the last call, and the descriptors that follow from them
 
     def _rows_of(self, name: str, t: torch.Tensor, b: B.Batch, heads: int) -> B._Tensor:
         shape, strides = t.shape, t.stride()
@@ -824,16 +835,21 @@ class SpindleKVPromptAttention(_OnDevice):
     def run(self, q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, scale: float = 0.0,
             stream=None) -> torch.Tensor:
         """``out`` (made by the call by default: zeros behind a sequence's rows) and ``lse`` ``[L, H_q, T]`` fp32, if given, are written; returns ``out``."""
-        if self._elsewhere():
+        if B.current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self.run(q, K, V, out, lse, scale, stream)
-        qd, kd, vd = self._rows_of("q", q, self.rows, self.Hq), self._rows_of("K", K, self.keys, self.Hkv), self._rows_of("V", V, self.keys, self.Hkv)
         if out is None:
             out = self._empty(q.shape, q.dtype, stream, zero=self.rows.cu_seqlens is not None or self.rows.layer_lens is not None)
-        if lse is not None:
-            self._mine("lse", lse, torch.float32, (self.rows.n_layers, self.Hq, self.rows.total_len))
-        B.spindlekv_prompt_attend(self._c[0], self._c[1], self.Hq, self.Hkv, self.d, scale, qd, kd, vd, self._rows_of("out", out, self.rows, self.Hq), lse, self.ws,
-                                  self._raw(stream))
+        # arguments laid out as those of the last call have been looked over
+        layouts = (_layout(q), _layout(K), _layout(V), _layout(out), _layout(lse))
+        if layouts != self._seen[0]:
+            rows = (("q", q, self.rows, self.Hq), ("K", K, self.keys, self.Hkv), ("V", V, self.keys, self.Hkv), ("out", out, self.rows, self.Hq))
+            if lse is not None:
+                self._mine("lse", lse, torch.float32, (self.rows.n_layers, self.Hq, self.rows.total_len))
+            self._seen = (layouts, tuple(self._rows_of(*r) for r in rows))
+        qd, kd, vd, od = self._seen[1]
+        qd.ptr, kd.ptr, vd.ptr, od.ptr = q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr()
+        B.spindlekv_prompt_attend(self._c[0], self._c[1], self.Hq, self.Hkv, self.d, scale, qd, kd, vd, od, lse, self.ws, self._raw(stream))
         return out
 
     def status(self) -> int:
@@ -845,7 +861,7 @@ class SpindleKVPromptAttention(_OnDevice):
 
 class SpindleKVLogits(_OnDevice):
     """Penalties for repeated tokens, biases and masks of allowed tokens (``spindlekv_logits_adjust``) for ``n_rows`` rows of logits over ``vocab`` tokens, e.g. the
-    beams of ``SpindleKVBeamSelect``.  No scratch: calls of one object need no order among themselves."""
+    beams of ``SpindleKVBeamSelect``.  No scratch: calls of one object need no order on the device; host threads take an object each."""
 
     def __init__(self, n_rows: int, vocab: int, device="cuda"):
         if not (0 < n_rows < 65536 and 0 < vocab <= 1 << 30):
@@ -853,6 +869,7 @@ class SpindleKVLogits(_OnDevice):
         self.n_rows, self.vocab = n_rows, vocab
         self.device = _device_of(device)
         self._index = self.device.index
+        self._seen = (None, None)                          # layouts of the last call, and the rules that follow from them
 
     def _logits(self, name: str, t: torch.Tensor, dtype=None) -> torch.Tensor:
         if t.shape != (self.n_rows, self.vocab) or (self.vocab > 1 and t.stride(1) != 1) or t.device != self.device or (dtype is not None and t.dtype != dtype):
@@ -866,27 +883,47 @@ class SpindleKVLogits(_OnDevice):
         """``history`` ``[n_rows, n]`` int32 (any row stride) with ``history_lens`` tokens each, of which the first ``n_prompt`` are the prompt's; ``repetition``,
         ``presence``, ``frequency`` fp32 ``[n_rows]``; ``bias_token`` int32 and ``bias_value`` fp32 ``[n_rows, n]``; ``allowed`` int32 or uint32 ``[n_rows or 1,
         ceil(vocab / 32)]``, a bit per token, the lowest first.  Returns ``out`` (``logits`` itself, in place, by default)."""
-        if self._elsewhere():
+        if B.current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self.adjust(logits, out, history, history_lens, n_prompt, repetition, presence, frequency, bias_token, bias_value, allowed, stream)
-        n = self.n_rows
+        if out is None:
+            out = logits
+        # arguments laid out as those of the last call have been looked over
+        layouts = (_layout(logits), _layout(out), _layout(history), _layout(history_lens), _layout(n_prompt), _layout(repetition), _layout(presence), _layout(frequency),
+                   _layout(bias_token), _layout(bias_value), _layout(allowed))
+        if layouts != self._seen[0]:
+            self._seen = (layouts, self._look_over(logits, out, history, history_lens, n_prompt, repetition, presence, frequency, bias_token, bias_value, allowed))
+        r = self._seen[1]
+        if r.max_history:
+            r.history = history.data_ptr()
+            r.history_lens = None if history_lens is None else history_lens.data_ptr()
+            r.n_prompt = None if n_prompt is None else n_prompt.data_ptr()
+            r.repetition = None if repetition is None else repetition.data_ptr()
+            r.presence = None if presence is None else presence.data_ptr()
+            r.frequency = None if frequency is None else frequency.data_ptr()
+        if r.n_bias:
+            r.bias_token, r.bias_value = bias_token.data_ptr(), bias_value.data_ptr()
+        if allowed is not None:
+            r.allowed = allowed.data_ptr()
+        B.spindlekv_logits_adjust(logits, out, r, self._raw(stream))
+        return out
+
+    def _look_over(self, logits, out, history, history_lens, n_prompt, repetition, presence, frequency, bias_token, bias_value, allowed) -> "B._LogitRules":
+        """Checks of ``adjust``; the rules without their addresses."""
+        r, n = B._LogitRules(), self.n_rows
         self._logits("logits", logits)
-        out = logits if out is None else self._logits("out", out, logits.dtype)
-        r = B._LogitRules()
+        self._logits("out", out, logits.dtype)
+        vectors = (("history_lens", history_lens, torch.int32), ("n_prompt", n_prompt, torch.int32), ("repetition", repetition, torch.float32),
+                   ("presence", presence, torch.float32), ("frequency", frequency, torch.float32))
+        for name, t, dtype in vectors:
+            if t is not None:
+                if history is None:
+                    raise ValueError(f"{name} without a history")
+                self._mine(name, t, dtype, (n,))
         if history is not None:
             if history.dim() != 2 or history.shape[0] != n or (history.shape[1] > 1 and history.stride(1) != 1) or history.dtype != torch.int32 or history.device != self.device:
                 raise ValueError(f"history: [{n}, tokens] int32 on {self.device} expected, rows contiguous, got {list(history.shape)} {history.dtype} on {history.device}")
-            if history.shape[1]:
-                r.history, r.history_stride, r.max_history = history.data_ptr(), history.stride(0), history.shape[1]
-        for name, t, dtype in (("history_lens", history_lens, torch.int32), ("n_prompt", n_prompt, torch.int32), ("repetition", repetition, torch.float32),
-                               ("presence", presence, torch.float32), ("frequency", frequency, torch.float32)):
-            if t is None:
-                continue
-            if history is None:
-                raise ValueError(f"{name} without a history")
-            self._mine(name, t, dtype, (n,))
-            if r.history:
-                setattr(r, name, t.data_ptr())
+            r.history_stride, r.max_history = history.stride(0), history.shape[1]
         if (bias_token is None) != (bias_value is None):
             raise ValueError("bias_token and bias_value belong together")
         if bias_token is not None:
@@ -894,16 +931,14 @@ class SpindleKVLogits(_OnDevice):
                 raise ValueError(f"bias_token: [{n}, biases] expected, got {list(bias_token.shape)}")
             self._mine("bias_token", bias_token, torch.int32)
             self._mine("bias_value", bias_value, torch.float32, bias_token.shape)
-            if bias_token.shape[1]:
-                r.n_bias, r.bias_token, r.bias_value = bias_token.shape[1], bias_token.data_ptr(), bias_value.data_ptr()
+            r.n_bias = bias_token.shape[1]
         if allowed is not None:
             words = (self.vocab + 31) // 32
             if allowed.dtype not in (torch.int32, torch.uint32) or allowed.dim() != 2 or allowed.shape[0] not in (1, n) or allowed.shape[1] != words:
                 raise ValueError(f"allowed: [{n} or 1, {words}] int32 or uint32 expected, got {list(allowed.shape)} {allowed.dtype}")
             self._mine("allowed", allowed)
-            r.allowed, r.allowed_stride = allowed.data_ptr(), words if allowed.shape[0] == n else 0
-        B.spindlekv_logits_adjust(logits, out, r, self._raw(stream))
-        return out
+            r.allowed_stride = words if allowed.shape[0] == n else 0
+        return r
 
 
 class SpindleKVBeamSelect(_OnDevice):
