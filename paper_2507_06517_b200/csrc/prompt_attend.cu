@@ -168,7 +168,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
 #pragma unroll
           for (int c = 0; c < 128; c += 2) top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
           const float high = max3(max3(top[0], top[1], top[2]), top[3], top[3]) * p.scale;
-          if (!(high < CUDART_INF_F)) l = CUDART_NAN_F;      // (and so it stays)
           if (j == 0) {
             m = high;
           } else if (__any_sync(0xffffffffu, high > m + kPromptLazy)) {

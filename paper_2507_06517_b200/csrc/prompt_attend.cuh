@@ -216,10 +216,10 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
-// The largest of three; NaN if one of them is
+// The largest of three (a NaN only if all are: the weights show it)
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 // NP x 16 bytes of a warp's 32 rows, a row in each lane, to memory: through shared memory, so that a store covers whole pieces of few rows.
