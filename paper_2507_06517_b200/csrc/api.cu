@@ -407,6 +407,8 @@ spindlekv_status spindlekv_paged_append_rotated(const spindlekv_page_pool* pool,
   if (idx && (K_out.ptr || n_q_heads)) return SPINDLEKV_INVALID_ARG;      // a list may name a row for some heads only
   if (n_q_heads < 0 || (K_out.ptr && !rows_out_ok(K, K_out)) || (n_q_heads && (!tensor_ok(Q) || !rows_out_ok(Q, Q_out)))) return SPINDLEKV_INVALID_ARG;
   if (K.ptr == V.ptr && K_out.ptr == K.ptr) return SPINDLEKV_INVALID_ARG;
+  if (K_out.ptr && !rows_apart(K_out, table->n_layers, table->n_seqs, pool->n_kv_heads, n_rows)) return SPINDLEKV_INVALID_ARG;
+  if (n_q_heads && !rows_apart(Q_out, table->n_layers, table->n_seqs, n_q_heads, n_rows)) return SPINDLEKV_INVALID_ARG;
   if (K.dtype != V.dtype || (K_out.ptr && K_out.dtype != K.dtype) || (n_q_heads && (Q.dtype != K.dtype || Q_out.dtype != K.dtype))) return SPINDLEKV_UNSUPPORTED;
   if (n_q_heads > 65536) return SPINDLEKV_UNSUPPORTED;
   return paged_append_rotated_impl(*pool, *table, start, max_new, K, V, n_rows, idx, idx_len, idx_seq, rope_table, table_positions, first_pos, K_out, n_q_heads, Q, Q_out,
@@ -516,6 +518,8 @@ spindlekv_status spindlekv_prompt_attend(const spindlekv_batch* keys, const spin
   if (!(scale >= 0.f && scale < INFINITY) || reinterpret_cast<uintptr_t>(lse) % 4) return SPINDLEKV_INVALID_ARG;
   if (out.ptr == q.ptr || out.ptr == k.ptr || out.ptr == v.ptr) return SPINDLEKV_INVALID_ARG;
   if (k.dtype != q.dtype || v.dtype != q.dtype || out.dtype != q.dtype) return SPINDLEKV_UNSUPPORTED;
+  if (!rows_apart(q, *rows, n_q_heads) || !rows_apart(k, *keys, n_kv_heads) || !rows_apart(v, *keys, n_kv_heads)) return SPINDLEKV_UNSUPPORTED;
+  if (!rows_apart(out, *rows, n_q_heads)) return SPINDLEKV_INVALID_ARG;
   return prompt_attend_impl(*keys, *rows, n_q_heads, n_kv_heads, head_dim, scale, q, k, v, out, lse, ws, ws_bytes, (cudaStream_t)stream);
 }
 

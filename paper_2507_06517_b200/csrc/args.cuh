@@ -16,6 +16,14 @@ inline bool tensor_ok(const spindlekv_tensor& t) {
   return true;
 }
 
+// no two rows at the same place (a stride of 0, as of an expanded tensor)
+inline bool rows_apart(const spindlekv_tensor& t, int64_t layers, int64_t seqs, int64_t heads, int64_t rows) {
+  return (layers < 2 || t.stride_layer > 0) && (seqs < 2 || t.stride_seq > 0) && (heads < 2 || t.stride_head > 0) && (rows < 2 || t.stride_tok > 0);
+}
+inline bool rows_apart(const spindlekv_tensor& t, const spindlekv_batch& b, int64_t heads) {
+  return rows_apart(t, b.n_layers, b.cu_seqlens ? 1 : b.n_seqs, heads, b.cu_seqlens ? b.total_len : b.max_len);
+}
+
 inline bool cfg_ok(const spindlekv_config* c) {
   if (!c) return false;
   if (c->n_layers <= 0 || c->n_q_heads <= 0 || c->n_kv_heads <= 0 || c->window <= 0) return false;

@@ -148,3 +148,15 @@ def test_refusals_of_the_class():
                dict(history=torch.zeros((3, 4), dtype=torch.int32, device="cuda"), history_lens=torch.zeros(2, dtype=torch.int32, device="cuda"))):
         with pytest.raises((ValueError, TypeError)):
             a.adjust(**{"logits": x, **kw})
+
+
+def test_offsets_beyond_32_bits():
+    gap = 1717986918                                       # two rows are beyond 2^31 elements
+    room = torch.empty(2 * gap + 5000, dtype=BF, device="cuda")
+    x = torch.as_strided(room, (3, 5000), (gap, 1))
+    x.copy_(logits(3, 5000, BF, 21))
+    r = rules(3, 5000, 300, 5, 22)
+    first = check(x.contiguous(), **r)
+    from paper_2507_06517_b200.pipeline import SpindleKVLogits
+    SpindleKVLogits(3, 5000).adjust(x, **r)
+    assert torch.equal(x, first)

@@ -220,3 +220,56 @@ def test_a_wait_that_gives_up_shows_in_the_status_and_leaves_nothing_behind(lens
         graph.replay()
         graph.replay()
         assert a.status() == B.OK
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_offsets_beyond_32_bits(dtype):
+    # layers 1.2 * 2^31 elements apart
+    keys, rows, q, k, v = make([200, 90], None, 4, 2, 64, dtype, False, n_layers=2, seed=31)
+    far, gap = [], 2576980480
+    room = torch.empty(gap + 3 * q[0].numel(), dtype=dtype, device="cuda")
+    at = 0
+    for t in (q, k, v):
+        f = torch.as_strided(room, t.shape, (gap, *t.stride()[1:]), at)
+        f.copy_(t)
+        far.append(f)
+        at += t[0].numel()
+    first = check(keys, rows, q, k, v)
+    assert all(torch.equal(a, b) for a, b in zip(first, attend(keys, rows, *far)))
+
+
+def test_objects_side_by_side_on_two_streams():
+    from paper_2507_06517_b200.pipeline import SpindleKVPromptAttention
+    sets = [make([700, 300], None, 8, 2, 128, dt, True, seed=s) for s, dt in ((41, BF), (42, F32))] + [make([3000], [4], 8, 2, 128, BF, False, seed=43)]
+    want = [attend(*s)[0] for s in sets]
+    objects = [SpindleKVPromptAttention(s[0], 8, 2, 128, s[2].dtype, rows=s[1]) for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    outs = [torch.full_like(s[2], 7.0) for s in sets]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for a, s, st, o in zip(objects, sets, streams, outs):
+            a.run(*s[2:], out=o, stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(outs, want)) and all(a.status() == B.OK for a in objects)
+
+
+def test_refusals_of_the_class_and_what_it_makes_itself():
+    from paper_2507_06517_b200.pipeline import SpindleKVPromptAttention
+    keys, rows, q, k, v = make([40, 17], None, 4, 2, 64, BF, False, seed=51)
+    with pytest.raises(TypeError):
+        SpindleKVPromptAttention(keys, 4, 2, 64, torch.float16)
+    with pytest.raises(ValueError):
+        SpindleKVPromptAttention(keys, 4, 3, 64, BF)
+    with pytest.raises(ValueError):
+        SpindleKVPromptAttention(B.Batch(1, 2, 40, 80, None, keys.layer_lens.cpu()), 4, 2, 64, BF)
+    a = SpindleKVPromptAttention(keys, 4, 2, 64, BF)
+    for kw in (dict(q=q.float()), dict(q=q[:, :, :3]), dict(K=k[:, :, :, :39]), dict(V=v.cpu()), dict(K=k.transpose(3, 4).contiguous().transpose(3, 4)),
+               dict(out=q[:, :1]), dict(lse=torch.zeros((1, 4, 79), device="cuda")), dict(lse=torch.zeros((1, 4, 80), device="cuda", dtype=BF))):
+        with pytest.raises(ValueError):
+            a.run(**{"q": q, "K": k, "V": v, **kw})
+    with pytest.raises(B.SpindleKVError):
+        a.run(q, k, v, out=q)
+    with pytest.raises(B.SpindleKVError):
+        a.run(q, k, v, scale=-1.0)
+    out = a.run(q, k, v)
+    assert (out[0, 1, :, 17:] == 0).all() and torch.equal(out[0, 1, :, :17], attend(keys, rows, q, k, v)[0][0, 1, :, :17])

@@ -181,3 +181,56 @@ def test_a_step_of_decoding_with_prompt_attention_logits_and_selection(dtype):
     again = [select.score, select.parent, select.token, got, qr, z]
     assert all(torch.equal(a, b) for a, b in zip(first, again))
     assert equal(qr, turned(q1, np.full((1, 3, 1, 1), 70), rope))
+
+
+def test_offsets_beyond_32_bits():
+    c, other = (make(2, 2, None, 2, 64, 20, 4, 32, "int8") for _ in range(2))
+    rope, lens, gap = table(100, 64), [[40, 33], [50, 1]], 2576980480
+    K, V, Q = (rows((2, 2, h, 50, 64), "bf16", i) for i, h in enumerate((2, 2, 4)))
+    room = torch.empty(gap + 5 * Q[0].numel(), dtype=torch.bfloat16, device="cuda")
+    far = [torch.as_strided(room, t.shape, (gap, *t.stride()[1:]), i * Q[0].numel()) for i, t in enumerate((K, V, K, Q, Q))]
+    for f, t in zip((far[0], far[1], far[3]), (K, V, Q)):
+        f.copy_(t)
+    outs = [torch.zeros_like(K), torch.zeros_like(Q)]
+    far[2].zero_()
+    far[4].zero_()
+    for x in (c, other):
+        x.resize(lens_t(lens))
+    c.append_rotated(K, V, rope, K_out=outs[0], Q=Q, Q_out=outs[1])
+    other.append_rotated(far[0], far[1], rope, K_out=far[2], Q=far[3], Q_out=far[4])
+    assert torch.equal(far[2], outs[0]) and torch.equal(far[4], outs[1])
+    same_state(other, ref_of(c))
+
+
+def test_what_eviction_kept_is_rotated_on_the_way_into_the_cache():
+    import gpu_util as U
+    from paper_2507_06517_b200 import synth
+    from paper_2507_06517_b200.pipeline import SpindleKVPagedCache, SpindleKVPass
+    wl = synth.Workload("rotated", 3, 1, 8, 2, 128, "bf16", 32, (600, 600), 40, (0.05, 0.3), 4, "recency", budget_tokens=200.0, seed=13)
+    host = U.generate(wl)
+    p = SpindleKVPass(U.make_config(wl), wl.seq_lens, U.torch_dtype(wl))
+    K, V = (U.stack_layers(wl, host, range(3), w) for w in "KV")
+    p.evict(K[1:], V[1:], U.stack_layers(wl, host, [1, 2], "Q"))
+    rope = table(600, 128)
+    one, two = (SpindleKVPagedCache(2, 2, 8, 2, 128, 60, 12, 32, "int8") for _ in range(2))
+    p.store_paged(K, V, one, rope_table=rope)
+    whole = turned(K, np.arange(600), rope).cuda()
+    p.store_paged(whole, V, two)
+    assert one.status() == 0
+    same_state(one, ref_of(two))
+
+
+def test_refusals_of_the_class():
+    c = make(1, 3, None, 2, 64, 20, 4, 32, "int8")
+    rope = table(50, 64)
+    K, V, Q = (rows((1, 3, h, 4, 64), "bf16", i) for i, h in enumerate((2, 2, 4)))
+    for kw in (dict(K=K[:, :2]), dict(V=V[:, :, :, :3]), dict(K=K.float().cpu()), dict(rope_table=rope[..., 0]), dict(rope_table=rope.double()), dict(rope_table=table(50, 128)),
+               dict(start=lens_t([[0, 0]])), dict(first_pos=torch.zeros((1, 3), device="cuda")), dict(Q=Q[:, :, :, :3]), dict(Q_out=Q), dict(K_out=K[:, :, :1]),
+               dict(idx=torch.zeros((1, 3, 12), dtype=torch.int32, device="cuda"))):
+        with pytest.raises((ValueError, TypeError)):
+            c.append_rotated(**{"K": K, "V": V, "rope_table": rope, **kw})
+    with pytest.raises(B.SpindleKVError):
+        c.append_rotated(K, V, rope, idx=torch.zeros((1, 2, 12), dtype=torch.int32, device="cuda"), K_out=torch.empty_like(K))
+    c.resize(lens_t([[4, 4, 4]]))
+    made = c.append_rotated(K, V, rope, Q=Q)
+    assert equal(made, turned(Q, np.arange(4), rope))
