@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == kAskRole) {
-      const PromptList list(p);
+      PromptList list(p);
       for (int pass = 0; pass == 0 || (pass == 1 && again()); ++pass) {
       for (int k = 0; ok; ++k) {
         while (pass && k < kPromptMaxItems && !(redo[k >> 5] >> (k & 31) & 1u)) ++k;

@@ -51,10 +51,14 @@ struct PromptItem {
 };
 
 // Items in falling order of their block's number, which is nearly that of their work: all sequences' last positions first.  A warp finds item
-// `i` by the number of blocks with a number of b or more, which falls with b.
+// `i` by the number of blocks with a number of b or more, which falls with b.  What the item before it showed (its number's share of the items, and the
+// sequences ahead of it) is kept, so that a call with many sequences does not count them for every item (32 layers x 32 sequences of 50 to 200 tokens,
+// 32 / 8 heads: 0.82 ms in place of 2.9).
 struct PromptList {
   Span rows, keys;            // of (layer, seq) lane, where there are up to 32
   int n_ls, all;
+  int blk, from, to;          // items' numbers [from, to) are those of block number blk
+  int group, before;          // the 32 (layer, seq) that held the last item, and how many of these blocks lie ahead of them
   __device__ __forceinline__ static Span span_at(const Batch& b, int ls) {
     const int layer = ls / b.n_seqs;
     return span_of(b, layer, ls - layer * b.n_seqs);
@@ -65,6 +69,7 @@ struct PromptList {
   }
   __device__ __forceinline__ int count(const PromptParams& p, int b) const {            // blocks with the number b or a larger one
     int n = 0;
+#pragma unroll 4
     for (int ls = threadIdx.x & 31; ls < (n_ls + 31) / 32 * 32; ls += 32) n += max(blocks_of(p, ls) - b, 0);
     return __reduce_add_sync(0xffffffffu, n);
   }
@@ -77,9 +82,10 @@ struct PromptList {
       keys = span_at(p.keys, lane);
     }
     all = count(p, 0);
+    blk = from = to = group = before = 0;
   }
   // The block's k-th item, or one with ls = -1; every other round goes backwards, so that no block gets the longest of all rounds
-  __device__ __forceinline__ PromptItem item(const PromptParams& p, int k) const {
+  __device__ __forceinline__ PromptItem item(const PromptParams& p, int k) {
     const int lane = threadIdx.x & 31;
     PromptItem it = {};
     it.ls = -1;
@@ -87,25 +93,34 @@ struct PromptList {
     const int per = p.heads * p.splits;
     if (i >= (long long)all * per) return it;
     const int q = i <= 0x7FFFFFFF ? (int)i / per : (int)(i / per), inner = (int)(i - (long long)q * per);
-    int lo = 0, hi = p.max_blocks - 1, above = 0;          // the largest b with more than q blocks of that number or more; `above`: those of b + 1 or more
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1, c = count(p, mid);
-      if (c > q) lo = mid;
-      else { hi = mid - 1; above = c; }
+    if (q < from || q >= to) {
+      int lo = 0, hi = p.max_blocks - 1;                   // the largest b with more than q blocks of that number or more
+      from = 0;
+      to = all;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1, c = count(p, mid);
+        if (c > q) { lo = mid; to = c; }
+        else { hi = mid - 1; from = c; }
+      }
+      blk = lo;
+      group = before = 0;
     }
-    int rank = q - above, found = -1;
-    for (int first = 0; first < n_ls && found < 0; first += 32) {
-      uint32_t has = __ballot_sync(0xffffffffu, blocks_of(p, first + lane) > lo);
+    if (q - from < before) group = before = 0;
+    int rank = q - from - before, found = -1;
+    for (; group < n_ls; group += 32) {
+      uint32_t has = __ballot_sync(0xffffffffu, blocks_of(p, group + lane) > blk);
       if (rank >= __popc(has)) {
         rank -= __popc(has);
+        before += __popc(has);
         continue;
       }
       while (rank-- > 0) has &= has - 1;
-      found = first + __ffs(has) - 1;
+      found = group + __ffs(has) - 1;
+      break;
     }
     if (found < 0) return it;
     it.ls = found;
-    it.blk = lo;
+    it.blk = blk;
     it.head = inner / p.splits;
     it.split = inner - it.head * p.splits;
     if (n_ls <= 32) {

@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
   bool ok = true;
   int n_kv = 0, n_q = 0;                  // tiles of keys (and of values) and row tiles so far
   if (warp == kExactAsk) {
-    const PromptList list(p);
+    PromptList list(p);
     for (int pass = 0; pass == 0 || (pass == 1 && again()); ++pass) {
       for (int k = 0; ok; ++k) {
         while (pass && k < kPromptMaxItems && !(redo[k >> 5] >> (k & 31) & 1u)) ++k;

@@ -105,6 +105,15 @@ def test_many_short_sequences(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("packed,layers", [(True, 1), (False, 2)])
+def test_many_sequences_of_several_blocks(packed, layers, dtype):
+    # more sequences than a warp has lanes, whose blocks are found from one item to the next
+    gen = torch.Generator().manual_seed(2)
+    lens = torch.randint(0, 500, (70,), generator=gen).tolist()
+    check(*make(lens, None, 16, 2, 64, dtype, packed, layers, seed=21))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_scores_of_every_size(dtype):
     # references that move late, and by much; scores all alike; a scale of one's own
     keys, rows, q, k, v = make([900], None, 4, 2, 128, dtype, seed=9, size=6.0)
