@@ -12,7 +12,7 @@ LIB = os.path.join(PKG, "libspindlekv.so")
 
 SOURCES = ["api.cu", "evict.cu", "codebook.cu", "compact.cu", "sim_tc.cu", "win_tc.cu", "extend.cu", "noalloc.cu", "decode.cu",
            "pages.cu", "paged_append.cu", "paged_append_rotated.cu", "paged_attend.cu", "paged_attend_tiles.cu", "beam.cu",
-           "prompt_attend.cu", "prompt_attend_f32.cu", "logits.cu"]
+           "prompt_attend.cu", "prompt_attend_f32.cu", "prompt_rows.cu", "logits.cu"]
 HEADERS = ["args.cuh", "common.cuh", "paged.cuh", "paged_attend.cuh", "paged_rounding.cuh", "prompt_attend.cuh", "simt_tile.cuh", "sm100_ptx.cuh"]
 
 

@@ -455,10 +455,11 @@ static int prompt_splits(const spindlekv_batch& keys, const spindlekv_batch& row
 static int prompt_per_item(int hn, int dtype) { return (dtype == SPINDLEKV_BF16 ? 2 : 1) * (kPromptRows / hn); }
 
 size_t prompt_workspace_bytes(const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int n_kv_heads, int head_dim, int dtype) {
-  const int splits = prompt_splits(keys, rows, n_kv_heads, prompt_per_item(n_q_heads / n_kv_heads, dtype));
+  const int few = prompt_few_rows(keys, rows, n_kv_heads, n_q_heads / n_kv_heads, head_dim, dtype);
+  const int splits = few ? few : prompt_splits(keys, rows, n_kv_heads, prompt_per_item(n_q_heads / n_kv_heads, dtype));
   const size_t numbers = (size_t)rows.n_layers * rows.total_len * n_q_heads;
   return kHeaderBytes + (splits > 1 ? align_up(splits * numbers * (head_dim * sizeof(float) + sizeof(float2)), 256) : 0) +
-         (dtype == SPINDLEKV_F32 ? prompt_pieces_bytes(keys, rows, n_q_heads, n_kv_heads, head_dim) : 0);
+         (dtype == SPINDLEKV_F32 && !few ? prompt_pieces_bytes(keys, rows, n_q_heads, n_kv_heads, head_dim) : 0);
 }
 
 template <int D>
@@ -491,7 +492,8 @@ spindlekv_status prompt_attend_impl(const spindlekv_batch& keys, const spindlekv
   p.pt = kPromptRows / p.hn;
   p.per_item = prompt_per_item(p.hn, q.dtype);
   p.max_blocks = ceil_div(rows.max_len, p.per_item);
-  p.splits = prompt_splits(keys, rows, n_kv_heads, p.per_item);
+  const int few = prompt_few_rows(keys, rows, n_kv_heads, p.hn, head_dim, q.dtype);
+  p.splits = few ? few : prompt_splits(keys, rows, n_kv_heads, p.per_item);
   p.scale = (scale == 0.f ? 1.f / sqrtf((float)head_dim) : scale) * 1.44269504088896340736f;
   p.lse = lse;
   const size_t numbers = (size_t)rows.n_layers * rows.total_len * n_q_heads;
@@ -501,6 +503,7 @@ spindlekv_status prompt_attend_impl(const spindlekv_batch& keys, const spindlekv
   const Tuning tune = current_tuning();
   p.wait_cycles = tune.mbar_wait_cycles;
   p.withhold = tune.paged_withhold;
+  if (few) return prompt_attend_few(p, rows.max_len, head_dim, st);
   const int64_t items = prompt_items(rows, n_kv_heads, p.per_item) * p.splits;
   // one block per SM; more only where a block's list of items would not do
   const int64_t blocks = std::min(items, std::max<int64_t>(kPromptSms, (items + kPromptMaxItems - 1) / kPromptMaxItems));

@@ -396,4 +396,8 @@ size_t prompt_pieces_bytes(const spindlekv_batch& keys, const spindlekv_batch& r
 spindlekv_status prompt_attend_f32(const PromptParams& p, const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int head_dim, void* pieces,
                                    int64_t blocks, cudaStream_t st);
 
+// few rows: parts of the keys, 0 where a call does not go that way; and the call
+int prompt_few_rows(const spindlekv_batch& keys, const spindlekv_batch& rows, int heads, int hn, int head_dim, int dtype);
+spindlekv_status prompt_attend_few(const PromptParams& p, int max_rows, int head_dim, cudaStream_t st);
+
 }  // namespace skv

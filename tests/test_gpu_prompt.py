@@ -88,6 +88,19 @@ def test_last_rows_of_long_prompts(lens, rows, packed, dtype):
     check(*make(lens, rows, 8, 2, 128, dtype, packed, seed=5))
 
 
+@pytest.mark.parametrize("lens,rows,hq,h,d", [
+    ([4000], [1], 1, 1, 64), ([4000], [1], 7, 1, 128), ([2500, 3, 0, 9000], [5, 5, 5, 5], 8, 2, 64), ([2500, 3, 0, 9000], [5, 2, 0, 1], 4, 2, 128),
+    ([7], [24], 2, 2, 128), ([5000], [24], 1, 1, 128), ([5000], [25], 1, 1, 128), ([6, 8, 9, 31], [3, 3, 3, 3], 8, 1, 64)])
+@pytest.mark.parametrize("packed", [True, False])
+def test_few_columns_of_a_head(lens, rows, hq, h, d, packed):
+    # fp32 with few rows and query heads: one pass over the keys, up to 24 columns
+    keys, rws, q, k, v = make(lens, rows, hq, h, d, F32, packed, 2, seed=41)
+    check(keys, rws, q, k, v)
+    if packed and min(lens) > 0:                           # the rows of a head behind one another
+        move = lambda t: t.transpose(1, 2).contiguous().transpose(1, 2)
+        check(keys, rws, q, move(k), move(v))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_rows_that_see_nothing(dtype):
     # more rows than keys: the first ones see none
