@@ -447,16 +447,20 @@ static int64_t prompt_items(const spindlekv_batch& rows, int heads, int per_item
   const int64_t blocks = rows.cu_seqlens ? (int64_t)rows.total_len / per_item + rows.n_seqs : (int64_t)rows.n_seqs * ((rows.max_len + per_item - 1) / per_item);
   return blocks * rows.n_layers * heads;
 }
-// Parts that the keys are cut into: as many as bring the items to one for each SM, of two tiles of keys at least
-static int prompt_splits(const spindlekv_batch& keys, const spindlekv_batch& rows, int heads, int per_item) {
+// Parts that the keys are cut into: as many as bring the items to one for each SM, of two tiles of keys at least, where that saves more than the parts' way
+// through memory and the kernel that joins them cost (128 keys take 1.4 us, in fp32 twice that; the join 3.5 us and its bytes; a whole prompt of 512, 32 / 8 heads, in two
+// parts 22 us, in one 15; one row of 2000 keys in seven parts 16 us, in three 18, in one 28)
+static int prompt_splits(const spindlekv_batch& keys, const spindlekv_batch& rows, int heads, int per_item, int row_bytes, int dtype) {
   const int64_t items = prompt_items(rows, heads, per_item);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(kPromptSms / items, keys.max_len / 256));
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kPromptSms / items, keys.max_len / 256));
+  const double saved = (dtype == SPINDLEKV_BF16 ? 1.4 : 2.8) * (keys.max_len / 128.) * (1. - 1. / most), bytes = 2. * most * rows.n_layers * rows.total_len * row_bytes;
+  return saved > 3.5 + bytes / 4e6 ? (int)most : 1;
 }
 static int prompt_per_item(int hn, int dtype) { return (dtype == SPINDLEKV_BF16 ? 2 : 1) * (kPromptRows / hn); }
 
 size_t prompt_workspace_bytes(const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int n_kv_heads, int head_dim, int dtype) {
   const int few = prompt_few_rows(keys, rows, n_kv_heads, n_q_heads / n_kv_heads, head_dim, dtype);
-  const int splits = few ? few : prompt_splits(keys, rows, n_kv_heads, prompt_per_item(n_q_heads / n_kv_heads, dtype));
+  const int splits = few ? few : prompt_splits(keys, rows, n_kv_heads, prompt_per_item(n_q_heads / n_kv_heads, dtype), n_q_heads * head_dim * 4, dtype);
   const size_t numbers = (size_t)rows.n_layers * rows.total_len * n_q_heads;
   return kHeaderBytes + (splits > 1 ? align_up(splits * numbers * (head_dim * sizeof(float) + sizeof(float2)), 256) : 0) +
          (dtype == SPINDLEKV_F32 && !few ? prompt_pieces_bytes(keys, rows, n_q_heads, n_kv_heads, head_dim) : 0);
@@ -493,7 +497,7 @@ spindlekv_status prompt_attend_impl(const spindlekv_batch& keys, const spindlekv
   p.per_item = prompt_per_item(p.hn, q.dtype);
   p.max_blocks = ceil_div(rows.max_len, p.per_item);
   const int few = prompt_few_rows(keys, rows, n_kv_heads, p.hn, head_dim, q.dtype);
-  p.splits = few ? few : prompt_splits(keys, rows, n_kv_heads, p.per_item);
+  p.splits = few ? few : prompt_splits(keys, rows, n_kv_heads, p.per_item, n_q_heads * head_dim * 4, q.dtype);
   p.scale = (scale == 0.f ? 1.f / sqrtf((float)head_dim) : scale) * 1.44269504088896340736f;
   p.lse = lse;
   const size_t numbers = (size_t)rows.n_layers * rows.total_len * n_q_heads;
