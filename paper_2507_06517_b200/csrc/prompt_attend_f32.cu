@@ -58,49 +58,54 @@ struct SplitSource {
   int heads, by_token;       // by_token: the heads of a token lie side by side
 };
 struct SplitParams { SplitSource t[3]; };
-constexpr int kSplitTokens = 16;
+// Memory bounds it (4 bytes in, 6 out for each element); a thread takes four times 8 elements, in the pieces' order, and asks for all of them at once
+constexpr int kSplitTurns = 4;
 
 template <int D>
 __global__ void __launch_bounds__(256) prompt_pieces_kernel(const __grid_constant__ SplitParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const SplitSource& t = p.t[blockIdx.y];
+  const SplitSource& t = p.t[blockIdx.z];
   const Batch& b = t.batch;
-  const int seqs = b.cu ? 1 : b.n_seqs, tokens = b.cu ? b.total_len : b.max_len, chunks = (tokens + kSplitTokens - 1) / kSplitTokens;
-  if (blockIdx.x >= (unsigned)chunks * seqs * b.n_layers) return;
-  const int ls = blockIdx.x / chunks, first = (blockIdx.x - ls * chunks) * kSplitTokens, layer = ls / seqs, seq = ls - layer * seqs;
+  const int seqs = b.cu ? 1 : b.n_seqs, tokens = b.cu ? b.total_len : b.max_len, ls = blockIdx.y;
+  const unsigned items = (unsigned)tokens * t.heads * (D / 8), first = blockIdx.x * (kSplitTurns * 256) + threadIdx.x;
+  if (ls >= seqs * b.n_layers) return;
+  const int layer = ls / seqs, seq = ls - layer * seqs;
   const int from = b.cu ? max(b.cu[0], 0) : 0, end = b.cu ? min(b.cu[b.n_seqs], b.total_len) : span_of(b, layer, seq).len;
-  const int64_t plane = (int64_t)b.n_layers * seqs * tokens * t.heads * D;
-  const int per_token = t.heads * (D / 8), n = min(kSplitTokens, tokens - first);
-  for (int i = threadIdx.x; i < n * per_token; i += 256) {
-    // neighbouring threads take neighbouring elements on both sides as far as the layouts go
-    int token, head;
-    const int d = i % (D / 8) * 8, rest = i / (D / 8);
-    if (t.by_token) { token = rest / t.heads; head = rest - token * t.heads; }
-    else { head = rest / n; token = rest - head * n; }
-    token += first;
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (token >= from && token < end) load8(reinterpret_cast<const float*>(t.from.ptr) + (int64_t)layer * t.from.sl + (b.cu ? 0 : (int64_t)seq * t.from.ss) +
-                                                (int64_t)head * t.from.sh + (int64_t)token * t.from.st + d, x);
+  const int64_t plane = (int64_t)b.n_layers * seqs * items * 8;
+  const float* src = reinterpret_cast<const float*>(t.from.ptr) + (int64_t)layer * t.from.sl + (b.cu ? 0 : (int64_t)seq * t.from.ss);
+  __nv_bfloat16* dst = t.to + (int64_t)ls * items * 8;
+  float x[kSplitTurns][8];
+#pragma unroll
+  for (int k = 0; k < kSplitTurns; ++k) {
+    const unsigned i = first + k * 256, row = i / (D / 8), major = row / (unsigned)(t.by_token ? t.heads : tokens), minor = row - major * (unsigned)(t.by_token ? t.heads : tokens);
+    const int token = t.by_token ? major : minor, head = t.by_token ? minor : major;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[k][u] = 0.f;
+    if (i < items && token >= from && token < end) load8(src + (int64_t)head * t.from.sh + (int64_t)token * t.from.st + i % (D / 8) * 8, x[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < kSplitTurns; ++k) {
+    const unsigned i = first + k * 256;
+    if (i >= items) return;
     uint32_t w[kPieces][4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int u = 0; u < 8; u += 2) {
       uint32_t y[2][kPieces];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const float z = x[2 * k + u];
-        pieces_of(z, y[u][0], y[u][1], y[u][2]);
+      for (int v = 0; v < 2; ++v) {
+        const float z = x[k][u + v];
+        pieces_of(z, y[v][0], y[v][1], y[v][2]);
         if (!(fabsf(z) < CUDART_INF_F)) {
-          y[u][0] = z != z ? 0x7FC00000u : __float_as_uint(z);
-          y[u][1] = y[u][2] = 0u;
+          y[v][0] = z != z ? 0x7FC00000u : __float_as_uint(z);
+          y[v][1] = y[v][2] = 0u;
         }
       }
 #pragma unroll
-      for (int c = 0; c < kPieces; ++c) w[c][k] = upper_halves(y[0][c], y[1][c]);
+      for (int c = 0; c < kPieces; ++c) w[c][u / 2] = upper_halves(y[0][c], y[1][c]);
     }
-    const int64_t at = ((int64_t)ls * tokens * t.heads + (t.by_token ? (int64_t)token * t.heads + head : (int64_t)head * tokens + token)) * D + d;
 #pragma unroll
-    for (int c = 0; c < kPieces; ++c) *reinterpret_cast<uint4*>(t.to + c * plane + at) = make_uint4(w[c][0], w[c][1], w[c][2], w[c][3]);
+    for (int c = 0; c < kPieces; ++c) *reinterpret_cast<uint4*>(dst + c * plane + (int64_t)i * 8) = make_uint4(w[c][0], w[c][1], w[c][2], w[c][3]);
   }
 }
 
@@ -520,12 +525,13 @@ static spindlekv_status launch_exact(const PromptParams& p, const spindlekv_batc
   sp.t[0] = {p.q, p.rows, to, n_q_heads, 1};
   sp.t[1] = {p.k, p.keys, to + nq, p.heads, 0};
   sp.t[2] = {p.v, p.keys, to + nq + nk, p.heads, 0};
-  int64_t grid = 0;
+  int64_t blocks_of = 0, units = 0;
   for (const SplitSource& t : sp.t) {
-    const int64_t seqs = t.batch.cu ? 1 : t.batch.n_seqs, tokens = t.batch.cu ? t.batch.total_len : t.batch.max_len;
-    grid = std::max(grid, (tokens + kSplitTokens - 1) / kSplitTokens * seqs * t.batch.n_layers);
+    const int64_t seqs = t.batch.cu ? 1 : t.batch.n_seqs, tokens = t.batch.cu ? t.batch.total_len : t.batch.max_len, items = tokens * t.heads * (D / 8);
+    if (items > 0xFFFF0000ll) return SPINDLEKV_UNSUPPORTED;      // more pieces than there is memory
+    blocks_of = std::max(blocks_of, (items + kSplitTurns * 256 - 1) / (kSplitTurns * 256));
+    units = std::max(units, seqs * t.batch.n_layers);
   }
-  if (grid > 0x7FFFFFFF) return SPINDLEKV_UNSUPPORTED;
   // the planes as tensors: three times as many layers
   spindlekv_batch kb = keys, rb = rows;
   kb.n_layers *= kPieces;
@@ -541,7 +547,7 @@ static spindlekv_status launch_exact(const PromptParams& p, const spindlekv_batc
     return SPINDLEKV_UNSUPPORTED;
   {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid, 3);
+    cfg.gridDim = dim3((unsigned)blocks_of, (unsigned)units, 3);
     cfg.blockDim = dim3(256);
     cfg.stream = st;
     cudaLaunchAttribute attr;
