@@ -507,7 +507,7 @@ spindlekv_status prompt_attend_impl(const spindlekv_batch& keys, const spindlekv
   const Tuning tune = current_tuning();
   p.wait_cycles = tune.mbar_wait_cycles;
   p.withhold = tune.paged_withhold;
-  if (few) return prompt_attend_few(p, rows.max_len, head_dim, st);
+  if (few) return prompt_attend_few(p, keys, rows.max_len, head_dim, k, v, st);
   const int64_t items = prompt_items(rows, n_kv_heads, p.per_item) * p.splits;
   // one block per SM; more only where a block's list of items would not do
   const int64_t blocks = std::min(items, std::max<int64_t>(kPromptSms, (items + kPromptMaxItems - 1) / kPromptMaxItems));

@@ -4,6 +4,8 @@
 #include <math.h>
 #include <math_constants.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 #include "sm100_ptx.cuh"
 
@@ -327,6 +329,16 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const __grid_constant_
   const Span r = span_of(p.rows, layer, seq);
   pos = p.rows.cu ? col - r.base : col - seq * p.rows.max_len;
   if (pos < 0 || pos >= r.len) return;
+  // Eight parts at a time, asked for ahead of what weighs them (a part without keys has the sum 0 and may hold anything)
+  constexpr int kAhead = 8;
+  using Piece = std::conditional_t<E == 4, float4, float2>;
+  const float* mine = p.part + number * D + lane * E;
+  Piece x[kAhead];
+  auto ask = [&](int z) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) x[i] = *reinterpret_cast<const Piece*>(mine + (int64_t)min(z + i, p.splits - 1) * rows * D);
+  };
+  ask(0);
   float top = -CUDART_INF_F, den = 0.f, num[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) num[e] = 0.f;
@@ -344,18 +356,19 @@ __global__ void __launch_bounds__(256) prompt_join_kernel(const __grid_constant_
     den = fmaf(den, was, d);
 #pragma unroll
     for (int e = 0; e < E; ++e) num[e] *= was;
-    const int n = min(32, p.splits - z0);
-#pragma unroll 8
-    for (int z = 0; z < n; ++z) {
-      const float w = __shfl_sync(0xffffffffu, f, z);
-      if (__shfl_sync(0xffffffffu, st.y, z) == 0.f) continue;      // no key: nothing was written
-      const float* part = p.part + ((int64_t)(z0 + z) * rows + number) * D + lane * E;
+    for (int z = z0; z < min(z0 + 32, p.splits); z += kAhead) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) num[e] = fmaf(w, part[e], num[e]);
+      for (int i = 0; i < kAhead; ++i) {
+        const float w = __shfl_sync(0xffffffffu, f, z + i - z0);
+        const float* y = reinterpret_cast<const float*>(&x[i]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) num[e] = w == 0.f ? num[e] : fmaf(w, y[e], num[e]);
+      }
+      ask(z + kAhead);
     }
   }
-  T* dst = reinterpret_cast<T*>(const_cast<void*>(p.out.ptr)) + row_offset(p.out, p.rows, layer, seq, r.base, head, pos) + lane * E;
   const float inv = den == 0.f ? 0.f : 1.f / den;
+  T* dst = reinterpret_cast<T*>(const_cast<void*>(p.out.ptr)) + row_offset(p.out, p.rows, layer, seq, r.base, head, pos) + lane * E;
 #pragma unroll
   for (int e = 0; e < E; ++e) dst[e] = T(num[e] * inv);
   if (lane == 0) put_lse(p, layer, col, head, top, den);
@@ -398,6 +411,7 @@ spindlekv_status prompt_attend_f32(const PromptParams& p, const spindlekv_batch&
 
 // few rows: parts of the keys, 0 where a call does not go that way; and the call
 int prompt_few_rows(const spindlekv_batch& keys, const spindlekv_batch& rows, int heads, int hn, int head_dim, int dtype);
-spindlekv_status prompt_attend_few(const PromptParams& p, int max_rows, int head_dim, cudaStream_t st);
+spindlekv_status prompt_attend_few(const PromptParams& p, const spindlekv_batch& keys, int max_rows, int head_dim, const spindlekv_tensor& k, const spindlekv_tensor& v,
+                                   cudaStream_t st);
 
 }  // namespace skv

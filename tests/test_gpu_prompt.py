@@ -101,6 +101,33 @@ def test_few_columns_of_a_head(lens, rows, hq, h, d, packed):
         check(keys, rws, q, move(k), move(v))
 
 
+@pytest.mark.parametrize("lens,rows,hq,h,d", [
+    ([4000], [1], 1, 1, 64), ([4000], [1], 7, 1, 128), ([2500, 3, 0, 9000], [5, 5, 5, 5], 8, 2, 64), ([2500, 3, 0, 9000], [5, 2, 0, 1], 4, 2, 128),
+    ([7], [24], 2, 2, 128), ([5000], [3], 5, 1, 128), ([5000], [16], 1, 1, 64), ([5000], [17], 2, 2, 128), ([6, 8, 9, 31], [3, 3, 3, 3], 8, 1, 64), ([15, 16, 17, 33], [1, 1, 1, 1], 8, 2, 128)])
+@pytest.mark.parametrize("packed", [True, False])
+def test_few_columns_of_a_head_in_bf16(lens, rows, hq, h, d, packed):
+    keys, rws, q, k, v = make(lens, rows, hq, h, d, BF, packed, 2, seed=43)
+    check(keys, rws, q, k, v)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,rows,hq", [(3000, 5, 2), (1000, 8, 1), (37, 3, 4), (16, 2, 6)])
+def test_values_that_some_of_few_columns_do_not_see(n, rows, hq, dtype):
+    # the last row alone sees the last value: the others' results are those without it
+    keys, rws, q, k, v = make([n, n], [rows, rows], hq, 1, 128, dtype, True, seed=44)
+    want, want_lse = attend(keys, rws, q, k, v)
+    for odd in (math.nan, math.inf):
+        w = v.clone()
+        w[0, n - 1], w[0, 2 * n - 1] = odd, odd
+        out, lse = attend(keys, rws, q, k, w)
+        last = torch.zeros(2 * rows, dtype=torch.bool, device="cuda")
+        last[rows - 1], last[2 * rows - 1] = True, True
+        assert not out[:, last].isfinite().any()
+        bound = R.attend(q, k, v, keys, rws)[2]
+        assert ((out.double() - want.double()).abs()[:, ~last] <= 2 * bound[:, ~last]).all()
+        assert torch.equal(lse, want_lse)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_rows_that_see_nothing(dtype):
     # more rows than keys: the first ones see none
