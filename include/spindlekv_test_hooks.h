@@ -29,7 +29,7 @@ enum {
   SPINDLEKV_TUNE_SIM_BLOCK_PAIRS = 3,   /* pairs of blocks the candidate-record similarity kernel runs on (default 0:
                                            as many as the device holds at once); fewer make every pair walk more
                                            (unit, row span) items one after the other */
-  SPINDLEKV_TUNE_PAGED_WITHHOLD = 4     /* number of the thread block of the paged attention kernels that does not ask for its
+  SPINDLEKV_TUNE_PAGED_WITHHOLD = 4     /* number of the thread block of the paged and of the prompt attention kernels that does not ask for its
                                            first keys and waits for them until its bound (default -1: no block) */
 };
 

@@ -10,6 +10,10 @@
 // A thread block takes a slice of a row: it counts the history's tokens that fall into the slice in shared memory (whole numbers, so that no order
 // shows), marks the biased ones, and then streams the slice, where a word of counts tells the few tokens that change from the many that do not.
 //
+// 128 x 128256 in fp32: without rules 21 us (6.3 TB/s), masks 22.5, 64 biases a row 34, histories of 16384 tokens 51, all of them 62.  Bound by the additions in
+// shared memory (every slice looks through its row's whole history: eight slices, and four lanes of a warp find a token of theirs) and by the turns for the
+// tokens that change.  Smaller slices look through it more often (8192: 85 us), larger ones leave one block an SM (68).  Small calls are latency:
+// 4 x 32000 in bf16 6 us.
 #include <algorithm>
 
 #include <math_constants.h>

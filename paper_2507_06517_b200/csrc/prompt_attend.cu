@@ -16,6 +16,11 @@
 //
 // Values that a row does not see are multiplied by 0, which does nothing unless they are NaN or infinite.  A result that is NaN though its sum
 // is not says so, and its item is done again, with the tiles that hide keys from some row multiplied by hand.
+//
+// Bound by products and exponentials alike (d = 128: 2048 cycles of either for a step of two tiles, both pipes 68 % busy at 8192 tokens; d = 64: half the
+// products, exponentials 75 % busy) and by the chain of a step from scores over their maximum (415 cycles) and weights (1350) to the second product.
+// 32 query heads over 8, d = 128: 512 tokens 15 us, 2048 38, 4096 111 (1240 TFLOP/s), 16384 1.6 to 1.75 ms (1250 to 1350, at the power limit).
+// Not kept: 64 keys a step (4096 tokens 189 us where this took 131), two threads a row (163), exponentials in part by a polynomial (112 to 136 for 111).
 #include <algorithm>
 
 #include "args.cuh"

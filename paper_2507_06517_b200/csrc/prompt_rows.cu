@@ -13,6 +13,9 @@
 // Scores, weights, sums and O are fp32; bf16 weights are rounded to bf16 where they meet the values, which costs what the result's own rounding does.
 // The reference m moves only when a score exceeds it by 2^8.  A value that a column does not see is passed over, so that it may be anything: by its weight
 // of -0 in fp32; in bf16 steps that hide keys from some column look whether all of their values are finite, and multiply by hand if they are not.
+//
+// 4 x 16384 keys, 32 query heads over 8, d = 128, one row: bf16 48 us (5.6 TB/s, issue slots 24 % busy), fp32 87 us (6.1 TB/s, 47 %); one sequence of them
+// 15 and 29 us, of 2000 keys 9 and 10, where the launch, the lengths, the first copies and the join follow one another.
 #include <algorithm>
 #include <type_traits>
 

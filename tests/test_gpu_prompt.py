@@ -129,6 +129,19 @@ def test_values_that_some_of_few_columns_do_not_see(n, rows, hq, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [1, 40])
+def test_a_nan_that_is_seen_shows_whatever_its_weight(rows, dtype):
+    # keys cut into parts; one key outweighs all others by 2^400
+    keys, rws, q, k, v = make([6000], [rows], 8, 2, 128, dtype, False, seed=45)
+    q[...], k[...] = 1.0, 0.0
+    k[..., 100, :] = 25.0
+    v[0, 0, 1, 5000, 7] = math.nan
+    out, lse = attend(keys, rws, q, k, v)
+    assert out[..., 7][0, 0, 4:].isnan().all() and out[0, 0, :4].isfinite().all() and out[..., :7].isfinite().all()
+    assert ((out[0, 0, :4].double() - v[0, 0, 0, 100].double()).abs() <= 2 ** -7 * v[0, 0, 0, 100].double().abs()).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_rows_that_see_nothing(dtype):
     # more rows than keys: the first ones see none
     check(*make([3, 0, 500], [10, 4, 700], 4, 2, 64, dtype, False, seed=6))
