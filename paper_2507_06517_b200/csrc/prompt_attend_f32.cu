@@ -6,7 +6,7 @@
 // in rising order into one fp32 accumulator; what is left out is below 2^-24 of |x y| each.  Six products at the bf16 rate are a sixth of it: half a
 // tf32 pair's three products would cost the same and keep 22 bits.
 //
-// A first kernel writes the pieces of q, k and v (zeros behind the sequences), three planes each, as bf16 tensors that TMA can read.  Then as
+// A first kernel writes the pieces of q, k and v, three planes each, as bf16 tensors that TMA can read.  Then as
 // for bf16, with one row tile of 128 (position, head) rows and 64 keys at a time: their pieces fill the shared memory.  The scores of the next keys are
 // multiplied while this one's weights are formed: two buffers of scores and of weights in tensor memory.
 //     tensor memory: S [2][64 columns], P [2][3 pieces][32 columns], O [d columns]
@@ -58,6 +58,7 @@ struct SplitSource {
   Batch batch;
   __nv_bfloat16* to;         // [piece][layer][seq] of (head, token) or (token, head), d
   int heads, by_token;       // by_token: the heads of a token lie side by side
+  int behind;                // tokens behind the last one that get zeros
 };
 struct SplitParams { SplitSource t[3]; };
 // Memory bounds it (4 bytes in, 6 out for each element); a thread takes four times 8 elements, in the pieces' order, and asks for all of them at once
@@ -78,18 +79,20 @@ __global__ void __launch_bounds__(256) prompt_pieces_kernel(const __grid_constan
   const float* src = reinterpret_cast<const float*>(t.from.ptr) + (int64_t)layer * t.from.sl + (b.cu ? 0 : (int64_t)seq * t.from.ss);
   __nv_bfloat16* dst = t.to + (int64_t)ls * items * 8;
   float x[kSplitTurns][8];
+  bool writes[kSplitTurns];
 #pragma unroll
   for (int k = 0; k < kSplitTurns; ++k) {
     const unsigned i = first + k * 256, row = i / (D / 8), major = row / (unsigned)(t.by_token ? t.heads : tokens), minor = row - major * (unsigned)(t.by_token ? t.heads : tokens);
     const int token = t.by_token ? major : minor, head = t.by_token ? minor : major;
+    writes[k] = i < items && token >= from && token < end + t.behind;
 #pragma unroll
     for (int u = 0; u < 8; ++u) x[k][u] = 0.f;
-    if (i < items && token >= from && token < end) load8(src + (int64_t)head * t.from.sh + (int64_t)token * t.from.st + i % (D / 8) * 8, x[k]);
+    if (writes[k] && token < end) load8(src + (int64_t)head * t.from.sh + (int64_t)token * t.from.st + i % (D / 8) * 8, x[k]);
   }
 #pragma unroll
   for (int k = 0; k < kSplitTurns; ++k) {
     const unsigned i = first + k * 256;
-    if (i >= items) return;
+    if (!writes[k]) continue;
     uint32_t w[kPieces][4];
 #pragma unroll
     for (int u = 0; u < 8; u += 2) {
@@ -524,9 +527,11 @@ static spindlekv_status launch_exact(const PromptParams& p, const spindlekv_batc
   __nv_bfloat16* to = static_cast<__nv_bfloat16*>(pieces);
   const size_t nq = rows_of(rows) * n_q_heads * D * kPieces, nk = rows_of(keys) * p.heads * D * kPieces;
   SplitParams sp;
-  sp.t[0] = {p.q, p.rows, to, n_q_heads, 1};
-  sp.t[1] = {p.k, p.keys, to + nq, p.heads, 0};
-  sp.t[2] = {p.v, p.keys, to + nq + nk, p.heads, 0};
+  // What lies behind a sequence's last row may be anything where rows and scores are concerned, which nobody reads or which are replaced; values are multiplied by
+  // weights of 0 up to the end of their tile
+  sp.t[0] = {p.q, p.rows, to, n_q_heads, 1, 0};
+  sp.t[1] = {p.k, p.keys, to + nq, p.heads, 0, 0};
+  sp.t[2] = {p.v, p.keys, to + nq + nk, p.heads, 0, kExactKeys};
   int64_t blocks_of = 0, units = 0;
   for (const SplitSource& t : sp.t) {
     const int64_t seqs = t.batch.cu ? 1 : t.batch.n_seqs, tokens = t.batch.cu ? t.batch.total_len : t.batch.max_len, items = tokens * t.heads * (D / 8);

@@ -142,6 +142,21 @@ def test_a_nan_that_is_seen_shows_whatever_its_weight(rows, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens,rows,packed", [([300, 70, 1, 0, 129], None, False), ([300, 70, 1, 0, 129], None, True), ([3000, 1700], [40, 33], False), ([2000, 100], [2, 2], False)])
+def test_scratch_full_of_nans(lens, rows, packed, dtype):
+    from paper_2507_06517_b200.pipeline import SpindleKVPromptAttention
+    keys, rws, q, k, v = make(lens, rows, 8, 2, 128, dtype, packed, room=0 if rows else 50, seed=46)
+    a = SpindleKVPromptAttention(keys, 8, 2, 128, dtype, rows=rws)
+    a.ws.fill_(0xFF)
+    out = torch.full_like(q, 7.0)
+    a.run(q, k, v, out=out)
+    want, _, bound = R.attend(q, k, v, keys, rws)
+    row = ~want.isnan()
+    assert a.status() == B.OK and (out[~row] == 7.0).all()
+    assert ((out.double() - want).abs()[row] <= bound[row]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_rows_that_see_nothing(dtype):
     # more rows than keys: the first ones see none
     check(*make([3, 0, 500], [10, 4, 700], 4, 2, 64, dtype, False, seed=6))
