@@ -11,7 +11,7 @@
 //
 // Large calls are bound by memory and, at 28 % of the warps an SM can have, by its latency: 22615 bf16 tokens of 8 KV heads and 32 query heads, keys and queries
 // given out, 120 us (4.8 TB/s, 73 % of the copy rate; one row at a time and table rows through registers 345); 16 layers x 8 x 1000 fp32 rows by list
-// 53 us (3.1 TB/s; a lane reads a list's entry, then the row, then rounds).  One token of 96 sequences is latency: 6.5 us.
+// 52 us (3.2 TB/s; the row, its position's turn, the block's maximum and the codes follow one another).  One token of 96 sequences is latency: 6 us.
 #include <algorithm>
 
 #include "paged_rounding.cuh"
@@ -170,11 +170,15 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateBlocks<T>) paged_append
   const int layer = u / p.table.n_seqs, s = u - layer * p.table.n_seqs;
   const int start = p.start[u], from = p.first_pos ? p.first_pos[u] : p.idx ? 0 : start;      // (the lengths are asked for before the first is looked at)
   const int len = unit_len(p.table, p.pool, u);
+  // A list's entries too, for a cache that begins here, which is what a list mostly fills (otherwise they are asked for again)
+  const int rel = (int)(item / (2u * p.pool.heads)), rest = (int)(item - (unsigned)rel * 2u * p.pool.heads), head = rest >> 1;
+  const int32_t* list = p.idx ? p.idx + ((int64_t)layer * p.pool.heads + head) * p.idx_len + (int64_t)s * p.idx_seq : nullptr;
+  int listed = -1;
+  if (p.idx && lane < kPagedBlock && rel * kPagedBlock + lane < p.max_new) listed = list[rel * kPagedBlock + lane];
   if (start < 0) return;
   const int end = (int)min((long long)len, (long long)start + p.max_new);
   if (start >= end) return;
   if (item >= p.n_kv) return rotate_queries<T, D>(p, layer, s, item - p.n_kv, from, min(end - start, p.n_rows));
-  const int rel = (int)(item / (2u * p.pool.heads)), rest = (int)(item - (unsigned)rel * 2u * p.pool.heads), head = rest >> 1;
   const bool is_v = (rest & 1) != 0;
   const int blk = start / kPagedBlock + rel, t0 = blk * kPagedBlock;
   if (t0 >= end) return;
@@ -192,7 +196,7 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateBlocks<T>) paged_append
   if (lane >= first && lane < last) {
     const int i = t0 + lane - start;
     my_row = i;
-    if (p.idx) my_row = p.idx[((int64_t)layer * p.pool.heads + head) * p.idx_len + (int64_t)s * p.idx_seq + i];
+    if (p.idx) my_row = start == 0 ? listed : list[i];
     if (my_row < 0 || my_row >= p.n_rows) my_row = -1;
   }
   // The rows' cosines and sines come into shared memory while the rows are on their way (into registers, two rows ahead: 79 us in place of 67 for keys,
