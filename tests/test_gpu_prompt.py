@@ -350,3 +350,56 @@ def test_refusals_of_the_class_and_what_it_makes_itself():
         a.run(q, k, v, scale=-1.0)
     out = a.run(q, k, v)
     assert (out[0, 1, :, 17:] == 0).all() and torch.equal(out[0, 1, :, :17], attend(keys, rows, q, k, v)[0][0, 1, :, :17])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_few_rows_far_apart(dtype):
+    # the second layer 1.2 * 2^31 elements behind the first
+    keys, rows, q, k, v = make([700, 90], [3, 3], 4, 2, 64, dtype, False, n_layers=2, seed=32)
+    far, gap = [], 2576980480
+    room = torch.empty(gap + q[0].numel() + k[0].numel() + v[0].numel(), dtype=dtype, device="cuda")
+    at = 0
+    for t in (q, k, v):
+        f = torch.as_strided(room, t.shape, (gap, *t.stride()[1:]), at)
+        f.copy_(t)
+        far.append(f)
+        at += t[0].numel()
+    first = check(keys, rows, q, k, v)
+    assert all(torch.equal(a, b) for a, b in zip(first, attend(keys, rows, *far)))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n_rows", [2, 70])
+def test_a_recorded_call_follows_the_lengths_on_the_device(n_rows, dtype):
+    from paper_2507_06517_b200.pipeline import SpindleKVPromptAttention, record_graph
+    gen = torch.Generator(device="cuda").manual_seed(47)
+    lens = torch.tensor([[2000, 5, 900]], dtype=torch.int32, device="cuda")
+    keys, rows = B.Batch(1, 3, 2500, 7500, None, lens), B.Batch(1, 3, n_rows, 3 * n_rows, None, torch.full_like(lens, n_rows))
+    q, k, v = tensor_of(rows, 8, 128, dtype, gen), tensor_of(keys, 2, 128, dtype, gen), tensor_of(keys, 2, 128, dtype, gen)
+    a = SpindleKVPromptAttention(keys, 8, 2, 128, dtype, rows=rows)
+    out = torch.full_like(q, 7.0)
+    graph = record_graph(lambda: a.run(q, k, v, out=out))
+    for now, new in (([2000, 5, 900], [n_rows] * 3), ([2500, 0, 1], [n_rows, 0, 1]), ([130, 2499, 64], [1, n_rows, n_rows])):
+        lens.copy_(torch.tensor([now]))
+        rows.layer_lens.copy_(torch.tensor([new]))
+        out.fill_(7.0)
+        graph.replay()
+        assert a.status() == B.OK
+        want, _, bound = R.attend(q, k, v, keys, rows)
+        row = ~want.isnan()
+        assert (out[~row] == 7.0).all() and ((out.double() - want).abs()[row] <= bound[row]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_more_sequences_than_a_grid_of_few_rows_takes(dtype):
+    # 9000 sequences x 8 heads go by whole tiles, the first hundred of them by themselves
+    gen = torch.Generator(device="cuda").manual_seed(48)
+    lens = torch.randint(0, 21, (1, 9000), generator=gen, dtype=torch.int32, device="cuda")
+    keys, rows = B.Batch(1, 9000, 20, 180000, None, lens), B.Batch(1, 9000, 1, 9000)
+    q, k, v = tensor_of(rows, 8, 64, dtype, gen), tensor_of(keys, 8, 64, dtype, gen), tensor_of(keys, 8, 64, dtype, gen)
+    out, lse = attend(keys, rows, q, k, v)
+    some = B.Batch(1, 100, 20, 2000, None, lens[:, :100].contiguous()), B.Batch(1, 100, 1, 100)
+    want, want_lse, bound = R.attend(q[:, :100], k[:, :100], v[:, :100], *some)
+    assert ((out[:, :100].double() - want).abs() <= bound).all()
+    check(*some, q[:, :100].contiguous(), k[:, :100].contiguous(), v[:, :100].contiguous())
+    assert out.isfinite().all() and (out[0, (lens == 0)[0]] == 0).all() and ((lse == -math.inf) == (lens == 0)[0]).all()
