@@ -189,11 +189,13 @@ spindlekv_status logits_adjust_impl(int n_rows, int vocab, const void* logits, i
   p.out_stride = out_stride;
   p.r = rules;
   p.vocab = vocab;
-  // slices of whole mask words, as many as give every SM a few blocks
-  const int64_t wanted = std::max<int64_t>(1, 4 * 148 / n_rows);
+  // Slices of whole mask words, as many as fill the SMs once with two blocks each (37 x 50257 bf16, histories of 2500: twice as many slices 12.7 us, these
+  // 10.1; masks alone 5.8 and 4.4; 100 x 50000 fp32, masks alone, where the largest slices are more than fill them, 7.2 and 8.0)
+  const bool counts = rules.history || rules.n_bias > 0;
+  const int64_t wanted = std::max<int64_t>(1, 2 * 148 / n_rows);
   const int64_t slice = std::min<int64_t>(kLogitsMaxSlice, std::max<int64_t>(2048, (vocab + wanted - 1) / wanted));
   p.slice = (int)((slice + 1023) / 1024 * 1024);
-  const size_t smem = rules.history || rules.n_bias > 0 ? (size_t)std::min(p.slice, (vocab + 3) / 4 * 4) * 4 : 0;
+  const size_t smem = counts ? (size_t)std::min(p.slice, (vocab + 3) / 4 * 4) * 4 : 0;
   static PerDeviceOnce once;
   const int dev = PerDeviceOnce::current();
   if (dev < 0) return SPINDLEKV_CUDA;
