@@ -435,6 +435,7 @@ spindlekv_status spindlekv_paged_append(const spindlekv_page_pool* pool, const s
  *   first_pos  device [n_layers][n_seqs], or NULL: start with rows in order, 0 with a list
  *   K_out      rotated keys [layer][seq][kv head][row][d], or ptr NULL: none.  May be K itself
  *   n_q_heads, Q, Q_out  0, or queries [layer][seq][q head][row][d] of the same rows, which are rotated alike and go nowhere else.  Q_out may be Q itself
+ * K_out and Q_out share memory with nothing but their own input, K and Q: rows are turned in no order.  INVALID_ARG where one begins at another tensor's address.
  * K_out and Q_out hold rows 0 .. lens - start - 1 (none of n_rows and above); those behind are left as they were, and so are all of a sequence that is
  * skipped.  A key's row is written even where its page is missing.  With `idx` both must be absent (lists differ from head to head).
  * The rotation is formed in fp32, its two products and their sum each rounded by itself, and then rounded to the rows' type: codes, scales and rows

@@ -406,11 +406,13 @@ spindlekv_status spindlekv_paged_append_rotated(const spindlekv_page_pool* pool,
   if (idx && (idx_seq < max_new || (int64_t)table->n_seqs * idx_seq > idx_len)) return SPINDLEKV_INVALID_ARG;
   if (idx && (K_out.ptr || n_q_heads)) return SPINDLEKV_INVALID_ARG;      // a list may name a row for some heads only
   if (n_q_heads < 0 || (K_out.ptr && !rows_out_ok(K, K_out)) || (n_q_heads && (!tensor_ok(Q) || !rows_out_ok(Q, Q_out)))) return SPINDLEKV_INVALID_ARG;
-  if (K.ptr == V.ptr && K_out.ptr == K.ptr) return SPINDLEKV_INVALID_ARG;
   if (K_out.ptr && !rows_apart(K_out, table->n_layers, table->n_seqs, pool->n_kv_heads, n_rows)) return SPINDLEKV_INVALID_ARG;
   if (n_q_heads && !rows_apart(Q_out, table->n_layers, table->n_seqs, n_q_heads, n_rows)) return SPINDLEKV_INVALID_ARG;
   if (K.dtype != V.dtype || (K_out.ptr && K_out.dtype != K.dtype) || (n_q_heads && (Q.dtype != K.dtype || Q_out.dtype != K.dtype))) return SPINDLEKV_UNSUPPORTED;
   if (n_q_heads > 65536) return SPINDLEKV_UNSUPPORTED;
+  // keys, values and queries are turned in no order: an output may lie on its own input, not where another one is still read or written
+  if (K_out.ptr && (K_out.ptr == V.ptr || (n_q_heads && (K_out.ptr == Q.ptr || K_out.ptr == Q_out.ptr)))) return SPINDLEKV_INVALID_ARG;
+  if (n_q_heads && (Q_out.ptr == K.ptr || Q_out.ptr == V.ptr)) return SPINDLEKV_INVALID_ARG;
   return paged_append_rotated_impl(*pool, *table, start, max_new, K, V, n_rows, idx, idx_len, idx_seq, rope_table, table_positions, first_pos, K_out, n_q_heads, Q, Q_out,
                                    (cudaStream_t)stream);
 }

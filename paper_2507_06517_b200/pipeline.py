@@ -697,7 +697,7 @@ class SpindleKVPagedCache(_OnDevice):
         """``append`` of keys that ``rope_table`` (``[n_positions, d/2, 2]`` fp32, ``spindlekv_rope_table``) rotates on the way: row ``r`` of a sequence by
         position ``first_pos + r`` (``first_pos`` ``[n_layers or 1, n_seqs]`` int32; ``start`` by default, 0 with ``idx``).  ``K_out``, if given, gets the rotated
         keys (it may be ``K``); queries ``Q`` ``[n_layers or 1, n_seqs, H_q, rows, d]`` of the same rows are rotated alike into ``Q_out`` (it may be ``Q``; by
-        default a new tensor, zeros behind the new rows), which is returned."""
+        default a new tensor, zeros behind the new rows), which is returned.  ``K_out`` and ``Q_out`` share memory with no other tensor of the call."""
         if B.current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self.append_rotated(K, V, rope_table, start, first_pos, idx, idx_seq, max_new, K_out, Q, Q_out, layer, stream)
