@@ -5,6 +5,7 @@ layers, compact).  No arithmetic happens here; this is buffer ownership and call
 from __future__ import annotations
 
 import dataclasses
+import threading
 from typing import Dict, Optional, Sequence
 
 import numpy as np
@@ -632,6 +633,7 @@ class SpindleKVPagedCache(_OnDevice):
         self.n_live = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._tables = {}
         self._rotated = (None, None)                       # layouts of the last append_rotated, and what follows from them
+        self._writing = threading.Lock()                   # of addresses into these
         self._out: Dict[tuple, torch.Tensor] = {}
         n = B.spindlekv_paged_workspace_bytes(self.pool, self.table, self.Hkv, 1)      # the same for every shape that is served
         self.ws_attend = torch.zeros(n, dtype=torch.uint8, device=self.device)
@@ -709,19 +711,20 @@ class SpindleKVPagedCache(_OnDevice):
             Q_out = self._empty(Q.shape, Q.dtype, stream, zero=True)
         # arguments laid out as those of the last call have been looked over
         layouts = (layer is None, _layout(K), _layout(V), _layout(rope_table), _layout(start), _layout(first_pos), _layout(idx), _layout(K_out), _layout(Q), _layout(Q_out))
-        if layouts != self._rotated[0]:
-            self._rotated = (layouts, self._look_over_rotated(table.n_layers, K, V, rope_table, start, first_pos, idx, K_out, Q, Q_out))
-        kd, vd, kod, qd, qod, hq, n_rows = self._rotated[1]
-        kd.ptr, vd.ptr = K.data_ptr(), V.data_ptr()
-        if K_out is not None:
-            kod.ptr = K_out.data_ptr()
-        if Q is not None:
-            qd.ptr, qod.ptr = Q.data_ptr(), Q_out.data_ptr()
-        if idx is not None and idx_seq is None:
-            idx_seq = idx.shape[2] // self.n_seqs
-        if max_new is None:
-            max_new = n_rows if idx is None else idx_seq
-        B.spindlekv_paged_append_rotated(self.pool, table, start, max_new, kd, vd, n_rows, rope_table, first_pos, kod, hq, qd, qod, idx, idx_seq or 0, self._raw(stream))
+        with self._writing:
+            if layouts != self._rotated[0]:
+                self._rotated = (layouts, self._look_over_rotated(table.n_layers, K, V, rope_table, start, first_pos, idx, K_out, Q, Q_out))
+            kd, vd, kod, qd, qod, hq, n_rows = self._rotated[1]
+            kd.ptr, vd.ptr = K.data_ptr(), V.data_ptr()
+            if K_out is not None:
+                kod.ptr = K_out.data_ptr()
+            if Q is not None:
+                qd.ptr, qod.ptr = Q.data_ptr(), Q_out.data_ptr()
+            if idx is not None and idx_seq is None:
+                idx_seq = idx.shape[2] // self.n_seqs
+            if max_new is None:
+                max_new = n_rows if idx is None else idx_seq
+            B.spindlekv_paged_append_rotated(self.pool, table, start, max_new, kd, vd, n_rows, rope_table, first_pos, kod, hq, qd, qod, idx, idx_seq or 0, self._raw(stream))
         return Q_out
 
     def _look_over_rotated(self, n_l, K, V, rope_table, start, first_pos, idx, K_out, Q, Q_out):
@@ -822,6 +825,7 @@ class SpindleKVPromptAttention(_OnDevice):
         self.ws = torch.empty(n, dtype=torch.uint8, device=dev)
         self._c = self.keys.c(), self.rows.c()
         self._seen = (None, None)                          # layouts of the last call, and the descriptors that follow from them
+        self._writing = threading.Lock()                   # of addresses into these
 
     def _rows_of(self, name: str, t: torch.Tensor, b: B.Batch, heads: int) -> B._Tensor:
         shape, strides = t.shape, t.stride()
@@ -842,14 +846,15 @@ class SpindleKVPromptAttention(_OnDevice):
             out = self._empty(q.shape, q.dtype, stream, zero=self.rows.cu_seqlens is not None or self.rows.layer_lens is not None)
         # arguments laid out as those of the last call have been looked over
         layouts = (_layout(q), _layout(K), _layout(V), _layout(out), _layout(lse))
-        if layouts != self._seen[0]:
-            rows = (("q", q, self.rows, self.Hq), ("K", K, self.keys, self.Hkv), ("V", V, self.keys, self.Hkv), ("out", out, self.rows, self.Hq))
-            if lse is not None:
-                self._mine("lse", lse, torch.float32, (self.rows.n_layers, self.Hq, self.rows.total_len))
-            self._seen = (layouts, tuple(self._rows_of(*r) for r in rows))
-        qd, kd, vd, od = self._seen[1]
-        qd.ptr, kd.ptr, vd.ptr, od.ptr = q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr()
-        B.spindlekv_prompt_attend(self._c[0], self._c[1], self.Hq, self.Hkv, self.d, scale, qd, kd, vd, od, lse, self.ws, self._raw(stream))
+        with self._writing:
+            if layouts != self._seen[0]:
+                rows = (("q", q, self.rows, self.Hq), ("K", K, self.keys, self.Hkv), ("V", V, self.keys, self.Hkv), ("out", out, self.rows, self.Hq))
+                if lse is not None:
+                    self._mine("lse", lse, torch.float32, (self.rows.n_layers, self.Hq, self.rows.total_len))
+                self._seen = (layouts, tuple(self._rows_of(*r) for r in rows))
+            qd, kd, vd, od = self._seen[1]
+            qd.ptr, kd.ptr, vd.ptr, od.ptr = q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr()
+            B.spindlekv_prompt_attend(self._c[0], self._c[1], self.Hq, self.Hkv, self.d, scale, qd, kd, vd, od, lse, self.ws, self._raw(stream))
         return out
 
     def status(self) -> int:
