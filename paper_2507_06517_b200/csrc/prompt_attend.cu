@@ -11,7 +11,7 @@
 // Roles: two warpgroups turn scores into weights, a thread for each row of their tile; one warp asks for Q, K and V (TMA); one issues the
 // products.  While one tile's weights are formed the products of the other run.  The reference m of a row moves only when a score exceeds
 // it by 2^8 (then O is multiplied by the row's thread: the products that wrote it are done when the scores that follow them are).
-// Sums and references are fp32; the weights enter the second product in bf16, where values are, to half a step of 2^-8: as much as the result's
+// Sums and references are fp32 (sums of very long keys are taken out of tensor memory: keep_sums); the weights enter the second product in bf16, where values are, to half a step of 2^-8: as much as the result's
 // own rounding, and independent from key to key.
 //
 // Values that a row does not see are multiplied by 0, which does nothing unless they are NaN or infinite.  A result that is NaN though its sum
@@ -47,7 +47,45 @@ struct PromptSmem {
 };
 static_assert(PromptSmem<128>::bytes <= 227 * 1024, "shared memory");
 
+// The accumulator in tensor memory cuts off what it adds, towards zero: with values of one sign results come out smaller by 7e-5 over 16384 keys, 3.6e-4 over 65536, 1.7e-3
+// over 262144 (half a step of bf16 is 2e-3).  So after every 128 tiles a row's thread adds what is there to a sum of its own in memory, rounding as usual, and the products begin
+// anew.  It does so between a tile's scores and its weights, where it may touch O anyway: the products that wrote it are done when the scores that follow them are.  Of a
+// warp: [element / 4][lane] 16 bytes, so that lanes lie next to one another, and behind them the reference that the sums go by.  7e-5 is then left at any length, and the longest
+// calls take 2 to 3 % more (2000 rows, 32 / 8 heads, d = 128: behind 40000 keys 980 -> 1000 us, 131072 3.25 -> 3.35 ms); others have a kernel without it, which the loop's changed registers would
+// cost 3 % too (4096 tokens 121 -> 125).
+constexpr int kPromptKeep = 128;          // tiles
+template <int D> constexpr int kPromptKept = (D + 1) * 256;      // numbers for the 256 rows of a block
+
 template <int D>
+__device__ __noinline__ void keep_sums(float* kept, uint32_t o_tmem, bool first, float m) {
+  const int lane = threadIdx.x & 31;
+  float4* sums = reinterpret_cast<float4*>(kept) + lane;
+  float* ref = kept + D * 32 + lane;
+  const float was = first ? m : *ref, f = was == m ? 1.f : pow2(was - m);
+  *ref = m;
+#pragma unroll 1
+  for (int c = 0; c < D; c += 64) {
+    float4 y[16];                         // (asked for together)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = first ? make_float4(0.f, 0.f, 0.f, 0.f) : sums[(c / 4 + i) * 32];
+#pragma unroll
+    for (int h = 0; h < 64; h += 32) {
+      uint32_t o[32];
+      __syncwarp();
+      ptx::tmem_ld_32x32_sync(o_tmem + c + h, o);
+#pragma unroll
+      for (int i = 0; i < 32; i += 4) {
+        const float4 z = y[(h + i) / 4];
+        sums[(c + h + i) / 4 * 32] = make_float4(fmaf(z.x, f, __uint_as_float(o[i])), fmaf(z.y, f, __uint_as_float(o[i + 1])), fmaf(z.z, f, __uint_as_float(o[i + 2])),
+                                                 fmaf(z.w, f, __uint_as_float(o[i + 3])));
+      }
+    }
+  }
+  __syncwarp();
+}
+
+// LONG: keys that are longer than this in some part
+template <int D, bool LONG>
 __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                                                                           const __grid_constant__ CUtensorMap vmap, const __grid_constant__ PromptParams p) {
   using S = PromptSmem<D>;
@@ -131,6 +169,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
     for (int pass = 0; pass == 0 || (pass == 1 && again()); ++pass) {
       const int w = warp >> 2, row = (warp & 3) * 32 + lane;
       uint8_t* stage = smem + S::stage + warp * 4096;
+      float* kept = LONG ? p.kept + ((int64_t)blockIdx.x * 8 + warp) * (kPromptKept<D> / 8) : nullptr;
       const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tmem + w * 128 + lanes, to = tmem_o + w * D + lanes;
       while (ok) {
         // The item stays in its slot until its result is written: registers are short here
@@ -157,7 +196,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
           sees = within < p.pt && pos < it.n_r ? seen_by(pos, it.n_r, it.n_k) : 0x7FFFFFFF;
         }
         float m = -CUDART_INF_F, l = 0.f;
-        for (int j = 0; j < n; ++j) {
+        for (int j0 = 0; j0 < (LONG ? n : 1); j0 += kPromptKeep) {
+        if (LONG && j0 > 0 && (!careful || j0 - kPromptKeep < even)) {
+          ok = wait(s_full + w, n_s) && ok;
+          __syncwarp();
+          ptx::tc_fence_after();
+          keep_sums<D>(kept, to, j0 == kPromptKeep, m);
+        }
+        for (int j = LONG ? j0 : 0, end = LONG ? min(n, j0 + kPromptKeep) : n; j < end; ++j) {
           ok = wait(s_full + w, n_s++) && ok;
           __syncwarp();
           ptx::tc_fence_after();
@@ -217,6 +263,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(p_full + w);
         }
+        }
         // ---- the item's result ----
         const PromptItem it = *held;
         __syncwarp();
@@ -228,13 +275,19 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
         __syncwarp();
         ptx::tc_fence_after();
         if (careful && n > even)
-          add_by_hand<T, D>(p, it, to, 0, D, even == 0, head, there ? pos : 0, (first + even) * KT, there ? min(sees, (first + n) * KT) : 0, m == -CUDART_INF_F ? 0.f : m);
+          add_by_hand<T, D>(p, it, to, 0, D, even <= (LONG ? (n - 1) / kPromptKeep * kPromptKeep : 0), head, there ? pos : 0, (first + even) * KT, there ? min(sees, (first + n) * KT) : 0, m == -CUDART_INF_F ? 0.f : m);
         const bool write = there && ok && !*abort_flag;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const int64_t number = row_number(p, layer, seq, it.base_r, head, pos), parts = (int64_t)it.split * p.rows.n_layers * p.rows.total_len * (p.heads * p.hn);
         const int64_t at = !write ? -1 : p.splits > 1 ? (parts + number) * D * 4 : row_offset(p.out, p.rows, layer, seq, it.base_r, head, pos) * 2;
         uint8_t* base = reinterpret_cast<uint8_t*>(p.splits > 1 ? p.part : const_cast<void*>(p.out.ptr));
         bool odd = false;
+        const bool keeps = LONG && n > kPromptKeep && (!careful || even > 0);
+        float f_kept = 0.f;
+        if (keeps) {
+          const float was = kept[D * 32 + lane];
+          f_kept = was == m ? 1.f : pow2(was - m);
+        }
 #pragma unroll 1
         for (int c = 0; c < D; c += 64) {
           float x[64];
@@ -247,6 +300,17 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
             }
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[i + e] = n > 0 ? __uint_as_float(o[e]) : 0.f;
+          }
+          if (keeps) {
+            const float4* sums = reinterpret_cast<const float4*>(kept) + c / 4 * 32 + lane;
+#pragma unroll
+            for (int e = 0; e < 64; e += 4) {
+              const float4 y = sums[e / 4 * 32];
+              x[e] = fmaf(y.x, f_kept, x[e]);
+              x[e + 1] = fmaf(y.y, f_kept, x[e + 1]);
+              x[e + 2] = fmaf(y.z, f_kept, x[e + 2]);
+              x[e + 3] = fmaf(y.w, f_kept, x[e + 3]);
+            }
           }
 #pragma unroll
           for (int e = 0; e < 64; ++e) odd |= x[e] != x[e];
@@ -399,7 +463,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attend_kernel(const 
               if (j >= even[w]) return;
 #pragma unroll
               for (int k = k0; k < k1; ++k)
-                ptx::umma_bf16_ts_elected(tmem_o + w * D, tmem + w * 128 + k * 8, dv + (av * S::kTile >> 4) + (k * 2048 >> 4), idesc_o, j == 0 && k == 0 ? 0u : 1u, issues);
+                ptx::umma_bf16_ts_elected(tmem_o + w * D, tmem + w * 128 + k * 8, dv + (av * S::kTile >> 4) + (k * 2048 >> 4), idesc_o, (LONG ? j % kPromptKeep : j) == 0 && k == 0 ? 0u : 1u, issues);
             };
             ok = __all_sync(0xffffffffu, wait(p_part + w, n_s[w]) && ok);
             if (ok) values(0, kPart / 16);
@@ -462,25 +526,35 @@ static int prompt_splits(const spindlekv_batch& keys, const spindlekv_batch& row
   return saved > 3.5 + bytes / 4e6 ? (int)most : 1;
 }
 static int prompt_per_item(int hn, int dtype) { return (dtype == SPINDLEKV_BF16 ? 2 : 1) * (kPromptRows / hn); }
+// One block per SM; more only where a block's list of items would not do
+static int64_t prompt_blocks(int64_t items) { return std::min(items, std::max<int64_t>(kPromptSms, (items + kPromptMaxItems - 1) / kPromptMaxItems)); }
+// bf16: bytes for the sums of keys that are longer, in a part, than the products sum up by themselves
+static size_t prompt_kept_bytes(const spindlekv_batch& keys, int64_t blocks, int splits, int head_dim) {
+  if (ceil_div(ceil_div(keys.max_len, 128), splits) <= kPromptKeep) return 0;
+  return (size_t)blocks * (head_dim == 64 ? kPromptKept<64> : kPromptKept<128>) * sizeof(float);
+}
 
 size_t prompt_workspace_bytes(const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int n_kv_heads, int head_dim, int dtype) {
   const int few = prompt_few_rows(keys, rows, n_kv_heads, n_q_heads / n_kv_heads, head_dim, dtype);
   const int splits = few ? few : prompt_splits(keys, rows, n_kv_heads, prompt_per_item(n_q_heads / n_kv_heads, dtype), n_q_heads * head_dim * 4, dtype);
   const size_t numbers = (size_t)rows.n_layers * rows.total_len * n_q_heads;
-  return kHeaderBytes + (splits > 1 ? align_up(splits * numbers * (head_dim * sizeof(float) + sizeof(float2)), 256) : 0) +
-         (dtype == SPINDLEKV_F32 && !few ? prompt_pieces_bytes(keys, rows, n_q_heads, n_kv_heads, head_dim) : 0);
+  const size_t parts = kHeaderBytes + (splits > 1 ? align_up(splits * numbers * (head_dim * sizeof(float) + sizeof(float2)), 256) : 0);
+  if (few) return parts;
+  if (dtype == SPINDLEKV_F32) return parts + prompt_pieces_bytes(keys, rows, n_q_heads, n_kv_heads, head_dim);
+  const int64_t items = prompt_items(rows, n_kv_heads, prompt_per_item(n_q_heads / n_kv_heads, dtype)) * splits;
+  return parts + prompt_kept_bytes(keys, prompt_blocks(items), splits, head_dim);
 }
 
-template <int D>
+template <int D, bool LONG>
 static spindlekv_status launch_prompt(const CUtensorMap& qmap, const CUtensorMap& kmap, const CUtensorMap& vmap, const PromptParams& p, int64_t blocks, cudaStream_t st) {
   static PerDeviceOnce once;
   const int dev = PerDeviceOnce::current();
   if (dev < 0) return SPINDLEKV_CUDA;
   if (!once.done[dev]) {
-    if (cudaFuncSetAttribute(prompt_attend_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptSmem<D>::bytes) != cudaSuccess) return SPINDLEKV_CUDA;
+    if (cudaFuncSetAttribute(prompt_attend_kernel<D, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptSmem<D>::bytes) != cudaSuccess) return SPINDLEKV_CUDA;
     once.done[dev] = true;
   }
-  const spindlekv_status s = launch_after(prompt_attend_kernel<D>, blocks, kPromptThreads, PromptSmem<D>::bytes, st, qmap, kmap, vmap, p);
+  const spindlekv_status s = launch_after(prompt_attend_kernel<D, LONG>, blocks, kPromptThreads, PromptSmem<D>::bytes, st, qmap, kmap, vmap, p);
   return s == SPINDLEKV_OK ? launch_prompt_join<__nv_bfloat16, D>(p, st) : s;
 }
 
@@ -508,24 +582,23 @@ spindlekv_status prompt_attend_impl(const spindlekv_batch& keys, const spindlekv
   const size_t numbers = (size_t)rows.n_layers * rows.total_len * n_q_heads;
   p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kHeaderBytes);
   p.stat = reinterpret_cast<float2*>(p.part + p.splits * numbers * head_dim);
+  p.kept = nullptr;
   p.hdr = static_cast<uint32_t*>(ws);
   const Tuning tune = current_tuning();
   p.wait_cycles = tune.mbar_wait_cycles;
   p.withhold = tune.paged_withhold;
   if (few) return prompt_attend_few(p, keys, rows.max_len, head_dim, k, v, st);
-  const int64_t items = prompt_items(rows, n_kv_heads, p.per_item) * p.splits;
-  // one block per SM; more only where a block's list of items would not do
-  const int64_t blocks = std::min(items, std::max<int64_t>(kPromptSms, (items + kPromptMaxItems - 1) / kPromptMaxItems));
+  const int64_t blocks = prompt_blocks(prompt_items(rows, n_kv_heads, p.per_item) * p.splits);
   if (blocks > 65535) return SPINDLEKV_UNSUPPORTED;
-  if (q.dtype == SPINDLEKV_F32) {
-    const size_t parts = p.splits > 1 ? align_up(p.splits * numbers * (head_dim * sizeof(float) + sizeof(float2)), 256) : 0;
-    return prompt_attend_f32(p, keys, rows, n_q_heads, head_dim, static_cast<uint8_t*>(ws) + kHeaderBytes + parts, blocks, st);
-  }
+  uint8_t* behind = static_cast<uint8_t*>(ws) + kHeaderBytes + (p.splits > 1 ? align_up(p.splits * numbers * (head_dim * sizeof(float) + sizeof(float2)), 256) : 0);
+  if (q.dtype == SPINDLEKV_F32) return prompt_attend_f32(p, keys, rows, n_q_heads, head_dim, behind, blocks, st);
+  if (prompt_kept_bytes(keys, blocks, p.splits, head_dim)) p.kept = reinterpret_cast<float*>(behind);
   CUtensorMap qmap, kmap, vmap;
   if (!make_rows_map_bf16(&qmap, q, rows, n_q_heads, head_dim, p.hn, p.pt) || !make_tensor_map_bf16(&kmap, k, keys, n_kv_heads, head_dim, 128) ||
       !make_tensor_map_bf16(&vmap, v, keys, n_kv_heads, head_dim, 128))
     return SPINDLEKV_UNSUPPORTED;
-  return head_dim == 64 ? launch_prompt<64>(qmap, kmap, vmap, p, blocks, st) : launch_prompt<128>(qmap, kmap, vmap, p, blocks, st);
+  if (head_dim == 64) return p.kept ? launch_prompt<64, true>(qmap, kmap, vmap, p, blocks, st) : launch_prompt<64, false>(qmap, kmap, vmap, p, blocks, st);
+  return p.kept ? launch_prompt<128, true>(qmap, kmap, vmap, p, blocks, st) : launch_prompt<128, false>(qmap, kmap, vmap, p, blocks, st);
 }
 
 }  // namespace skv

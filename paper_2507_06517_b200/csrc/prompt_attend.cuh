@@ -28,6 +28,7 @@ struct PromptParams {
   float* lse;                // [layer][query head][T], or null
   float* part;               // [splits][layer][T][query head][d] and
   float2* stat;              // [splits][layer][T][query head]: O, reference and sum of a part
+  float* kept;               // bf16: sums of long keys (keep_sums), kPromptKept<d> numbers for each block
   uint32_t* hdr;
   long long wait_cycles;
   int withhold;              // for tests: the block that does not ask for its first keys; -1: none
