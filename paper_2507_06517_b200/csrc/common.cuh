@@ -210,15 +210,6 @@ __device__ __forceinline__ int last_to_arrive(unsigned long long* word, int n, b
   return old >> 16 & 1u ? 2 : 1;
 }
 
-// Some of a block's warps meet at barrier `id`; and whether `x` holds for one of their threads
-__device__ __forceinline__ void warps_meet(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-__device__ __forceinline__ bool warps_any(int id, int threads, bool x) {
-  uint32_t y;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(y) : "r"((uint32_t)x), "r"(id), "r"(threads) : "memory");
-  return y != 0;
-}
-
 // Per-device "done once" flags for host-side set-up (function attributes, occupancy queries): the
 // library may be used from several devices of one process.
 constexpr int kMaxDevices = 64;

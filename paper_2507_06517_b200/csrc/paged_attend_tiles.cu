@@ -42,6 +42,14 @@ constexpr int kTilesThreads = 32 * (kWidenFirst + kWidenWarps);
 constexpr float kTileEven = 0.00390625f;   // smallest scale, in units of the power of two above the largest, that joins the weights
 constexpr int kRawBytes = kTile * 128, kWideBytes = 2 * kRawBytes;
 
+// Some of a block's warps meet at barrier `id`; and whether `x` holds for one of their threads
+__device__ __forceinline__ void warps_meet(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ bool warps_any(int id, int threads, bool x) {
+  uint32_t y;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(y) : "r"((uint32_t)x), "r"(id), "r"(threads) : "memory");
+  return y != 0;
+}
 // Eight values per lane -> each of the eight reduced over the warp's lanes; lane i gets the one of number reduced_by(i).  Half of the values
 // change hands at each of the first three steps: 9 shuffles in place of 40.
 __device__ __forceinline__ int reduced_by(int lane) { return (lane >> 2 & 4) | (lane >> 2 & 2) | (lane >> 2 & 1); }
