@@ -487,7 +487,7 @@ spindlekv_status spindlekv_paged_attend(const spindlekv_page_pool* pool, const s
  * Sums, softmax statistics and out are formed in fp32, in an order that the arguments and the lengths fix: the same call gives the same bits.  bf16: the
  * weights are rounded to bf16 where they meet the values, and tensor cores cut off what they add: less than 1e-4 of values of one sign, at any length (measured).  fp32: every factor enters in three pieces of 8 bits, six products of them; products below
  * 2^-24 of the largest are left out (calls of few rows multiply in fp32 as it is).  Keys and values that a row does not see do not reach it, not even if
- * they are NaN or infinite; of those that it sees, a NaN leaves a NaN, and an infinity may.  A wait that gave up shows in the status word of `ws` (spindlekv_poll_status).
+ * they are NaN or infinite; of those that it sees, a NaN leaves a NaN, and an infinity may (fp32: by the number of rows).  A wait that gave up shows in the status word of `ws` (spindlekv_poll_status).
  * UNSUPPORTED: layer_lens per head, more than 128 query heads per KV head, 65535 (layer, sequence) pairs, tensors that repeat memory (a stride of 0
  * where there is more than one).
  */

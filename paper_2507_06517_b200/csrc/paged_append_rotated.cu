@@ -10,7 +10,7 @@
 // tokens of eight heads and keeps a token's cosines and sines for all of them.
 //
 // Large calls are bound by memory and, at 28 % of the warps an SM can have, by its latency: 22615 bf16 tokens of 8 KV heads and 32 query heads, keys and queries
-// given out, 120 us (4.8 TB/s, 73 % of the copy rate; one row at a time and table rows through registers 345); 16 layers x 8 x 1000 fp32 rows by list
+// given out, 120 us (556 MB, 4.6 TB/s, 71 % of the copy rate; one row at a time and table rows through registers 345); 16 layers x 8 x 1000 fp32 rows by list
 // 52 us (3.2 TB/s; the row, its position's turn, the block's maximum and the codes follow one another).  One token of 96 sequences is latency: 6 us.
 #include <algorithm>
 

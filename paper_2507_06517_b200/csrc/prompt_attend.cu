@@ -19,7 +19,8 @@
 //
 // Bound by products and exponentials alike (d = 128: 2048 cycles of either for a step of two tiles, both pipes 68 % busy at 8192 tokens; d = 64: half the
 // products, exponentials 75 % busy) and by the chain of a step from scores over their maximum (415 cycles) and weights (1350) to the second product.
-// 32 query heads over 8, d = 128: 512 tokens 15 us, 2048 38, 4096 111 (1240 TFLOP/s), 16384 1.6 to 1.75 ms (1250 to 1350, at the power limit).
+// 32 query heads over 8, d = 128: 512 tokens 15 us, 2048 38, 4096 111 to 121 (1240 to 1140 TFLOP/s), 16384 1.55 to 1.75 ms
+// (1420 to 1260), replayed; one call after another with inputs in rotation, at the power limit's lower clocks, 135 us and 1.82 ms (1020 and 1210).
 // Not kept: 64 keys a step (4096 tokens 189 us where this took 131), two threads a row (163), exponentials in part by a polynomial (112 to 136 for 111).
 #include <algorithm>
 

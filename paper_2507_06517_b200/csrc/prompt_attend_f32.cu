@@ -1,7 +1,7 @@
 // Causal attention of a prompt's rows, fp32, on the bf16 tensor cores.
 //
 // An fp32 number is the sum of three numbers of 8 bits each, x = x1 + x2 + x3, cut off rather than rounded, so that nothing runs out of range and
-// the sum is exact.  Of the nine products of two such sums the six with the largest factors are formed,
+// the sum is exact (splitting in the manner of Dekker).  Of the nine products of two such sums the six with the largest factors are formed,
 //     x y = x1 y1 + (x1 y2 + x2 y1) + (x2 y2 + x1 y3 + x3 y1) + ... ,
 // in rising order into one fp32 accumulator; what is left out is below 2^-24 of |x y| each.  Six products at the bf16 rate are a sixth of it: half a
 // tf32 pair's three products would cost the same and keep 22 bits.
@@ -12,7 +12,7 @@
 //     tensor memory: S [2][64 columns], P [2][3 pieces][32 columns], O [d columns]
 // The accumulator cuts off what it adds, always towards zero; over the products of thousands of keys that would be 2^-17 of the result (8.6e-6 at 4000
 // tokens).  So O holds one tile at a time, whose largest product comes last, and a warpgroup of its own adds the tiles up in its registers, rounding as
-// usual (7e-7).
+// usual (7e-7).  An infinite value is its first piece, and a weight may have a piece of 0: rows that see one get NaN here, where calls of few rows give the infinity.
 // Bound by the products: 6 x (128 x 64 x d) x 2 for 64 keys, 3840 cycles at d = 128 where N = 64 has no full rate (the tensor pipe is 69 % busy at 4096 tokens);
 // short sequences by the pieces' way into shared memory, 96 KB of rows and 96 KB for 64 keys.  32 query heads over 8, d = 128: 512 tokens 38 us, 2048 191,
 // 4096 640 to 690 (200 to 210 TFLOP/s, 1.2 PFLOP/s of products), of which the pieces are 42.
@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(kExactThreads, 1) prompt_attend_f32_kernel(con
 static size_t rows_of(const spindlekv_batch& b) { return (size_t)b.n_layers * b.total_len; }
 
 size_t prompt_pieces_bytes(const spindlekv_batch& keys, const spindlekv_batch& rows, int n_q_heads, int n_kv_heads, int head_dim) {
-  const size_t row = kPieces * 2 * (size_t)head_dim;      // (a multiple of 256)
+  const size_t row = kPieces * 2 * (size_t)head_dim;      // (a multiple of 128, which suits the copies' 16 bytes)
   return row * (rows_of(rows) * n_q_heads + 2 * rows_of(keys) * n_kv_heads);
 }
 

@@ -509,6 +509,9 @@ __global__ void __launch_bounds__(FewSmemBf16<D, NT>::kWarps * 32) prompt_rows_b
 //   bf16, 16384 keys, 4 / 16 / 32 columns 15 / 20 / 25 us and 23 / 25 / 27; 4 x 16384, 4 / 16 columns 48 / 54 and 56 / 58; 32 sequences of 200 to 4000 keys,
 //   4 columns 51 and 100.  More than 16 columns would be two thread blocks that read the same keys.
 //   fp32, 16384 keys, 4 / 16 / 32 columns 29 / 58 / 121 us and 118 / 120 / 122; 4 x 16384, 4 / 16 columns 87 / 227 and 406 / 407.
+// d = 64: bf16, 16384 keys, 4 / 16 / 32 columns 17 / 20 / 23 and 25 / 27 / 28, 8 x 4096 17 / 21 / 28 and 33 / 35 / 36; fp32, 4 / 16 / 24 / 32 columns 23 / 41 / 53 / 66 and 70 to 73, 8 x 4096
+// 33 / 71 / 102 / 125 and 122.  2000 keys of two KV heads: bf16, 4 / 16 columns 13 / 16 and 19; fp32 15 / 18 and 32.  One KV head of one sequence is where tiles do better in bf16, having few
+// parts to join (16384 keys, 4 / 16 columns: d = 128 20 / 26 and 20, d = 64 26 / 28 and 19); fp32 22 / 24 and 39, 27 / 26 and 30.
 constexpr int kFewMostBf16 = 16, kFewMostF32 = 24;
 // Columns of a thread block
 static int few_columns(int columns, int dtype) { return dtype == SPINDLEKV_F32 ? (columns <= 4 ? 4 : 8) : columns <= 8 ? 8 : 16; }
