@@ -87,3 +87,23 @@ def test_scratch_full_of_nans_and_one_object_for_long_and_short():
         want, _, bound = R.attend(q, k, v, keys, rows)
         row = ~want.isnan()
         assert (out[~row] == 7.0).all() and ((out.double() - want).abs()[row] <= bound[row]).all()
+
+
+def test_a_wait_that_gives_up_over_long_keys():
+    from paper_2507_06517_b200.pipeline import SpindleKVPromptAttention
+    keys, rws, q, k, v = make([40000], [900], 32, 4, 128, BF, False, seed=75)
+    a = SpindleKVPromptAttention(keys, 32, 4, 128, BF, rows=rws)
+    want, _, bound = R.attend(q, k, v, keys, rws)
+    out = torch.zeros_like(q)
+    for block in (0, 77):
+        a.ws.random_(0, 256)
+        try:
+            B.spindlekv_set_tuning(B.TUNE_MBAR_WAIT_CYCLES, 2_000_000)
+            B.spindlekv_set_tuning(B.TUNE_PAGED_WITHHOLD, block)
+            a.run(q, k, v, out=out)
+            assert a.status() == B.TIMEOUT
+        finally:
+            for key in (B.TUNE_MBAR_WAIT_CYCLES, B.TUNE_PAGED_WITHHOLD):
+                B.spindlekv_set_tuning(key, -1)
+        a.run(q, k, v, out=out)
+        assert a.status() == B.OK and ((out.double() - want).abs() <= bound).all()
